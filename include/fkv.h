@@ -266,6 +266,66 @@ int fkv_append_decode_attn(fkv_cache *c, int layer, const void *k, const void *v
 int fkv_decode_step(fkv_cache *c, const void *k, const void *v, const int32_t *pos, const void *q, void *out,
                     float scale, void *stream);
 
+/*
+ * ---- sliding windows and sinks ----
+ * fkv_decode_attn / fkv_append_decode_attn of a layer whose queries see only part of the retained set: a query of
+ * position p sees the pairs of positions (p - window, p] and those of positions below `sinks` (the first tokens, that
+ * stay visible).  Positions are the stored ones, so a window means the same before and after an eviction.  window >= 1,
+ * sinks >= 0 (else FKV_ERR_INVALID_ARG).  The rest is as in the calls without a window, but that the query is NOT put on
+ * record for the attention features (they describe attention over the whole retained set).
+ *
+ * Positions must grow from pair to pair of a segment, and k and v must be finite where some of the queries of a call see a
+ * pair and others do not.
+ *
+ * fkv_decode_attn_window: q_pos dev [max_batch] int32 positions of the queries (pairs of later positions are not seen), or
+ * NULL: the position of the last pair.  A query that sees no pair gets zeros.  fkv_append_decode_attn_window: the query's
+ * position is the new pair's; a sequence outside seq_mask attends from its last pair.
+ */
+int fkv_decode_attn_window(fkv_cache *c, int layer, const void *q, const int32_t *q_pos, int32_t window, int32_t sinks,
+                           void *out, float scale, void *stream);
+int fkv_append_decode_attn_window(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos,
+                                  const uint64_t *seq_mask, const void *q, int32_t window, int32_t sinks, void *out,
+                                  float scale, void *stream);
+
+/*
+ * ---- chunks of new tokens (a prompt in pieces, the draft tokens of a speculative decoder) ----
+ *
+ * chunk_lens: host [max_batch], the number of tokens of every sequence in this call (0: it takes no part); at most 2^24 in
+ * all.  Tensors over tokens are packed: the tokens of sequence 0, then those of sequence 1, ...; nothing is read or
+ * written behind the last one.  k, v: dev [tokens][Hkv][D] bf16; q, out: dev [tokens][Hkv*g][D] bf16; all 16-byte
+ * aligned (FKV_ERR_INVALID_ARG otherwise).  Host arrays are read before the call returns.
+ *
+ * fkv_append_chunk: stores the chunk behind the pairs that stay.  keep_lens: host [max_batch], the number of pairs that
+ * stay of every sequence, at most its length (the pairs behind are dropped and their pages returned: rejected drafts; with
+ * chunk_lens all 0 the call only rolls back, and k, v may be NULL), or NULL: all.  pos: dev [tokens] int32, or NULL: the
+ * positions after the last pair that stays (from 0 for an empty segment).  The feature rows of the new pairs are zero.
+ * Decode queries on record (feature_window) whose tokens are dropped leave the record; a record that has wrapped starts
+ * over then.  FKV_ERR_CAPACITY if a sequence would exceed max_tokens_per_head.  If the pool runs out of pages nothing is
+ * stored (FKV_DEV_POOL_EXHAUSTED).
+ *
+ * fkv_chunk_attn: attention of a chunk's queries, the chunk's pairs being the last chunk_lens[s] pairs of their segments:
+ *     out[j] = sum_i softmax_i(scale <q_j, k_i>) v_i,   lse_out[j] = ln sum_i exp(scale <q_j, k_i>),
+ * over the pairs i up to query j's own and, with window > 0, inside its window or among the sinks (as above; window = 0:
+ * every pair).  lse_out: dev [tokens][Hkv*g] fp32 or NULL.  scale 0 means 1/sqrt(D); a negative or infinite one is
+ * FKV_ERR_INVALID_ARG, as is a chunk longer than its segment.  Errors as fkv_evict_rkv for the tensor maps.
+ * P is rounded to bf16 for the product with V (as V is); everything else is fp32.
+ *
+ * fkv_append_chunk_attn: the two calls in one.
+ *
+ * Stream capture: all three only enqueue kernels.  A replayed fkv_append_chunk appends once more from the recorded buffers
+ * (with keep_lens: behind the same number of pairs again); the device's lengths count, a sequence that would pass its
+ * capacity (FKV_DEV_CAPACITY) or is shorter than keep_lens or its chunk (FKV_DEV_BAD_INDEX) is skipped.  Call
+ * fkv_sync_lengths after the last replay.  The calls of one cache share its workspace: graphs that hold them must not run
+ * at the same time.
+ */
+int fkv_append_chunk(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos, const int32_t *keep_lens,
+                     const int32_t *chunk_lens, void *stream);
+int fkv_chunk_attn(fkv_cache *c, int layer, const void *q, const int32_t *chunk_lens, int32_t window, int32_t sinks,
+                   float scale, void *out, float *lse_out, void *stream);
+int fkv_append_chunk_attn(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos,
+                          const int32_t *keep_lens, const int32_t *chunk_lens, const void *q, int32_t window,
+                          int32_t sinks, float scale, void *out, float *lse_out, void *stream);
+
 /* ---- staged entry points: one kernel each, for per-step checks ---- */
 
 /*
@@ -322,6 +382,9 @@ int fkv_score_stride(const fkv_cache *c, int32_t *cap);
  */
 int fkv_export_head(fkv_cache *c, int layer, int seq, int kv_head, void *k, void *v, float *feat, int32_t *pos,
                     void *stream);
+
+/* Dense copy of the features of one (layer, sequence): feat dev [Hkv][n][F] fp32 (the layout fkv_set_features takes). */
+int fkv_export_features(fkv_cache *c, int layer, int seq, float *feat, void *stream);
 
 /* Current lengths of `layer`: host_out [max_batch] (host mirror, no device access). */
 int fkv_get_lengths(const fkv_cache *c, int layer, int32_t *host_out);

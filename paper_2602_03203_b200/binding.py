@@ -27,7 +27,8 @@ EXPORTS = ["fkv_workspace_bytes", "fkv_init_cache", "fkv_destroy", "fkv_reset", 
            "fkv_compact", "fkv_score_stride", "fkv_export_head", "fkv_get_lengths", "fkv_device_status",
            "fkv_launch_count", "fkv_last_cuda_error", "fkv_sync_lengths", "fkv_set_timing", "fkv_get_evict_timing",
            "fkv_decode_step", "fkv_decode_attn_dense_noalloc", "fkv_append_decode_attn", "fkv_evict_sampled", "fkv_select_sampled", "fkv_update_features", "fkv_evict_by_feature", "fkv_golden_steps", "fkv_golden_eviction", "fkv_golden_select",
-           "fkv_evict_rkv", "fkv_score_rkv"]
+           "fkv_evict_rkv", "fkv_score_rkv", "fkv_append_chunk", "fkv_chunk_attn", "fkv_append_chunk_attn",
+           "fkv_decode_attn_window", "fkv_append_decode_attn_window", "fkv_export_features"]
 
 
 class FkvConfig(ctypes.Structure):
@@ -62,6 +63,11 @@ def lib():
         _lib.fkv_append_decode_attn.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, f32, vp]
         _lib.fkv_decode_step.argtypes = [vp, vp, vp, vp, vp, vp, f32, vp]
         _lib.fkv_evict.argtypes = [vp, i32, vp]
+        _lib.fkv_append_chunk.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp]
+        _lib.fkv_chunk_attn.argtypes = [vp, i32, vp, vp, i32, i32, f32, vp, vp, vp]
+        _lib.fkv_append_chunk_attn.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, i32, i32, f32, vp, vp, vp]
+        _lib.fkv_decode_attn_window.argtypes = [vp, i32, vp, vp, i32, i32, vp, f32, vp]
+        _lib.fkv_append_decode_attn_window.argtypes = [vp, i32, vp, vp, vp, vp, vp, i32, i32, vp, f32, vp]
     return _lib
 
 
@@ -94,6 +100,15 @@ def _mask(seq_mask, max_batch):
     words = (max_batch + 63) // 64
     arr = (ctypes.c_uint64 * words)(*[(seq_mask >> (64 * i)) & 0xFFFFFFFFFFFFFFFF for i in range(words)])
     return arr, ctypes.cast(arr, ctypes.c_void_p)
+
+
+def _lens(x, max_batch, what):
+    """A list of max_batch integers as the host array the library reads (NULL for None)."""
+    if x is None:
+        return None
+    if len(x) != max_batch:
+        raise ValueError(f"{what}: expected {max_batch} entries, one per sequence, got {len(x)}")
+    return (ctypes.c_int32 * max_batch)(*x)
 
 
 def _stream():
@@ -244,6 +259,77 @@ class Cache:
         _check(lib().fkv_decode_step(self._h, _ptr(k, torch.bfloat16), _ptr(v, torch.bfloat16), _ptr(pos, torch.int32),
                                      _ptr(q, torch.bfloat16), _ptr(out, torch.bfloat16), scale, _stream()),
                "fkv_decode_step")
+        return out
+
+    # -- sliding windows and sinks
+    def decode_attn_window(self, layer, q, window, sinks=0, q_pos=None, out=None, scale=0.0):
+        """decode_attn over the last `window` positions up to the query's and the positions below `sinks`.
+        q_pos [batch] int32: positions of the queries (None: the last pair's)."""
+        if out is None:
+            out = torch.empty_like(q)
+        _check(lib().fkv_decode_attn_window(self._h, layer, _ptr(q, torch.bfloat16), _ptr(q_pos, torch.int32), window, sinks,
+                                            _ptr(out, torch.bfloat16), scale, _stream()), "fkv_decode_attn_window")
+        return out
+
+    def append_decode_attn_window(self, layer, k, v, q, window, sinks=0, out=None, pos=None, seq_mask=0, scale=0.0):
+        """append(k, v) then decode_attn_window(q) on one layer, as one launch."""
+        if out is None:
+            out = torch.empty_like(q)
+        keep, m = _mask(seq_mask, self.cfg.max_batch)
+        _check(lib().fkv_append_decode_attn_window(self._h, layer, _ptr(k, torch.bfloat16), _ptr(v, torch.bfloat16),
+                                                   _ptr(pos, torch.int32), m, _ptr(q, torch.bfloat16), window, sinks,
+                                                   _ptr(out, torch.bfloat16), scale, _stream()),
+               "fkv_append_decode_attn_window")
+        return out
+
+    # -- chunks of new tokens: tensors are packed over the tokens of all sequences, chunk_lens has one entry per sequence
+    def _check_chunk(self, chunk_lens, **tensors):
+        total, c = sum(chunk_lens), self.cfg
+        for name, t in tensors.items():
+            heads = c.num_kv_heads * (1 if name in ("k", "v") else c.group_size)
+            want = (total, heads) if name == "lse" else (total,) if name == "pos" else (total, heads, c.head_dim)
+            if t is not None and tuple(t.shape) != want:
+                raise ValueError(f"{name}: expected shape {want}, got {tuple(t.shape)}")
+
+    def append_chunk(self, layer, k, v, chunk_lens, pos=None, keep_lens=None):
+        """Store chunk_lens[s] new pairs behind the first keep_lens[s] pairs of every sequence (None: behind all)."""
+        self._check_chunk(chunk_lens, k=k, v=v, pos=pos)
+        lens, keep = _lens(chunk_lens, self.cfg.max_batch, "chunk_lens"), _lens(keep_lens, self.cfg.max_batch, "keep_lens")
+        _check(lib().fkv_append_chunk(self._h, layer, _ptr(k, torch.bfloat16), _ptr(v, torch.bfloat16), _ptr(pos, torch.int32),
+                                      keep, lens, _stream()), "fkv_append_chunk")
+
+    def chunk_attn(self, layer, q, chunk_lens, window=0, sinks=0, out=None, lse=None, scale=0.0):
+        """Attention of the queries q [tokens][Hq][D] of the last chunk_lens[s] pairs of every sequence, each over the pairs
+        up to its own; lse [tokens][Hq] fp32, if given, gets the log-sum-exp of the scores."""
+        if out is None:
+            out = torch.empty_like(q)
+        self._check_chunk(chunk_lens, q=q, out=out, lse=lse)
+        _check(lib().fkv_chunk_attn(self._h, layer, _ptr(q, torch.bfloat16), _lens(chunk_lens, self.cfg.max_batch, "chunk_lens"),
+                                    window, sinks, scale, _ptr(out, torch.bfloat16), _ptr(lse, torch.float32), _stream()),
+               "fkv_chunk_attn")
+        return out
+
+    def append_chunk_attn(self, layer, k, v, q, chunk_lens, pos=None, keep_lens=None, window=0, sinks=0, out=None, lse=None,
+                          scale=0.0):
+        """append_chunk(k, v) then chunk_attn(q) in one call."""
+        if out is None:
+            out = torch.empty_like(q)
+        self._check_chunk(chunk_lens, k=k, v=v, q=q, out=out, lse=lse, pos=pos)
+        lens, keep = _lens(chunk_lens, self.cfg.max_batch, "chunk_lens"), _lens(keep_lens, self.cfg.max_batch, "keep_lens")
+        _check(lib().fkv_append_chunk_attn(self._h, layer, _ptr(k, torch.bfloat16), _ptr(v, torch.bfloat16),
+                                           _ptr(pos, torch.int32), keep, lens, _ptr(q, torch.bfloat16), window, sinks, scale,
+                                           _ptr(out, torch.bfloat16), _ptr(lse, torch.float32), _stream()),
+               "fkv_append_chunk_attn")
+        return out
+
+    def export_features(self, layer, seq, out=None):
+        """The features of one (layer, sequence): [Hkv][n][6 g] fp32."""
+        shape = (self.cfg.num_kv_heads, self.lengths(layer)[seq], self.feat_dim)
+        if out is None:
+            out = torch.empty(shape, dtype=torch.float32, device="cuda")
+        elif tuple(out.shape) != shape:
+            raise ValueError(f"out: expected shape {shape}, got {tuple(out.shape)}")
+        _check(lib().fkv_export_features(self._h, layer, seq, _ptr(out, torch.float32), _stream()), "fkv_export_features")
         return out
 
     # -- staged entry points

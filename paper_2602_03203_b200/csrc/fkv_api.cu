@@ -11,11 +11,13 @@
 #include <cmath>
 #include <new>
 #include <string>
+#include <utility>
 #include <vector>
 
 #include "../../include/fkv.h"
 #include "fkv_attend.cuh"
 #include "fkv_aux.cuh"
+#include "fkv_chunk.cuh"
 #include "fkv_compact.cuh"
 #include "fkv_dev.cuh"
 #include "fkv_features.cuh"
@@ -54,7 +56,7 @@ struct SmemOptIn {
 };
 
 struct Layout {
-  size_t pool, free_stack, ctrl, planhdr, pt, pt_new, len, budget, sp, scores, idx, plan, work, tile1, seq_tickets, seq_fail, att_part, att_tickets, hist_q, hist_mp, hist_n, hist_cnt, total;
+  size_t pool, free_stack, ctrl, planhdr, pt, pt_new, len, budget, sp, scores, idx, plan, work, tile1, seq_tickets, seq_fail, att_part, att_tickets, hist_q, hist_mp, hist_n, hist_cnt, chunk_part, chunk_ml, chunk_info, total;
   int cap, max_pages, num_pages, page_bytes, F, att_smax, sp_stride, sp_off_wf, sp_off_b1, sp_off_w2, sp_off_b2;
 };
 
@@ -117,6 +119,10 @@ Layout make_layout(const fkv_config &c) {
   L.hist_mp = take(ls * Wp * Hq * 4);
   L.hist_n = take(ls * W * 4);
   L.hist_cnt = take(W ? ls * 4 : 0);
+  // Attention over chunks: two slots of 2 x 128 query rows per CTA, whatever the shape of the cache.
+  L.chunk_part = take((size_t)kChunkCtas * 2 * 256 * D * 4);
+  L.chunk_ml = take((size_t)kChunkCtas * 2 * 256 * 8);
+  L.chunk_info = take((size_t)kChunkCtas * kChunkInfo * 4);
   L.total = off;
   return L;
 }
@@ -148,11 +154,11 @@ struct fkv_cache {
   std::vector<uint8_t> staging;
   uint64_t launches = 0;
   int sm_count = 148;
-  int max_cluster = 0;        // largest attention cluster the device places (found at the first stand-alone launch)
+  int max_cluster[2] = {0, 0};   // largest attention cluster the device places (found at the first stand-alone launch): plain, windowed
   float feature_scale = 0.f;  // softmax scale of the recorded queries (the last decode call's)
   bool timing = false, timed = false;
-  CUtensorMap k_rows;         // the page pool's K rows as [page][row][64-channel half][64 channels] (R-KV's tensor copies)
-  bool k_rows_ready = false;
+  CUtensorMap page_rows;      // the page pool's K and V rows as [page][row][64-channel part][64 channels] (tensor copies)
+  bool page_rows_ready = false;
   cudaEvent_t ev[7] = {nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};  // [6]: after the plan
 };
 
@@ -284,14 +290,12 @@ int launch_features(fkv_cache *c, int max_old, int nwork_bound, cudaStream_t st)
                                 : launch_features_t<64>(c, max_old, nwork_bound, scale_log2, st);
 }
 
-// The tensor map of R-KV's copies: bf16 [num_pages][16 rows][D / 64 halves][64 channels] over the page pool, one box =
-// the 16 rows x 64 channels of one page (2 KB, 16 rows of 128 bytes in shared memory; the record's own chunk swizzle
-// stays as it is).  The driver's encoder is reached through the runtime, so the library links no driver stub.
-int ensure_k_rows_map(fkv_cache *c) {
-  if (c->k_rows_ready) return FKV_OK;
-  typedef CUresult (*encode_fn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+// The driver's tensor-map encoder, reached through the runtime, so the library links no driver stub.
+typedef CUresult (*encode_fn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                              const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+int tensor_map(CUtensorMap *map, void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box,
+               CUtensorMapSwizzle swizzle) {
   void *fn = nullptr;
   cudaDriverEntryPointQueryResult found;
   FKV_CUDA(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found));
@@ -299,18 +303,28 @@ int ensure_k_rows_map(fkv_cache *c) {
     g_cuda_error = "cuTensorMapEncodeTiled is not available from this driver";
     return FKV_ERR_CUDA;
   }
-  const int D = c->cfg.head_dim;
-  const cuuint64_t dims[4] = {64, (cuuint64_t)(D / 64), (cuuint64_t)kPage, (cuuint64_t)c->ctx.num_pages};
-  const cuuint64_t strides[3] = {128, (cuuint64_t)(4 * D), (cuuint64_t)c->ctx.page_bytes};   // bytes, dimensions 1 .. 3
-  const cuuint32_t box[4] = {64, 1, (cuuint32_t)kPage, 1}, step[4] = {1, 1, 1, 1};
-  const CUresult r = reinterpret_cast<encode_fn>(fn)(&c->k_rows, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, c->ctx.pool, dims, strides,
-                                                     box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
-                                                     CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  const cuuint32_t step[5] = {1, 1, 1, 1, 1};
+  const CUresult r = reinterpret_cast<encode_fn>(fn)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, base, dims, strides, box, step,
+                                                     CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                                                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
     g_cuda_error = "cuTensorMapEncodeTiled failed with driver error " + std::to_string((int)r);
     return FKV_ERR_CUDA;
   }
-  c->k_rows_ready = true;
+  return FKV_OK;
+}
+
+// The tensor map of the page copies: bf16 [num_pages][16 rows][2 D / 64][64 channels] over the page pool (K's 64-channel
+// parts, then V's), one box = the 16 rows x 64 channels of one page (2 KB, 16 rows of 128 bytes in shared memory; the
+// record's own chunk swizzle stays as it is).
+int ensure_page_rows_map(fkv_cache *c) {
+  if (c->page_rows_ready) return FKV_OK;
+  const int D = c->cfg.head_dim;
+  const cuuint64_t dims[4] = {64, (cuuint64_t)(2 * D / 64), (cuuint64_t)kPage, (cuuint64_t)c->ctx.num_pages};
+  const cuuint64_t strides[3] = {128, (cuuint64_t)(4 * D), (cuuint64_t)c->ctx.page_bytes};   // bytes, dimensions 1 .. 3
+  const cuuint32_t box[4] = {64, 1, (cuuint32_t)kPage, 1};
+  if (int e = tensor_map(&c->page_rows, c->ctx.pool, 4, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE)) return e;
+  c->page_rows_ready = true;
   return FKV_OK;
 }
 
@@ -321,7 +335,7 @@ template <int D>
 int launch_rkv_t(fkv_cache *c, float *out, int seg_base, int max_old, int nwork_bound, long long tiles, float la, float ls,
                  cudaStream_t st) {
   if (max_old <= 0 || nwork_bound <= 0) return FKV_OK;
-  if (int e = ensure_k_rows_map(c)) return e;
+  if (int e = ensure_page_rows_map(c)) return e;
   float *rn = reinterpret_cast<float *>(c->ctx.idx);
   k_rkv_prepare<D><<<dim3(nwork_bound, (max_old + 127) / 128), 128, 0, st>>>(c->ctx, out, rn, seg_base,
                                                                              FKV_FEATURE_WINDOW8);
@@ -342,13 +356,13 @@ int launch_rkv_t(fkv_cache *c, float *out, int seg_base, int max_old, int nwork_
     at[0].val.clusterDim.x = 2; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    FKV_CUDA(cudaLaunchKernelEx(&cfg, k_rkv_score_pair<D>, c->ctx, c->k_rows, out, (const float *)rn, seg_base, la, ls));
+    FKV_CUDA(cudaLaunchKernelEx(&cfg, k_rkv_score_pair<D>, c->ctx, c->page_rows, out, (const float *)rn, seg_base, la, ls));
   } else {
     const size_t smem = RkvSmem::bytes(D);
     static SmemOptIn opt_in;
     FKV_CUDA(opt_in.ensure(k_rkv_score<D>, smem));
     const int grid = (int)std::max<long long>(1, std::min<long long>(c->sm_count, tiles));
-    k_rkv_score<D><<<grid, kRkvThreads, smem, st>>>(c->ctx, c->k_rows, out, rn, seg_base, la, ls);
+    k_rkv_score<D><<<grid, kRkvThreads, smem, st>>>(c->ctx, c->page_rows, out, rn, seg_base, la, ls);
   }
   FKV_LAUNCHED(c);
   return FKV_OK;
@@ -373,10 +387,10 @@ int launch_compact(fkv_cache *c, const int32_t *idx, int seg_base, int max_new, 
 // One launch of the attention kernel: `splits` CTAs per segment.  pdl: the launch may run alongside the one
 // before it on the stream.  cluster: the splits of a segment are one thread-block cluster (the merge goes through
 // distributed shared memory).
-template <int D, int NCW, int SLOTS, bool CLUSTER>
+template <int D, int NCW, int SLOTS, bool CLUSTER, bool WIN>
 int launch_attend_t(fkv_cache *c, const AttendArgs *a, int splits, bool pdl, cudaStream_t st) {
   const size_t smem = AttendSmem::bytes(D, NCW, SLOTS, CLUSTER);
-  auto kern = k_attend<D, NCW, SLOTS, CLUSTER>;
+  auto kern = k_attend<D, NCW, SLOTS, CLUSTER, WIN>;
   static SmemOptIn opt_in;
   FKV_CUDA(opt_in.ensure(kern, smem));
   cudaLaunchConfig_t cfg = {};
@@ -405,9 +419,9 @@ int launch_attend_t(fkv_cache *c, const AttendArgs *a, int splits, bool pdl, cud
 
 // The largest cluster of attention CTAs this device places: 16 (needs the non-portable opt-in), else 8; found once
 // per handle.
-template <int D, int NCW, int SLOTS>
+template <int D, int NCW, int SLOTS, bool WIN>
 int attend_max_cluster(fkv_cache *c) {
-  auto kern = k_attend<D, NCW, SLOTS, true>;
+  auto kern = k_attend<D, NCW, SLOTS, true, WIN>;
   const size_t smem = AttendSmem::bytes(D, NCW, SLOTS, true);
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess ||
       cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
@@ -429,23 +443,33 @@ int attend_max_cluster(fkv_cache *c) {
   return ok16 ? kClusterSplits : 8;
 }
 
+template <bool WIN>
 int attend_dispatch(fkv_cache *c, const AttendArgs *a, int splits, bool pdl, bool cluster, cudaStream_t st) {
   if (cluster)
-    return c->cfg.head_dim == 128 ? launch_attend_t<128, 4, 8, true>(c, a, splits, pdl, st)
-                                  : launch_attend_t<64, 4, 16, true>(c, a, splits, pdl, st);
-  return c->cfg.head_dim == 128 ? launch_attend_t<128, 4, 8, false>(c, a, splits, pdl, st)
-                                : launch_attend_t<64, 4, 16, false>(c, a, splits, pdl, st);
+    return c->cfg.head_dim == 128 ? launch_attend_t<128, 4, 8, true, WIN>(c, a, splits, pdl, st)
+                                  : launch_attend_t<64, 4, 16, true, WIN>(c, a, splits, pdl, st);
+  return c->cfg.head_dim == 128 ? launch_attend_t<128, 4, 8, false, WIN>(c, a, splits, pdl, st)
+                                : launch_attend_t<64, 4, 16, false, WIN>(c, a, splits, pdl, st);
 }
+
+// The windowed form of a decode launch: window == 0 is the plain one.
+struct Window {
+  int window = 0, sinks = 0;
+  const int32_t *q_pos = nullptr;
+};
 
 // Attention over `layer`, with the new pair of every participating sequence appended first when k_new is given.
 int launch_attend(fkv_cache *c, int layer, const void *q, void *out, float scale, const void *k_new, const void *v_new,
-                  const int32_t *pos, const SeqMask &seq_mask, bool pdl, cudaStream_t st) {
+                  const int32_t *pos, const SeqMask &seq_mask, bool pdl, cudaStream_t st, const Window &w = Window()) {
   const int batch = c->cfg.max_batch, Hkv = c->cfg.num_kv_heads, D = c->cfg.head_dim;
   const bool app = k_new != nullptr;
   int maxpages = 0;
   for (int s = 0; s < batch; ++s) {
     const int n = c->h_len[(size_t)layer * batch + s] + ((app && seq_mask.has(s)) ? 1 : 0);
-    maxpages = std::max(maxpages, (n + kPage - 1) / kPage);
+    int pages = (n + kPage - 1) / kPage;
+    if (w.window)   // a window of W positions holds at most W pairs, which may begin and end inside a page
+      pages = (int)std::min<long long>(pages, ((long long)w.window + kPage - 1) / kPage + 1 + (std::min(w.sinks, n) + kPage - 1) / kPage);
+    maxpages = std::max(maxpages, pages);
   }
   // Splits per segment, at least kAttendMinPages pages each.  Consecutive launches of a decode step share the SMs
   // (three CTAs fit on one): CTAs for about three quarters of the SMs per launch.  A launch on its own has the GPU to
@@ -465,26 +489,169 @@ int launch_attend(fkv_cache *c, int layer, const void *q, void *out, float scale
   // above, whose split count is free, fills the GPU better.
   bool cluster = false;
   if (!pdl && nseg * kClusterSplits <= c->sm_count * 3 / 2) {
-    if (c->max_cluster == 0)
-      c->max_cluster = c->cfg.head_dim == 128 ? attend_max_cluster<128, 4, 8>(c) : attend_max_cluster<64, 4, 16>(c);
+    int &max_cluster = c->max_cluster[w.window ? 1 : 0];
+    if (max_cluster == 0) {
+      if (w.window)
+        max_cluster = c->cfg.head_dim == 128 ? attend_max_cluster<128, 4, 8, true>(c) : attend_max_cluster<64, 4, 16, true>(c);
+      else
+        max_cluster = c->cfg.head_dim == 128 ? attend_max_cluster<128, 4, 8, false>(c) : attend_max_cluster<64, 4, 16, false>(c);
+    }
     int cs = 1;
-    while (cs * 2 <= c->max_cluster && cs * 2 <= kClusterSplits && maxpages / (cs * 2) >= kAttendMinPages) cs *= 2;
+    while (cs * 2 <= max_cluster && cs * 2 <= kClusterSplits && maxpages / (cs * 2) >= kAttendMinPages) cs *= 2;
     if (cs >= 8) { cluster = true; splits = cs; }
   }
   const int pps = std::max(1, (maxpages + splits - 1) / splits);
   if (scale == 0.f) scale = 1.f / sqrtf((float)D);
-  if (app) c->feature_scale = scale;
+  if (app && !w.window) c->feature_scale = scale;
   AttendArgs a;
   a.layer = layer; a.q = (const __nv_bfloat16 *)q; a.out = (__nv_bfloat16 *)out;
   a.scale_log2 = scale * 1.4426950408889634f; a.pps = pps; a.append = app ? 1 : 0;
   a.k_new = (const uint8_t *)k_new; a.v_new = (const uint8_t *)v_new; a.pos_new = pos; a.seq_mask = seq_mask;
+  a.window = w.window; a.sinks = w.sinks; a.q_pos = w.q_pos;
   a.wait_first = pdl ? 0 : 1;
-  const int rc = attend_dispatch(c, &a, splits, pdl, cluster, st);
+  const int rc = w.window ? attend_dispatch<true>(c, &a, splits, pdl, cluster, st) : attend_dispatch<false>(c, &a, splits, pdl, cluster, st);
   if (rc) return rc;
   if (app)
     for (int s = 0; s < batch; ++s)
       if (seq_mask.has(s)) ++c->h_len[(size_t)layer * batch + s];
   return FKV_OK;
+}
+
+// ---------------------------------------------------------------- chunks
+inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+constexpr int kMaxChunkTokens = 1 << 24;   // of one call, over all sequences
+
+// Prefix sums of the chunk lengths; false if a length is negative or they are too many.
+bool make_lens(const fkv_cache *c, const int32_t *chunk_lens, ChunkLens &l) {
+  long long t = 0;
+  l.tok[0] = 0;
+  for (int s = 0; s < kMaxBatch; ++s) {
+    if (s < c->cfg.max_batch) {
+      if (chunk_lens[s] < 0) return false;
+      t += chunk_lens[s];
+      if (t > kMaxChunkTokens) return false;
+    }
+    l.tok[s + 1] = (int)t;
+  }
+  return true;
+}
+
+// A launch with the programmatic attribute whose kernel waits for the launch before it ahead of its first global read.
+template <class... P, class... A>
+cudaError_t launch_waiting(void (*kern)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, A &&...args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, std::forward<A>(args)...);
+}
+
+int check_append_chunk(const fkv_cache *c, int layer, const void *k, const void *v, const int32_t *keep_lens,
+                       const int32_t *chunk_lens, ChunkLens &lens) {
+  if (!c || !layer_ok(c, layer) || !chunk_lens || !make_lens(c, chunk_lens, lens)) return FKV_ERR_INVALID_ARG;
+  const int batch = c->cfg.max_batch;
+  if (lens.tok[batch] > 0 && (!k || !v || !aligned(k, 16) || !aligned(v, 16))) return FKV_ERR_INVALID_ARG;
+  for (int s = 0; s < batch; ++s) {
+    const int n = c->h_len[(size_t)layer * batch + s], keep = keep_lens ? keep_lens[s] : n;
+    if (keep < 0 || keep > n) return FKV_ERR_INVALID_ARG;
+    if (keep + (long long)chunk_lens[s] > c->lay.cap) return FKV_ERR_CAPACITY;
+  }
+  return FKV_OK;
+}
+
+int launch_append_chunk(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos, const int32_t *keep_lens,
+                        const int32_t *chunk_lens, const ChunkLens &lens, cudaStream_t st) {
+  const int batch = c->cfg.max_batch;
+  ChunkKeep keep = {};
+  bool any = lens.tok[batch] > 0;
+  if (keep_lens) {
+    keep.use = 1;
+    for (int s = 0; s < batch; ++s) {
+      keep.keep[s] = keep_lens[s];
+      any = any || keep_lens[s] != c->h_len[(size_t)layer * batch + s];
+    }
+  }
+  if (!any) return FKV_OK;
+  // A warp per pair, up to four CTAs of eight warps on every SM: more pairs than that go round.
+  const long long tasks = (long long)lens.tok[batch] * c->cfg.num_kv_heads;
+  const int grid = (int)std::max<long long>(1, std::min<long long>((tasks + 7) / 8, 4LL * c->sm_count));
+  FKV_CUDA(launch_waiting(k_append_chunk, dim3(grid), 256, 0, st, c->ctx, layer, (const uint8_t *)k, (const uint8_t *)v, pos, lens, keep));
+  ++c->launches;
+  for (int s = 0; s < batch; ++s) {
+    int &n = c->h_len[(size_t)layer * batch + s];
+    n = (keep_lens ? keep_lens[s] : n) + chunk_lens[s];
+  }
+  return FKV_OK;
+}
+
+int check_chunk(const fkv_cache *c, int layer, const void *q, const int32_t *chunk_lens, int32_t window, int32_t sinks,
+                float scale, ChunkLens &lens) {
+  if (!c || !layer_ok(c, layer) || !chunk_lens || !make_lens(c, chunk_lens, lens)) return FKV_ERR_INVALID_ARG;
+  if (window < 0 || sinks < 0 || !(scale >= 0.f) || !std::isfinite(scale)) return FKV_ERR_INVALID_ARG;
+  if (lens.tok[c->cfg.max_batch] > 0 && (!q || !aligned(q, 16))) return FKV_ERR_INVALID_ARG;
+  return FKV_OK;
+}
+// The chunk's own pairs have to be the last ones of their segments (after the append, if the call makes one).
+bool chunk_is_stored(const fkv_cache *c, int layer, const int32_t *chunk_lens) {
+  for (int s = 0; s < c->cfg.max_batch; ++s)
+    if (chunk_lens[s] > c->h_len[(size_t)layer * c->cfg.max_batch + s]) return false;
+  return true;
+}
+
+// q as [tokens][query heads][D]: one box = 64 channels x `heads` heads x `tokens` tokens, rows of 128 swizzled bytes.
+int query_map(const fkv_cache *c, const void *q, int tokens, int box_heads, int box_tokens, CUtensorMap *map) {
+  const int D = c->cfg.head_dim, Hq = c->cfg.num_kv_heads * c->cfg.group_size;
+  const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)Hq, (cuuint64_t)tokens};
+  const cuuint64_t strides[2] = {(cuuint64_t)(2 * D), (cuuint64_t)(2 * D * Hq)};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_tokens};
+  return tensor_map(map, const_cast<void *>(q), 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+template <int D>
+int launch_chunk_attend_t(fkv_cache *c, const CUtensorMap &tmq, const ChunkArgs &a, int grid, cudaStream_t st) {
+  constexpr size_t smem = ChunkSmem<D>::bytes();
+  static_assert(smem <= kMaxSmem, "one CTA's shared memory");
+  static SmemOptIn opt_in;
+  FKV_CUDA(opt_in.ensure(k_chunk_attend<D>, smem));
+  FKV_CUDA(launch_waiting(k_chunk_attend<D>, dim3(grid), kChunkThreads, smem, st, c->ctx, c->page_rows, tmq, a));
+  ++c->launches;
+  if (grid > 1) {   // (a single CTA cuts nothing)
+    const int rows = std::min(256, 2 * kChunkRows);
+    FKV_CUDA(launch_waiting(k_chunk_merge<D>, dim3(grid, rows / 8), 256, 0, st, c->ctx, a));
+    ++c->launches;
+  }
+  return FKV_OK;
+}
+
+int launch_chunk_attend(fkv_cache *c, int layer, const void *q, const int32_t *chunk_lens, const ChunkLens &lens, int window,
+                        int sinks, float scale, void *out, float *lse, cudaStream_t st) {
+  const int batch = c->cfg.max_batch, D = c->cfg.head_dim, G = c->cfg.group_size;
+  if (lens.tok[batch] == 0) return FKV_OK;
+  if (int e = ensure_page_rows_map(c)) return e;
+  ChunkArgs a;
+  a.layer = layer; a.window = window; a.sinks = window ? sinks : 0;
+  a.scale = scale == 0.f ? 1.f / sqrtf((float)D) : scale;
+  a.scale_log2 = a.scale * 1.4426950408889634f;
+  a.out = (__nv_bfloat16 *)out; a.lse = lse; a.lens = lens;
+  CUtensorMap tmq;
+  const int tokens_per_tile = kChunkRows / G, block = 2 * tokens_per_tile;
+  if (int e = query_map(c, q, lens.tok[batch], G, tokens_per_tile, &tmq)) return e;
+  // As many CTAs as there is work for: the pages of all items, by the lengths the host knows (the kernel goes by its own).
+  long long pages = 0;
+  for (int s = 0; s < batch; ++s) {
+    const int T = chunk_lens[s], n = c->h_len[(size_t)layer * batch + s];
+    for (int j = 0; j < T && pages < (1LL << 20); j += block) pages += (n - T + std::min(T, j + block) + kPage - 1) / kPage;
+  }
+  pages *= c->cfg.num_kv_heads;
+  const int most = std::min(kChunkCtas, c->sm_count);
+  const int grid = (int)std::max<long long>(1, std::min<long long>(most, (pages + kChunkMinPages - 1) / kChunkMinPages));
+  return D == 128 ? launch_chunk_attend_t<128>(c, tmq, a, grid, st) : launch_chunk_attend_t<64>(c, tmq, a, grid, st);
 }
 
 }  // namespace
@@ -524,6 +691,7 @@ int fkv_init_cache(const fkv_config *cfg, void *dev_workspace, size_t bytes, voi
   x.att_part = (float *)(ws + L.att_part); x.att_tickets = (int *)(ws + L.att_tickets); x.att_smax = L.att_smax;
   x.hist_w = cfg->feature_window; x.hist_q = ws + L.hist_q; x.hist_mp = (float *)(ws + L.hist_mp); x.hist_wp = (cfg->feature_window + 15) & ~15;
   x.hist_n = (int *)(ws + L.hist_n); x.hist_cnt = (int *)(ws + L.hist_cnt);
+  x.chunk_part = (float *)(ws + L.chunk_part); x.chunk_ml = (float *)(ws + L.chunk_ml); x.chunk_info = (int *)(ws + L.chunk_info);
   c->h_len.assign((size_t)cfg->num_layers * cfg->max_batch, 0);
   c->h_budget.assign(cfg->max_batch, cfg->budget);
   c->loaded.assign((size_t)cfg->num_layers * cfg->num_kv_heads, 0);
@@ -840,6 +1008,63 @@ int fkv_decode_step(fkv_cache *c, const void *k, const void *v, const int32_t *p
                                  (cudaStream_t)stream);
     if (rc) return rc;
   }
+  return FKV_OK;
+}
+
+int fkv_append_chunk(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos, const int32_t *keep_lens,
+                     const int32_t *chunk_lens, void *stream) {
+  ChunkLens lens;
+  if (int e = check_append_chunk(c, layer, k, v, keep_lens, chunk_lens, lens)) return e;
+  return launch_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens, (cudaStream_t)stream);
+}
+
+int fkv_chunk_attn(fkv_cache *c, int layer, const void *q, const int32_t *chunk_lens, int32_t window, int32_t sinks, float scale,
+                   void *out, float *lse_out, void *stream) {
+  ChunkLens lens;
+  if (int e = check_chunk(c, layer, q, chunk_lens, window, sinks, scale, lens)) return e;
+  if (lens.tok[c->cfg.max_batch] > 0 && (!out || !aligned(out, 16))) return FKV_ERR_INVALID_ARG;
+  if (!chunk_is_stored(c, layer, chunk_lens)) return FKV_ERR_INVALID_ARG;
+  return launch_chunk_attend(c, layer, q, chunk_lens, lens, window, sinks, scale, out, lse_out, (cudaStream_t)stream);
+}
+
+int fkv_append_chunk_attn(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos, const int32_t *keep_lens,
+                          const int32_t *chunk_lens, const void *q, int32_t window, int32_t sinks, float scale, void *out,
+                          float *lse_out, void *stream) {
+  ChunkLens lens;
+  if (int e = check_chunk(c, layer, q, chunk_lens, window, sinks, scale, lens)) return e;
+  if (int e = check_append_chunk(c, layer, k, v, keep_lens, chunk_lens, lens)) return e;
+  if (lens.tok[c->cfg.max_batch] > 0 && (!out || !aligned(out, 16))) return FKV_ERR_INVALID_ARG;
+  if (int e = launch_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens, (cudaStream_t)stream)) return e;
+  return launch_chunk_attend(c, layer, q, chunk_lens, lens, window, sinks, scale, out, lse_out, (cudaStream_t)stream);
+}
+
+int fkv_decode_attn_window(fkv_cache *c, int layer, const void *q, const int32_t *q_pos, int32_t window, int32_t sinks, void *out,
+                           float scale, void *stream) {
+  if (!c || !layer_ok(c, layer) || !q || !out || window < 1 || sinks < 0) return FKV_ERR_INVALID_ARG;
+  Window w;
+  w.window = window; w.sinks = sinks; w.q_pos = q_pos;
+  return launch_attend(c, layer, q, out, scale, nullptr, nullptr, nullptr, make_mask(c, nullptr), false, (cudaStream_t)stream, w);
+}
+
+int fkv_append_decode_attn_window(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos,
+                                  const uint64_t *seq_mask, const void *q, int32_t window, int32_t sinks, void *out, float scale,
+                                  void *stream) {
+  if (!c || !layer_ok(c, layer) || !k || !v || !q || !out || window < 1 || sinks < 0) return FKV_ERR_INVALID_ARG;
+  const int batch = c->cfg.max_batch;
+  const SeqMask m = make_mask(c, seq_mask);
+  for (int s = 0; s < batch; ++s)
+    if (m.has(s) && c->h_len[(size_t)layer * batch + s] >= c->lay.cap) return FKV_ERR_CAPACITY;
+  Window w;
+  w.window = window; w.sinks = sinks;
+  return launch_attend(c, layer, q, out, scale, k, v, pos, m, false, (cudaStream_t)stream, w);
+}
+
+int fkv_export_features(fkv_cache *c, int layer, int seq, float *feat, void *stream) {
+  if (!c || !layer_ok(c, layer) || seq < 0 || seq >= c->cfg.max_batch || !feat) return FKV_ERR_INVALID_ARG;
+  const int n = c->h_len[(size_t)layer * c->cfg.max_batch + seq];
+  if (n == 0) return FKV_OK;
+  k_export_features<<<dim3((n + 7) / 8, c->cfg.num_kv_heads), 256, 0, (cudaStream_t)stream>>>(c->ctx, layer, seq, n, feat);
+  FKV_LAUNCHED(c);
   return FKV_OK;
 }
 

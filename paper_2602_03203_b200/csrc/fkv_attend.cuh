@@ -85,6 +85,8 @@ struct AttendArgs {
   const uint8_t *k_new, *v_new;  // [batch][Hkv][D] bf16
   const int32_t *pos_new;   // [batch] or null (last position + 1)
   SeqMask seq_mask;         // sequences that append
+  int window, sinks;        // windowed attention (template WIN): last `window` positions and those below `sinks`
+  const int32_t *q_pos;     // [batch] positions of the queries or null (the last pair's); not used when appending
   int wait_first;           // 1: the grid was launched with the programmatic attribute but depends on everything
                             // before it: wait for the launch before it ahead of the first global read
 };
@@ -191,7 +193,11 @@ __device__ __forceinline__ void merge_partials(const float *part, int nact, int 
 // segment's output, receives that slice of every split's partial, and after one cluster barrier reduces and writes
 // it - no partial leaves the SMs and no ticket is taken.  For launches that run on their own (the per-layer entry
 // points at small batch), where the merge's round trips to L2 are a sixth of the launch.
-template <int D, int NCW, int SLOTS, bool CLUSTER>
+// WIN: the query sees the pairs of the last `window` positions up to its own and those of the first `sinks` positions.
+// Positions grow with the slot, so these are slots [0, wa) and [wb, we), found by looking at three stored positions (a
+// search only where positions are missing); the CTAs share out the pages that hold them, and no other page is read.
+// Windowed launches leave no query record: the features describe attention over the whole retained set.
+template <int D, int NCW, int SLOTS, bool CLUSTER, bool WIN>
 __global__ void __launch_bounds__((NCW + 1) * 32, NCW <= 4 ? 3 : 1) k_attend(Ctx c, AttendArgs a) {
   constexpr int KSQ = D / 16;  // k-steps of K Q^T
   constexpr int MT = D / 16;   // m-tiles (16 channels) of O^T = V^T P^T
@@ -222,7 +228,7 @@ __global__ void __launch_bounds__((NCW + 1) * 32, NCW <= 4 ? 3 : 1) k_attend(Ctx
   // pages-per-split figure puts them (entries past the segment's pages are never used), so that the two reads
   // overlap instead of following one another.
   int ptv = 0, ptn = 0;
-  if (warp == NCW) {
+  if (!WIN && warp == NCW) {
     const int e = rank * a.pps + lane;
     if (e < c.max_pages) ptv = __ldcg(ptrow + e);
     if (e + 32 < c.max_pages) ptn = __ldcg(ptrow + e + 32);
@@ -233,7 +239,37 @@ __global__ void __launch_bounds__((NCW + 1) * 32, NCW <= 4 ? 3 : 1) k_attend(Ctx
   const bool app = want && n_old < c.cap;
   if (want && !app && tid == 0 && rank == 0) set_status(c, kDevCapacity);
   const int n = n_old + (app ? 1 : 0);
-  const int npages = (n + kPage - 1) / kPage;
+  // Windowed: slots [0, wa) and [wb, we) are seen; their pages are [0, wsp) and [wp0, ...), counted through.
+  int wa = 0, wb = 0, we = n, wsp = 0, wp0 = 0;
+  int npages = (n + kPage - 1) / kPage;
+  if (WIN) {
+    int stored = 0;   // slots of the stored pairs that are not behind the query's position
+    if (n_old > 0) {
+      const int lo = max(0, n_old - a.window), m = min(a.sinks, n_old);
+      const int pid_last = __ldcg(ptrow + (n_old - 1) / kPage), pid_lo = __ldcg(ptrow + lo / kPage);
+      const int pid_m = __ldcg(ptrow + max(m - 1, 0) / kPage);
+      auto pos_at = [&](int pid, int slot) {
+        return __ldcg(reinterpret_cast<const int32_t *>(meta_row(c, c.pool + (size_t)pid * c.page_bytes, slot % kPage)) + c.F);
+      };
+      const int x_last = pos_at(pid_last, n_old - 1), x_lo = pos_at(pid_lo, lo), x_m = pos_at(pid_m, max(m - 1, 0));
+      const int p = app ? (a.pos_new ? __ldcg(a.pos_new + seq) : x_last + 1) : a.q_pos ? __ldcg(a.q_pos + seq) : x_last;
+      const int first = window_start(p, a.window);
+      stored = n_old;
+      if (x_last > p) {   // some pairs are younger than the query
+        stored = slot_lower_bound(c, ptrow, 0, n_old - 1, p + 1);
+        wb = slot_lower_bound(c, ptrow, 0, stored, first);
+      } else {
+        wb = x_lo >= first ? lo : slot_lower_bound(c, ptrow, lo + 1, n_old, first);
+      }
+      wa = m == 0 ? 0 : min(stored, x_m < a.sinks ? m : slot_lower_bound(c, ptrow, 0, m - 1, a.sinks));
+      wb = max(wa, wb);
+    }
+    we = app ? n : stored;
+    wsp = (wa + kPage - 1) / kPage;
+    wp0 = max(wsp, wb / kPage);
+    npages = wsp + (wb < we ? max(0, (we + kPage - 1) / kPage - wp0) : 0);
+  }
+  auto page_of = [&](int v) { return WIN ? (v < wsp ? v : v - wsp + wp0) : v; };   // page number v of the ones to read
   // Pages per split: the host's figure, or more when the segment has outgrown it since the launch was recorded.
   const int pps = max(a.pps, (npages + S - 1) / S);
   const int pg0 = rank * pps, pg1 = min(npages, pg0 + pps);
@@ -243,7 +279,7 @@ __global__ void __launch_bounds__((NCW + 1) * 32, NCW <= 4 ? 3 : 1) k_attend(Ctx
   const bool fresh = tail && (n_old % kPage) == 0;      // ... which opens a new page: nothing to copy for it
   const size_t qrow0 = ((size_t)seq * c.Hkv + head) * G;  // first query head of the group
   // Query record for the attention features: ring slot of this token in the (layer, sequence) history.
-  const bool rec = app && c.hist_w > 0;
+  const bool rec = !WIN && app && c.hist_w > 0;
   const int hcnt = rec ? __ldcg(c.hist_cnt + a.layer * c.batch + seq) : 0;
   const int hslot = rec ? hcnt % c.hist_w : 0;
   const size_t hhead = (size_t)(a.layer * c.batch + seq) * (c.Hkv * G) + (size_t)head * G;   // first query head of the group in the record
@@ -282,9 +318,9 @@ __global__ void __launch_bounds__((NCW + 1) * 32, NCW <= 4 ? 3 : 1) k_attend(Ctx
     }
     __syncwarp();
     // ptv / ptn: page ids of the CTA's pages [0, 32) and [32, 64), one per lane.
-    if (active && pps != a.pps) {   // the early read looked in the wrong place
-      ptv = lane < npg ? __ldcg(ptrow + pg0 + lane) : 0;
-      ptn = 32 + lane < npg ? __ldcg(ptrow + pg0 + 32 + lane) : 0;
+    if (active && (WIN || pps != a.pps)) {   // the early read looked in the wrong place
+      ptv = lane < npg ? __ldcg(ptrow + page_of(pg0 + lane)) : 0;
+      ptn = 32 + lane < npg ? __ldcg(ptrow + page_of(pg0 + 32 + lane)) : 0;
     }
     if (lane < SLOTS && lane < npg) issue(lane, ptv);         // the ring is empty: no wait
     cta_sync();
@@ -333,12 +369,12 @@ __global__ void __launch_bounds__((NCW + 1) * 32, NCW <= 4 ? 3 : 1) k_attend(Ctx
             atomicOr(&c.seq_fail[a.layer * c.batch + seq], 1);
           } else {
             npid = __ldcg(c.free_stack + old - 1);
-            ptrow[npages - 1] = npid;
+            ptrow[page_of(npages - 1)] = npid;
           }
         }
         npid = __shfl_sync(0xffffffffu, npid, 0);
       } else {
-        npid = __ldcg(ptrow + npages - 1);
+        npid = __ldcg(ptrow + page_of(npages - 1));
       }
       if (npid >= 0) {
         int32_t pdef = 0;
@@ -361,7 +397,7 @@ __global__ void __launch_bounds__((NCW + 1) * 32, NCW <= 4 ? 3 : 1) k_attend(Ctx
     for (int i = SLOTS; i < npg; i += NCW) {
       if ((i & 31) == 0) {
         ptv = ptn;
-        ptn = i + 32 + lane < npg ? __ldcg(ptrow + pg0 + i + 32 + lane) : 0;
+        ptn = i + 32 + lane < npg ? __ldcg(ptrow + page_of(pg0 + i + 32 + lane)) : 0;
       }
       const int pid = __shfl_sync(0xffffffffu, ptv, (i + lane) & 31);
       bool ok = true;
@@ -414,6 +450,16 @@ __global__ void __launch_bounds__((NCW + 1) * 32, NCW <= 4 ? 3 : 1) k_attend(Ctx
               newrow;
         __syncwarp();
       }
+      const int slot0 = page_of(pg0 + i) * kPage;
+      auto seen = [&](int slot) { return WIN ? slot < wa || (slot >= wb && slot < we) : slot < n; };
+      if (WIN && !__all_sync(0xffffffffu, seen(slot0 + (lane & 15)))) {
+        // Hidden rows get p = 0, but zero times an infinity is not zero: their V rows are cleared.
+        for (int j = lane; j < kPage * NCH; j += 32)
+          if (!seen(slot0 + j / NCH))
+            *reinterpret_cast<uint4 *>(page + 2 * D + kv_chunk_off(j / NCH, j % NCH, D)) = make_uint4(0u, 0u, 0u, 0u);
+        fence_proxy_async();   // (the next copy into this slot comes after these writes)
+        __syncwarp();
+      }
       const uint32_t kbase = smem_u32(page), vbase = kbase + 2 * D;
       // S^T (16 keys x 8 queries) = K (16 x D) Q^T (D x 8): keys on the M axis, two accumulation chains.
       float sa[4] = {0.f, 0.f, 0.f, 0.f}, sb[4] = {0.f, 0.f, 0.f, 0.f};
@@ -426,8 +472,8 @@ __global__ void __launch_bounds__((NCW + 1) * 32, NCW <= 4 ? 3 : 1) k_attend(Ctx
         mma_bf16(sb, z[0], z[1], z[2], z[3], qb[ks + 1][0], qb[ks + 1][1]);
       }
       // This lane: keys gid and gid + 8 of the page, queries 2 tig and 2 tig + 1.
-      const int slot = (pg0 + i) * kPage + gid;
-      const bool ok0 = slot < n, ok1 = slot + 8 < n;
+      const int slot = slot0 + gid;
+      const bool ok0 = seen(slot), ok1 = seen(slot + 8);
       const float v0 = ok0 ? (sa[0] + sb[0]) * a.scale_log2 : -INFINITY, v1 = ok0 ? (sa[1] + sb[1]) * a.scale_log2 : -INFINITY;
       const float v2 = ok1 ? (sa[2] + sb[2]) * a.scale_log2 : -INFINITY, v3 = ok1 ? (sa[3] + sb[3]) * a.scale_log2 : -INFINITY;
       float mx0 = fmaxf(v0, v2), mx1 = fmaxf(v1, v3);

@@ -83,6 +83,16 @@ __global__ void k_export_rows(Ctx c, int layer, int seq, int head, uint8_t *k, u
               feat ? feat + (size_t)i * c.F : nullptr, pos ? pos + i : nullptr, lane, 0);
 }
 
+// grid (ceil(n / 8), Hkv), 256 threads: dense copy [Hkv][n][F] of a (layer, sequence)'s features, one warp per pair.
+__global__ void k_export_features(Ctx c, int layer, int seq, int n, float *feat) {
+  if (c.len[layer * c.batch + seq] != n) return;  // not the length the caller's tensor was made for
+  const int lane = threadIdx.x & 31, i = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5), h = blockIdx.y;
+  if (i >= n) return;
+  const int seg = seg_of(c, layer, seq, h);
+  const float *pf = meta_row(c, c.pool + (size_t)c.pt[(size_t)seg * c.max_pages + i / kPage] * c.page_bytes, i % kPage);
+  for (int f = lane; f < c.F; f += 32) feat[((size_t)h * n + i) * c.F + f] = pf[f];
+}
+
 // ---------------------------------------------------------------- append
 // grid = batch, block = 32 * Hkv: one warp per KV head writes the new pair at
 // slot n; a new page per head is popped from the free stack when n % 16 == 0.

@@ -1,0 +1,914 @@
+// Kernel 8: a chunk of new tokens per sequence - the pairs are stored behind the ones that stay, and every token of the
+// chunk attends over the pairs up to its own:
+//     z_ji = scale <q_j, k_i>,   lse_j = ln sum_{i in Seen(j)} e^{z_ji},   o_j = sum_{i in Seen(j)} e^{z_ji - lse_j} v_i,
+// Seen(j) = the pairs i at or before query j's own slot with (no window, or p_j - x_i < window, or x_i < sinks): x_i and
+// p_j are token positions, so a window means the same before and after an eviction.  Positions grow with the slot: the
+// pairs a query sees are slots [0, a) and [w_j, e_j), a and w_j found by searching the stored positions.
+//
+// Bound: 4 D flops and one exp2 per (query head, seen pair); with few query rows per KV head the bytes of the pairs
+// (4 D each, once per group) take longer.
+//
+// Layout of the contraction.  The g query heads of a group share K and V, so a tile of 128 query rows is (128 / g tokens)
+// x (g heads); an item of work is one KV head x two such tiles over the pages their tokens see.  One persistent CTA per
+// SM; the pages of all items form one line that is cut into equal ranges, one per CTA, so the split is even whatever the
+// batch looks like (one long sequence, many short ones, drafts of a few tokens over long caches).  An item that a cut
+// goes through leaves partial results (O, m, l) which k_chunk_merge joins.
+//   warp 0      tensor copies (TMA): the item's query tiles, then K and V page by page (one copy = 16 rows x 64 channels;
+//               the page record's swizzle is the shared-memory swizzle) into a ring of key tiles of up to eight pages;
+//   warp 1      one lane issues tcgen05.mma: S = Q K^T (K-major operands) into tensor memory, O += P V with P read from
+//               tensor memory and V as an MN-major operand (channels run along its rows: no transpose anywhere);
+//   warp 2      walks the items ahead of the others and searches the positions;
+//   warps 4-11  two warpgroups, each with a stream of its own (S and O accumulators): thread = query row; running
+//               maximum, exp2, row sum in fp32, P rounded to bf16 into the columns of S.  O is rescaled only when the
+//               maximum has grown by more than 2^8: until then P is at most 256, which bf16 holds as exactly as 1.
+// The streams are the item's two query tiles; an item with one tile gives its key tiles to the streams in turn, and the
+// streams' results are joined through shared memory.
+// Every wait is bounded; tensor memory is freed at the common exit.
+#pragma once
+#include <cuda.h>
+#include <limits.h>
+#include "fkv_dev.cuh"
+#include "fkv_attend.cuh"
+#include "fkv_features.cuh"
+#include "fkv_rkv.cuh"
+
+namespace fkv {
+
+constexpr int kChunkCtas = 148;       // most CTAs of a launch: each has two slots for partial results in the workspace
+constexpr int kChunkThreads = 384;
+constexpr int kChunkRows = 128;       // query rows of a tile = M of the mma
+constexpr int kChunkPages = 8;        // pages of a key tile: N of S, K of O
+constexpr int kChunkMinPages = 8;     // least work of a CTA
+constexpr int kChunkInfo = 8;         // words that describe a CTA's unfinished item to the merge
+constexpr float kChunkGrow = 8.f;     // log2 of the growth of a row's maximum that O is rescaled for
+constexpr int kChunkItems = 2;        // items the walk may be ahead by
+
+// Prefix sums of the chunk lengths over the sequences, and the pairs that stay (use == 0: all of them).
+struct ChunkLens {
+  int tok[kMaxBatch + 1];
+};
+struct ChunkKeep {
+  int use;
+  int keep[kMaxBatch];
+};
+
+// ---------------------------------------------------------------- storing the chunk
+// Every CTA works the page arithmetic out for itself (one thread per sequence, two prefix sums): pages to take from the
+// free stack where a sequence grows past its last page, pages to return where it shrinks.  A warp stores one pair.  The
+// last CTA to finish returns pages, moves the stack top and the lengths and takes rolled-back queries off the record.
+// A sequence that the device finds past its capacity or shorter than `keep` is skipped; without enough free pages the
+// whole call is.
+__global__ void __launch_bounds__(256) k_append_chunk(Ctx c, int layer, const uint8_t *k, const uint8_t *v, const int32_t *pos,
+                                                      const __grid_constant__ ChunkLens lens,
+                                                      const __grid_constant__ ChunkKeep keep) {
+  static_assert(kMaxBatch <= 256, "one thread per sequence");
+  __shared__ int s_scan[33];
+  __shared__ int s_keep[kMaxBatch], s_old[kMaxBatch], s_pop[kMaxBatch], s_push[kMaxBatch];
+  __shared__ int s_last;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  griddep_wait();
+  griddep_launch();
+  const int s = tid;
+  int n_old = 0, kp = 0, T = 0, pop = 0, push = 0, bad = 0;
+  if (s < c.batch) {
+    n_old = __ldcg(c.len + layer * c.batch + s);
+    T = lens.tok[s + 1] - lens.tok[s];
+    kp = keep.use ? keep.keep[s] : n_old;
+    if (kp > n_old) { bad = (int)kDevBadIndex; kp = -1; }
+    else if (kp + T > c.cap) { bad = (int)kDevCapacity; kp = -1; }
+    if (kp >= 0) {
+      const int delta = (kp + T + kPage - 1) / kPage - (n_old + kPage - 1) / kPage;
+      pop = delta > 0 ? delta * c.Hkv : 0;
+      push = delta < 0 ? -delta * c.Hkv : 0;
+    }
+    s_keep[s] = kp;
+    s_old[s] = n_old;
+  }
+  int pops, pushes;
+  const int pop_off = block_excl_scan(pop, s_scan, pops);
+  const int push_off = block_excl_scan(push, s_scan, pushes);
+  if (s < c.batch) { s_pop[s] = pop_off; s_push[s] = push_off; }
+  const int top = __ldcg(c.ctrl + CTRL_FREE_TOP);
+  const bool exhausted = pops > top;
+  if (blockIdx.x == 0) {
+    if (bad) set_status(c, (unsigned)bad);
+    if (exhausted && tid == 0) set_status(c, kDevPoolExhausted);
+  }
+  __syncthreads();
+  if (!exhausted) {
+    const long long tasks = (long long)lens.tok[c.batch] * c.Hkv;
+    for (long long t = (long long)blockIdx.x * 8 + warp; t < tasks; t += (long long)gridDim.x * 8) {
+      const int row = (int)(t / c.Hkv), h = (int)(t - (long long)row * c.Hkv);
+      int lo = 0, hi = c.batch;   // the sequence of the row: the last one that starts at or before it
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (lens.tok[mid] <= row) lo = mid; else hi = mid;
+      }
+      const int kp_s = s_keep[lo];
+      if (kp_s < 0) continue;
+      const int j = row - lens.tok[lo], slot = kp_s + j, pg = slot / kPage;
+      const int np_old = (s_old[lo] + kPage - 1) / kPage;
+      const int grow = (kp_s + lens.tok[lo + 1] - lens.tok[lo] + kPage - 1) / kPage - np_old;
+      int *ptrow = c.pt + (size_t)seg_of(c, layer, lo, h) * c.max_pages;
+      int pid;
+      if (pg < np_old) {
+        pid = __ldcg(ptrow + pg);
+      } else {
+        pid = __ldcg(c.free_stack + top - 1 - (s_pop[lo] + h * grow + pg - np_old));
+        if (lane == 0 && (slot % kPage == 0 || j == 0)) ptrow[pg] = pid;
+      }
+      int32_t pdef = j;
+      if (!pos && kp_s > 0) {   // the position after the last pair that stays
+        const uint8_t *prev = c.pool + (size_t)__ldcg(ptrow + (kp_s - 1) / kPage) * c.page_bytes;
+        pdef = __ldcg(reinterpret_cast<const int32_t *>(meta_row(c, prev, (kp_s - 1) % kPage)) + c.F) + 1 + j;
+      }
+      const size_t at = ((size_t)row * c.Hkv + h) * c.D * 2;
+      move_row<0>(c, c.pool + (size_t)pid * c.page_bytes, slot % kPage, const_cast<uint8_t *>(k) + at,
+                  const_cast<uint8_t *>(v) + at, nullptr, pos ? const_cast<int32_t *>(pos) + row : nullptr, lane, pdef);
+    }
+  }
+  __threadfence();
+  __syncthreads();
+  if (tid == 0) s_last = atomicAdd(&c.ctrl[CTRL_CHUNK_TICKET], 1) == (int)gridDim.x - 1;
+  __syncthreads();
+  if (!s_last) return;
+  __threadfence();
+  if (tid == 0) c.ctrl[CTRL_CHUNK_TICKET] = 0;
+  if (exhausted) return;
+  // Freed pages go where the taken ones came from and above (every CTA has read those entries by now).
+  for (int q = 0; q < c.batch; ++q) {
+    if (s_keep[q] < 0) continue;
+    const int np_new = (s_keep[q] + lens.tok[q + 1] - lens.tok[q] + kPage - 1) / kPage;
+    const int cnt = (s_old[q] + kPage - 1) / kPage - np_new;
+    for (int i = tid; i < cnt * c.Hkv; i += blockDim.x) {
+      const int h = i / cnt, p = i - h * cnt;
+      c.free_stack[top - pops + s_push[q] + i] = __ldcg(c.pt + (size_t)seg_of(c, layer, q, h) * c.max_pages + np_new + p);
+    }
+  }
+  if (tid == 0) c.ctrl[CTRL_FREE_TOP] = top - pops + pushes;
+  if (s < c.batch && kp >= 0) {
+    const int ls = layer * c.batch + s;
+    c.len[ls] = kp + T;
+    if (c.hist_w && kp < n_old) {
+      // Queries of rolled-back tokens leave the record (lengths seen grow along it, so they are its newest entries); a
+      // record that has wrapped has lost the entries that would take their place and starts over.
+      const int cnt0 = c.hist_cnt[ls];
+      int cnt = cnt0;
+      while (cnt > 0 && cnt > cnt0 - c.hist_w && c.hist_n[(size_t)ls * c.hist_w + (cnt - 1) % c.hist_w] > kp) --cnt;
+      c.hist_cnt[ls] = (cnt < cnt0 && cnt0 > c.hist_w) ? 0 : cnt;
+    }
+  }
+}
+
+// ---------------------------------------------------------------- attention over the chunk
+struct ChunkArgs {
+  int layer, window, sinks;
+  float scale, scale_log2;
+  __nv_bfloat16 *out;   // [tokens][Hkv * g][D]
+  float *lse;           // [tokens][Hkv * g] or null
+  ChunkLens lens;
+};
+
+// One item as the walk hands it to the other roles: slots and pages are those of the item's segment.
+struct ChunkItem {
+  int kind;        // 0: no more items, 1: two query tiles, 2: one query tile
+  int head, seg;
+  int row0;        // packed index of the first token
+  int ntok[2];     // tokens of the two tiles
+  int e0;          // slots up to and with the first token's own
+  int n;           // pairs of the segment
+  int a;           // slots [0, a) are sinks
+  int pa0, pa1;    // pages of the sinks ...
+  int pb0, pb1;    // ... and of the rest that this CTA takes
+  int part;        // -1: the whole item is here; 0 / 1: the slot for the partial result
+  int pad[2];
+};
+
+template <int D>
+struct ChunkSmem {
+  static constexpr int kSlots = D == 128 ? 4 : 8;
+  static constexpr size_t kTile = (size_t)(D / 64) * 128 * 128;   // 128 rows: [D / 64][128][128 B]
+  static constexpr size_t kMerge = 32 * 128 * 4;
+  static constexpr size_t kOffRing = 2 * kTile;
+  static constexpr size_t kOffMerge = kOffRing + kSlots * kTile;
+  static constexpr size_t kOffMl = kOffMerge + kMerge;                 // (m, l) of the second stream's rows
+  static constexpr size_t kOffItems = kOffMl + 128 * 8;
+  static constexpr size_t kOffWlo = kOffItems + kChunkItems * sizeof(ChunkItem);   // first slot of every token's window
+  static constexpr size_t kOffLen = kOffWlo + kChunkItems * 256 * 4;
+  static constexpr size_t kOffBlk = kOffLen + kMaxBatch * 4;
+  static constexpr size_t kOffBars = (kOffBlk + (kMaxBatch + 1) * 4 + 15) & ~(size_t)15;
+  static constexpr size_t bytes() { return 1024 + kOffBars + 512; }   // (more than half an SM's: one CTA each)
+};
+
+// Pages that the tokens [j0, j1) of a chunk of T tokens may see in a segment of n pairs, from the lengths alone (a window
+// of W positions holds at most W pairs): sink pages [0, sp) and pages [b0, b1).
+struct ChunkRange {
+  int sp, b0, b1;
+  __device__ __forceinline__ int units() const { return sp + b1 - b0; }
+};
+__device__ __forceinline__ ChunkRange chunk_range(int n, int T, int j0, int j1, int W, int S) {
+  ChunkRange r;
+  const int e_first = n - T + j0 + 1, e_last = n - T + j1;
+  r.b1 = (e_last + kPage - 1) / kPage;
+  r.b0 = W ? max(0, e_first - W) / kPage : 0;
+  r.sp = W ? (min(S, e_last) + kPage - 1) / kPage : 0;
+  if (r.b0 <= r.sp) r.b0 = r.sp = 0;
+  return r;
+}
+
+// Matrix descriptor of an operand whose channels run along its 128-byte rows (MN-major, 128-byte swizzle): 64 channels
+// to a row, 8-row groups 1024 bytes apart along K, the next 64 channels a whole tile half (128 rows) further.
+__device__ __forceinline__ uint64_t umma_desc_mn_sw128(uint32_t smem_addr) {
+  return (uint64_t)((smem_addr & 0x3ffffu) >> 4) | ((uint64_t)(128u * 128u >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) |
+         (1ull << 46) | (2ull << 61);
+}
+// D += A B with A (128 rows x 16, bf16, two to a column) in tensor memory.
+__device__ __forceinline__ void umma_bf16_ta(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+               ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]),
+               "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// 64 channels of the g heads x the tokens of one query tile (rows of 128 bytes, swizzled).
+__device__ __forceinline__ void tma_chunk_q(uint32_t dst, const CUtensorMap *tm, int ch, int head, int tok, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(ch), "r"(head), "r"(tok), "r"(bar)
+      : "memory");
+}
+
+template <int D>
+__global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const __grid_constant__ CUtensorMap tmkv,
+                                                                   const __grid_constant__ CUtensorMap tmq,
+                                                                   const __grid_constant__ ChunkArgs a) {
+  using SM = ChunkSmem<D>;
+  constexpr int NS = SM::kSlots, NQ = D / 64, TP = kChunkPages;
+  constexpr uint32_t PAGE_HALF = kPage * 128;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  uint8_t *Qt = smem, *Ring = smem + SM::kOffRing;
+  float *Mg = reinterpret_cast<float *>(smem + SM::kOffMerge);
+  float2 *Ml = reinterpret_cast<float2 *>(smem + SM::kOffMl);
+  ChunkItem *Items = reinterpret_cast<ChunkItem *>(smem + SM::kOffItems);
+  int *Wlo = reinterpret_cast<int *>(smem + SM::kOffWlo);
+  int *Len = reinterpret_cast<int *>(smem + SM::kOffLen), *Blk = reinterpret_cast<int *>(smem + SM::kOffBlk);
+  uint64_t *bars = reinterpret_cast<uint64_t *>(smem + SM::kOffBars);
+  uint64_t *kv_full = bars, *kv_empty = kv_full + NS, *q_full = kv_empty + NS, *q_empty = q_full + 2;
+  uint64_t *s_full = q_empty + 2, *p_full = s_full + 2, *o_full = p_full + 2, *o_empty = o_full + 2;
+  uint64_t *it_full = o_empty + 2, *it_empty = it_full + kChunkItems, *j_full = it_empty + kChunkItems, *j_empty = j_full + 1;
+  uint64_t *mma_done = j_empty + 1;
+  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(mma_done + 1);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, G = c.G, TPT = kChunkRows / G;
+
+  if (warp == 3) tmem_alloc(smem_u32(tmem_slot), 512);
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < NS; ++s) { mbar_init(smem_u32(&kv_full[s]), 1); mbar_init(smem_u32(&kv_empty[s]), 1); }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(smem_u32(&q_full[t]), 1); mbar_init(smem_u32(&q_empty[t]), 1);
+      mbar_init(smem_u32(&s_full[t]), 1); mbar_init(smem_u32(&p_full[t]), 4);
+      mbar_init(smem_u32(&o_full[t]), 1); mbar_init(smem_u32(&o_empty[t]), 4);
+    }
+    for (int i = 0; i < kChunkItems; ++i) { mbar_init(smem_u32(&it_full[i]), 1); mbar_init(smem_u32(&it_empty[i]), 10); }
+    mbar_init(smem_u32(j_full), 4); mbar_init(smem_u32(j_empty), 4);
+    mbar_init(smem_u32(mma_done), 1);
+    fence_barrier_init();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;   // columns: S0 | S1 | O0 | O1, 128 each
+  griddep_wait();                          // everything below reads what earlier launches wrote
+  griddep_launch();
+
+  if (warp == 2) {
+    // ---------------- the walk over this CTA's range of the line of pages ----------------
+    const int batch = c.batch, W = a.window, S = a.sinks, TB = 2 * TPT;
+    for (int s = lane; s < batch; s += 32) {
+      const int n = __ldcg(c.len + a.layer * batch + s);
+      Len[s] = n;
+      // (the host checks the lengths it knows; a replayed launch is checked here)
+      if (blockIdx.x == 0 && n < a.lens.tok[s + 1] - a.lens.tok[s]) set_status(c, kDevBadIndex);
+    }
+    int NB = 0;   // blocks of two query tiles, over the sequences
+    for (int s0 = 0; s0 < batch; s0 += 32) {
+      const int s = s0 + lane;
+      const int nb = s < batch ? (a.lens.tok[s + 1] - a.lens.tok[s] + TB - 1) / TB : 0;
+      int inc = nb;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += t;
+      }
+      if (s < batch) Blk[s] = NB + inc - nb;
+      NB += __shfl_sync(0xffffffffu, inc, 31);
+    }
+    if (lane == 0) Blk[batch] = NB;
+    __syncwarp();
+    struct Block { int s, j0, j1, n, T; ChunkRange r; int units; };
+    auto block = [&](int f) {
+      Block b;
+      int lo = 0, hi = batch;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (Blk[mid] <= f) lo = mid; else hi = mid;
+      }
+      b.s = lo;
+      b.T = a.lens.tok[lo + 1] - a.lens.tok[lo];
+      b.n = Len[lo];
+      b.j0 = (f - Blk[lo]) * TB;
+      b.j1 = min(b.T, b.j0 + TB);
+      b.units = 0;
+      if (b.n >= b.T) {
+        b.r = chunk_range(b.n, b.T, b.j0, b.j1, W, S);
+        b.units = b.r.units();
+      }
+      return b;
+    };
+    long long P = 0;   // pages of one KV head
+    for (int f0 = 0; f0 < NB; f0 += 32) {
+      int u = f0 + lane < NB ? block(f0 + lane).units : 0;
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1) u += __shfl_xor_sync(0xffffffffu, u, o);
+      P += u;
+    }
+    const long long total = P * c.Hkv;
+    const long long per = max((long long)kChunkMinPages, (total + gridDim.x - 1) / gridDim.x);
+    long long u = per * blockIdx.x;
+    const long long u_end = min(total, u + per);
+    int *info = c.chunk_info + blockIdx.x * kChunkInfo;
+    int head = 0, f = 0, off = 0, it = 0;
+    bool open = false;   // this CTA begins an item that others go on with
+    if (u < u_end) {
+      head = (int)(u / P);
+      long long rem = u - head * P;
+      for (int f0 = 0; f0 < NB; f0 += 32) {   // the block that holds page `rem`
+        const int un = f0 + lane < NB ? block(f0 + lane).units : 0;
+        int inc = un;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int t = __shfl_up_sync(0xffffffffu, inc, o);
+          if (lane >= o) inc += t;
+        }
+        const unsigned in = __ballot_sync(0xffffffffu, rem < inc);
+        if (in) {
+          const int l = __ffs(in) - 1;
+          f = f0 + l;
+          off = (int)rem - __shfl_sync(0xffffffffu, inc - un, l);
+          break;
+        }
+        rem -= __shfl_sync(0xffffffffu, inc, 31);
+      }
+    }
+    bool ok = true;
+    while (ok) {
+      const int ri = it % kChunkItems;
+      const bool more = u < u_end;
+      if (!mbar_wait_warp(smem_u32(&it_empty[ri]), ((it / kChunkItems) & 1) ^ 1)) { set_status(c, kDevWaitTimeout); break; }
+      ChunkItem *x = Items + ri;
+      if (!more) {
+        if (lane == 0) { x->kind = 0; mbar_arrive(smem_u32(&it_full[ri])); }
+        break;
+      }
+      const Block b = block(f);
+      if (b.units > 0) {
+        const int take = (int)min((long long)(b.units - off), u_end - u);
+        const int ntok = b.j1 - b.j0, nt0 = min(ntok, TPT), seg = seg_of(c, a.layer, b.s, head);
+        const int *ptrow = c.pt + (size_t)seg * c.max_pages;
+        // This CTA's pages of the item: [pa0, pa1) at the front, [pb0, pb1) behind; with a window, less the pages that
+        // the stored positions show to be hidden from every token.
+        int pa0 = min(off, b.r.sp), pa1 = min(off + take, b.r.sp);
+        int pb0 = b.r.b0 + max(off - b.r.sp, 0), pb1 = b.r.b0 + max(off + take - b.r.sp, 0);
+        int na = 0;
+        if (W) {
+          na = S ? slot_sinks(c, ptrow, b.n, S) : 0;
+          const int e0 = b.n - b.T + b.j0 + 1;
+          int first = 0;
+          for (int i0 = 0; i0 < ntok; i0 += 32) {
+            int w = 0;
+            if (i0 + lane < ntok) {
+              const int last = e0 + i0 + lane - 1;
+              w = slot_window(c, ptrow, last, slot_pos(c, ptrow, last), W);
+              Wlo[ri * 256 + i0 + lane] = w;
+            }
+            if (i0 == 0) first = __shfl_sync(0xffffffffu, w, 0);
+          }
+          const int a16 = (na + kPage - 1) / kPage, w16 = first / kPage;
+          if (b.r.sp == 0) {   // one run of pages: split it around the hidden ones
+            pa0 = pb0;
+            pa1 = max(pa0, min(pb1, a16));
+            pb0 = min(pb1, max(pb0, max(a16, w16)));
+          } else {
+            pa1 = max(pa0, min(pa1, a16));
+            pb0 = min(pb1, max(pb0, w16));
+          }
+        }
+        const long long U0 = u - off;
+        const int cf = (int)(U0 / per), cl = (int)((U0 + b.units - 1) / per);
+        const int part = cf == cl ? -1 : cf == (int)blockIdx.x ? 1 : 0;
+        if (lane == 0) {
+          x->kind = ntok > nt0 ? 1 : 2;
+          x->head = head; x->seg = seg;
+          x->row0 = a.lens.tok[b.s] + b.j0;
+          x->ntok[0] = nt0; x->ntok[1] = ntok - nt0;
+          x->e0 = b.n - b.T + b.j0 + 1;
+          x->n = b.n; x->a = na;
+          x->pa0 = pa0; x->pa1 = pa1; x->pb0 = pb0; x->pb1 = pb1;
+          x->part = part;
+          if (part == 1) {
+            info[0] = cl; info[1] = head; info[2] = x->row0; info[3] = nt0; info[4] = ntok - nt0;
+          }
+        }
+        if (part == 1) open = true;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&it_full[ri]));
+        ++it;
+        u += take;
+      }
+      off = 0;
+      if (++f == NB) { f = 0; ++head; }
+    }
+    if (!open && lane == 0) info[0] = -1;
+  } else if (warp == 0) {
+    // ---------------- copies ----------------
+    FeatRing rr{0, 0};
+    int it = 0, nq[2] = {0, 0};
+    uint32_t armed = 0, armed_par = 0;    // bit s: ring slot s (bit 16 + t: query tile t) has been armed / its last parity
+    bool ok = true;
+    const int pg = lane & 7, half = lane >> 3;
+    while (ok) {
+      const int ri = it % kChunkItems;
+      if (!mbar_wait_warp(smem_u32(&it_full[ri]), (it / kChunkItems) & 1)) { set_status(c, kDevWaitTimeout); break; }
+      const ChunkItem x = Items[ri];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&it_empty[ri]));
+      ++it;
+      if (x.kind == 0) break;
+      const int ntA = (x.pa1 - x.pa0 + TP - 1) / TP, nt = ntA + (x.pb1 - x.pb0 + TP - 1) / TP;
+      if (nt == 0) continue;
+      for (int t = 0; t < (x.kind == 1 ? 2 : 1) && ok; ++t) {
+        if (!mbar_wait_warp(smem_u32(&q_empty[t]), (nq[t] & 1) ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+        if (lane == 0) {
+          mbar_arrive_expect_tx(smem_u32(&q_full[t]), (uint32_t)(NQ * TPT * G * 128));
+          for (int q = 0; q < NQ; ++q)
+            tma_chunk_q(smem_u32(Qt + t * SM::kTile + (size_t)q * 128 * 128), &tmq, q * 64, x.head * G, x.row0 + t * TPT,
+                        smem_u32(&q_full[t]));
+        }
+        armed |= 1u << (16 + t);
+        armed_par = (armed_par & ~(1u << (16 + t))) | ((uint32_t)(nq[t] & 1) << (16 + t));
+        ++nq[t];
+      }
+      if (!ok) break;
+      const int *ptrow = c.pt + (size_t)x.seg * c.max_pages;
+      auto pages = [&](int i, int &p0) {   // pages of key tile i
+        p0 = i < ntA ? x.pa0 + TP * i : x.pb0 + TP * (i - ntA);
+        return min(TP, (i < ntA ? x.pa1 : x.pb1) - p0);
+      };
+      auto page_id = [&](int i) {
+        if (i >= nt) return 0;
+        int p0;
+        const int np = pages(i, p0);
+        return pg < np ? __ldcg(ptrow + p0 + pg) : 0;
+      };
+      auto copy = [&](int i, int pid, int what) {   // K (0) or V (1) of key tile i
+        int p0;
+        const int np = pages(i, p0);
+        if (!mbar_wait_warp(smem_u32(&kv_empty[rr.i]), rr.ph ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; return; }
+        const uint32_t bar = smem_u32(&kv_full[rr.i]);
+        if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(np * NQ) * PAGE_HALF);
+        armed |= 1u << rr.i;
+        armed_par = (armed_par & ~(1u << rr.i)) | ((uint32_t)rr.ph << rr.i);
+        __syncwarp();
+        if (pg < np && half < NQ)
+          tma_page_k(smem_u32(Ring + rr.i * SM::kTile + (size_t)half * 128 * 128 + (size_t)pg * PAGE_HALF), &tmkv,
+                     what * NQ + half, pid, bar);
+        rr.next(NS);
+      };
+      // K of the first tile(s), then V of a tile and K of the one that the same stream multiplies next.
+      const int ahead = x.kind;   // key tiles between a stream's tile and its next one
+      int id0 = page_id(0), id1 = page_id(1);
+      int idk = ahead == 1 ? id1 : page_id(2);
+      copy(0, id0, 0);
+      if (ahead == 2 && nt > 1 && ok) copy(1, id1, 0);
+      for (int i = 0; i < nt && ok; ++i) {
+        const int idn = page_id(i + ahead + 1);
+        copy(i, id0, 1);
+        if (i + ahead < nt && ok) copy(i + ahead, idk, 0);
+        id0 = id1;
+        id1 = ahead == 1 ? idn : idk;
+        if (ahead == 1) { id0 = idk; }
+        idk = idn;
+      }
+    }
+    // No copy may be in flight at the exit.
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+      if (((armed >> s) & 1u) && !mbar_wait_warp(smem_u32(&kv_full[s]), (armed_par >> s) & 1u)) set_status(c, kDevWaitTimeout);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+      if (((armed >> (16 + t)) & 1u) && !mbar_wait_warp(smem_u32(&q_full[t]), (armed_par >> (16 + t)) & 1u)) set_status(c, kDevWaitTimeout);
+  } else if (warp == 1) {
+    // ---------------- multiplies: the warp stays together, lane 0 issues ----------------
+    FeatRing rr{0, 0};
+    int it = 0, nq[2] = {0, 0};
+    uint32_t np_ph = 0, no_ph = 0;   // bit t: parity of stream t's next p_full / o_empty
+    bool ok = true;
+    const uint32_t idesc_o = umma_idesc_bf16(kChunkRows, D) | (1u << 16);   // B runs along N
+    while (ok) {
+      const int ri = it % kChunkItems;
+      if (!mbar_spin(smem_u32(&it_full[ri]), (it / kChunkItems) & 1)) { set_status(c, kDevWaitTimeout); break; }
+      const ChunkItem x = Items[ri];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&it_empty[ri]));
+      ++it;
+      if (x.kind == 0) break;
+      const int ntA = (x.pa1 - x.pa0 + TP - 1) / TP, nt = ntA + (x.pb1 - x.pb0 + TP - 1) / TP;
+      if (nt == 0) continue;
+      const int ns = x.kind == 1 ? 2 : 1;   // query tiles
+      for (int t = 0; t < ns; ++t) {
+        if (!mbar_spin(smem_u32(&q_full[t]), nq[t] & 1)) { set_status(c, kDevWaitTimeout); ok = false; }
+        ++nq[t];
+      }
+      if (!ok) break;
+      auto pages = [&](int i, int &p0) {
+        p0 = i < ntA ? x.pa0 + TP * i : x.pb0 + TP * (i - ntA);
+        return min(TP, (i < ntA ? x.pa1 : x.pb1) - p0);
+      };
+      auto wait_slot = [&](const FeatRing &r) {
+        if (!mbar_spin(smem_u32(&kv_full[r.i]), r.ph)) { set_status(c, kDevWaitTimeout); ok = false; }
+      };
+      // S of stream t = (query tile qt) (key tile i)^T
+      auto mul_s = [&](int t, int qt, int i, int slot) {
+        int p0;
+        const int np = pages(i, p0);
+        tc_fence_after();
+        if (lane == 0) {
+          const uint32_t idesc = umma_idesc_bf16(kChunkRows, np * kPage);
+          const uint64_t ad = umma_desc_sw128(smem_u32(Qt + qt * SM::kTile)), bd = umma_desc_sw128(smem_u32(Ring + slot * SM::kTile));
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ++ks) {
+            const uint64_t o = (uint64_t)(((ks >> 2) * 128 * 128 + (ks & 3) * 32) >> 4);
+            umma_bf16(tmem_base + t * 128, ad + o, bd + o, idesc, ks > 0);
+          }
+          umma_commit(smem_u32(&s_full[t]));
+        }
+        __syncwarp();
+      };
+      // O of stream t += P (key tile i's V); `first`: the stream's first tile of the item
+      auto mul_o = [&](int t, int i, int slot, bool first) {
+        int p0;
+        const int np = pages(i, p0);
+        if (first) {
+          if (!mbar_spin(smem_u32(&o_empty[t]), ((no_ph >> t) & 1) ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; }
+          no_ph ^= 1u << t;
+        }
+        if (!mbar_spin(smem_u32(&p_full[t]), (np_ph >> t) & 1)) { set_status(c, kDevWaitTimeout); ok = false; }
+        np_ph ^= 1u << t;
+        if (!ok) return;
+        tc_fence_after();
+        if (lane == 0) {
+          const uint64_t bd = umma_desc_mn_sw128(smem_u32(Ring + slot * SM::kTile));
+          for (int ks = 0; ks < np; ++ks)
+            umma_bf16_ta(tmem_base + 256 + t * 128, tmem_base + t * 128 + ks * 8, bd + (uint64_t)((ks * PAGE_HALF) >> 4), idesc_o,
+                         !first || ks > 0);
+        }
+        __syncwarp();
+      };
+      // Rows of the last page past the segment's end hold whatever the page held before: P is zero there, but zero times
+      // an infinity is not, so they are cleared.
+      auto clear_tail = [&](int i, int slot) {
+        int p0;
+        const int np = pages(i, p0), r0 = x.n - p0 * kPage;
+        if (r0 >= np * kPage) return;
+        for (int e = lane; e < (np * kPage - r0) * NQ * 8; e += 32) {
+          const int r = r0 + e / (NQ * 8), ch = e % (NQ * 8);
+          *reinterpret_cast<uint4 *>(Ring + slot * SM::kTile + (size_t)(ch >> 3) * 128 * 128 + r * 128 + (ch & 7) * 16) =
+              make_uint4(0u, 0u, 0u, 0u);
+        }
+        fence_proxy_async();
+        __syncwarp();
+      };
+      auto release = [&](int slot) {
+        if (lane == 0) umma_commit(smem_u32(&kv_empty[slot]));
+        __syncwarp();
+      };
+      if (x.kind == 1) {
+        FeatRing k = rr, v;
+        rr.next(NS);
+        wait_slot(k);
+        if (!ok) break;
+        mul_s(0, 0, 0, k.i);
+        mul_s(1, 1, 0, k.i);
+        release(k.i);
+        for (int i = 0; i < nt && ok; ++i) {
+          const bool more = i + 1 < nt;
+          v = rr;
+          rr.next(NS);
+          k = rr;
+          if (more) rr.next(NS);
+          wait_slot(v);
+          if (!ok) break;
+          clear_tail(i, v.i);
+          for (int t = 0; t < 2 && ok; ++t) {
+            mul_o(t, i, v.i, i == 0);
+            if (!ok) break;
+            if (t == 1) release(v.i);
+            if (!more) {
+              if (lane == 0) umma_commit(smem_u32(&o_full[t]));
+              __syncwarp();
+              continue;
+            }
+            if (t == 0) wait_slot(k);
+            if (!ok) break;
+            mul_s(t, t, i + 1, k.i);
+            if (t == 1) release(k.i);
+            if (i + 2 == nt && lane == 0) umma_commit(smem_u32(&q_empty[t]));   // the tile's last product
+            __syncwarp();
+          }
+        }
+        if (nt == 1 && ok && lane == 0) { umma_commit(smem_u32(&q_empty[0])); umma_commit(smem_u32(&q_empty[1])); }
+      } else {
+        FeatRing k = rr, v;
+        for (int t = 0; t < min(2, nt) && ok; ++t) {
+          k = rr;
+          rr.next(NS);
+          wait_slot(k);
+          if (!ok) break;
+          mul_s(t, 0, t, k.i);
+          release(k.i);
+        }
+        for (int i = 0; i < nt && ok; ++i) {
+          const int t = i & 1;
+          const bool more = i + 2 < nt;
+          v = rr;
+          rr.next(NS);
+          k = rr;
+          if (more) rr.next(NS);
+          wait_slot(v);
+          if (!ok) break;
+          clear_tail(i, v.i);
+          mul_o(t, i, v.i, i < 2);
+          if (!ok) break;
+          release(v.i);
+          if (!more) {
+            if (lane == 0) umma_commit(smem_u32(&o_full[t]));
+            __syncwarp();
+            continue;
+          }
+          wait_slot(k);
+          if (!ok) break;
+          mul_s(t, 0, i + 2, k.i);
+          release(k.i);
+        }
+        if (ok && lane == 0) umma_commit(smem_u32(&q_empty[0]));
+      }
+      __syncwarp();
+    }
+    if (lane == 0) umma_commit(smem_u32(mma_done));   // nothing may be in flight when tensor memory is freed
+    __syncwarp();
+    if (!mbar_spin(smem_u32(mma_done), 0)) set_status(c, kDevWaitTimeout);
+  } else if (warp >= 4) {
+    // ---------------- softmax: thread = query row of stream t ----------------
+    const int t = (warp - 4) >> 2, quarter = warp & 3, R = quarter * 32 + lane;
+    const int tok = R / G, hq = R - tok * G;
+    const uint32_t trow = tmem_base + ((uint32_t)(quarter * 32) << 16);
+    const uint32_t ts = trow + t * 128, to = trow + 256 + t * 128;
+    int it = 0;
+    uint32_t sp = 0, op = 0, jp = 0;   // parities of s_full, o_full and the join's barriers
+    bool ok = true;
+    while (ok) {
+      const int ri = it % kChunkItems;
+      if (!mbar_wait_warp(smem_u32(&it_full[ri]), (it / kChunkItems) & 1)) { set_status(c, kDevWaitTimeout); break; }
+      const ChunkItem x = Items[ri];
+      const int qt = x.kind == 1 ? t : 0;          // the stream's query tile
+      const int tj = qt * TPT + tok;
+      const bool live = x.kind != 0 && tok < (qt ? x.ntok[1] : x.ntok[0]);
+      const bool any = __any_sync(0xffffffffu, live);   // (a warp without a row in use only keeps the hand-overs going)
+      const int e = live ? x.e0 + tj : INT_MAX;    // this row sees slots [0, a) and [wlo, e)
+      const int wlo = live && a.window ? Wlo[ri * 256 + tj] : 0;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&it_empty[ri]));
+      ++it;
+      if (x.kind == 0) break;
+      const int ntA = (x.pa1 - x.pa0 + TP - 1) / TP, nt = ntA + (x.pb1 - x.pb0 + TP - 1) / TP;
+      const int step = x.kind, i0 = x.kind == 1 ? 0 : t;
+      float m = -INFINITY, l = 0.f;
+      for (int i = i0; i < nt; i += step) {
+        const int p0 = i < ntA ? x.pa0 + TP * i : x.pb0 + TP * (i - ntA);
+        const int cols = min(TP, (i < ntA ? x.pa1 : x.pb1) - p0) * kPage;
+        const int hi = min(cols, e - p0 * kPage), lo = wlo - p0 * kPage, na = x.a - p0 * kPage;
+        if (!mbar_wait_warp(smem_u32(&s_full[t]), sp)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+        sp ^= 1;
+        if (!any) {
+          if (lane == 0) mbar_arrive(smem_u32(&p_full[t]));
+          continue;
+        }
+        tc_fence_after();
+        uint32_t s[4][32];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tmem_ld32_issue(ts + q * 32, s[q]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tmem_ld_wait(s[q]);
+        if (!__all_sync(0xffffffffu, hi >= 128 && (lo <= 0 || na >= 128))) {
+#pragma unroll
+          for (int j = 0; j < 128; ++j)
+            if (j >= hi || (j < lo && j >= na)) s[j >> 5][j & 31] = 0xff800000u;   // hidden: -infinity
+        }
+        float mx = -INFINITY;
+        {
+          float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int j = 0; j < 128; j += 8)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              m4[q] = max3(m4[q], __uint_as_float(s[j >> 5][(j & 31) + 2 * q]), __uint_as_float(s[j >> 5][(j & 31) + 2 * q + 1]));
+          mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+        }
+        // The reference follows the maximum only when it has grown by more than 2^8 (or there was none yet).
+        const bool grow = mx > m && (mx - m) * a.scale_log2 > kChunkGrow;
+        if (__any_sync(0xffffffffu, grow)) {
+          const float f = grow ? ex2((m - mx) * a.scale_log2) : 1.f;
+          if (grow) m = mx;
+          l *= f;
+          if (i != i0) {   // the stream's products up to the tile before are complete: this S was multiplied after them
+#pragma unroll
+            for (int q = 0; q < D / 32; ++q) {
+              uint32_t o[32];
+              tmem_ld32_issue(to + q * 32, o);
+              tmem_ld_wait(o);
+#pragma unroll
+              for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+              tmem_st32(to + q * 32, o);
+            }
+          }
+        }
+        const float ms = m == -INFINITY ? 0.f : m * a.scale_log2;
+        float l4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t p[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            const float x0 = ex2(fmaf(__uint_as_float(s[2 * h + (j >> 4)][(2 * j) & 31]), a.scale_log2, -ms));
+            const float x1 = ex2(fmaf(__uint_as_float(s[2 * h + (j >> 4)][(2 * j + 1) & 31]), a.scale_log2, -ms));
+            l4[j & 3] += x0 + x1;
+            p[j] = pack_bf16(x0, x1);   // P in bf16, as V is: at most half a step (2^-9) off, the row sum is not rounded
+          }
+          tmem_st32(ts + h * 32, p);
+        }
+        l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&p_full[t]));
+      }
+      if (!ok) break;
+      // ---- the item's end: this stream's O is complete ----
+      const bool has = i0 < nt;
+      if (has) {
+        if (!mbar_wait_warp(smem_u32(&o_full[t]), op)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+        op ^= 1;
+        tc_fence_after();
+      }
+      const bool join = x.kind == 2 && nt > 1;   // both streams worked on the same rows
+      const size_t orow = ((size_t)(x.row0 + tj) * c.Hkv + x.head) * G + hq;
+      const size_t prow = (size_t)(blockIdx.x * 2 + max(x.part, 0)) * 256 + qt * kChunkRows + R;
+      float f0 = 1.f, f1 = 0.f;   // weights of the two streams' results
+      const bool writes = live && (x.kind == 1 || t == 0);
+#pragma unroll
+      for (int q = 0; q < D / 32; ++q) {
+        uint32_t o[32];
+        if (has) {
+          tmem_ld32_issue(to + q * 32, o);
+          tmem_ld_wait(o);
+        }
+        if (q == D / 32 - 1 && has) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&o_empty[t]));
+        }
+        if (join) {
+          // 32 columns at a time, the second stream hands its O (and, first, m and l) to the first.
+          if (!mbar_wait_warp(smem_u32(t == 1 ? j_empty : j_full), t == 1 ? jp ^ 1 : jp)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+          jp ^= 1;
+          __syncwarp();
+          if (t == 1) {
+            if (q == 0) Ml[R] = make_float2(m, l);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) Mg[j * 128 + R] = __uint_as_float(o[j]);
+          } else {
+            if (q == 0) {
+              const float2 other = Ml[R];
+              const float M = fmaxf(m, other.x);
+              f0 = m == -INFINITY ? 0.f : ex2((m - M) * a.scale_log2);
+              f1 = other.x == -INFINITY ? 0.f : ex2((other.x - M) * a.scale_log2);
+              m = M;
+              l = l * f0 + other.y * f1;
+            }
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(fmaf(Mg[j * 128 + R], f1, __uint_as_float(o[j]) * f0));
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(t == 1 ? j_full : j_empty));
+        }
+        if (!writes) continue;
+        if (x.part >= 0) {
+          float *dst = c.chunk_part + prow * D + q * 32;
+          if (has)
+#pragma unroll
+            for (int j = 0; j < 32; j += 4)
+              __stcg(reinterpret_cast<float4 *>(dst + j), make_float4(__uint_as_float(o[j]), __uint_as_float(o[j + 1]),
+                                                                      __uint_as_float(o[j + 2]), __uint_as_float(o[j + 3])));
+        } else {
+          const float inv = l == 0.f ? 0.f : 1.f / l;   // a row that sees nothing gives zeros
+          uint4 *dst = reinterpret_cast<uint4 *>(a.out + orow * D + q * 32);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              w[k] = pack_bf16(__uint_as_float(o[8 * j + 2 * k]) * inv, __uint_as_float(o[8 * j + 2 * k + 1]) * inv);
+            dst[j] = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+      }
+      if (!ok) break;
+      if (writes) {
+        // (a row whose scores are all NaN has found no maximum, but must not count as one that saw nothing)
+        if (x.part >= 0)
+          __stcg(reinterpret_cast<float2 *>(c.chunk_ml) + prow, make_float2(l != l ? 0.f : m, l));
+        else if (a.lse)
+          a.lse[orow] = l == 0.f ? -INFINITY : fmaf(m, a.scale, logf(l));
+      }
+    }
+  }
+  // ---- common exit ----
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 3) tmem_dealloc(tmem_base, 512);
+}
+
+// Joins the partial results of the items that cuts go through: grid (CTAs of the attention launch, row groups), a warp
+// per query row.  CTA x looks after the item that CTA x of the attention left open: its own part, and those of the CTAs up
+// to the last one that the item reached.
+template <int D>
+__global__ void __launch_bounds__(256) k_chunk_merge(Ctx c, const __grid_constant__ ChunkArgs a) {
+  griddep_wait();
+  griddep_launch();
+  const int *info = c.chunk_info + blockIdx.x * kChunkInfo;
+  const int cl = __ldcg(info);
+  if (cl < 0) return;
+  const int cf = blockIdx.x, head = __ldcg(info + 1), row0 = __ldcg(info + 2), G = c.G, TPT = kChunkRows / G;
+  const int nt0 = __ldcg(info + 3), ntok = nt0 + __ldcg(info + 4), lane = threadIdx.x & 31;
+  const float2 *ml = reinterpret_cast<const float2 *>(c.chunk_ml);
+  for (int r = blockIdx.y * 8 + (threadIdx.x >> 5); r < ntok * G; r += gridDim.y * 8) {
+    const int tj = r / G, hq = r - tj * G;
+    const int prow = tj < nt0 ? tj * G + hq : kChunkRows + (tj - TPT) * G + hq;   // row inside a CTA's slot
+    auto row_of = [&](int p) { return (size_t)(p * 2 + (p == cf ? 1 : 0)) * 256 + prow; };
+    float M = -INFINITY, L = 0.f;
+    for (int p = cf + lane; p <= cl; p += 32) M = fmaxf(M, __ldcg(ml + row_of(p)).x);
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+    float acc[D / 32];
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) acc[j] = 0.f;
+    for (int p0 = cf; p0 <= cl; p0 += 32) {
+      const float2 x = p0 + lane <= cl ? __ldcg(ml + row_of(p0 + lane)) : make_float2(-INFINITY, 0.f);
+      const float f = x.x == -INFINITY ? 0.f : ex2((x.x - M) * a.scale_log2);
+      L += f * x.y;
+      const int cnt = min(32, cl + 1 - p0);
+#pragma unroll 4
+      for (int i = 0; i < cnt; ++i) {
+        const float fi = __shfl_sync(0xffffffffu, f, i);
+        if (fi == 0.f) continue;   // the part saw nothing of this row (its O may not have been written)
+        const float *o = c.chunk_part + row_of(p0 + i) * D + lane * (D / 32);
+        if (D == 128) {
+          const float4 w = __ldcg(reinterpret_cast<const float4 *>(o));
+          acc[0] = fmaf(fi, w.x, acc[0]); acc[1] = fmaf(fi, w.y, acc[1]);
+          acc[D / 32 - 2] = fmaf(fi, w.z, acc[D / 32 - 2]); acc[D / 32 - 1] = fmaf(fi, w.w, acc[D / 32 - 1]);
+        } else {
+          const float2 w = __ldcg(reinterpret_cast<const float2 *>(o));
+          acc[0] = fmaf(fi, w.x, acc[0]); acc[1] = fmaf(fi, w.y, acc[1]);
+        }
+      }
+    }
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    const size_t orow = ((size_t)(row0 + tj) * c.Hkv + head) * G + hq;
+    uint32_t *dst = reinterpret_cast<uint32_t *>(a.out + orow * D) + lane * (D / 64);
+    dst[0] = pack_bf16(acc[0] * inv, acc[1] * inv);
+    if (D == 128) dst[1] = pack_bf16(acc[D / 32 - 2] * inv, acc[D / 32 - 1] * inv);
+    if (a.lse && lane == 0) a.lse[orow] = L == 0.f ? -INFINITY : fmaf(M, a.scale, logf(L));
+  }
+}
+
+}  // namespace fkv

@@ -4,6 +4,7 @@
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <limits.h>
 #include <stdint.h>
 
 namespace fkv {
@@ -15,7 +16,7 @@ constexpr int kHidden = 16;      // scorer hidden width (Section 4.1)
 constexpr unsigned kDevPoolExhausted = 1u, kDevCapacity = 2u, kDevWaitTimeout = 4u, kDevBadIndex = 8u;
 
 // ctrl[] slots
-enum { CTRL_FREE_TOP = 0, CTRL_STATUS = 1, CTRL_WORDS = 8 };
+enum { CTRL_FREE_TOP = 0, CTRL_STATUS = 1, CTRL_CHUNK_TICKET = 2, CTRL_WORDS = 8 };
 // planhdr[] slots
 enum { PH_NWORK = 0, PH_TILES1 = 1, PH_NEW_PAGES = 2, PH_OLD_PAGES = 3, PH_PUSH_START = 4, PH_WORDS = 8 };
 
@@ -67,6 +68,10 @@ struct Ctx {
   float *att_part;
   int *att_tickets;
   int att_smax;
+  // Attention over chunks: per CTA of a launch two slots of 256 rows for partial results (O, then m and l), and the
+  // description of the item it leaves open (k_chunk_merge).
+  float *chunk_part, *chunk_ml;
+  int *chunk_info;
   // Record of the decode queries of the current chunk (attention-feature maintenance; hist_w = 0: off).
   int hist_w;          // ring capacity W in queries
   int hist_wp;         // W rounded up to a multiple of 16: the row count of one operand tile
@@ -258,6 +263,38 @@ __device__ __forceinline__ unsigned long long dsmem_ld_u64(uint32_t addr) {
   unsigned long long v;
   asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
   return v;
+}
+
+// ---------------------------------------------------------------- positions
+// Stored positions grow with the slot.  They sit in the meta rows, a pair's position behind its features, so a look at
+// one is two dependent reads (page id, position).
+// Position of the pair at `slot` of a segment.
+__device__ __forceinline__ int slot_pos(const Ctx &c, const int *ptrow, int slot) {
+  const uint8_t *page = c.pool + (size_t)__ldcg(ptrow + slot / kPage) * c.page_bytes;
+  return __ldcg(reinterpret_cast<const int32_t *>(meta_row(c, page, slot % kPage)) + c.F);
+}
+// The first slot in [lo, hi) whose position is at least p (hi if there is none).
+__device__ __forceinline__ int slot_lower_bound(const Ctx &c, const int *ptrow, int lo, int hi, int p) {
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (slot_pos(c, ptrow, mid) < p) lo = mid + 1; else hi = mid;
+  }
+  return lo;
+}
+// The first position that a window of W positions up to p holds.
+__device__ __forceinline__ int window_start(int p, int W) { return (int)max((long long)p - W + 1, (long long)INT_MIN); }
+// Slots [0, a) hold the positions below S: at most S of them, and all of the first S when nothing was evicted there.
+__device__ __forceinline__ int slot_sinks(const Ctx &c, const int *ptrow, int n, int S) {
+  const int m = min(S, n);
+  if (m == 0) return 0;
+  return slot_pos(c, ptrow, m - 1) < S ? m : slot_lower_bound(c, ptrow, 0, m - 1, S);
+}
+// The first slot at or below `last` whose position is above p - W, p >= the position at `last`: at most W slots back,
+// and exactly W when no position is missing there, which is looked at first.
+__device__ __forceinline__ int slot_window(const Ctx &c, const int *ptrow, int last, int p, int W) {
+  const int lo = max(0, last + 1 - W), first = window_start(p, W);
+  if (slot_pos(c, ptrow, lo) >= first) return lo;
+  return slot_lower_bound(c, ptrow, lo + 1, last + 1, first);
 }
 
 // ---------------------------------------------------------------- row movers
