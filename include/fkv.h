@@ -326,6 +326,19 @@ int fkv_append_chunk_attn(fkv_cache *c, int layer, const void *k, const void *v,
                           const int32_t *keep_lens, const int32_t *chunk_lens, const void *q, int32_t window,
                           int32_t sinks, float scale, void *out, float *lse_out, void *stream);
 
+/*
+ * The attention features of Appendix B.1 from the queries of a chunk, so that fkv_evict and fkv_evict_by_feature
+ * (FKV_FEATURE_CUM_SUM: accumulated attention) can follow a prompt.  The chunk's pairs are the last chunk_lens[s] pairs of
+ * their segments; q, window, sinks and scale are those of fkv_chunk_attn, lse what it wrote (dev [tokens][Hkv*g]).  With
+ * P_ji = exp(scale <q_j, k_i> - lse_j) for the pairs that query j sees and 0 for the others, the features of EVERY pair of
+ * the sequences with tokens become, per query head, the means of P over the chunk's last 8 / 16 / 32 queries (fewer queries
+ * still divide by 8 / 16 / 32) and over the whole chunk, previous sum + the latter, 0.9 * previous decayed sum + the latter:
+ * one chunk of the recurrence described at fkv_update_features.  Needs no feature_window; decode queries on record are
+ * neither used nor dropped.  Errors as fkv_chunk_attn.
+ */
+int fkv_chunk_features(fkv_cache *c, int layer, const void *q, const float *lse, const int32_t *chunk_lens, int32_t window,
+                       int32_t sinks, float scale, void *stream);
+
 /* ---- staged entry points: one kernel each, for per-step checks ---- */
 
 /*

@@ -28,7 +28,7 @@ EXPORTS = ["fkv_workspace_bytes", "fkv_init_cache", "fkv_destroy", "fkv_reset", 
            "fkv_launch_count", "fkv_last_cuda_error", "fkv_sync_lengths", "fkv_set_timing", "fkv_get_evict_timing",
            "fkv_decode_step", "fkv_decode_attn_dense_noalloc", "fkv_append_decode_attn", "fkv_evict_sampled", "fkv_select_sampled", "fkv_update_features", "fkv_evict_by_feature", "fkv_golden_steps", "fkv_golden_eviction", "fkv_golden_select",
            "fkv_evict_rkv", "fkv_score_rkv", "fkv_append_chunk", "fkv_chunk_attn", "fkv_append_chunk_attn",
-           "fkv_decode_attn_window", "fkv_append_decode_attn_window", "fkv_export_features"]
+           "fkv_decode_attn_window", "fkv_append_decode_attn_window", "fkv_export_features", "fkv_chunk_features"]
 
 
 class FkvConfig(ctypes.Structure):
@@ -66,6 +66,7 @@ def lib():
         _lib.fkv_append_chunk.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp]
         _lib.fkv_chunk_attn.argtypes = [vp, i32, vp, vp, i32, i32, f32, vp, vp, vp]
         _lib.fkv_append_chunk_attn.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, i32, i32, f32, vp, vp, vp]
+        _lib.fkv_chunk_features.argtypes = [vp, i32, vp, vp, vp, i32, i32, f32, vp]
         _lib.fkv_decode_attn_window.argtypes = [vp, i32, vp, vp, i32, i32, vp, f32, vp]
         _lib.fkv_append_decode_attn_window.argtypes = [vp, i32, vp, vp, vp, vp, vp, i32, i32, vp, f32, vp]
     return _lib
@@ -321,6 +322,13 @@ class Cache:
                                            _ptr(out, torch.bfloat16), _ptr(lse, torch.float32), _stream()),
                "fkv_append_chunk_attn")
         return out
+
+    def chunk_features(self, layer, q, lse, chunk_lens, window=0, sinks=0, scale=0.0):
+        """Features of all pairs from the queries of a chunk and the log-sum-exp that chunk_attn gave for them."""
+        self._check_chunk(chunk_lens, q=q, lse=lse)
+        _check(lib().fkv_chunk_features(self._h, layer, _ptr(q, torch.bfloat16), _ptr(lse, torch.float32),
+                                        _lens(chunk_lens, self.cfg.max_batch, "chunk_lens"), window, sinks, scale, _stream()),
+               "fkv_chunk_features")
 
     def export_features(self, layer, seq, out=None):
         """The features of one (layer, sequence): [Hkv][n][6 g] fp32."""

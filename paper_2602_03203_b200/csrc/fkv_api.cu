@@ -18,6 +18,7 @@
 #include "fkv_attend.cuh"
 #include "fkv_aux.cuh"
 #include "fkv_chunk.cuh"
+#include "fkv_chunk_features.cuh"
 #include "fkv_compact.cuh"
 #include "fkv_dev.cuh"
 #include "fkv_features.cuh"
@@ -654,6 +655,36 @@ int launch_chunk_attend(fkv_cache *c, int layer, const void *q, const int32_t *c
   return D == 128 ? launch_chunk_attend_t<128>(c, tmq, a, grid, st) : launch_chunk_attend_t<64>(c, tmq, a, grid, st);
 }
 
+template <int D>
+int launch_chunk_features_t(fkv_cache *c, const CUtensorMap &tmq, const ChunkFeatArgs &a, int grid, cudaStream_t st) {
+  constexpr size_t smem = CfSmem<D>::bytes();
+  static_assert(smem <= kMaxSmem, "one CTA's shared memory");
+  static SmemOptIn opt_in;
+  FKV_CUDA(opt_in.ensure(k_chunk_features<D>, smem));
+  FKV_CUDA(launch_waiting(k_chunk_features<D>, dim3(grid), kCfThreads, smem, st, c->ctx, c->page_rows, tmq, a));
+  ++c->launches;
+  return FKV_OK;
+}
+
+int launch_chunk_features(fkv_cache *c, int layer, const void *q, const float *lse, const int32_t *chunk_lens, const ChunkLens &lens,
+                          int window, int sinks, float scale, cudaStream_t st) {
+  const int batch = c->cfg.max_batch, D = c->cfg.head_dim;
+  if (lens.tok[batch] == 0) return FKV_OK;
+  if (int e = ensure_page_rows_map(c)) return e;
+  ChunkFeatArgs a;
+  a.layer = layer; a.window = window; a.sinks = window ? sinks : 0;
+  a.scale_log2 = (scale == 0.f ? 1.f / sqrtf((float)D) : scale) * 1.4426950408889634f;
+  a.lse = lse; a.lens = lens;
+  CUtensorMap tmq;
+  if (int e = query_map(c, q, lens.tok[batch], 1, kCfQueries, &tmq)) return e;
+  long long units = 0;   // (pair of tiles, query head)
+  for (int s = 0; s < batch; ++s)
+    if (chunk_lens[s] > 0) units += (c->h_len[(size_t)layer * batch + s] + kCfPairs - 1) / kCfPairs;
+  units *= c->cfg.num_kv_heads * c->cfg.group_size;
+  const int grid = (int)std::max<long long>(1, std::min<long long>(c->sm_count, units));
+  return D == 128 ? launch_chunk_features_t<128>(c, tmq, a, grid, st) : launch_chunk_features_t<64>(c, tmq, a, grid, st);
+}
+
 }  // namespace
 
 extern "C" {
@@ -1038,6 +1069,15 @@ int fkv_append_chunk_attn(fkv_cache *c, int layer, const void *k, const void *v,
   return launch_chunk_attend(c, layer, q, chunk_lens, lens, window, sinks, scale, out, lse_out, (cudaStream_t)stream);
 }
 
+int fkv_chunk_features(fkv_cache *c, int layer, const void *q, const float *lse, const int32_t *chunk_lens, int32_t window,
+                       int32_t sinks, float scale, void *stream) {
+  ChunkLens lens;
+  if (int e = check_chunk(c, layer, q, chunk_lens, window, sinks, scale, lens)) return e;
+  if (lens.tok[c->cfg.max_batch] > 0 && (!lse || !aligned(lse, 4))) return FKV_ERR_INVALID_ARG;
+  if (!chunk_is_stored(c, layer, chunk_lens)) return FKV_ERR_INVALID_ARG;
+  return launch_chunk_features(c, layer, q, lse, chunk_lens, lens, window, sinks, scale, (cudaStream_t)stream);
+}
+
 int fkv_decode_attn_window(fkv_cache *c, int layer, const void *q, const int32_t *q_pos, int32_t window, int32_t sinks, void *out,
                            float scale, void *stream) {
   if (!c || !layer_ok(c, layer) || !q || !out || window < 1 || sinks < 0) return FKV_ERR_INVALID_ARG;
@@ -1060,9 +1100,10 @@ int fkv_append_decode_attn_window(fkv_cache *c, int layer, const void *k, const 
 }
 
 int fkv_export_features(fkv_cache *c, int layer, int seq, float *feat, void *stream) {
-  if (!c || !layer_ok(c, layer) || seq < 0 || seq >= c->cfg.max_batch || !feat) return FKV_ERR_INVALID_ARG;
+  if (!c || !layer_ok(c, layer) || seq < 0 || seq >= c->cfg.max_batch) return FKV_ERR_INVALID_ARG;
   const int n = c->h_len[(size_t)layer * c->cfg.max_batch + seq];
-  if (n == 0) return FKV_OK;
+  if (n == 0) return FKV_OK;   // (an empty tensor may have no address)
+  if (!feat) return FKV_ERR_INVALID_ARG;
   k_export_features<<<dim3((n + 7) / 8, c->cfg.num_kv_heads), 256, 0, (cudaStream_t)stream>>>(c->ctx, layer, seq, n, feat);
   FKV_LAUNCHED(c);
   return FKV_OK;

@@ -22,3 +22,8 @@ def test_length_lists_have_one_entry_per_sequence():
     assert list(binding._lens([1, 0, 2], 3, "x")) == [1, 0, 2]
     with pytest.raises(ValueError):
         binding._lens([1, 2], 3, "x")
+
+
+def test_null_handle_of_the_features_is_refused():
+    lens = (ctypes.c_int32 * 1)(1)
+    assert binding.lib().fkv_chunk_features(None, 0, None, None, lens, 0, 0, 0.0, None) == -1
