@@ -236,6 +236,12 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
                "r"(taddr)
                : "memory");
 }
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+               ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+               "r"(taddr)
+               : "memory");
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // 64 channels of the g heads x the tokens of one query tile (rows of 128 bytes, swizzled).
@@ -244,6 +250,13 @@ __device__ __forceinline__ void tma_chunk_q(uint32_t dst, const CUtensorMap *tm,
       "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
       ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(ch), "r"(head), "r"(tok), "r"(bar)
       : "memory");
+}
+
+// Scores of columns [c0, c0 + 32) that the row does not see ([na, lo) and from hi on) become -infinity.
+__device__ __forceinline__ void chunk_mask(uint32_t (&v)[32], int c0, int lo, int hi, int na) {
+#pragma unroll
+  for (int j = 0; j < 32; ++j)
+    if (c0 + j >= hi || (c0 + j < lo && c0 + j >= na)) v[j] = 0xff800000u;
 }
 
 template <int D>
@@ -440,7 +453,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
   } else if (warp == 0) {
     // ---------------- copies ----------------
     FeatRing rr{0, 0};
-    int it = 0, nq[2] = {0, 0};
+    int it = 0;
+    uint32_t qp = 0;                      // bit t: parity of query tile t's next phase
     uint32_t armed = 0, armed_par = 0;    // bit s: ring slot s (bit 16 + t: query tile t) has been armed / its last parity
     bool ok = true;
     const int pg = lane & 7, half = lane >> 3;
@@ -455,7 +469,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       const int ntA = (x.pa1 - x.pa0 + TP - 1) / TP, nt = ntA + (x.pb1 - x.pb0 + TP - 1) / TP;
       if (nt == 0) continue;
       for (int t = 0; t < (x.kind == 1 ? 2 : 1) && ok; ++t) {
-        if (!mbar_wait_warp(smem_u32(&q_empty[t]), (nq[t] & 1) ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+        if (!mbar_wait_warp(smem_u32(&q_empty[t]), ((qp >> t) & 1) ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; break; }
         if (lane == 0) {
           mbar_arrive_expect_tx(smem_u32(&q_full[t]), (uint32_t)(NQ * TPT * G * 128));
           for (int q = 0; q < NQ; ++q)
@@ -463,8 +477,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
                         smem_u32(&q_full[t]));
         }
         armed |= 1u << (16 + t);
-        armed_par = (armed_par & ~(1u << (16 + t))) | ((uint32_t)(nq[t] & 1) << (16 + t));
-        ++nq[t];
+        armed_par = (armed_par & ~(1u << (16 + t))) | (((qp >> t) & 1) << (16 + t));
+        qp ^= 1u << t;
       }
       if (!ok) break;
       const int *ptrow = c.pt + (size_t)x.seg * c.max_pages;
@@ -518,8 +532,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
   } else if (warp == 1) {
     // ---------------- multiplies: the warp stays together, lane 0 issues ----------------
     FeatRing rr{0, 0};
-    int it = 0, nq[2] = {0, 0};
-    uint32_t np_ph = 0, no_ph = 0;   // bit t: parity of stream t's next p_full / o_empty
+    int it = 0;
+    uint32_t qp = 0, np_ph = 0, no_ph = 0;   // bit t: parity of query tile t's next phase / stream t's next p_full / o_empty
     bool ok = true;
     const uint32_t idesc_o = umma_idesc_bf16(kChunkRows, D) | (1u << 16);   // B runs along N
     while (ok) {
@@ -534,8 +548,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       if (nt == 0) continue;
       const int ns = x.kind == 1 ? 2 : 1;   // query tiles
       for (int t = 0; t < ns; ++t) {
-        if (!mbar_spin(smem_u32(&q_full[t]), nq[t] & 1)) { set_status(c, kDevWaitTimeout); ok = false; }
-        ++nq[t];
+        if (!mbar_spin(smem_u32(&q_full[t]), (qp >> t) & 1)) { set_status(c, kDevWaitTimeout); ok = false; }
+        qp ^= 1u << t;
       }
       if (!ok) break;
       auto pages = [&](int i, int &p0) {
@@ -712,26 +726,24 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
           continue;
         }
         tc_fence_after();
-        uint32_t s[4][32];
+        // S is read twice, 32 columns at a time with the next ones on their way: once for the maximum, once for the
+        // exponentials.  (All 128 scores in registers at once do not fit beside the rest: they spilled.)
+        const bool masked = !__all_sync(0xffffffffu, hi >= 128 && (lo <= 0 || na >= 128));
+        uint32_t s[2][32];
+        tmem_ld32_issue(ts, s[0]);
+        float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int q = 0; q < 4; ++q) tmem_ld32_issue(ts + q * 32, s[q]);
+        for (int q = 0; q < 4; ++q) {
+          uint32_t(&v)[32] = s[q & 1];
+          tmem_ld_wait(v);
+          tmem_ld32_issue(ts + ((q + 1) & 3) * 32, s[(q + 1) & 1]);   // (after the last: the first once more)
+          if (masked) chunk_mask(v, q * 32, lo, hi, na);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) tmem_ld_wait(s[q]);
-        if (!__all_sync(0xffffffffu, hi >= 128 && (lo <= 0 || na >= 128))) {
+          for (int j = 0; j < 32; j += 8)
 #pragma unroll
-          for (int j = 0; j < 128; ++j)
-            if (j >= hi || (j < lo && j >= na)) s[j >> 5][j & 31] = 0xff800000u;   // hidden: -infinity
+            for (int k = 0; k < 4; ++k) m4[k] = max3(m4[k], __uint_as_float(v[j + 2 * k]), __uint_as_float(v[j + 2 * k + 1]));
         }
-        float mx = -INFINITY;
-        {
-          float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-          for (int j = 0; j < 128; j += 8)
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-              m4[q] = max3(m4[q], __uint_as_float(s[j >> 5][(j & 31) + 2 * q]), __uint_as_float(s[j >> 5][(j & 31) + 2 * q + 1]));
-          mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-        }
+        const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
         // The reference follows the maximum only when it has grown by more than 2^8 (or there was none yet).
         const bool grow = mx > m && (mx - m) * a.scale_log2 > kChunkGrow;
         if (__any_sync(0xffffffffu, grow)) {
@@ -739,7 +751,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
           if (grow) m = mx;
           l *= f;
           if (i != i0) {   // the stream's products up to the tile before are complete: this S was multiplied after them
-#pragma unroll
+            tmem_ld_wait(s[0]);
+#pragma unroll 1
             for (int q = 0; q < D / 32; ++q) {
               uint32_t o[32];
               tmem_ld32_issue(to + q * 32, o);
@@ -753,16 +766,20 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
         const float ms = m == -INFINITY ? 0.f : m * a.scale_log2;
         float l4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t p[32];
+        for (int q = 0; q < 4; ++q) {
+          uint32_t(&v)[32] = s[q & 1];
+          tmem_ld_wait(v);
+          if (q < 3) tmem_ld32_issue(ts + (q + 1) * 32, s[(q + 1) & 1]);
+          if (masked) chunk_mask(v, q * 32, lo, hi, na);
+          uint32_t p[16];   // (its columns are those of scores that have been read)
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const float x0 = ex2(fmaf(__uint_as_float(s[2 * h + (j >> 4)][(2 * j) & 31]), a.scale_log2, -ms));
-            const float x1 = ex2(fmaf(__uint_as_float(s[2 * h + (j >> 4)][(2 * j + 1) & 31]), a.scale_log2, -ms));
+          for (int j = 0; j < 16; ++j) {
+            const float x0 = ex2(fmaf(__uint_as_float(v[2 * j]), a.scale_log2, -ms));
+            const float x1 = ex2(fmaf(__uint_as_float(v[2 * j + 1]), a.scale_log2, -ms));
             l4[j & 3] += x0 + x1;
-            p[j] = pack_bf16(x0, x1);   // P in bf16, as V is: at most half a step (2^-9) off, the row sum is not rounded
+            p[j] = pack_bf16(x0, x1);   // P in bf16, as V is: at most half a step (2^-8) off; the row sum is not rounded
           }
-          tmem_st32(ts + h * 32, p);
+          tmem_st16(ts + q * 16, p);
         }
         l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
         tmem_st_wait();
