@@ -158,6 +158,7 @@ struct fkv_cache {
   int max_cluster[2] = {0, 0};   // largest attention cluster the device places (found at the first stand-alone launch): plain, windowed
   float feature_scale = 0.f;  // softmax scale of the recorded queries (the last decode call's)
   bool timing = false, timed = false;
+  CUtensorMap page_parts;     // ... as [page][64-channel part][row][64 channels]
   CUtensorMap page_rows;      // the page pool's K and V rows as [page][row][64-channel part][64 channels] (tensor copies)
   bool page_rows_ready = false;
   cudaEvent_t ev[7] = {nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr};  // [6]: after the plan
@@ -325,6 +326,11 @@ int ensure_page_rows_map(fkv_cache *c) {
   const cuuint64_t strides[3] = {128, (cuuint64_t)(4 * D), (cuuint64_t)c->ctx.page_bytes};   // bytes, dimensions 1 .. 3
   const cuuint32_t box[4] = {64, 1, (cuuint32_t)kPage, 1};
   if (int e = tensor_map(&c->page_rows, c->ctx.pool, 4, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE)) return e;
+  // The same with the rows inside the parts: one box = 16 rows of D channels, 64 channels after another (all of K or V).
+  const cuuint64_t dims2[4] = {64, (cuuint64_t)kPage, (cuuint64_t)(2 * D / 64), (cuuint64_t)c->ctx.num_pages};
+  const cuuint64_t strides2[3] = {(cuuint64_t)(4 * D), 128, (cuuint64_t)c->ctx.page_bytes};
+  const cuuint32_t box2[4] = {64, (cuuint32_t)kPage, (cuuint32_t)(D / 64), 1};
+  if (int e = tensor_map(&c->page_parts, c->ctx.pool, 4, dims2, strides2, box2, CU_TENSOR_MAP_SWIZZLE_NONE)) return e;
   c->page_rows_ready = true;
   return FKV_OK;
 }
@@ -620,7 +626,7 @@ int launch_chunk_attend_t(fkv_cache *c, const CUtensorMap &tmq, const ChunkArgs 
   static_assert(smem <= kMaxSmem, "one CTA's shared memory");
   static SmemOptIn opt_in;
   FKV_CUDA(opt_in.ensure(k_chunk_attend<D>, smem));
-  FKV_CUDA(launch_waiting(k_chunk_attend<D>, dim3(grid), kChunkThreads, smem, st, c->ctx, c->page_rows, tmq, a));
+  FKV_CUDA(launch_waiting(k_chunk_attend<D>, dim3(grid), kChunkThreads, smem, st, c->ctx, c->page_rows, c->page_parts, tmq, a));
   ++c->launches;
   if (grid > 1) {   // (a single CTA cuts nothing)
     const int rows = std::min(256, 2 * kChunkRows);

@@ -13,14 +13,16 @@
 // SM; the pages of all items form one line that is cut into equal ranges, one per CTA, so the split is even whatever the
 // batch looks like (one long sequence, many short ones, drafts of a few tokens over long caches).  An item that a cut
 // goes through leaves partial results (O, m, l) which k_chunk_merge joins.
-//   warp 0      tensor copies (TMA): the item's query tiles, then K and V page by page (one copy = 16 rows x 64 channels;
-//               the page record's swizzle is the shared-memory swizzle) into a ring of key tiles of up to eight pages;
-//   warp 1      one lane issues tcgen05.mma: S = Q K^T (K-major operands) into tensor memory, O += P V with P read from
-//               tensor memory and V as an MN-major operand (channels run along its rows: no transpose anywhere);
-//   warp 2      walks the items ahead of the others and searches the positions;
+//   warp 0      tensor copies (TMA) of the item's query tiles and of K, page by page (one copy = 16 rows x 64 channels; the
+//               page record's swizzle is the shared-memory swizzle), into a ring of key tiles of up to eight pages;
+//   warps 1, 3  one lane each issues the tcgen05.mma of one stream: S = Q K^T (K-major operands) into tensor memory,
+//               O += P V with P read from tensor memory and V as an MN-major operand (channels run along its rows: no
+//               transpose anywhere);
+//   warp 2      walks the items ahead of the others, searches the positions, and copies V (one copy = a page's 16 rows): a
+//               warp issues a copy per 80 - 100 cycles, so one for K and V would not keep up;
 //   warps 4-11  two warpgroups, each with a stream of its own (S and O accumulators): thread = query row; running
 //               maximum, exp2, row sum in fp32, P rounded to bf16 into the columns of S.  O is rescaled only when the
-//               maximum has grown by more than 2^8: until then P is at most 256, which bf16 holds as exactly as 1.
+//               maximum has grown by more than 2^24: until then P is at most 2^24, which bf16 holds as exactly as 1.
 // The streams are the item's two query tiles; an item with one tile gives its key tiles to the streams in turn, and the
 // streams' results are joined through shared memory.
 // Every wait is bounded; tensor memory is freed at the common exit.
@@ -40,8 +42,8 @@ constexpr int kChunkRows = 128;       // query rows of a tile = M of the mma
 constexpr int kChunkPages = 8;        // pages of a key tile: N of S, K of O
 constexpr int kChunkMinPages = 8;     // least work of a CTA
 constexpr int kChunkInfo = 8;         // words that describe a CTA's unfinished item to the merge
-constexpr float kChunkGrow = 8.f;     // log2 of the growth of a row's maximum that O is rescaled for
-constexpr int kChunkItems = 2;        // items the walk may be ahead by
+constexpr float kChunkGrow = 24.f;    // log2 of the growth of a row's maximum that O is rescaled for
+constexpr int kChunkItems = 3;        // items in use: being finished, being worked on, being read ahead
 
 // Prefix sums of the chunk lengths over the sequences, and the pairs that stay (use == 0: all of them).
 struct ChunkLens {
@@ -184,13 +186,24 @@ struct ChunkItem {
   int pad[2];
 };
 
+// The key tiles of an item: up to eight pages each, those of the sinks first.
+struct ChunkTiles {
+  int pa0, pa1, pb0, pb1, na, nt;
+  __device__ __forceinline__ explicit ChunkTiles(const ChunkItem &x) : pa0(x.pa0), pa1(x.pa1), pb0(x.pb0), pb1(x.pb1) {
+    na = (pa1 - pa0 + kChunkPages - 1) / kChunkPages;
+    nt = na + (pb1 - pb0 + kChunkPages - 1) / kChunkPages;
+  }
+  __device__ __forceinline__ int first(int i) const { return i < na ? pa0 + kChunkPages * i : pb0 + kChunkPages * (i - na); }
+  __device__ __forceinline__ int pages(int i) const { return min(kChunkPages, (i < na ? pa1 : pb1) - first(i)); }
+};
+
 template <int D>
 struct ChunkSmem {
-  static constexpr int kSlots = D == 128 ? 4 : 8;
+  static constexpr int kSlots = D == 128 ? 2 : 4;                 // key tiles in flight, of K and of V
   static constexpr size_t kTile = (size_t)(D / 64) * 128 * 128;   // 128 rows: [D / 64][128][128 B]
   static constexpr size_t kMerge = 32 * 128 * 4;
-  static constexpr size_t kOffRing = 2 * kTile;
-  static constexpr size_t kOffMerge = kOffRing + kSlots * kTile;
+  static constexpr size_t kOffK = 2 * kTile, kOffV = kOffK + kSlots * kTile;
+  static constexpr size_t kOffMerge = kOffV + kSlots * kTile;
   static constexpr size_t kOffMl = kOffMerge + kMerge;                 // (m, l) of the second stream's rows
   static constexpr size_t kOffItems = kOffMl + 128 * 8;
   static constexpr size_t kOffWlo = kOffItems + kChunkItems * sizeof(ChunkItem);   // first slot of every token's window
@@ -217,33 +230,54 @@ __device__ __forceinline__ ChunkRange chunk_range(int n, int T, int j0, int j1, 
 }
 
 // Matrix descriptor of an operand whose channels run along its 128-byte rows (MN-major, 128-byte swizzle): 64 channels
-// to a row, 8-row groups 1024 bytes apart along K, the next 64 channels a whole tile half (128 rows) further.
+// to a row, 8-row groups 1024 bytes apart along K, the next 64 channels behind the 16 rows of a page.
 __device__ __forceinline__ uint64_t umma_desc_mn_sw128(uint32_t smem_addr) {
-  return (uint64_t)((smem_addr & 0x3ffffu) >> 4) | ((uint64_t)(128u * 128u >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) |
+  return (uint64_t)((smem_addr & 0x3ffffu) >> 4) | ((uint64_t)(kPage * 128u >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) |
          (1ull << 46) | (2ull << 61);
 }
-// D += A B with A (128 rows x 16, bf16, two to a column) in tensor memory.
-__device__ __forceinline__ void umma_bf16_ta(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+// The multiplies of a warp that stays together: every lane comes by, the one with on != 0 issues.  (Inside a branch that
+// one lane takes, every operand has to be moved to a uniform register for every instruction, and one thread then issues no
+// more than a multiply per 100 cycles; guarded instructions in straight code take theirs from where they were worked out.)
+__device__ __forceinline__ void umma_bf16_if(uint32_t on, uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-      ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(on)
       : "memory");
 }
+// D += A B with A (128 rows x 16, bf16, two to a column) in tensor memory.
+__device__ __forceinline__ void umma_bf16_ta_if(uint32_t on, uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(on)
+      : "memory");
+}
+__device__ __forceinline__ void umma_commit_if(uint32_t on, uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
+      ::"r"(bar), "r"(on)
+      : "memory");
+}
+// A value that is the same in all lanes, as the compiler can see.
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
                ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]),
                "r"(taddr)
                : "memory");
 }
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
-               ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-               "r"(taddr)
-               : "memory");
-}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// One page's V rows, all channels (from part part0 of the page's row): per 64 channels 16 rows of 128 bytes.
+__device__ __forceinline__ void tma_page_v(uint32_t dst, const CUtensorMap *tm, int part0, int page, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(0), "r"(0), "r"(part0), "r"(page), "r"(bar)
+      : "memory");
+}
 // 64 channels of the g heads x the tokens of one query tile (rows of 128 bytes, swizzled).
 __device__ __forceinline__ void tma_chunk_q(uint32_t dst, const CUtensorMap *tm, int ch, int head, int tok, uint32_t bar) {
   asm volatile(
@@ -252,15 +286,81 @@ __device__ __forceinline__ void tma_chunk_q(uint32_t dst, const CUtensorMap *tm,
       : "memory");
 }
 
-// Scores of columns [c0, c0 + 32) that the row does not see ([na, lo) and from hi on) become -infinity.
-__device__ __forceinline__ void chunk_mask(uint32_t (&v)[32], int c0, int lo, int hi, int na) {
+// 16 columns (see tmem_ld32_issue).
+__device__ __forceinline__ void tmem_ld16_issue(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ld16_wait(uint32_t (&r)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+               :
+               : "memory");
+}
+
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+               ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+               "r"(taddr)
+               : "memory");
+}
+// The scores of the columns that the row does not see ([na, lo) and from hi on) become -infinity, in tensor memory: the
+// few tiles at an edge pay for a walk of their own, and the walk that every tile takes has no masks in it.
+__device__ __forceinline__ void chunk_mask(uint32_t ts, int lo, int hi, int na) {
+#pragma unroll 1
+  for (int q = 0; q < 128; q += 16) {
+    uint32_t v[16];
+    tmem_ld16_issue(ts + q, v);
+    tmem_ld16_wait(v);
 #pragma unroll
-  for (int j = 0; j < 32; ++j)
-    if (c0 + j >= hi || (c0 + j < lo && c0 + j >= na)) v[j] = 0xff800000u;
+    for (int j = 0; j < 16; ++j)
+      if (q + j >= hi || (q + j < lo && q + j >= na)) v[j] = 0xff800000u;
+    tmem_st16(ts + q, v);
+  }
+  tmem_st_wait();
+}
+
+// A row's 128 scores from tensor memory: their maximum mx, P = 2^(scale s - ms) rounded to bf16 (as V is: at most half a
+// step, 2^-8, off) and its unrounded sum lt.
+__device__ __forceinline__ void chunk_scores(uint32_t ts, float scale_log2, float ms, uint32_t (&p)[2][32], float &lt, float &mx) {
+  uint32_t s[2][16];
+  tmem_ld16_issue(ts, s[0]);
+  float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+  float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+  const float2 sc = make_float2(scale_log2, scale_log2), off = make_float2(-ms, -ms);
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    uint32_t(&v)[16] = s[q & 1];
+    tmem_ld16_wait(v);
+    if (q < 7) tmem_ld16_issue(ts + (q + 1) * 16, s[(q + 1) & 1]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float2 z = make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
+      m4[j & 3] = max3(m4[j & 3], z.x, z.y);
+      float2 x = __ffma2_rn(z, sc, off);
+      x.x = ex2(x.x);
+      x.y = ex2(x.y);
+      l2[j & 1] = __fadd2_rn(l2[j & 1], x);
+      p[q >> 2][(q & 3) * 8 + j] = pack_bf16(x.x, x.y);
+    }
+  }
+  mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+  lt = (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
+}
+
+// A warp's wait for something that is not urgent: the thread that looks is suspended meanwhile, so that it takes no issue
+// slots from the warps that compute.
+__device__ __forceinline__ bool mbar_sleep_warp(uint32_t bar, uint32_t parity) {
+  bool ok = true;
+  if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity);
+  return __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
 }
 
 template <int D>
-__global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const __grid_constant__ CUtensorMap tmkv,
+__global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const __grid_constant__ CUtensorMap tmk,
+                                                                   const __grid_constant__ CUtensorMap tmv,
                                                                    const __grid_constant__ CUtensorMap tmq,
                                                                    const __grid_constant__ ChunkArgs a) {
   using SM = ChunkSmem<D>;
@@ -268,31 +368,36 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
   constexpr uint32_t PAGE_HALF = kPage * 128;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  uint8_t *Qt = smem, *Ring = smem + SM::kOffRing;
+  uint8_t *Qt = smem, *Kt = smem + SM::kOffK, *Vt = smem + SM::kOffV;
   float *Mg = reinterpret_cast<float *>(smem + SM::kOffMerge);
   float2 *Ml = reinterpret_cast<float2 *>(smem + SM::kOffMl);
   ChunkItem *Items = reinterpret_cast<ChunkItem *>(smem + SM::kOffItems);
   int *Wlo = reinterpret_cast<int *>(smem + SM::kOffWlo);
   int *Len = reinterpret_cast<int *>(smem + SM::kOffLen), *Blk = reinterpret_cast<int *>(smem + SM::kOffBlk);
   uint64_t *bars = reinterpret_cast<uint64_t *>(smem + SM::kOffBars);
-  uint64_t *kv_full = bars, *kv_empty = kv_full + NS, *q_full = kv_empty + NS, *q_empty = q_full + 2;
+  uint64_t *k_full = bars, *k_empty = k_full + NS, *v_full = k_empty + NS, *v_empty = v_full + NS;
+  uint64_t *q_full = v_empty + NS, *q_empty = q_full + 2;
   uint64_t *s_full = q_empty + 2, *p_full = s_full + 2, *o_full = p_full + 2, *o_empty = o_full + 2;
   uint64_t *it_full = o_empty + 2, *it_empty = it_full + kChunkItems, *j_full = it_empty + kChunkItems, *j_empty = j_full + 1;
-  uint64_t *mma_done = j_empty + 1;
+  uint64_t *turn = j_empty + 1, *mma_done = turn + 2;
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(mma_done + 1);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, G = c.G, TPT = kChunkRows / G;
 
   if (warp == 3) tmem_alloc(smem_u32(tmem_slot), 512);
   if (threadIdx.x == 0) {
-    for (int s = 0; s < NS; ++s) { mbar_init(smem_u32(&kv_full[s]), 1); mbar_init(smem_u32(&kv_empty[s]), 1); }
+    for (int s = 0; s < NS; ++s) {
+      mbar_init(smem_u32(&k_full[s]), 1); mbar_init(smem_u32(&k_empty[s]), 2);
+      mbar_init(smem_u32(&v_full[s]), 1); mbar_init(smem_u32(&v_empty[s]), 2);
+    }
     for (int t = 0; t < 2; ++t) {
-      mbar_init(smem_u32(&q_full[t]), 1); mbar_init(smem_u32(&q_empty[t]), 1);
+      mbar_init(smem_u32(&turn[t]), 1);
+      mbar_init(smem_u32(&q_full[t]), 1); mbar_init(smem_u32(&q_empty[t]), 2 - t);
       mbar_init(smem_u32(&s_full[t]), 1); mbar_init(smem_u32(&p_full[t]), 4);
       mbar_init(smem_u32(&o_full[t]), 1); mbar_init(smem_u32(&o_empty[t]), 4);
     }
-    for (int i = 0; i < kChunkItems; ++i) { mbar_init(smem_u32(&it_full[i]), 1); mbar_init(smem_u32(&it_empty[i]), 10); }
+    for (int i = 0; i < kChunkItems; ++i) { mbar_init(smem_u32(&it_full[i]), 1); mbar_init(smem_u32(&it_empty[i]), 11); }
     mbar_init(smem_u32(j_full), 4); mbar_init(smem_u32(j_empty), 4);
-    mbar_init(smem_u32(mma_done), 1);
+    mbar_init(smem_u32(mma_done), 2);
     fence_barrier_init();
   }
   tc_fence_before();
@@ -381,77 +486,108 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
         rem -= __shfl_sync(0xffffffffu, inc, 31);
       }
     }
-    bool ok = true;
-    while (ok) {
+    bool ok = true, ended = false;
+    // Hands the next item (or the end) to the other roles.
+    auto publish = [&]() {
       const int ri = it % kChunkItems;
-      const bool more = u < u_end;
-      if (!mbar_wait_warp(smem_u32(&it_empty[ri]), ((it / kChunkItems) & 1) ^ 1)) { set_status(c, kDevWaitTimeout); break; }
+      if (!mbar_sleep_warp(smem_u32(&it_empty[ri]), ((it / kChunkItems) & 1) ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; return; }
+      ++it;
       ChunkItem *x = Items + ri;
-      if (!more) {
+      if (u >= u_end) {
         if (lane == 0) { x->kind = 0; mbar_arrive(smem_u32(&it_full[ri])); }
-        break;
-      }
-      const Block b = block(f);
-      if (b.units > 0) {
-        const int take = (int)min((long long)(b.units - off), u_end - u);
-        const int ntok = b.j1 - b.j0, nt0 = min(ntok, TPT), seg = seg_of(c, a.layer, b.s, head);
-        const int *ptrow = c.pt + (size_t)seg * c.max_pages;
-        // This CTA's pages of the item: [pa0, pa1) at the front, [pb0, pb1) behind; with a window, less the pages that
-        // the stored positions show to be hidden from every token.
-        int pa0 = min(off, b.r.sp), pa1 = min(off + take, b.r.sp);
-        int pb0 = b.r.b0 + max(off - b.r.sp, 0), pb1 = b.r.b0 + max(off + take - b.r.sp, 0);
-        int na = 0;
-        if (W) {
-          na = S ? slot_sinks(c, ptrow, b.n, S) : 0;
-          const int e0 = b.n - b.T + b.j0 + 1;
-          int first = 0;
-          for (int i0 = 0; i0 < ntok; i0 += 32) {
-            int w = 0;
-            if (i0 + lane < ntok) {
-              const int last = e0 + i0 + lane - 1;
-              w = slot_window(c, ptrow, last, slot_pos(c, ptrow, last), W);
-              Wlo[ri * 256 + i0 + lane] = w;
-            }
-            if (i0 == 0) first = __shfl_sync(0xffffffffu, w, 0);
-          }
-          const int a16 = (na + kPage - 1) / kPage, w16 = first / kPage;
-          if (b.r.sp == 0) {   // one run of pages: split it around the hidden ones
-            pa0 = pb0;
-            pa1 = max(pa0, min(pb1, a16));
-            pb0 = min(pb1, max(pb0, max(a16, w16)));
-          } else {
-            pa1 = max(pa0, min(pa1, a16));
-            pb0 = min(pb1, max(pb0, w16));
-          }
-        }
-        const long long U0 = u - off;
-        const int cf = (int)(U0 / per), cl = (int)((U0 + b.units - 1) / per);
-        const int part = cf == cl ? -1 : cf == (int)blockIdx.x ? 1 : 0;
-        if (lane == 0) {
-          x->kind = ntok > nt0 ? 1 : 2;
-          x->head = head; x->seg = seg;
-          x->row0 = a.lens.tok[b.s] + b.j0;
-          x->ntok[0] = nt0; x->ntok[1] = ntok - nt0;
-          x->e0 = b.n - b.T + b.j0 + 1;
-          x->n = b.n; x->a = na;
-          x->pa0 = pa0; x->pa1 = pa1; x->pb0 = pb0; x->pb1 = pb1;
-          x->part = part;
-          if (part == 1) {
-            info[0] = cl; info[1] = head; info[2] = x->row0; info[3] = nt0; info[4] = ntok - nt0;
-          }
-        }
-        if (part == 1) open = true;
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&it_full[ri]));
-        ++it;
-        u += take;
+        ended = true;
+        return;
       }
+      Block b = block(f);
+      while (b.units == 0) {
+        if (++f == NB) { f = 0; ++head; }
+        b = block(f);
+      }
+      const int take = (int)min((long long)(b.units - off), u_end - u);
+      const int ntok = b.j1 - b.j0, nt0 = min(ntok, TPT), seg = seg_of(c, a.layer, b.s, head), e0 = b.n - b.T + b.j0 + 1;
+      const int *ptrow = c.pt + (size_t)seg * c.max_pages;
+      // This CTA's pages of the item: [pa0, pa1) at the front, [pb0, pb1) behind; with a window, less the pages that the
+      // stored positions show to be hidden from every token.
+      int pa0 = min(off, b.r.sp), pa1 = min(off + take, b.r.sp);
+      int pb0 = b.r.b0 + max(off - b.r.sp, 0), pb1 = b.r.b0 + max(off + take - b.r.sp, 0);
+      int na = 0;
+      if (W) {
+        na = S ? slot_sinks(c, ptrow, b.n, S) : 0;
+        int first = 0;
+        for (int i0 = 0; i0 < ntok; i0 += 32) {
+          int w = 0;
+          if (i0 + lane < ntok) {
+            const int last = e0 + i0 + lane - 1;
+            w = slot_window(c, ptrow, last, slot_pos(c, ptrow, last), W);
+            Wlo[ri * 256 + i0 + lane] = w;
+          }
+          if (i0 == 0) first = __shfl_sync(0xffffffffu, w, 0);
+        }
+        const int a16 = (na + kPage - 1) / kPage, w16 = first / kPage;
+        if (b.r.sp == 0) {   // one run of pages: split it around the hidden ones
+          pa0 = pb0;
+          pa1 = max(pa0, min(pb1, a16));
+          pb0 = min(pb1, max(pb0, max(a16, w16)));
+        } else {
+          pa1 = max(pa0, min(pa1, a16));
+          pb0 = min(pb1, max(pb0, w16));
+        }
+      }
+      // Whole, or cut by an end of this CTA's range: then its part goes to slot 1 if the item begins here, else to slot 0.
+      const bool begins = u - off >= per * blockIdx.x, ends = off + take == b.units;
+      const int part = begins ? (ends ? -1 : 1) : 0;
+      if (lane == 0) {
+        x->kind = ntok > nt0 ? 1 : 2;
+        x->head = head; x->seg = seg;
+        x->row0 = a.lens.tok[b.s] + b.j0;
+        x->ntok[0] = nt0; x->ntok[1] = ntok - nt0;
+        x->e0 = e0; x->n = b.n; x->a = na;
+        x->pa0 = pa0; x->pa1 = pa1; x->pb0 = pb0; x->pb1 = pb1;
+        x->part = part;
+        if (part == 1) {   // for the merge, with the last CTA that the item reaches
+          info[0] = (int)((u - off + b.units - 1) / per);
+          info[1] = head; info[2] = x->row0; info[3] = nt0; info[4] = ntok - nt0;
+        }
+      }
+      if (part == 1) open = true;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&it_full[ri]));
+      u += take;
       off = 0;
       if (++f == NB) { f = 0; ++head; }
+    };
+    // V of an item, one item behind the walk.
+    FeatRing rr{0, 0};
+    uint32_t armed = 0, armed_par = 0;    // bit s: slot s has been armed / its last parity
+    publish();
+    for (int vi = 0; ok; ++vi) {
+      if (!ended) publish();
+      const ChunkItem &x = Items[vi % kChunkItems];
+      if (!ok || x.kind == 0) break;
+      const ChunkTiles tl(x);
+      const int *ptrow = c.pt + (size_t)x.seg * c.max_pages;
+      auto page_id = [&](int i) { return i < tl.nt && (lane & 7) < tl.pages(i) ? __ldcg(ptrow + tl.first(i) + (lane & 7)) : 0; };
+      int id = page_id(0);
+      for (int i = 0; i < tl.nt; ++i) {
+        const int idn = page_id(i + 1), np = tl.pages(i);
+        if (!mbar_wait_warp(smem_u32(&v_empty[rr.i]), rr.ph ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+        const uint32_t bar = smem_u32(&v_full[rr.i]);
+        if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(np * NQ) * PAGE_HALF);
+        armed |= 1u << rr.i;
+        armed_par = (armed_par & ~(1u << rr.i)) | ((uint32_t)rr.ph << rr.i);
+        __syncwarp();
+        if (lane < np) tma_page_v(smem_u32(Vt + rr.i * SM::kTile + (size_t)lane * NQ * PAGE_HALF), &tmv, NQ, id, bar);
+        rr.next(NS);
+        id = idn;
+      }
     }
     if (!open && lane == 0) info[0] = -1;
+#pragma unroll
+    for (int s = 0; s < NS; ++s)   // no copy may be in flight at the exit
+      if (((armed >> s) & 1u) && !mbar_wait_warp(smem_u32(&v_full[s]), (armed_par >> s) & 1u)) set_status(c, kDevWaitTimeout);
   } else if (warp == 0) {
-    // ---------------- copies ----------------
+    // ---------------- copies of the query tiles and of K ----------------
     FeatRing rr{0, 0};
     int it = 0;
     uint32_t qp = 0;                      // bit t: parity of query tile t's next phase
@@ -460,16 +596,16 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
     const int pg = lane & 7, half = lane >> 3;
     while (ok) {
       const int ri = it % kChunkItems;
-      if (!mbar_wait_warp(smem_u32(&it_full[ri]), (it / kChunkItems) & 1)) { set_status(c, kDevWaitTimeout); break; }
+      if (!mbar_sleep_warp(smem_u32(&it_full[ri]), (it / kChunkItems) & 1)) { set_status(c, kDevWaitTimeout); break; }
       const ChunkItem x = Items[ri];
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&it_empty[ri]));
       ++it;
       if (x.kind == 0) break;
-      const int ntA = (x.pa1 - x.pa0 + TP - 1) / TP, nt = ntA + (x.pb1 - x.pb0 + TP - 1) / TP;
-      if (nt == 0) continue;
+      const ChunkTiles tl(x);
+      if (tl.nt == 0) continue;
       for (int t = 0; t < (x.kind == 1 ? 2 : 1) && ok; ++t) {
-        if (!mbar_wait_warp(smem_u32(&q_empty[t]), ((qp >> t) & 1) ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+        if (!mbar_sleep_warp(smem_u32(&q_empty[t]), ((qp >> t) & 1) ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; break; }
         if (lane == 0) {
           mbar_arrive_expect_tx(smem_u32(&q_full[t]), (uint32_t)(NQ * TPT * G * 128));
           for (int q = 0; q < NQ; ++q)
@@ -482,59 +618,40 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       }
       if (!ok) break;
       const int *ptrow = c.pt + (size_t)x.seg * c.max_pages;
-      auto pages = [&](int i, int &p0) {   // pages of key tile i
-        p0 = i < ntA ? x.pa0 + TP * i : x.pb0 + TP * (i - ntA);
-        return min(TP, (i < ntA ? x.pa1 : x.pb1) - p0);
-      };
-      auto page_id = [&](int i) {
-        if (i >= nt) return 0;
-        int p0;
-        const int np = pages(i, p0);
-        return pg < np ? __ldcg(ptrow + p0 + pg) : 0;
-      };
-      auto copy = [&](int i, int pid, int what) {   // K (0) or V (1) of key tile i
-        int p0;
-        const int np = pages(i, p0);
-        if (!mbar_wait_warp(smem_u32(&kv_empty[rr.i]), rr.ph ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; return; }
-        const uint32_t bar = smem_u32(&kv_full[rr.i]);
+      auto page_id = [&](int i) { return i < tl.nt && pg < tl.pages(i) ? __ldcg(ptrow + tl.first(i) + pg) : 0; };
+      int id = page_id(0);
+      for (int i = 0; i < tl.nt; ++i) {   // a lane per copy: page pg, 64 channels
+        const int idn = page_id(i + 1), np = tl.pages(i);
+        if (!mbar_wait_warp(smem_u32(&k_empty[rr.i]), rr.ph ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+        const uint32_t bar = smem_u32(&k_full[rr.i]);
         if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(np * NQ) * PAGE_HALF);
         armed |= 1u << rr.i;
         armed_par = (armed_par & ~(1u << rr.i)) | ((uint32_t)rr.ph << rr.i);
         __syncwarp();
         if (pg < np && half < NQ)
-          tma_page_k(smem_u32(Ring + rr.i * SM::kTile + (size_t)half * 128 * 128 + (size_t)pg * PAGE_HALF), &tmkv,
-                     what * NQ + half, pid, bar);
+          tma_page_k(smem_u32(Kt + rr.i * SM::kTile + (size_t)half * 128 * 128 + (size_t)pg * PAGE_HALF), &tmk, half, id, bar);
         rr.next(NS);
-      };
-      // K of the first tile(s), then V of a tile and K of the one that the same stream multiplies next.
-      const int ahead = x.kind;   // key tiles between a stream's tile and its next one
-      int id0 = page_id(0), id1 = page_id(1);
-      int idk = ahead == 1 ? id1 : page_id(2);
-      copy(0, id0, 0);
-      if (ahead == 2 && nt > 1 && ok) copy(1, id1, 0);
-      for (int i = 0; i < nt && ok; ++i) {
-        const int idn = page_id(i + ahead + 1);
-        copy(i, id0, 1);
-        if (i + ahead < nt && ok) copy(i + ahead, idk, 0);
-        id0 = id1;
-        id1 = ahead == 1 ? idn : idk;
-        if (ahead == 1) { id0 = idk; }
-        idk = idn;
+        id = idn;
       }
     }
     // No copy may be in flight at the exit.
 #pragma unroll
     for (int s = 0; s < NS; ++s)
-      if (((armed >> s) & 1u) && !mbar_wait_warp(smem_u32(&kv_full[s]), (armed_par >> s) & 1u)) set_status(c, kDevWaitTimeout);
+      if (((armed >> s) & 1u) && !mbar_wait_warp(smem_u32(&k_full[s]), (armed_par >> s) & 1u)) set_status(c, kDevWaitTimeout);
 #pragma unroll
     for (int t = 0; t < 2; ++t)
       if (((armed >> (16 + t)) & 1u) && !mbar_wait_warp(smem_u32(&q_full[t]), (armed_par >> (16 + t)) & 1u)) set_status(c, kDevWaitTimeout);
-  } else if (warp == 1) {
-    // ---------------- multiplies: the warp stays together, lane 0 issues ----------------
-    FeatRing rr{0, 0};
+  } else if (warp == 1 || warp == 3) {
+    // ---------------- multiplies: a warp for each stream; it stays together, lane 0 issues.  A stream's O += P V and its
+    // next S go out in one run, and the streams take turns with their runs: one exponentiates while the other multiplies.
+    // (Left alone they fall into step, both waiting for the same unit all the time.) ----------------
+    const int t = uniform(warp >> 1);
+    const uint32_t on = lane == 0;
+    FeatRing kr{0, 0}, vr{0, 0};
     int it = 0;
-    uint32_t qp = 0, np_ph = 0, no_ph = 0;   // bit t: parity of query tile t's next phase / stream t's next p_full / o_empty
+    uint32_t qp = 0, pp = 0, op = 0, tp = t ^ 1;   // parities: bit t of the query tiles' next phase; the next p_full, o_empty, turn
     bool ok = true;
+    const uint32_t ts = uniform(tmem_base + t * 128), to = ts + 256;
     const uint32_t idesc_o = umma_idesc_bf16(kChunkRows, D) | (1u << 16);   // B runs along N
     while (ok) {
       const int ri = it % kChunkItems;
@@ -544,150 +661,102 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       if (lane == 0) mbar_arrive(smem_u32(&it_empty[ri]));
       ++it;
       if (x.kind == 0) break;
-      const int ntA = (x.pa1 - x.pa0 + TP - 1) / TP, nt = ntA + (x.pb1 - x.pb0 + TP - 1) / TP;
+      const ChunkTiles tl(x);
+      const int nt = uniform(tl.nt);
       if (nt == 0) continue;
-      const int ns = x.kind == 1 ? 2 : 1;   // query tiles
-      for (int t = 0; t < ns; ++t) {
-        if (!mbar_spin(smem_u32(&q_full[t]), (qp >> t) & 1)) { set_status(c, kDevWaitTimeout); ok = false; }
-        qp ^= 1u << t;
-      }
-      if (!ok) break;
-      auto pages = [&](int i, int &p0) {
-        p0 = i < ntA ? x.pa0 + TP * i : x.pb0 + TP * (i - ntA);
-        return min(TP, (i < ntA ? x.pa1 : x.pb1) - p0);
+      const int step = uniform(x.kind), qt = step == 1 ? t : 0;   // key tiles between a stream's tile and its next one
+      if (!mbar_spin(smem_u32(&q_full[qt]), (qp >> qt) & 1)) { set_status(c, kDevWaitTimeout); break; }
+      qp ^= step == 1 ? 3u : 1u;
+      // The next slot of a ring, filled.
+      auto wait_slot = [&](FeatRing &r, uint64_t *full) {
+        const int slot = uniform(r.i);
+        if (!mbar_spin(smem_u32(&full[r.i]), r.ph)) { set_status(c, kDevWaitTimeout); ok = false; }
+        r.next(NS);
+        return slot;
       };
-      auto wait_slot = [&](const FeatRing &r) {
-        if (!mbar_spin(smem_u32(&kv_full[r.i]), r.ph)) { set_status(c, kDevWaitTimeout); ok = false; }
+      // A slot is free again when both streams have let it go; the one that has no use for it does so at once.
+      auto skip_slot = [&](FeatRing &r, uint64_t *full, uint64_t *empty) {
+        const int slot = wait_slot(r, full);
+        if (lane == 0 && ok) mbar_arrive(smem_u32(&empty[slot]));
       };
-      // S of stream t = (query tile qt) (key tile i)^T
-      auto mul_s = [&](int t, int qt, int i, int slot) {
-        int p0;
-        const int np = pages(i, p0);
-        tc_fence_after();
-        if (lane == 0) {
-          const uint32_t idesc = umma_idesc_bf16(kChunkRows, np * kPage);
-          const uint64_t ad = umma_desc_sw128(smem_u32(Qt + qt * SM::kTile)), bd = umma_desc_sw128(smem_u32(Ring + slot * SM::kTile));
+      auto key_desc = [&](int slot) { return umma_desc_sw128(smem_u32(Kt + slot * SM::kTile)); };
+      // S = (query tile) (key tile)^T
+      const uint64_t qd = umma_desc_sw128(smem_u32(Qt + qt * SM::kTile));
+      auto mul_s = [&](uint64_t kd, uint32_t idesc) {
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks) {
-            const uint64_t o = (uint64_t)(((ks >> 2) * 128 * 128 + (ks & 3) * 32) >> 4);
-            umma_bf16(tmem_base + t * 128, ad + o, bd + o, idesc, ks > 0);
-          }
-          umma_commit(smem_u32(&s_full[t]));
+        for (int ks = 0; ks < D / 16; ++ks) {
+          const uint64_t o = (uint64_t)(((ks >> 2) * 128 * 128 + (ks & 3) * 32) >> 4);
+          umma_bf16_if(on, ts, qd + o, kd + o, idesc, ks > 0);
         }
-        __syncwarp();
+        umma_commit_if(on, smem_u32(&s_full[t]));
       };
-      // O of stream t += P (key tile i's V); `first`: the stream's first tile of the item
-      auto mul_o = [&](int t, int i, int slot, bool first) {
-        int p0;
-        const int np = pages(i, p0);
-        if (first) {
-          if (!mbar_spin(smem_u32(&o_empty[t]), ((no_ph >> t) & 1) ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; }
-          no_ph ^= 1u << t;
-        }
-        if (!mbar_spin(smem_u32(&p_full[t]), (np_ph >> t) & 1)) { set_status(c, kDevWaitTimeout); ok = false; }
-        np_ph ^= 1u << t;
-        if (!ok) return;
-        tc_fence_after();
-        if (lane == 0) {
-          const uint64_t bd = umma_desc_mn_sw128(smem_u32(Ring + slot * SM::kTile));
-          for (int ks = 0; ks < np; ++ks)
-            umma_bf16_ta(tmem_base + 256 + t * 128, tmem_base + t * 128 + ks * 8, bd + (uint64_t)((ks * PAGE_HALF) >> 4), idesc_o,
-                         !first || ks > 0);
-        }
-        __syncwarp();
-      };
-      // Rows of the last page past the segment's end hold whatever the page held before: P is zero there, but zero times
-      // an infinity is not, so they are cleared.
-      auto clear_tail = [&](int i, int slot) {
-        int p0;
-        const int np = pages(i, p0), r0 = x.n - p0 * kPage;
-        if (r0 >= np * kPage) return;
-        for (int e = lane; e < (np * kPage - r0) * NQ * 8; e += 32) {
-          const int r = r0 + e / (NQ * 8), ch = e % (NQ * 8);
-          *reinterpret_cast<uint4 *>(Ring + slot * SM::kTile + (size_t)(ch >> 3) * 128 * 128 + r * 128 + (ch & 7) * 16) =
-              make_uint4(0u, 0u, 0u, 0u);
-        }
-        fence_proxy_async();
-        __syncwarp();
-      };
-      auto release = [&](int slot) {
-        if (lane == 0) umma_commit(smem_u32(&kv_empty[slot]));
-        __syncwarp();
-      };
-      if (x.kind == 1) {
-        FeatRing k = rr, v;
-        rr.next(NS);
-        wait_slot(k);
+      for (int i = 0; i < min(step, nt) && ok; ++i) {
+        if (step == 2 && i != t) { skip_slot(kr, k_full, k_empty); continue; }
+        const int slot = wait_slot(kr, k_full);
         if (!ok) break;
-        mul_s(0, 0, 0, k.i);
-        mul_s(1, 1, 0, k.i);
-        release(k.i);
-        for (int i = 0; i < nt && ok; ++i) {
-          const bool more = i + 1 < nt;
-          v = rr;
-          rr.next(NS);
-          k = rr;
-          if (more) rr.next(NS);
-          wait_slot(v);
-          if (!ok) break;
-          clear_tail(i, v.i);
-          for (int t = 0; t < 2 && ok; ++t) {
-            mul_o(t, i, v.i, i == 0);
-            if (!ok) break;
-            if (t == 1) release(v.i);
-            if (!more) {
-              if (lane == 0) umma_commit(smem_u32(&o_full[t]));
-              __syncwarp();
-              continue;
-            }
-            if (t == 0) wait_slot(k);
-            if (!ok) break;
-            mul_s(t, t, i + 1, k.i);
-            if (t == 1) release(k.i);
-            if (i + 2 == nt && lane == 0) umma_commit(smem_u32(&q_empty[t]));   // the tile's last product
-            __syncwarp();
-          }
-        }
-        if (nt == 1 && ok && lane == 0) { umma_commit(smem_u32(&q_empty[0])); umma_commit(smem_u32(&q_empty[1])); }
-      } else {
-        FeatRing k = rr, v;
-        for (int t = 0; t < min(2, nt) && ok; ++t) {
-          k = rr;
-          rr.next(NS);
-          wait_slot(k);
-          if (!ok) break;
-          mul_s(t, 0, t, k.i);
-          release(k.i);
-        }
-        for (int i = 0; i < nt && ok; ++i) {
-          const int t = i & 1;
-          const bool more = i + 2 < nt;
-          v = rr;
-          rr.next(NS);
-          k = rr;
-          if (more) rr.next(NS);
-          wait_slot(v);
-          if (!ok) break;
-          clear_tail(i, v.i);
-          mul_o(t, i, v.i, i < 2);
-          if (!ok) break;
-          release(v.i);
-          if (!more) {
-            if (lane == 0) umma_commit(smem_u32(&o_full[t]));
-            __syncwarp();
-            continue;
-          }
-          wait_slot(k);
-          if (!ok) break;
-          mul_s(t, 0, i + 2, k.i);
-          release(k.i);
-        }
-        if (ok && lane == 0) umma_commit(smem_u32(&q_empty[0]));
+        tc_fence_after();
+        mul_s(key_desc(slot), umma_idesc_bf16(kChunkRows, uniform(tl.pages(i)) * kPage));
+        umma_commit_if(on, smem_u32(&k_empty[slot]));
       }
-      __syncwarp();
+      for (int i = 0; i < nt && ok; ++i) {
+        const bool more = i + step < nt, mine = step == 1 || (i & 1) == t;
+        if (!mine) {
+          skip_slot(vr, v_full, v_empty);
+          if (more && ok) skip_slot(kr, k_full, k_empty);
+          if (t == 1 && i + 1 == nt && ok) {   // an odd tile at the end is the first stream's: its turn is handed back
+            if (!mbar_spin(smem_u32(&turn[1]), tp)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+            tp ^= 1;
+            if (lane == 0) mbar_arrive(smem_u32(&turn[0]));
+          }
+          continue;
+        }
+        // Everything but P is waited for and worked out first.
+        const int np = uniform(tl.pages(i)), nk = uniform(more ? tl.pages(i + step) : 0), r0 = x.n - tl.first(i) * kPage;
+        const int vs = wait_slot(vr, v_full), ks_ = more ? wait_slot(kr, k_full) : 0;
+        if (!ok) break;
+        // Rows of the last page past the segment's end hold whatever the page held before: P is zero there, but zero
+        // times an infinity is not, so they are cleared.
+        if (r0 < np * kPage) {
+          for (int e = lane; e < (np * kPage - r0) * NQ * 8; e += 32) {
+            const int r = r0 + e / (NQ * 8), ch = e % (NQ * 8);
+            *reinterpret_cast<uint4 *>(Vt + vs * SM::kTile + (size_t)((r / kPage * NQ + (ch >> 3)) * kPage + r % kPage) * 128 + (ch & 7) * 16) =
+                make_uint4(0u, 0u, 0u, 0u);
+          }
+          fence_proxy_async();
+          __syncwarp();
+        }
+        const bool first = i < step;
+        if (first) {
+          if (!mbar_spin(smem_u32(&o_empty[t]), op ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+          op ^= 1;
+        }
+        const uint64_t vd = umma_desc_mn_sw128(smem_u32(Vt + vs * SM::kTile)), kd = key_desc(ks_);
+        const uint32_t idesc_s = umma_idesc_bf16(kChunkRows, nk * kPage);
+        const bool mine_now = mbar_spin(smem_u32(&turn[t]), tp);
+        if (!__all_sync(0xffffffffu, mine_now && mbar_spin(smem_u32(&p_full[t]), pp))) { set_status(c, kDevWaitTimeout); ok = false; break; }
+        tp ^= 1;
+        pp ^= 1;
+        tc_fence_after();
+        umma_bf16_ta_if(on, to, ts, vd, idesc_o, !first);
+        if (np == TP) {
+#pragma unroll
+          for (int ks = 1; ks < TP; ++ks) umma_bf16_ta_if(on, to, ts + ks * 8, vd + (uint64_t)((ks * NQ * PAGE_HALF) >> 4), idesc_o, 1);
+        } else {
+          for (int ks = 1; ks < np; ++ks) umma_bf16_ta_if(on, to, ts + ks * 8, vd + (uint64_t)((ks * NQ * PAGE_HALF) >> 4), idesc_o, 1);
+        }
+        if (more) mul_s(kd, idesc_s);
+        else umma_commit_if(on, smem_u32(&o_full[t]));
+        if (lane == 0) mbar_arrive(smem_u32(&turn[t ^ 1]));
+        umma_commit_if(on, smem_u32(&v_empty[vs]));
+        if (more) umma_commit_if(on, smem_u32(&k_empty[ks_]));
+      }
+      // The query tiles are free when their products are done: tile 0 when both streams say so.
+      if (ok) {
+        umma_commit_if(on, smem_u32(&q_empty[0]));
+        if (step == 1 && t == 1) umma_commit_if(on, smem_u32(&q_empty[1]));
+      }
     }
-    if (lane == 0) umma_commit(smem_u32(mma_done));   // nothing may be in flight when tensor memory is freed
-    __syncwarp();
+    umma_commit_if(on, smem_u32(mma_done));   // nothing may be in flight when tensor memory is freed
     if (!mbar_spin(smem_u32(mma_done), 0)) set_status(c, kDevWaitTimeout);
   } else if (warp >= 4) {
     // ---------------- softmax: thread = query row of stream t ----------------
@@ -701,23 +770,20 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
     while (ok) {
       const int ri = it % kChunkItems;
       if (!mbar_wait_warp(smem_u32(&it_full[ri]), (it / kChunkItems) & 1)) { set_status(c, kDevWaitTimeout); break; }
-      const ChunkItem x = Items[ri];
+      const ChunkItem &x = Items[ri];              // (let go at the item's end: registers are short here)
       const int qt = x.kind == 1 ? t : 0;          // the stream's query tile
       const int tj = qt * TPT + tok;
       const bool live = x.kind != 0 && tok < (qt ? x.ntok[1] : x.ntok[0]);
       const bool any = __any_sync(0xffffffffu, live);   // (a warp without a row in use only keeps the hand-overs going)
       const int e = live ? x.e0 + tj : INT_MAX;    // this row sees slots [0, a) and [wlo, e)
       const int wlo = live && a.window ? Wlo[ri * 256 + tj] : 0;
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&it_empty[ri]));
       ++it;
       if (x.kind == 0) break;
-      const int ntA = (x.pa1 - x.pa0 + TP - 1) / TP, nt = ntA + (x.pb1 - x.pb0 + TP - 1) / TP;
-      const int step = x.kind, i0 = x.kind == 1 ? 0 : t;
+      const ChunkTiles tl(x);
+      const int nt = tl.nt, step = x.kind, i0 = x.kind == 1 ? 0 : t;
       float m = -INFINITY, l = 0.f;
       for (int i = i0; i < nt; i += step) {
-        const int p0 = i < ntA ? x.pa0 + TP * i : x.pb0 + TP * (i - ntA);
-        const int cols = min(TP, (i < ntA ? x.pa1 : x.pb1) - p0) * kPage;
+        const int p0 = tl.first(i), cols = tl.pages(i) * kPage;
         const int hi = min(cols, e - p0 * kPage), lo = wlo - p0 * kPage, na = x.a - p0 * kPage;
         if (!mbar_wait_warp(smem_u32(&s_full[t]), sp)) { set_status(c, kDevWaitTimeout); ok = false; break; }
         sp ^= 1;
@@ -726,62 +792,35 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
           continue;
         }
         tc_fence_after();
-        // S is read twice, 32 columns at a time with the next ones on their way: once for the maximum, once for the
-        // exponentials.  (All 128 scores in registers at once do not fit beside the rest: they spilled.)
-        const bool masked = !__all_sync(0xffffffffu, hi >= 128 && (lo <= 0 || na >= 128));
-        uint32_t s[2][32];
-        tmem_ld32_issue(ts, s[0]);
-        float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          uint32_t(&v)[32] = s[q & 1];
-          tmem_ld_wait(v);
-          tmem_ld32_issue(ts + ((q + 1) & 3) * 32, s[(q + 1) & 1]);   // (after the last: the first once more)
-          if (masked) chunk_mask(v, q * 32, lo, hi, na);
-#pragma unroll
-          for (int j = 0; j < 32; j += 8)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) m4[k] = max3(m4[k], __uint_as_float(v[j + 2 * k]), __uint_as_float(v[j + 2 * k + 1]));
-        }
-        const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-        // The reference follows the maximum only when it has grown by more than 2^8 (or there was none yet).
+        // One walk over S, 16 columns at a time with the next ones on their way: exponentials against the reference m, and
+        // the maximum on the side.  m follows the maximum only when a score has passed it by more than 2^24; then (and in
+        // the stream's first tile, which has no m yet) O and l are rescaled and the walk is made again, which is why P
+        // waits in registers.
+        if (!__all_sync(0xffffffffu, hi >= 128 && (lo <= 0 || na >= 128))) chunk_mask(ts, lo, hi, na);
+        uint32_t p[2][32];
+        float lt, mx;
+        chunk_scores(ts, a.scale_log2, m == -INFINITY ? 0.f : m * a.scale_log2, p, lt, mx);
         const bool grow = mx > m && (mx - m) * a.scale_log2 > kChunkGrow;
         if (__any_sync(0xffffffffu, grow)) {
           const float f = grow ? ex2((m - mx) * a.scale_log2) : 1.f;
           if (grow) m = mx;
           l *= f;
           if (i != i0) {   // the stream's products up to the tile before are complete: this S was multiplied after them
-            tmem_ld_wait(s[0]);
 #pragma unroll 1
-            for (int q = 0; q < D / 32; ++q) {
-              uint32_t o[32];
-              tmem_ld32_issue(to + q * 32, o);
-              tmem_ld_wait(o);
+            for (int q = 0; q < D; q += 16) {
+              uint32_t o[16];
+              tmem_ld16_issue(to + q, o);
+              tmem_ld16_wait(o);
 #pragma unroll
-              for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-              tmem_st32(to + q * 32, o);
+              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+              tmem_st16(to + q, o);
             }
           }
+          chunk_scores(ts, a.scale_log2, m == -INFINITY ? 0.f : m * a.scale_log2, p, lt, mx);
         }
-        const float ms = m == -INFINITY ? 0.f : m * a.scale_log2;
-        float l4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          uint32_t(&v)[32] = s[q & 1];
-          tmem_ld_wait(v);
-          if (q < 3) tmem_ld32_issue(ts + (q + 1) * 32, s[(q + 1) & 1]);
-          if (masked) chunk_mask(v, q * 32, lo, hi, na);
-          uint32_t p[16];   // (its columns are those of scores that have been read)
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const float x0 = ex2(fmaf(__uint_as_float(v[2 * j]), a.scale_log2, -ms));
-            const float x1 = ex2(fmaf(__uint_as_float(v[2 * j + 1]), a.scale_log2, -ms));
-            l4[j & 3] += x0 + x1;
-            p[j] = pack_bf16(x0, x1);   // P in bf16, as V is: at most half a step (2^-8) off; the row sum is not rounded
-          }
-          tmem_st16(ts + q * 16, p);
-        }
-        l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+        l += lt;
+        tmem_st32(ts, p[0]);
+        tmem_st32(ts + 32, p[1]);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -800,7 +839,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       const size_t prow = (size_t)(blockIdx.x * 2 + max(x.part, 0)) * 256 + qt * kChunkRows + R;
       float f0 = 1.f, f1 = 0.f;   // weights of the two streams' results
       const bool writes = live && (x.kind == 1 || t == 0);
-#pragma unroll
+#pragma unroll 1
       for (int q = 0; q < D / 32; ++q) {
         uint32_t o[32];
         if (has) {
@@ -865,6 +904,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
         else if (a.lse)
           a.lse[orow] = l == 0.f ? -INFINITY : fmaf(m, a.scale, logf(l));
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&it_empty[ri]));
     }
   }
   // ---- common exit ----
