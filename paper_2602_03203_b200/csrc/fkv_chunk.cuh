@@ -407,6 +407,159 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
   griddep_wait();                          // everything below reads what earlier launches wrote
   griddep_launch();
 
+  if (warp >= 4) {
+    // The block was launched with 384 x 168 registers (64512 = 256 x 192 + 128 x 120).
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+    // ---------------- softmax: thread = query row of stream t ----------------
+    const int t = (warp - 4) >> 2, quarter = warp & 3, R = quarter * 32 + lane;
+    const int tok = R / G, hq = R - tok * G;
+    const uint32_t trow = tmem_base + ((uint32_t)(quarter * 32) << 16);
+    const uint32_t ts = trow + t * 128, to = trow + 256 + t * 128;
+    int it = 0;
+    uint32_t sp = 0, op = 0, jp = 0;   // parities of s_full, o_full and the join's barriers
+    bool ok = true;
+    while (ok) {
+      const int ri = it % kChunkItems;
+      if (!mbar_sleep_warp(smem_u32(&it_full[ri]), (it / kChunkItems) & 1)) { set_status(c, kDevWaitTimeout); break; }
+      const ChunkItem &x = Items[ri];              // (let go at the item's end: registers are short here)
+      const int qt = x.kind == 1 ? t : 0;          // the stream's query tile
+      const int tj = qt * TPT + tok;
+      const bool live = x.kind != 0 && tok < (qt ? x.ntok[1] : x.ntok[0]);
+      const bool any = __any_sync(0xffffffffu, live);   // (a warp without a row in use only keeps the hand-overs going)
+      const int e = live ? x.e0 + tj : INT_MAX;    // this row sees slots [0, a) and [wlo, e)
+      const int wlo = live && a.window ? Wlo[ri * 256 + tj] : 0;
+      ++it;
+      if (x.kind == 0) break;
+      const ChunkTiles tl(x);
+      const int nt = tl.nt, step = x.kind, i0 = x.kind == 1 ? 0 : t;
+      float m = -INFINITY, l = 0.f;
+      for (int i = i0; i < nt; i += step) {
+        const int p0 = tl.first(i), cols = tl.pages(i) * kPage;
+        const int hi = min(cols, e - p0 * kPage), lo = wlo - p0 * kPage, na = x.a - p0 * kPage;
+        if (!mbar_sleep_warp(smem_u32(&s_full[t]), sp)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+        sp ^= 1;
+        if (!any) {
+          if (lane == 0) mbar_arrive(smem_u32(&p_full[t]));
+          continue;
+        }
+        tc_fence_after();
+        // One walk over S, 16 columns at a time with the next ones on their way: exponentials against the reference m, and
+        // the maximum on the side.  m follows the maximum only when a score has passed it by more than 2^24; then (and in
+        // the stream's first tile, which has no m yet) O and l are rescaled and the walk is made again, which is why P
+        // waits in registers.
+        if (!__all_sync(0xffffffffu, hi >= 128 && (lo <= 0 || na >= 128))) chunk_mask(ts, lo, hi, na);
+        uint32_t p[2][32];
+        float lt, mx;
+        chunk_scores(ts, a.scale_log2, m == -INFINITY ? 0.f : m * a.scale_log2, p, lt, mx);
+        const bool grow = mx > m && (mx - m) * a.scale_log2 > kChunkGrow;
+        if (__any_sync(0xffffffffu, grow)) {
+          const float f = grow ? ex2((m - mx) * a.scale_log2) : 1.f;
+          if (grow) m = mx;
+          l *= f;
+          if (i != i0) {   // the stream's products up to the tile before are complete: this S was multiplied after them
+#pragma unroll 1
+            for (int q = 0; q < D; q += 16) {
+              uint32_t o[16];
+              tmem_ld16_issue(to + q, o);
+              tmem_ld16_wait(o);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+              tmem_st16(to + q, o);
+            }
+          }
+          chunk_scores(ts, a.scale_log2, m == -INFINITY ? 0.f : m * a.scale_log2, p, lt, mx);
+        }
+        l += lt;
+        tmem_st32(ts, p[0]);
+        tmem_st32(ts + 32, p[1]);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&p_full[t]));
+      }
+      if (!ok) break;
+      // ---- the item's end: this stream's O is complete ----
+      const bool has = i0 < nt;
+      if (has) {
+        if (!mbar_sleep_warp(smem_u32(&o_full[t]), op)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+        op ^= 1;
+        tc_fence_after();
+      }
+      const bool join = x.kind == 2 && nt > 1;   // both streams worked on the same rows
+      const size_t orow = ((size_t)(x.row0 + tj) * c.Hkv + x.head) * G + hq;
+      const size_t prow = (size_t)(blockIdx.x * 2 + max(x.part, 0)) * 256 + qt * kChunkRows + R;
+      float f0 = 1.f, f1 = 0.f;   // weights of the two streams' results
+      const bool writes = live && (x.kind == 1 || t == 0);
+#pragma unroll 1
+      for (int q = 0; q < D / 32; ++q) {
+        uint32_t o[32];
+        if (has) {
+          tmem_ld32_issue(to + q * 32, o);
+          tmem_ld_wait(o);
+        }
+        if (q == D / 32 - 1 && has) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&o_empty[t]));
+        }
+        if (join) {
+          // 32 columns at a time, the second stream hands its O (and, first, m and l) to the first.
+          if (!mbar_sleep_warp(smem_u32(t == 1 ? j_empty : j_full), t == 1 ? jp ^ 1 : jp)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+          jp ^= 1;
+          __syncwarp();
+          if (t == 1) {
+            if (q == 0) Ml[R] = make_float2(m, l);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) Mg[j * 128 + R] = __uint_as_float(o[j]);
+          } else {
+            if (q == 0) {
+              const float2 other = Ml[R];
+              const float M = fmaxf(m, other.x);
+              f0 = m == -INFINITY ? 0.f : ex2((m - M) * a.scale_log2);
+              f1 = other.x == -INFINITY ? 0.f : ex2((other.x - M) * a.scale_log2);
+              m = M;
+              l = l * f0 + other.y * f1;
+            }
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(fmaf(Mg[j * 128 + R], f1, __uint_as_float(o[j]) * f0));
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(t == 1 ? j_full : j_empty));
+        }
+        if (!writes) continue;
+        if (x.part >= 0) {
+          float *dst = c.chunk_part + prow * D + q * 32;
+          if (has)
+#pragma unroll
+            for (int j = 0; j < 32; j += 4)
+              __stcg(reinterpret_cast<float4 *>(dst + j), make_float4(__uint_as_float(o[j]), __uint_as_float(o[j + 1]),
+                                                                      __uint_as_float(o[j + 2]), __uint_as_float(o[j + 3])));
+        } else {
+          const float inv = l == 0.f ? 0.f : 1.f / l;   // a row that sees nothing gives zeros
+          uint4 *dst = reinterpret_cast<uint4 *>(a.out + orow * D + q * 32);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              w[k] = pack_bf16(__uint_as_float(o[8 * j + 2 * k]) * inv, __uint_as_float(o[8 * j + 2 * k + 1]) * inv);
+            dst[j] = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+      }
+      if (!ok) break;
+      if (writes) {
+        // (a row whose scores are all NaN has found no maximum, but must not count as one that saw nothing)
+        if (x.part >= 0)
+          __stcg(reinterpret_cast<float2 *>(c.chunk_ml) + prow, make_float2(l != l ? 0.f : m, l));
+        else if (a.lse)
+          a.lse[orow] = l == 0.f ? -INFINITY : fmaf(m, a.scale, logf(l));
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&it_empty[ri]));
+    }
+  } else {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
   if (warp == 2) {
     // ---------------- the walk over this CTA's range of the line of pages ----------------
     const int batch = c.batch, W = a.window, S = a.sinks, TB = 2 * TPT;
@@ -571,7 +724,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       int id = page_id(0);
       for (int i = 0; i < tl.nt; ++i) {
         const int idn = page_id(i + 1), np = tl.pages(i);
-        if (!mbar_wait_warp(smem_u32(&v_empty[rr.i]), rr.ph ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+        if (!mbar_sleep_warp(smem_u32(&v_empty[rr.i]), rr.ph ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; break; }
         const uint32_t bar = smem_u32(&v_full[rr.i]);
         if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(np * NQ) * PAGE_HALF);
         armed |= 1u << rr.i;
@@ -585,7 +738,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
     if (!open && lane == 0) info[0] = -1;
 #pragma unroll
     for (int s = 0; s < NS; ++s)   // no copy may be in flight at the exit
-      if (((armed >> s) & 1u) && !mbar_wait_warp(smem_u32(&v_full[s]), (armed_par >> s) & 1u)) set_status(c, kDevWaitTimeout);
+      if (((armed >> s) & 1u) && !mbar_sleep_warp(smem_u32(&v_full[s]), (armed_par >> s) & 1u)) set_status(c, kDevWaitTimeout);
   } else if (warp == 0) {
     // ---------------- copies of the query tiles and of K ----------------
     FeatRing rr{0, 0};
@@ -622,7 +775,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       int id = page_id(0);
       for (int i = 0; i < tl.nt; ++i) {   // a lane per copy: page pg, 64 channels
         const int idn = page_id(i + 1), np = tl.pages(i);
-        if (!mbar_wait_warp(smem_u32(&k_empty[rr.i]), rr.ph ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+        if (!mbar_sleep_warp(smem_u32(&k_empty[rr.i]), rr.ph ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; break; }
         const uint32_t bar = smem_u32(&k_full[rr.i]);
         if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(np * NQ) * PAGE_HALF);
         armed |= 1u << rr.i;
@@ -637,10 +790,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
     // No copy may be in flight at the exit.
 #pragma unroll
     for (int s = 0; s < NS; ++s)
-      if (((armed >> s) & 1u) && !mbar_wait_warp(smem_u32(&k_full[s]), (armed_par >> s) & 1u)) set_status(c, kDevWaitTimeout);
+      if (((armed >> s) & 1u) && !mbar_sleep_warp(smem_u32(&k_full[s]), (armed_par >> s) & 1u)) set_status(c, kDevWaitTimeout);
 #pragma unroll
     for (int t = 0; t < 2; ++t)
-      if (((armed >> (16 + t)) & 1u) && !mbar_wait_warp(smem_u32(&q_full[t]), (armed_par >> (16 + t)) & 1u)) set_status(c, kDevWaitTimeout);
+      if (((armed >> (16 + t)) & 1u) && !mbar_sleep_warp(smem_u32(&q_full[t]), (armed_par >> (16 + t)) & 1u)) set_status(c, kDevWaitTimeout);
   } else if (warp == 1 || warp == 3) {
     // ---------------- multiplies: a warp for each stream; it stays together, lane 0 issues.  A stream's O += P V and its
     // next S go out in one run, and the streams take turns with their runs: one exponentiates while the other multiplies.
@@ -655,7 +808,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
     const uint32_t idesc_o = umma_idesc_bf16(kChunkRows, D) | (1u << 16);   // B runs along N
     while (ok) {
       const int ri = it % kChunkItems;
-      if (!mbar_spin(smem_u32(&it_full[ri]), (it / kChunkItems) & 1)) { set_status(c, kDevWaitTimeout); break; }
+      if (!mbar_wait(smem_u32(&it_full[ri]), (it / kChunkItems) & 1)) { set_status(c, kDevWaitTimeout); break; }
       const ChunkItem x = Items[ri];
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&it_empty[ri]));
@@ -665,12 +818,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       const int nt = uniform(tl.nt);
       if (nt == 0) continue;
       const int step = uniform(x.kind), qt = step == 1 ? t : 0;   // key tiles between a stream's tile and its next one
-      if (!mbar_spin(smem_u32(&q_full[qt]), (qp >> qt) & 1)) { set_status(c, kDevWaitTimeout); break; }
+      if (!mbar_wait(smem_u32(&q_full[qt]), (qp >> qt) & 1)) { set_status(c, kDevWaitTimeout); break; }
       qp ^= step == 1 ? 3u : 1u;
       // The next slot of a ring, filled.
       auto wait_slot = [&](FeatRing &r, uint64_t *full) {
         const int slot = uniform(r.i);
-        if (!mbar_spin(smem_u32(&full[r.i]), r.ph)) { set_status(c, kDevWaitTimeout); ok = false; }
+        if (!mbar_wait(smem_u32(&full[r.i]), r.ph)) { set_status(c, kDevWaitTimeout); ok = false; }
         r.next(NS);
         return slot;
       };
@@ -704,7 +857,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
           skip_slot(vr, v_full, v_empty);
           if (more && ok) skip_slot(kr, k_full, k_empty);
           if (t == 1 && i + 1 == nt && ok) {   // an odd tile at the end is the first stream's: its turn is handed back
-            if (!mbar_spin(smem_u32(&turn[1]), tp)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+            if (!mbar_wait(smem_u32(&turn[1]), tp)) { set_status(c, kDevWaitTimeout); ok = false; break; }
             tp ^= 1;
             if (lane == 0) mbar_arrive(smem_u32(&turn[0]));
           }
@@ -727,13 +880,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
         }
         const bool first = i < step;
         if (first) {
-          if (!mbar_spin(smem_u32(&o_empty[t]), op ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+          if (!mbar_wait(smem_u32(&o_empty[t]), op ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; break; }
           op ^= 1;
         }
         const uint64_t vd = umma_desc_mn_sw128(smem_u32(Vt + vs * SM::kTile)), kd = key_desc(ks_);
         const uint32_t idesc_s = umma_idesc_bf16(kChunkRows, nk * kPage);
-        const bool mine_now = mbar_spin(smem_u32(&turn[t]), tp);
-        if (!__all_sync(0xffffffffu, mine_now && mbar_spin(smem_u32(&p_full[t]), pp))) { set_status(c, kDevWaitTimeout); ok = false; break; }
+        const bool mine_now = mbar_wait(smem_u32(&turn[t]), tp);
+        if (!__all_sync(0xffffffffu, mine_now && mbar_wait(smem_u32(&p_full[t]), pp))) { set_status(c, kDevWaitTimeout); ok = false; break; }
         tp ^= 1;
         pp ^= 1;
         tc_fence_after();
@@ -757,156 +910,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       }
     }
     umma_commit_if(on, smem_u32(mma_done));   // nothing may be in flight when tensor memory is freed
-    if (!mbar_spin(smem_u32(mma_done), 0)) set_status(c, kDevWaitTimeout);
-  } else if (warp >= 4) {
-    // ---------------- softmax: thread = query row of stream t ----------------
-    const int t = (warp - 4) >> 2, quarter = warp & 3, R = quarter * 32 + lane;
-    const int tok = R / G, hq = R - tok * G;
-    const uint32_t trow = tmem_base + ((uint32_t)(quarter * 32) << 16);
-    const uint32_t ts = trow + t * 128, to = trow + 256 + t * 128;
-    int it = 0;
-    uint32_t sp = 0, op = 0, jp = 0;   // parities of s_full, o_full and the join's barriers
-    bool ok = true;
-    while (ok) {
-      const int ri = it % kChunkItems;
-      if (!mbar_wait_warp(smem_u32(&it_full[ri]), (it / kChunkItems) & 1)) { set_status(c, kDevWaitTimeout); break; }
-      const ChunkItem &x = Items[ri];              // (let go at the item's end: registers are short here)
-      const int qt = x.kind == 1 ? t : 0;          // the stream's query tile
-      const int tj = qt * TPT + tok;
-      const bool live = x.kind != 0 && tok < (qt ? x.ntok[1] : x.ntok[0]);
-      const bool any = __any_sync(0xffffffffu, live);   // (a warp without a row in use only keeps the hand-overs going)
-      const int e = live ? x.e0 + tj : INT_MAX;    // this row sees slots [0, a) and [wlo, e)
-      const int wlo = live && a.window ? Wlo[ri * 256 + tj] : 0;
-      ++it;
-      if (x.kind == 0) break;
-      const ChunkTiles tl(x);
-      const int nt = tl.nt, step = x.kind, i0 = x.kind == 1 ? 0 : t;
-      float m = -INFINITY, l = 0.f;
-      for (int i = i0; i < nt; i += step) {
-        const int p0 = tl.first(i), cols = tl.pages(i) * kPage;
-        const int hi = min(cols, e - p0 * kPage), lo = wlo - p0 * kPage, na = x.a - p0 * kPage;
-        if (!mbar_wait_warp(smem_u32(&s_full[t]), sp)) { set_status(c, kDevWaitTimeout); ok = false; break; }
-        sp ^= 1;
-        if (!any) {
-          if (lane == 0) mbar_arrive(smem_u32(&p_full[t]));
-          continue;
-        }
-        tc_fence_after();
-        // One walk over S, 16 columns at a time with the next ones on their way: exponentials against the reference m, and
-        // the maximum on the side.  m follows the maximum only when a score has passed it by more than 2^24; then (and in
-        // the stream's first tile, which has no m yet) O and l are rescaled and the walk is made again, which is why P
-        // waits in registers.
-        if (!__all_sync(0xffffffffu, hi >= 128 && (lo <= 0 || na >= 128))) chunk_mask(ts, lo, hi, na);
-        uint32_t p[2][32];
-        float lt, mx;
-        chunk_scores(ts, a.scale_log2, m == -INFINITY ? 0.f : m * a.scale_log2, p, lt, mx);
-        const bool grow = mx > m && (mx - m) * a.scale_log2 > kChunkGrow;
-        if (__any_sync(0xffffffffu, grow)) {
-          const float f = grow ? ex2((m - mx) * a.scale_log2) : 1.f;
-          if (grow) m = mx;
-          l *= f;
-          if (i != i0) {   // the stream's products up to the tile before are complete: this S was multiplied after them
-#pragma unroll 1
-            for (int q = 0; q < D; q += 16) {
-              uint32_t o[16];
-              tmem_ld16_issue(to + q, o);
-              tmem_ld16_wait(o);
-#pragma unroll
-              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-              tmem_st16(to + q, o);
-            }
-          }
-          chunk_scores(ts, a.scale_log2, m == -INFINITY ? 0.f : m * a.scale_log2, p, lt, mx);
-        }
-        l += lt;
-        tmem_st32(ts, p[0]);
-        tmem_st32(ts + 32, p[1]);
-        tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&p_full[t]));
-      }
-      if (!ok) break;
-      // ---- the item's end: this stream's O is complete ----
-      const bool has = i0 < nt;
-      if (has) {
-        if (!mbar_wait_warp(smem_u32(&o_full[t]), op)) { set_status(c, kDevWaitTimeout); ok = false; break; }
-        op ^= 1;
-        tc_fence_after();
-      }
-      const bool join = x.kind == 2 && nt > 1;   // both streams worked on the same rows
-      const size_t orow = ((size_t)(x.row0 + tj) * c.Hkv + x.head) * G + hq;
-      const size_t prow = (size_t)(blockIdx.x * 2 + max(x.part, 0)) * 256 + qt * kChunkRows + R;
-      float f0 = 1.f, f1 = 0.f;   // weights of the two streams' results
-      const bool writes = live && (x.kind == 1 || t == 0);
-#pragma unroll 1
-      for (int q = 0; q < D / 32; ++q) {
-        uint32_t o[32];
-        if (has) {
-          tmem_ld32_issue(to + q * 32, o);
-          tmem_ld_wait(o);
-        }
-        if (q == D / 32 - 1 && has) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&o_empty[t]));
-        }
-        if (join) {
-          // 32 columns at a time, the second stream hands its O (and, first, m and l) to the first.
-          if (!mbar_wait_warp(smem_u32(t == 1 ? j_empty : j_full), t == 1 ? jp ^ 1 : jp)) { set_status(c, kDevWaitTimeout); ok = false; break; }
-          jp ^= 1;
-          __syncwarp();
-          if (t == 1) {
-            if (q == 0) Ml[R] = make_float2(m, l);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) Mg[j * 128 + R] = __uint_as_float(o[j]);
-          } else {
-            if (q == 0) {
-              const float2 other = Ml[R];
-              const float M = fmaxf(m, other.x);
-              f0 = m == -INFINITY ? 0.f : ex2((m - M) * a.scale_log2);
-              f1 = other.x == -INFINITY ? 0.f : ex2((other.x - M) * a.scale_log2);
-              m = M;
-              l = l * f0 + other.y * f1;
-            }
-#pragma unroll
-            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(fmaf(Mg[j * 128 + R], f1, __uint_as_float(o[j]) * f0));
-          }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(t == 1 ? j_full : j_empty));
-        }
-        if (!writes) continue;
-        if (x.part >= 0) {
-          float *dst = c.chunk_part + prow * D + q * 32;
-          if (has)
-#pragma unroll
-            for (int j = 0; j < 32; j += 4)
-              __stcg(reinterpret_cast<float4 *>(dst + j), make_float4(__uint_as_float(o[j]), __uint_as_float(o[j + 1]),
-                                                                      __uint_as_float(o[j + 2]), __uint_as_float(o[j + 3])));
-        } else {
-          const float inv = l == 0.f ? 0.f : 1.f / l;   // a row that sees nothing gives zeros
-          uint4 *dst = reinterpret_cast<uint4 *>(a.out + orow * D + q * 32);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t w[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              w[k] = pack_bf16(__uint_as_float(o[8 * j + 2 * k]) * inv, __uint_as_float(o[8 * j + 2 * k + 1]) * inv);
-            dst[j] = make_uint4(w[0], w[1], w[2], w[3]);
-          }
-        }
-      }
-      if (!ok) break;
-      if (writes) {
-        // (a row whose scores are all NaN has found no maximum, but must not count as one that saw nothing)
-        if (x.part >= 0)
-          __stcg(reinterpret_cast<float2 *>(c.chunk_ml) + prow, make_float2(l != l ? 0.f : m, l));
-        else if (a.lse)
-          a.lse[orow] = l == 0.f ? -INFINITY : fmaf(m, a.scale, logf(l));
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&it_empty[ri]));
-    }
+    if (!mbar_wait(smem_u32(mma_done), 0)) set_status(c, kDevWaitTimeout);
+  }
   }
   // ---- common exit ----
   tc_fence_before();
