@@ -15,9 +15,9 @@
 // goes through leaves partial results (O, m, l) which k_chunk_merge joins.
 //   warp 0      tensor copies (TMA) of the item's query tiles and of K, page by page (one copy = 16 rows x 64 channels; the
 //               page record's swizzle is the shared-memory swizzle), into a ring of key tiles of up to eight pages;
-//   warps 1, 3  one lane each issues the tcgen05.mma of one stream: S = Q K^T (K-major operands) into tensor memory,
-//               O += P V with P read from tensor memory and V as an MN-major operand (channels run along its rows: no
-//               transpose anywhere);
+//   warp 1      one lane issues tcgen05.mma S = Q K^T (K-major operands) into tensor memory;
+//   warp 3      ... and O += P V with P read from tensor memory and V as an MN-major operand (channels run along its
+//               rows: no transpose anywhere);
 //   warp 2      walks the items ahead of the others, searches the positions, and copies V (one copy = a page's 16 rows): a
 //               warp issues a copy per 80 - 100 cycles, so one for K and V would not keep up;
 //   warps 4-11  two warpgroups, each with a stream of its own (S and O accumulators): thread = query row; running
@@ -39,7 +39,6 @@ namespace fkv {
 constexpr int kChunkCtas = 148;       // most CTAs of a launch: each has two slots for partial results in the workspace
 constexpr int kChunkThreads = 384;
 constexpr int kChunkRows = 128;       // query rows of a tile = M of the mma
-constexpr int kChunkPages = 8;        // pages of a key tile: N of S, K of O
 constexpr int kChunkMinPages = 8;     // least work of a CTA
 constexpr int kChunkInfo = 8;         // words that describe a CTA's unfinished item to the merge
 constexpr float kChunkGrow = 24.f;    // log2 of the growth of a row's maximum that O is rescaled for
@@ -186,24 +185,33 @@ struct ChunkItem {
   int pad[2];
 };
 
-// The key tiles of an item: up to eight pages each, those of the sinks first.
+// The key tiles of an item: up to TP pages each, those of the sinks first.
+template <int TP>
 struct ChunkTiles {
   int pa0, pa1, pb0, pb1, na, nt;
   __device__ __forceinline__ explicit ChunkTiles(const ChunkItem &x) : pa0(x.pa0), pa1(x.pa1), pb0(x.pb0), pb1(x.pb1) {
-    na = (pa1 - pa0 + kChunkPages - 1) / kChunkPages;
-    nt = na + (pb1 - pb0 + kChunkPages - 1) / kChunkPages;
+    na = (pa1 - pa0 + TP - 1) / TP;
+    nt = na + (pb1 - pb0 + TP - 1) / TP;
   }
-  __device__ __forceinline__ int first(int i) const { return i < na ? pa0 + kChunkPages * i : pb0 + kChunkPages * (i - na); }
-  __device__ __forceinline__ int pages(int i) const { return min(kChunkPages, (i < na ? pa1 : pb1) - first(i)); }
+  __device__ __forceinline__ int first(int i) const { return i < na ? pa0 + TP * i : pb0 + TP * (i - na); }
+  __device__ __forceinline__ int pages(int i) const { return min(TP, (i < na ? pa1 : pb1) - first(i)); }
 };
 
 template <int D>
 struct ChunkSmem {
-  static constexpr int kSlots = D == 128 ? 2 : 4;                 // key tiles in flight, of K and of V
-  static constexpr size_t kTile = (size_t)(D / 64) * 128 * 128;   // 128 rows: [D / 64][128][128 B]
-  static constexpr size_t kMerge = 32 * 128 * 4;
-  static constexpr size_t kOffK = 2 * kTile, kOffV = kOffK + kSlots * kTile;
-  static constexpr size_t kOffMerge = kOffV + kSlots * kTile;
+  // Tensor memory holds, per stream, S, P and O side by side (a column is 4 bytes of each of 128 rows): with P apart from S
+  // the next S is multiplied as soon as the warps have read this one.  That sets the pages of a key tile (N of S, K of O):
+  // D = 128 has 256 columns for 80 + 40 + 128; D = 64 would have room for 128 + 64 + 64, but a thread has not for a row's
+  // 128 scores and 64 words of P: 96 + 48 + 64.
+  static constexpr int kPages = D == 128 ? 5 : 6, kCols = kPages * kPage;
+  static constexpr int kColP = kCols, kColO = D == 128 ? 128 : kCols + kCols / 2, kStream = 256;   // S at 0; per stream
+  static_assert(kColP + kCols / 2 <= kColO && kColO + D <= kStream, "a stream's columns");
+  static constexpr int kSlots = D == 128 ? 3 : 4;                 // key tiles in flight, of K and of V
+  static constexpr size_t kTile = (size_t)(D / 64) * 128 * 128;   // a query tile: [D / 64][128 rows][128 B]
+  static constexpr size_t kKv = (size_t)kPages * kPage * D * 2;   // a key tile: K [D / 64][rows][128 B], V [page][D / 64][16][128 B]
+  static constexpr size_t kMerge = 64 * 128 * 4;
+  static constexpr size_t kOffK = 2 * kTile, kOffV = kOffK + kSlots * kKv;
+  static constexpr size_t kOffMerge = kOffV + kSlots * kKv;
   static constexpr size_t kOffMl = kOffMerge + kMerge;                 // (m, l) of the second stream's rows
   static constexpr size_t kOffItems = kOffMl + 128 * 8;
   static constexpr size_t kOffWlo = kOffItems + kChunkItems * sizeof(ChunkItem);   // first slot of every token's window
@@ -263,12 +271,6 @@ __device__ __forceinline__ void umma_commit_if(uint32_t on, uint32_t bar) {
 // A value that is the same in all lanes, as the compiler can see.
 __device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
-               ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]),
-               "r"(taddr)
-               : "memory");
-}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // One page's V rows, all channels (from part part0 of the page's row): per 64 channels 16 rows of 128 bytes.
@@ -306,45 +308,38 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
                "r"(taddr)
                : "memory");
 }
-// The scores of the columns that the row does not see ([na, lo) and from hi on) become -infinity, in tensor memory: the
-// few tiles at an edge pay for a walk of their own, and the walk that every tile takes has no masks in it.
-__device__ __forceinline__ void chunk_mask(uint32_t ts, int lo, int hi, int na) {
-#pragma unroll 1
-  for (int q = 0; q < 128; q += 16) {
-    uint32_t v[16];
-    tmem_ld16_issue(ts + q, v);
-    tmem_ld16_wait(v);
-#pragma unroll
-    for (int j = 0; j < 16; ++j)
-      if (q + j >= hi || (q + j < lo && q + j >= na)) v[j] = 0xff800000u;
-    tmem_st16(ts + q, v);
-  }
-  tmem_st_wait();
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+               ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(taddr)
+               : "memory");
 }
 
-// A row's 128 scores from tensor memory: their maximum mx, P = 2^(scale s - ms) rounded to bf16 (as V is: at most half a
-// step, 2^-8, off) and its unrounded sum lt.
-__device__ __forceinline__ void chunk_scores(uint32_t ts, float scale_log2, float ms, uint32_t (&p)[2][32], float &lt, float &mx) {
-  uint32_t s[2][16];
-  tmem_ld16_issue(ts, s[0]);
+// A row's scores v: P = 2^(scale v - ms) in bf16 to tensor memory at tp (`ready` comes ahead of the first store), its sum
+// lt, the scores' maximum mx.
+template <int TP, class Ready>
+__device__ __forceinline__ void chunk_weights(const uint32_t (&v)[TP][16], float scale_log2, float ms, uint32_t tp, Ready ready, float &lt,
+                                              float &mx) {
   float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
   float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
   const float2 sc = make_float2(scale_log2, scale_log2), off = make_float2(-ms, -ms);
+  uint32_t p[2][8];
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    uint32_t(&v)[16] = s[q & 1];
-    tmem_ld16_wait(v);
-    if (q < 7) tmem_ld16_issue(ts + (q + 1) * 16, s[(q + 1) & 1]);
+  for (int q = 0; q < TP; ++q) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float2 z = make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
-      m4[j & 3] = max3(m4[j & 3], z.x, z.y);
+      const float2 z = make_float2(__uint_as_float(v[q][2 * j]), __uint_as_float(v[q][2 * j + 1]));
       float2 x = __ffma2_rn(z, sc, off);
       x.x = ex2(x.x);
       x.y = ex2(x.y);
+      m4[j & 3] = max3(m4[j & 3], z.x, z.y);
       l2[j & 1] = __fadd2_rn(l2[j & 1], x);
-      p[q >> 2][(q & 3) * 8 + j] = pack_bf16(x.x, x.y);
+      p[q & 1][j] = pack_bf16(x.x, x.y);
     }
+    if (q == 1) {
+      ready();
+      tmem_st8(tp, p[0]);
+    }
+    if (q >= 1) tmem_st8(tp + q * 8, p[q & 1]);
   }
   mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
   lt = (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
@@ -364,7 +359,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
                                                                    const __grid_constant__ CUtensorMap tmq,
                                                                    const __grid_constant__ ChunkArgs a) {
   using SM = ChunkSmem<D>;
-  constexpr int NS = SM::kSlots, NQ = D / 64, TP = kChunkPages;
+  constexpr int NS = SM::kSlots, NQ = D / 64, TP = SM::kPages;
   constexpr uint32_t PAGE_HALF = kPage * 128;
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -377,22 +372,24 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
   uint64_t *bars = reinterpret_cast<uint64_t *>(smem + SM::kOffBars);
   uint64_t *k_full = bars, *k_empty = k_full + NS, *v_full = k_empty + NS, *v_empty = v_full + NS;
   uint64_t *q_full = v_empty + NS, *q_empty = q_full + 2;
-  uint64_t *s_full = q_empty + 2, *p_full = s_full + 2, *o_full = p_full + 2, *o_empty = o_full + 2;
+  uint64_t *s_full = q_empty + 2, *s_empty = s_full + 2, *p_full = s_empty + 2, *p_empty = p_full + 2;
+  uint64_t *o_full = p_empty + 2, *o_empty = o_full + 2;
   uint64_t *it_full = o_empty + 2, *it_empty = it_full + kChunkItems, *j_full = it_empty + kChunkItems, *j_empty = j_full + 1;
-  uint64_t *turn = j_empty + 1, *mma_done = turn + 2;
+  uint64_t *mma_done = j_empty + 1;
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(mma_done + 1);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, G = c.G, TPT = kChunkRows / G;
 
   if (warp == 3) tmem_alloc(smem_u32(tmem_slot), 512);
   if (threadIdx.x == 0) {
+    for (const CUtensorMap *tm : {&tmk, &tmv, &tmq}) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tm)) : "memory");
     for (int s = 0; s < NS; ++s) {
-      mbar_init(smem_u32(&k_full[s]), 1); mbar_init(smem_u32(&k_empty[s]), 2);
-      mbar_init(smem_u32(&v_full[s]), 1); mbar_init(smem_u32(&v_empty[s]), 2);
+      mbar_init(smem_u32(&k_full[s]), 1); mbar_init(smem_u32(&k_empty[s]), 1);
+      mbar_init(smem_u32(&v_full[s]), 1); mbar_init(smem_u32(&v_empty[s]), 1);
     }
     for (int t = 0; t < 2; ++t) {
-      mbar_init(smem_u32(&turn[t]), 1);
-      mbar_init(smem_u32(&q_full[t]), 1); mbar_init(smem_u32(&q_empty[t]), 2 - t);
-      mbar_init(smem_u32(&s_full[t]), 1); mbar_init(smem_u32(&p_full[t]), 4);
+      mbar_init(smem_u32(&q_full[t]), 1); mbar_init(smem_u32(&q_empty[t]), 1);
+      mbar_init(smem_u32(&s_full[t]), 1); mbar_init(smem_u32(&s_empty[t]), 4);
+      mbar_init(smem_u32(&p_full[t]), 4); mbar_init(smem_u32(&p_empty[t]), 1);
       mbar_init(smem_u32(&o_full[t]), 1); mbar_init(smem_u32(&o_empty[t]), 4);
     }
     for (int i = 0; i < kChunkItems; ++i) { mbar_init(smem_u32(&it_full[i]), 1); mbar_init(smem_u32(&it_empty[i]), 11); }
@@ -403,20 +400,18 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem_base = *tmem_slot;   // columns: S0 | S1 | O0 | O1, 128 each
+  const uint32_t tmem_base = *tmem_slot;
   griddep_wait();                          // everything below reads what earlier launches wrote
   griddep_launch();
 
   if (warp >= 4) {
-    // The block was launched with 384 x 168 registers (64512 = 256 x 192 + 128 x 120).
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
     // ---------------- softmax: thread = query row of stream t ----------------
     const int t = (warp - 4) >> 2, quarter = warp & 3, R = quarter * 32 + lane;
     const int tok = R / G, hq = R - tok * G;
     const uint32_t trow = tmem_base + ((uint32_t)(quarter * 32) << 16);
-    const uint32_t ts = trow + t * 128, to = trow + 256 + t * 128;
+    const uint32_t ts = trow + t * SM::kStream, tp = ts + SM::kColP, to = ts + SM::kColO;
     int it = 0;
-    uint32_t sp = 0, op = 0, jp = 0;   // parities of s_full, o_full and the join's barriers
+    uint32_t sp = 0, pe = 1, op = 0, jp = 0;   // parities of s_full, p_empty, o_full and the join's barriers
     bool ok = true;
     while (ok) {
       const int ri = it % kChunkItems;
@@ -430,7 +425,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       const int wlo = live && a.window ? Wlo[ri * 256 + tj] : 0;
       ++it;
       if (x.kind == 0) break;
-      const ChunkTiles tl(x);
+      const ChunkTiles<TP> tl(x);
       const int nt = tl.nt, step = x.kind, i0 = x.kind == 1 ? 0 : t;
       float m = -INFINITY, l = 0.f;
       for (int i = i0; i < nt; i += step) {
@@ -438,41 +433,64 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
         const int hi = min(cols, e - p0 * kPage), lo = wlo - p0 * kPage, na = x.a - p0 * kPage;
         if (!mbar_sleep_warp(smem_u32(&s_full[t]), sp)) { set_status(c, kDevWaitTimeout); ok = false; break; }
         sp ^= 1;
-        if (!any) {
-          if (lane == 0) mbar_arrive(smem_u32(&p_full[t]));
-          continue;
-        }
         tc_fence_after();
-        // One walk over S, 16 columns at a time with the next ones on their way: exponentials against the reference m, and
-        // the maximum on the side.  m follows the maximum only when a score has passed it by more than 2^24; then (and in
-        // the stream's first tile, which has no m yet) O and l are rescaled and the walk is made again, which is why P
-        // waits in registers.
-        if (!__all_sync(0xffffffffu, hi >= 128 && (lo <= 0 || na >= 128))) chunk_mask(ts, lo, hi, na);
-        uint32_t p[2][32];
-        float lt, mx;
-        chunk_scores(ts, a.scale_log2, m == -INFINITY ? 0.f : m * a.scale_log2, p, lt, mx);
-        const bool grow = mx > m && (mx - m) * a.scale_log2 > kChunkGrow;
-        if (__any_sync(0xffffffffu, grow)) {
-          const float f = grow ? ex2((m - mx) * a.scale_log2) : 1.f;
-          if (grow) m = mx;
-          l *= f;
-          if (i != i0) {   // the stream's products up to the tile before are complete: this S was multiplied after them
-#pragma unroll 1
-            for (int q = 0; q < D; q += 16) {
-              uint32_t o[16];
-              tmem_ld16_issue(to + q, o);
-              tmem_ld16_wait(o);
+        bool waited = false;
+        // The products with P of the tile before: P's columns are free, and O may be rescaled.
+        auto wait_products = [&]() {
+          if (waited) return;
+          waited = true;
+          if (!mbar_sleep_warp(smem_u32(&p_empty[t]), pe)) { set_status(c, kDevWaitTimeout); ok = false; }
+          pe ^= 1;
+          tc_fence_after();
+        };
+        if (any) {
+          // S into registers; from here on its columns may take the next tile's products.
+          uint32_t v[TP][16];
 #pragma unroll
-              for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-              tmem_st16(to + q, o);
-            }
+          for (int q = 0; q < TP; ++q) tmem_ld16_issue(ts + q * 16, v[q]);
+#pragma unroll
+          for (int q = 0; q < TP; ++q) tmem_ld16_wait(v[q]);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&s_empty[t]));
+          if (!__all_sync(0xffffffffu, hi >= SM::kCols && (lo <= 0 || na >= SM::kCols))) {   // hidden scores become -infinity
+            asm volatile("" ::: "memory");   // (a branch: tiles without an edge should not pay for the comparisons)
+#pragma unroll
+            for (int q = 0; q < TP; ++q)
+#pragma unroll
+              for (int j = 0; j < 16; ++j)
+                if (q * 16 + j >= hi || (q * 16 + j < lo && q * 16 + j >= na)) v[q][j] = 0xff800000u;
           }
-          chunk_scores(ts, a.scale_log2, m == -INFINITY ? 0.f : m * a.scale_log2, p, lt, mx);
+          // P = 2^(scale s - ms) against the reference m, rounded to bf16 (as V is: at most half a step, 2^-8, off); its sum
+          // is not rounded.  The maximum is found on the side: m follows it only when a score has passed m by more than 2^24
+          // (or there is no m yet); then O and l are rescaled and P is worked out again.
+          float mx, lt;
+          chunk_weights<TP>(v, a.scale_log2, m == -INFINITY ? 0.f : m * a.scale_log2, tp, wait_products, lt, mx);
+          const bool grow = mx > m && (mx - m) * a.scale_log2 > kChunkGrow;
+          if (__any_sync(0xffffffffu, grow)) {
+            const float f = grow ? ex2((m - mx) * a.scale_log2) : 1.f;
+            if (grow) m = mx;
+            l *= f;
+            if (i != i0) {
+#pragma unroll 1
+              for (int q = 0; q < D; q += 16) {
+                uint32_t o[16];
+                tmem_ld16_issue(to + q, o);
+                tmem_ld16_wait(o);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                tmem_st16(to + q, o);
+              }
+            }
+            chunk_weights<TP>(v, a.scale_log2, m == -INFINITY ? 0.f : m * a.scale_log2, tp, wait_products, lt, mx);
+          }
+          l += lt;
+          tmem_st_wait();
+        } else {   // (no row of the warp is in use: only the hand-overs)
+          if (lane == 0) mbar_arrive(smem_u32(&s_empty[t]));
+          wait_products();
         }
-        l += lt;
-        tmem_st32(ts, p[0]);
-        tmem_st32(ts + 32, p[1]);
-        tmem_st_wait();
+        if (!ok) break;
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&p_full[t]));
@@ -485,32 +503,33 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
         op ^= 1;
         tc_fence_after();
       }
-      const bool join = x.kind == 2 && nt > 1;   // both streams worked on the same rows
+      // Both streams of one query tile: where the item goes on elsewhere the merge takes both results, else they meet here.
+      const bool join = x.kind == 2 && nt > 1 && x.part < 0;
       const size_t orow = ((size_t)(x.row0 + tj) * c.Hkv + x.head) * G + hq;
-      const size_t prow = (size_t)(blockIdx.x * 2 + max(x.part, 0)) * 256 + qt * kChunkRows + R;
+      const size_t prow = (size_t)(blockIdx.x * 2 + max(x.part, 0)) * 256 + t * kChunkRows + R;
       float f0 = 1.f, f1 = 0.f;   // weights of the two streams' results
-      const bool writes = live && (x.kind == 1 || t == 0);
+      const bool writes = live && (x.kind == 1 || t == 0 || x.part >= 0);
+      float *part = c.chunk_part + prow * D;
+      __nv_bfloat16 *out = a.out + orow * D;
+      // 16 columns at a time: short calls end here, and code that runs for the first time costs more than its arithmetic.
 #pragma unroll 1
-      for (int q = 0; q < D / 32; ++q) {
-        uint32_t o[32];
+      for (int q = 0; q < D; q += 16) {
+        uint32_t o[16];
         if (has) {
-          tmem_ld32_issue(to + q * 32, o);
-          tmem_ld_wait(o);
+          tmem_ld16_issue(to + q, o);
+          tmem_ld16_wait(o);
         }
-        if (q == D / 32 - 1 && has) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&o_empty[t]));
-        }
-        if (join) {
-          // 32 columns at a time, the second stream hands its O (and, first, m and l) to the first.
-          if (!mbar_sleep_warp(smem_u32(t == 1 ? j_empty : j_full), t == 1 ? jp ^ 1 : jp)) { set_status(c, kDevWaitTimeout); ok = false; break; }
-          jp ^= 1;
-          __syncwarp();
+        if (join) {   // the second stream hands its O over, 64 columns at a time, with m and l ahead of the first
+          if (q % 64 == 0) {
+            if (!mbar_sleep_warp(smem_u32(t == 1 ? j_empty : j_full), t == 1 ? jp ^ 1 : jp)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+            jp ^= 1;
+            __syncwarp();
+          }
+          float *mg = Mg + (q % 64) * 128 + R;
           if (t == 1) {
             if (q == 0) Ml[R] = make_float2(m, l);
 #pragma unroll
-            for (int j = 0; j < 32; ++j) Mg[j * 128 + R] = __uint_as_float(o[j]);
+            for (int j = 0; j < 16; ++j) mg[j * 128] = __uint_as_float(o[j]);
           } else {
             if (q == 0) {
               const float2 other = Ml[R];
@@ -521,31 +540,34 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
               l = l * f0 + other.y * f1;
             }
 #pragma unroll
-            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(fmaf(Mg[j * 128 + R], f1, __uint_as_float(o[j]) * f0));
+            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(fmaf(mg[j * 128], f1, __uint_as_float(o[j]) * f0));
           }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(t == 1 ? j_full : j_empty));
+          if (q % 64 == 48) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(t == 1 ? j_full : j_empty));
+          }
         }
         if (!writes) continue;
         if (x.part >= 0) {
-          float *dst = c.chunk_part + prow * D + q * 32;
-          if (has)
+          if (has) {
 #pragma unroll
-            for (int j = 0; j < 32; j += 4)
-              __stcg(reinterpret_cast<float4 *>(dst + j), make_float4(__uint_as_float(o[j]), __uint_as_float(o[j + 1]),
-                                                                      __uint_as_float(o[j + 2]), __uint_as_float(o[j + 3])));
+            for (int j = 0; j < 16; j += 4) __stcg(reinterpret_cast<uint4 *>(part + q + j), make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]));
+          }
         } else {
           const float inv = l == 0.f ? 0.f : 1.f / l;   // a row that sees nothing gives zeros
-          uint4 *dst = reinterpret_cast<uint4 *>(a.out + orow * D + q * 32);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
+          for (int h = 0; h < 2; ++h) {
             uint32_t w[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              w[k] = pack_bf16(__uint_as_float(o[8 * j + 2 * k]) * inv, __uint_as_float(o[8 * j + 2 * k + 1]) * inv);
-            dst[j] = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int k = 0; k < 4; ++k) w[k] = pack_bf16(__uint_as_float(o[8 * h + 2 * k]) * inv, __uint_as_float(o[8 * h + 2 * k + 1]) * inv);
+            *reinterpret_cast<uint4 *>(out + q + 8 * h) = make_uint4(w[0], w[1], w[2], w[3]);
           }
         }
+      }
+      if (has) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&o_empty[t]));
       }
       if (!ok) break;
       if (writes) {
@@ -559,7 +581,6 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       if (lane == 0) mbar_arrive(smem_u32(&it_empty[ri]));
     }
   } else {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
   if (warp == 2) {
     // ---------------- the walk over this CTA's range of the line of pages ----------------
     const int batch = c.batch, W = a.window, S = a.sinks, TB = 2 * TPT;
@@ -604,25 +625,25 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       }
       return b;
     };
-    long long P = 0;   // pages of one KV head
-    for (int f0 = 0; f0 < NB; f0 += 32) {
-      int u = f0 + lane < NB ? block(f0 + lane).units : 0;
-#pragma unroll
-      for (int o = 16; o >= 1; o >>= 1) u += __shfl_xor_sync(0xffffffffu, u, o);
-      P += u;
-    }
+    // The pages of one KV head, summed over the blocks 32 at a time; the first 32 stay at hand.
+    auto strip = [&](int f0) { return f0 + lane < NB ? block(f0 + lane).units : 0; };
+    const int un0 = strip(0);
+    long long P = 0;
+    for (int f0 = 0; f0 < NB; f0 += 32) P += __reduce_add_sync(0xffffffffu, f0 == 0 ? un0 : strip(f0));
     const long long total = P * c.Hkv;
-    const long long per = max((long long)kChunkMinPages, (total + gridDim.x - 1) / gridDim.x);
+    // (long divisions take hundreds of cycles, and the first tile waits for these)
+    auto quotient = [](long long x, long long y) { return (x | y) >> 32 ? x / y : (long long)((unsigned)x / (unsigned)y); };
+    const long long per = max((long long)kChunkMinPages, quotient(total + gridDim.x - 1, gridDim.x));
     long long u = per * blockIdx.x;
     const long long u_end = min(total, u + per);
     int *info = c.chunk_info + blockIdx.x * kChunkInfo;
     int head = 0, f = 0, off = 0, it = 0;
     bool open = false;   // this CTA begins an item that others go on with
     if (u < u_end) {
-      head = (int)(u / P);
+      head = (int)quotient(u, P);
       long long rem = u - head * P;
       for (int f0 = 0; f0 < NB; f0 += 32) {   // the block that holds page `rem`
-        const int un = f0 + lane < NB ? block(f0 + lane).units : 0;
+        const int un = f0 == 0 ? un0 : strip(f0);
         int inc = un;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -699,8 +720,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
         x->pa0 = pa0; x->pa1 = pa1; x->pb0 = pb0; x->pb1 = pb1;
         x->part = part;
         if (part == 1) {   // for the merge, with the last CTA that the item reaches
-          info[0] = (int)((u - off + b.units - 1) / per);
-          info[1] = head; info[2] = x->row0; info[3] = nt0; info[4] = ntok - nt0;
+          info[0] = (int)quotient(u - off + b.units - 1, per);
+          info[1] = head; info[2] = x->row0; info[3] = nt0; info[4] = ntok - nt0;   // (no second tile: two streams of one)
         }
       }
       if (part == 1) open = true;
@@ -718,7 +739,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       if (!ended) publish();
       const ChunkItem &x = Items[vi % kChunkItems];
       if (!ok || x.kind == 0) break;
-      const ChunkTiles tl(x);
+      const ChunkTiles<TP> tl(x);
       const int *ptrow = c.pt + (size_t)x.seg * c.max_pages;
       auto page_id = [&](int i) { return i < tl.nt && (lane & 7) < tl.pages(i) ? __ldcg(ptrow + tl.first(i) + (lane & 7)) : 0; };
       int id = page_id(0);
@@ -730,7 +751,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
         armed |= 1u << rr.i;
         armed_par = (armed_par & ~(1u << rr.i)) | ((uint32_t)rr.ph << rr.i);
         __syncwarp();
-        if (lane < np) tma_page_v(smem_u32(Vt + rr.i * SM::kTile + (size_t)lane * NQ * PAGE_HALF), &tmv, NQ, id, bar);
+        if (lane < np) tma_page_v(smem_u32(Vt + rr.i * SM::kKv + (size_t)lane * NQ * PAGE_HALF), &tmv, NQ, id, bar);
         rr.next(NS);
         id = idn;
       }
@@ -755,7 +776,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       if (lane == 0) mbar_arrive(smem_u32(&it_empty[ri]));
       ++it;
       if (x.kind == 0) break;
-      const ChunkTiles tl(x);
+      const ChunkTiles<TP> tl(x);
       if (tl.nt == 0) continue;
       for (int t = 0; t < (x.kind == 1 ? 2 : 1) && ok; ++t) {
         if (!mbar_sleep_warp(smem_u32(&q_empty[t]), ((qp >> t) & 1) ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; break; }
@@ -782,7 +803,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
         armed_par = (armed_par & ~(1u << rr.i)) | ((uint32_t)rr.ph << rr.i);
         __syncwarp();
         if (pg < np && half < NQ)
-          tma_page_k(smem_u32(Kt + rr.i * SM::kTile + (size_t)half * 128 * 128 + (size_t)pg * PAGE_HALF), &tmk, half, id, bar);
+          tma_page_k(smem_u32(Kt + rr.i * SM::kKv + (size_t)half * TP * PAGE_HALF + (size_t)pg * PAGE_HALF), &tmk, half, id, bar);
         rr.next(NS);
         id = idn;
       }
@@ -795,17 +816,17 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
     for (int t = 0; t < 2; ++t)
       if (((armed >> (16 + t)) & 1u) && !mbar_sleep_warp(smem_u32(&q_full[t]), (armed_par >> (16 + t)) & 1u)) set_status(c, kDevWaitTimeout);
   } else if (warp == 1 || warp == 3) {
-    // ---------------- multiplies: a warp for each stream; it stays together, lane 0 issues.  A stream's O += P V and its
-    // next S go out in one run, and the streams take turns with their runs: one exponentiates while the other multiplies.
-    // (Left alone they fall into step, both waiting for the same unit all the time.) ----------------
-    const int t = uniform(warp >> 1);
+    // ---------------- multiplies: one warp S = Q K^T, the other O += P V, for both streams; a warp stays together, lane 0
+    // issues.  (One warp for both kinds spends longer on its waits and hand-overs than the tensor core on the products.)
+    const bool scores = warp == 1;
     const uint32_t on = lane == 0;
-    FeatRing kr{0, 0}, vr{0, 0};
+    FeatRing r{0, 0};
     int it = 0;
-    uint32_t qp = 0, pp = 0, op = 0, tp = t ^ 1;   // parities: bit t of the query tiles' next phase; the next p_full, o_empty, turn
+    uint32_t qp = 0, se = 3, pp = 0, op = 3;   // bit t: parities of query tile t's next phase, of stream t's next s_empty, p_full, o_empty
     bool ok = true;
-    const uint32_t ts = uniform(tmem_base + t * 128), to = ts + 256;
+    const uint32_t tb = uniform(tmem_base);
     const uint32_t idesc_o = umma_idesc_bf16(kChunkRows, D) | (1u << 16);   // B runs along N
+    uint64_t *full = scores ? k_full : v_full, *empty = scores ? k_empty : v_empty;
     while (ok) {
       const int ri = it % kChunkItems;
       if (!mbar_wait(smem_u32(&it_full[ri]), (it / kChunkItems) & 1)) { set_status(c, kDevWaitTimeout); break; }
@@ -814,99 +835,74 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       if (lane == 0) mbar_arrive(smem_u32(&it_empty[ri]));
       ++it;
       if (x.kind == 0) break;
-      const ChunkTiles tl(x);
-      const int nt = uniform(tl.nt);
+      const ChunkTiles<TP> tl(x);
+      const int nt = uniform(tl.nt), step = uniform(x.kind);   // step: key tiles between a stream's tile and its next one
       if (nt == 0) continue;
-      const int step = uniform(x.kind), qt = step == 1 ? t : 0;   // key tiles between a stream's tile and its next one
-      if (!mbar_wait(smem_u32(&q_full[qt]), (qp >> qt) & 1)) { set_status(c, kDevWaitTimeout); break; }
-      qp ^= step == 1 ? 3u : 1u;
-      // The next slot of a ring, filled.
-      auto wait_slot = [&](FeatRing &r, uint64_t *full) {
-        const int slot = uniform(r.i);
-        if (!mbar_wait(smem_u32(&full[r.i]), r.ph)) { set_status(c, kDevWaitTimeout); ok = false; }
-        r.next(NS);
-        return slot;
-      };
-      // A slot is free again when both streams have let it go; the one that has no use for it does so at once.
-      auto skip_slot = [&](FeatRing &r, uint64_t *full, uint64_t *empty) {
-        const int slot = wait_slot(r, full);
-        if (lane == 0 && ok) mbar_arrive(smem_u32(&empty[slot]));
-      };
-      auto key_desc = [&](int slot) { return umma_desc_sw128(smem_u32(Kt + slot * SM::kTile)); };
-      // S = (query tile) (key tile)^T
-      const uint64_t qd = umma_desc_sw128(smem_u32(Qt + qt * SM::kTile));
-      auto mul_s = [&](uint64_t kd, uint32_t idesc) {
-#pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-          const uint64_t o = (uint64_t)(((ks >> 2) * 128 * 128 + (ks & 3) * 32) >> 4);
-          umma_bf16_if(on, ts, qd + o, kd + o, idesc, ks > 0);
+      if (scores)
+        for (int t = 0; t < (step == 1 ? 2 : 1); ++t) {
+          if (!mbar_wait(smem_u32(&q_full[t]), (qp >> t) & 1)) { set_status(c, kDevWaitTimeout); ok = false; }
+          qp ^= 1u << t;
         }
-        umma_commit_if(on, smem_u32(&s_full[t]));
-      };
-      for (int i = 0; i < min(step, nt) && ok; ++i) {
-        if (step == 2 && i != t) { skip_slot(kr, k_full, k_empty); continue; }
-        const int slot = wait_slot(kr, k_full);
-        if (!ok) break;
-        tc_fence_after();
-        mul_s(key_desc(slot), umma_idesc_bf16(kChunkRows, uniform(tl.pages(i)) * kPage));
-        umma_commit_if(on, smem_u32(&k_empty[slot]));
-      }
       for (int i = 0; i < nt && ok; ++i) {
-        const bool more = i + step < nt, mine = step == 1 || (i & 1) == t;
-        if (!mine) {
-          skip_slot(vr, v_full, v_empty);
-          if (more && ok) skip_slot(kr, k_full, k_empty);
-          if (t == 1 && i + 1 == nt && ok) {   // an odd tile at the end is the first stream's: its turn is handed back
-            if (!mbar_wait(smem_u32(&turn[1]), tp)) { set_status(c, kDevWaitTimeout); ok = false; break; }
-            tp ^= 1;
-            if (lane == 0) mbar_arrive(smem_u32(&turn[0]));
-          }
-          continue;
-        }
-        // Everything but P is waited for and worked out first.
-        const int np = uniform(tl.pages(i)), nk = uniform(more ? tl.pages(i + step) : 0), r0 = x.n - tl.first(i) * kPage;
-        const int vs = wait_slot(vr, v_full), ks_ = more ? wait_slot(kr, k_full) : 0;
-        if (!ok) break;
-        // Rows of the last page past the segment's end hold whatever the page held before: P is zero there, but zero
-        // times an infinity is not, so they are cleared.
-        if (r0 < np * kPage) {
-          for (int e = lane; e < (np * kPage - r0) * NQ * 8; e += 32) {
-            const int r = r0 + e / (NQ * 8), ch = e % (NQ * 8);
-            *reinterpret_cast<uint4 *>(Vt + vs * SM::kTile + (size_t)((r / kPage * NQ + (ch >> 3)) * kPage + r % kPage) * 128 + (ch & 7) * 16) =
-                make_uint4(0u, 0u, 0u, 0u);
-          }
-          fence_proxy_async();
-          __syncwarp();
-        }
-        const bool first = i < step;
-        if (first) {
-          if (!mbar_wait(smem_u32(&o_empty[t]), op ^ 1)) { set_status(c, kDevWaitTimeout); ok = false; break; }
-          op ^= 1;
-        }
-        const uint64_t vd = umma_desc_mn_sw128(smem_u32(Vt + vs * SM::kTile)), kd = key_desc(ks_);
-        const uint32_t idesc_s = umma_idesc_bf16(kChunkRows, nk * kPage);
-        const bool mine_now = mbar_wait(smem_u32(&turn[t]), tp);
-        if (!__all_sync(0xffffffffu, mine_now && mbar_wait(smem_u32(&p_full[t]), pp))) { set_status(c, kDevWaitTimeout); ok = false; break; }
-        tp ^= 1;
-        pp ^= 1;
-        tc_fence_after();
-        umma_bf16_ta_if(on, to, ts, vd, idesc_o, !first);
-        if (np == TP) {
+        const int np = uniform(tl.pages(i)), slot = uniform(r.i);
+        if (!mbar_wait(smem_u32(&full[slot]), r.ph)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+        r.next(NS);
+        const int t0 = step == 1 ? 0 : i & 1, t1 = step == 1 ? 2 : t0 + 1;
+        if (scores) {
+          const uint64_t kd = umma_desc_sw128(smem_u32(Kt + slot * SM::kKv));
+          const uint32_t idesc = umma_idesc_bf16(kChunkRows, np * kPage);
+          for (int t = t0; t < t1; ++t) {   // as soon as the warps have read the S before
+            const uint64_t qd = umma_desc_sw128(smem_u32(Qt + (step == 1 ? t : 0) * SM::kTile));
+            const uint32_t ts = tb + t * SM::kStream;
+            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&s_empty[t]), (se >> t) & 1))) { set_status(c, kDevWaitTimeout); ok = false; break; }
+            se ^= 1u << t;
+            tc_fence_after();
 #pragma unroll
-          for (int ks = 1; ks < TP; ++ks) umma_bf16_ta_if(on, to, ts + ks * 8, vd + (uint64_t)((ks * NQ * PAGE_HALF) >> 4), idesc_o, 1);
+            for (int ks = 0; ks < D / 16; ++ks)
+              umma_bf16_if(on, ts, qd + (uint64_t)(((ks >> 2) * 128 * 128 + (ks & 3) * 32) >> 4),
+                           kd + (uint64_t)(((ks >> 2) * TP * (int)PAGE_HALF + (ks & 3) * 32) >> 4), idesc, ks > 0);
+            umma_commit_if(on, smem_u32(&s_full[t]));
+          }
         } else {
-          for (int ks = 1; ks < np; ++ks) umma_bf16_ta_if(on, to, ts + ks * 8, vd + (uint64_t)((ks * NQ * PAGE_HALF) >> 4), idesc_o, 1);
+          // Rows of the last page past the segment's end hold whatever the page held before: P is zero there, but zero
+          // times an infinity is not, so they are cleared.
+          const int r0 = x.n - tl.first(i) * kPage;
+          if (r0 < np * kPage) {
+            for (int e = lane; e < (np * kPage - r0) * NQ * 8; e += 32) {
+              const int row = r0 + e / (NQ * 8), ch = e % (NQ * 8);
+              *reinterpret_cast<uint4 *>(Vt + slot * SM::kKv + (size_t)((row / kPage * NQ + (ch >> 3)) * kPage + row % kPage) * 128 +
+                                         (ch & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            fence_proxy_async();
+            __syncwarp();
+          }
+          const uint64_t vd = umma_desc_mn_sw128(smem_u32(Vt + slot * SM::kKv));
+          const bool first = i < step;   // the stream's first tile of the item
+          for (int t = t0; t < t1; ++t) {
+            const uint32_t ts = tb + t * SM::kStream, tp = ts + SM::kColP, to = ts + SM::kColO;
+            if (first) {
+              if (!mbar_wait(smem_u32(&o_empty[t]), (op >> t) & 1)) { set_status(c, kDevWaitTimeout); ok = false; break; }
+              op ^= 1u << t;
+            }
+            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&p_full[t]), (pp >> t) & 1))) { set_status(c, kDevWaitTimeout); ok = false; break; }
+            pp ^= 1u << t;
+            tc_fence_after();
+            umma_bf16_ta_if(on, to, tp, vd, idesc_o, !first);
+            if (np == TP) {
+#pragma unroll
+              for (int ks = 1; ks < TP; ++ks) umma_bf16_ta_if(on, to, tp + ks * 8, vd + (uint64_t)((ks * NQ * PAGE_HALF) >> 4), idesc_o, 1);
+            } else {
+              for (int ks = 1; ks < np; ++ks) umma_bf16_ta_if(on, to, tp + ks * 8, vd + (uint64_t)((ks * NQ * PAGE_HALF) >> 4), idesc_o, 1);
+            }
+            umma_commit_if(on, smem_u32(&p_empty[t]));
+            if (i + step >= nt) umma_commit_if(on, smem_u32(&o_full[t]));
+          }
         }
-        if (more) mul_s(kd, idesc_s);
-        else umma_commit_if(on, smem_u32(&o_full[t]));
-        if (lane == 0) mbar_arrive(smem_u32(&turn[t ^ 1]));
-        umma_commit_if(on, smem_u32(&v_empty[vs]));
-        if (more) umma_commit_if(on, smem_u32(&k_empty[ks_]));
+        if (ok) umma_commit_if(on, smem_u32(&empty[slot]));
       }
-      // The query tiles are free when their products are done: tile 0 when both streams say so.
-      if (ok) {
+      if (scores && ok) {
         umma_commit_if(on, smem_u32(&q_empty[0]));
-        if (step == 1 && t == 1) umma_commit_if(on, smem_u32(&q_empty[1]));
+        if (step == 1) umma_commit_if(on, smem_u32(&q_empty[1]));
       }
     }
     umma_commit_if(on, smem_u32(mma_done));   // nothing may be in flight when tensor memory is freed
@@ -931,35 +927,50 @@ __global__ void __launch_bounds__(256) k_chunk_merge(Ctx c, const __grid_constan
   if (cl < 0) return;
   const int cf = blockIdx.x, head = __ldcg(info + 1), row0 = __ldcg(info + 2), G = c.G, TPT = kChunkRows / G;
   const int nt0 = __ldcg(info + 3), ntok = nt0 + __ldcg(info + 4), lane = threadIdx.x & 31;
+  const bool two = ntok == nt0;
+  const int parts = (cl + 1 - cf) * (two ? 2 : 1);
   const float2 *ml = reinterpret_cast<const float2 *>(c.chunk_ml);
   for (int r = blockIdx.y * 8 + (threadIdx.x >> 5); r < ntok * G; r += gridDim.y * 8) {
     const int tj = r / G, hq = r - tj * G;
     const int prow = tj < nt0 ? tj * G + hq : kChunkRows + (tj - TPT) * G + hq;   // row inside a CTA's slot
-    auto row_of = [&](int p) { return (size_t)(p * 2 + (p == cf ? 1 : 0)) * 256 + prow; };
+    // Part p: of CTA cf + p, or, where two streams worked on one query tile, of CTA cf + p / 2 and stream p % 2.
+    auto row_of = [&](int p) {
+      const int cta = two ? p >> 1 : p;
+      return (size_t)((cf + cta) * 2 + (cta == 0 ? 1 : 0)) * 256 + prow + (two ? (p & 1) * kChunkRows : 0);
+    };
     float M = -INFINITY, L = 0.f;
-    for (int p = cf + lane; p <= cl; p += 32) M = fmaxf(M, __ldcg(ml + row_of(p)).x);
+    for (int p = lane; p < parts; p += 32) M = fmaxf(M, __ldcg(ml + row_of(p)).x);
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
     float acc[D / 32];
 #pragma unroll
     for (int j = 0; j < D / 32; ++j) acc[j] = 0.f;
-    for (int p0 = cf; p0 <= cl; p0 += 32) {
-      const float2 x = p0 + lane <= cl ? __ldcg(ml + row_of(p0 + lane)) : make_float2(-INFINITY, 0.f);
+    for (int p0 = 0; p0 < parts; p0 += 32) {
+      const float2 x = p0 + lane < parts ? __ldcg(ml + row_of(p0 + lane)) : make_float2(-INFINITY, 0.f);
       const float f = x.x == -INFINITY ? 0.f : ex2((x.x - M) * a.scale_log2);
       L += f * x.y;
-      const int cnt = min(32, cl + 1 - p0);
-#pragma unroll 4
-      for (int i = 0; i < cnt; ++i) {
-        const float fi = __shfl_sync(0xffffffffu, f, i);
-        if (fi == 0.f) continue;   // the part saw nothing of this row (its O may not have been written)
-        const float *o = c.chunk_part + row_of(p0 + i) * D + lane * (D / 32);
-        if (D == 128) {
-          const float4 w = __ldcg(reinterpret_cast<const float4 *>(o));
-          acc[0] = fmaf(fi, w.x, acc[0]); acc[1] = fmaf(fi, w.y, acc[1]);
-          acc[D / 32 - 2] = fmaf(fi, w.z, acc[D / 32 - 2]); acc[D / 32 - 1] = fmaf(fi, w.w, acc[D / 32 - 1]);
-        } else {
-          const float2 w = __ldcg(reinterpret_cast<const float2 *>(o));
-          acc[0] = fmaf(fi, w.x, acc[0]); acc[1] = fmaf(fi, w.y, acc[1]);
+      const int cnt = min(32, parts - p0);
+      // Eight parts' rows are asked for before the first is used.  One that saw nothing of the row may not have been
+      // written: whatever was read there counts for nothing.
+      for (int i0 = 0; i0 < cnt; i0 += 8) {
+        float w[8][D / 32];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float *o = c.chunk_part + row_of(p0 + min(i0 + i, cnt - 1)) * D + lane * (D / 32);
+          if (D == 128) {
+            const float4 x4 = __ldcg(reinterpret_cast<const float4 *>(o));
+            w[i][0] = x4.x; w[i][1] = x4.y; w[i][D / 32 - 2] = x4.z; w[i][D / 32 - 1] = x4.w;
+          } else {
+            const float2 x2 = __ldcg(reinterpret_cast<const float2 *>(o));
+            w[i][0] = x2.x; w[i][1] = x2.y;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float fi = __shfl_sync(0xffffffffu, i0 + i < cnt ? f : 0.f, min(i0 + i, 31));
+          const bool on = i0 + i < cnt && fi != 0.f;
+#pragma unroll
+          for (int j = 0; j < D / 32; ++j) acc[j] = on ? fmaf(fi, w[i][j], acc[j]) : acc[j];
         }
       }
     }
