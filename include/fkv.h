@@ -306,7 +306,7 @@ int fkv_append_decode_attn_window(fkv_cache *c, int layer, const void *k, const 
  * fkv_chunk_attn: attention of a chunk's queries, the chunk's pairs being the last chunk_lens[s] pairs of their segments:
  *     out[j] = sum_i softmax_i(scale <q_j, k_i>) v_i,   lse_out[j] = ln sum_i exp(scale <q_j, k_i>),
  * over the pairs i up to query j's own and, with window > 0, inside its window or among the sinks (as above; window = 0:
- * every pair).  lse_out: dev [tokens][Hkv*g] fp32 or NULL.  scale 0 means 1/sqrt(D); a negative or infinite one is
+ * every pair).  lse_out: dev [tokens][Hkv*g] fp32 or NULL.  scale 0 means 1/sqrt(D); one outside [2^-100, 2^100] is
  * FKV_ERR_INVALID_ARG, as is a chunk longer than its segment.  Errors as fkv_evict_rkv for the tensor maps.
  * P is rounded to bf16 for the product with V (as V is); everything else is fp32.
  *

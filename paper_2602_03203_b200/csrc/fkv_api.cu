@@ -600,7 +600,8 @@ int launch_append_chunk(fkv_cache *c, int layer, const void *k, const void *v, c
 int check_chunk(const fkv_cache *c, int layer, const void *q, const int32_t *chunk_lens, int32_t window, int32_t sinks,
                 float scale, ChunkLens &lens) {
   if (!c || !layer_ok(c, layer) || !chunk_lens || !make_lens(c, chunk_lens, lens)) return FKV_ERR_INVALID_ARG;
-  if (window < 0 || sinks < 0 || !(scale >= 0.f) || !std::isfinite(scale)) return FKV_ERR_INVALID_ARG;
+  if (window < 0 || sinks < 0) return FKV_ERR_INVALID_ARG;
+  if (scale != 0.f && !(scale >= 0x1p-100f && scale <= 0x1p100f)) return FKV_ERR_INVALID_ARG;   // (NaN too)
   if (lens.tok[c->cfg.max_batch] > 0 && (!q || !aligned(q, 16))) return FKV_ERR_INVALID_ARG;
   return FKV_OK;
 }
@@ -665,11 +666,14 @@ int launch_chunk_attend(fkv_cache *c, int layer, const void *q, const int32_t *c
 }
 
 template <int D>
-int launch_chunk_features_t(fkv_cache *c, const CUtensorMap &tmq, const ChunkFeatArgs &a, int grid, cudaStream_t st) {
+int launch_chunk_features_t(fkv_cache *c, const CUtensorMap &tmq, ChunkFeatArgs &a, int grid, cudaStream_t st) {
   constexpr size_t smem = CfSmem<D>::bytes();
   static_assert(smem <= kMaxSmem, "one CTA's shared memory");
   static SmemOptIn opt_in;
   FKV_CUDA(opt_in.ensure(k_chunk_features<D>, smem));
+  int longest = 0;
+  for (int s = 0; s < c->cfg.max_batch; ++s) longest = std::max(longest, a.lens.tok[s + 1] - a.lens.tok[s]);
+  a.nq = CfSmem<D>::rings(longest, a.nk);
   FKV_CUDA(launch_waiting(k_chunk_features<D>, dim3(grid), kCfThreads, smem, st, c->ctx, c->page_rows, tmq, a));
   ++c->launches;
   return FKV_OK;
@@ -682,7 +686,10 @@ int launch_chunk_features(fkv_cache *c, int layer, const void *q, const float *l
   if (int e = ensure_page_rows_map(c)) return e;
   ChunkFeatArgs a;
   a.layer = layer; a.window = window; a.sinks = window ? sinks : 0;
-  a.scale_log2 = (scale == 0.f ? 1.f / sqrtf((float)D) : scale) * 1.4426950408889634f;
+  if (scale == 0.f) scale = 1.f / sqrtf((float)D);
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.inv_hi = (float)(1.0 / (double)scale);
+  a.inv_lo = (float)(1.0 / (double)scale - (double)a.inv_hi);
   a.lse = lse; a.lens = lens;
   CUtensorMap tmq;
   if (int e = query_map(c, q, lens.tok[batch], 1, kCfQueries, &tmq)) return e;

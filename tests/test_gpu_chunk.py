@@ -475,7 +475,7 @@ def test_refusals():
         assert append(**bad) == inval, bad
     assert append(lens=i2(45, 0)) == capacity and append(keep=i2(20, 10), lens=i2(0, 55)) == capacity
     for bad in [dict(layer=1), dict(qq=None), dict(qq=p(q, 2)), dict(o=None), dict(o=p(out, 4)), dict(lens=None), dict(lens=i2(-1, 0)),
-                dict(lens=i2(21, 0)), dict(window=-1), dict(sinks=-1), dict(scale=-1.0), dict(scale=math.inf), dict(scale=math.nan)]:
+                dict(lens=i2(21, 0)), dict(window=-1), dict(sinks=-1), dict(scale=-1.0), dict(scale=math.inf), dict(scale=math.nan), dict(scale=1e-32), dict(scale=1e32)]:
         assert attn(**bad) == inval, bad
     assert attn(lens=i2(0, 0), qq=None, o=None) == 0 and append(lens=i2(0, 0), kk=None, vv=None) == 0
     assert lib.fkv_append_chunk_attn(h, 0, p(k), p(v), None, None, i2(3, 2), p(q, 2), 0, 0, 0.0, p(out), None, st) == inval
