@@ -256,12 +256,12 @@ __global__ void __launch_bounds__((NCW + 1) * 32, NCW <= 4 ? 3 : 1) k_attend(Ctx
       const int first = window_start(p, a.window);
       stored = n_old;
       if (x_last > p) {   // some pairs are younger than the query
-        stored = slot_lower_bound(c, ptrow, 0, n_old - 1, p + 1);
-        wb = slot_lower_bound(c, ptrow, 0, stored, first);
+        stored = slot_lower_bound_warp(c, ptrow, 0, n_old - 1, p + 1);
+        wb = slot_lower_bound_warp(c, ptrow, 0, stored, first);
       } else {
-        wb = x_lo >= first ? lo : slot_lower_bound(c, ptrow, lo + 1, n_old, first);
+        wb = x_lo >= first ? lo : slot_lower_bound_warp(c, ptrow, lo + 1, n_old, first);
       }
-      wa = m == 0 ? 0 : min(stored, x_m < a.sinks ? m : slot_lower_bound(c, ptrow, 0, m - 1, a.sinks));
+      wa = m == 0 ? 0 : min(stored, x_m < a.sinks ? m : slot_lower_bound_warp(c, ptrow, 0, m - 1, a.sinks));
       wb = max(wa, wb);
     }
     we = app ? n : stored;
@@ -271,7 +271,8 @@ __global__ void __launch_bounds__((NCW + 1) * 32, NCW <= 4 ? 3 : 1) k_attend(Ctx
   }
   auto page_of = [&](int v) { return WIN ? (v < wsp ? v : v - wsp + wp0) : v; };   // page number v of the ones to read
   // Pages per split: the host's figure, or more when the segment has outgrown it since the launch was recorded.
-  const int pps = max(a.pps, (npages + S - 1) / S);
+  // (A window's host figure is an upper bound - a pruned cache holds fewer of its positions - and nothing is read by it.)
+  const int pps = max(WIN ? 1 : a.pps, (npages + S - 1) / S);
   const int pg0 = rank * pps, pg1 = min(npages, pg0 + pps);
   const bool active = pg0 < pg1;
   const int npg = active ? pg1 - pg0 : 0;               // pages of this CTA

@@ -215,7 +215,8 @@ struct ChunkSmem {
   static constexpr size_t kOffMl = kOffMerge + kMerge;                 // (m, l) of the second stream's rows
   static constexpr size_t kOffItems = kOffMl + 128 * 8;
   static constexpr size_t kOffWlo = kOffItems + kChunkItems * sizeof(ChunkItem);   // first slot of every token's window
-  static constexpr size_t kOffLen = kOffWlo + kChunkItems * 256 * 4;
+  static constexpr size_t kOffPos = kOffWlo + kChunkItems * 256 * 4;               // positions behind the item's first window
+  static constexpr size_t kOffLen = kOffPos + 256 * 4;
   static constexpr size_t kOffBlk = kOffLen + kMaxBatch * 4;
   static constexpr size_t kOffBars = (kOffBlk + (kMaxBatch + 1) * 4 + 15) & ~(size_t)15;
   static constexpr size_t bytes() { return 1024 + kOffBars + 512; }   // (more than half an SM's: one CTA each)
@@ -367,7 +368,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
   float *Mg = reinterpret_cast<float *>(smem + SM::kOffMerge);
   float2 *Ml = reinterpret_cast<float2 *>(smem + SM::kOffMl);
   ChunkItem *Items = reinterpret_cast<ChunkItem *>(smem + SM::kOffItems);
-  int *Wlo = reinterpret_cast<int *>(smem + SM::kOffWlo);
+  int *Wlo = reinterpret_cast<int *>(smem + SM::kOffWlo), *Pos = reinterpret_cast<int *>(smem + SM::kOffPos);
   int *Len = reinterpret_cast<int *>(smem + SM::kOffLen), *Blk = reinterpret_cast<int *>(smem + SM::kOffBlk);
   uint64_t *bars = reinterpret_cast<uint64_t *>(smem + SM::kOffBars);
   uint64_t *k_full = bars, *k_empty = k_full + NS, *v_full = k_empty + NS, *v_empty = v_full + NS;
@@ -688,15 +689,28 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       int na = 0;
       if (W) {
         na = S ? slot_sinks(c, ptrow, b.n, S) : 0;
-        int first = 0;
-        for (int i0 = 0; i0 < ntok; i0 += 32) {
-          int w = 0;
-          if (i0 + lane < ntok) {
-            const int last = e0 + i0 + lane - 1;
-            w = slot_window(c, ptrow, last, slot_pos(c, ptrow, last), W);
-            Wlo[ri * 256 + i0 + lane] = w;
+        // Where the first token's window begins, then the others': a window that begins d positions later begins at most d
+        // slots later, so the positions of those slots decide, read together (a search of its own for a token whose
+        // window is further off: a chunk with gaps in its positions).
+        const int p_first = slot_pos(c, ptrow, e0 - 1), lo0 = max(0, e0 - W), start = window_start(p_first, W);
+        const int first = slot_pos(c, ptrow, lo0) >= start ? lo0 : slot_lower_bound_warp(c, ptrow, lo0 + 1, e0, start);
+        __syncwarp();
+        for (int i = lane; i < 256 && first + i < b.n; i += 32) Pos[i] = slot_pos(c, ptrow, first + i);
+        __syncwarp();
+        for (int i = lane; i < ntok; i += 32) {
+          const int last = e0 + i - 1, p = slot_pos(c, ptrow, last);
+          const long long apart = (long long)p - p_first;   // (>= 0)
+          const int from = window_start(p, W);
+          int lo = first, hi = (int)min((long long)last, first + apart);
+          if (hi - first < 256) {
+            while (lo < hi) {
+              const int mid = (lo + hi) >> 1;
+              if (Pos[mid - first] < from) lo = mid + 1; else hi = mid;
+            }
+          } else {
+            lo = slot_lower_bound(c, ptrow, lo, hi, from);
           }
-          if (i0 == 0) first = __shfl_sync(0xffffffffu, w, 0);
+          Wlo[ri * 256 + i] = lo;
         }
         const int a16 = (na + kPage - 1) / kPage, w16 = first / kPage;
         if (b.r.sp == 0) {   // one run of pages: split it around the hidden ones

@@ -281,20 +281,28 @@ __device__ __forceinline__ int slot_lower_bound(const Ctx &c, const int *ptrow, 
   }
   return lo;
 }
+// The same, by a whole warp for one answer: 32 places are looked at together, so 32768 pairs take three rounds of two
+// dependent reads instead of fifteen.
+__device__ __forceinline__ int slot_lower_bound_warp(const Ctx &c, const int *ptrow, int lo, int hi, int p) {
+  const int lane = threadIdx.x & 31;
+  while (lo < hi) {
+    const int step = (hi - lo + 31) / 32, at = lo + lane * step;   // places lo, lo + step, ...: the answer is behind the last smaller one
+    const unsigned smaller = __ballot_sync(0xffffffffu, at < hi && slot_pos(c, ptrow, min(at, hi - 1)) < p);
+    const int k = __popc(smaller);   // (positions grow: the smaller ones come first)
+    if (k == 0) return lo;
+    hi = min(hi, lo + k * step);
+    lo = lo + (k - 1) * step + 1;
+  }
+  return lo;
+}
 // The first position that a window of W positions up to p holds.
 __device__ __forceinline__ int window_start(int p, int W) { return (int)max((long long)p - W + 1, (long long)INT_MIN); }
-// Slots [0, a) hold the positions below S: at most S of them, and all of the first S when nothing was evicted there.
+// (A whole warp, for one answer.)  Slots [0, a) hold the positions below S: at most S of them, and all of the first S when
+// nothing was evicted there.
 __device__ __forceinline__ int slot_sinks(const Ctx &c, const int *ptrow, int n, int S) {
   const int m = min(S, n);
   if (m == 0) return 0;
-  return slot_pos(c, ptrow, m - 1) < S ? m : slot_lower_bound(c, ptrow, 0, m - 1, S);
-}
-// The first slot at or below `last` whose position is above p - W, p >= the position at `last`: at most W slots back,
-// and exactly W when no position is missing there, which is looked at first.
-__device__ __forceinline__ int slot_window(const Ctx &c, const int *ptrow, int last, int p, int W) {
-  const int lo = max(0, last + 1 - W), first = window_start(p, W);
-  if (slot_pos(c, ptrow, lo) >= first) return lo;
-  return slot_lower_bound(c, ptrow, lo + 1, last + 1, first);
+  return slot_pos(c, ptrow, m - 1) < S ? m : slot_lower_bound_warp(c, ptrow, 0, m - 1, S);
 }
 
 // ---------------------------------------------------------------- row movers
