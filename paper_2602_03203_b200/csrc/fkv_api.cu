@@ -8,6 +8,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <new>
 #include <string>
@@ -298,12 +299,16 @@ typedef CUresult (*encode_fn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, vo
                               CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 int tensor_map(CUtensorMap *map, void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box,
                CUtensorMapSwizzle swizzle) {
-  void *fn = nullptr;
-  cudaDriverEntryPointQueryResult found;
-  FKV_CUDA(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found));
-  if (fn == nullptr || found != cudaDriverEntryPointSuccess) {
-    g_cuda_error = "cuTensorMapEncodeTiled is not available from this driver";
-    return FKV_ERR_CUDA;
+  static std::atomic<void *> known{nullptr};   // (a query's map is encoded at every call)
+  void *fn = known.load();
+  if (fn == nullptr) {
+    cudaDriverEntryPointQueryResult found;
+    FKV_CUDA(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found));
+    if (fn == nullptr || found != cudaDriverEntryPointSuccess) {
+      g_cuda_error = "cuTensorMapEncodeTiled is not available from this driver";
+      return FKV_ERR_CUDA;
+    }
+    known.store(fn);
   }
   const cuuint32_t step[5] = {1, 1, 1, 1, 1};
   const CUresult r = reinterpret_cast<encode_fn>(fn)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, base, dims, strides, box, step,

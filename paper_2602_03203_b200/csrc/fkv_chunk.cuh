@@ -71,6 +71,7 @@ __global__ void __launch_bounds__(256) k_append_chunk(Ctx c, int layer, const ui
   griddep_launch();
   const int s = tid;
   int n_old = 0, kp = 0, T = 0, pop = 0, push = 0, bad = 0;
+  const int top = __ldcg(c.ctrl + CTRL_FREE_TOP);
   if (s < c.batch) {
     n_old = __ldcg(c.len + layer * c.batch + s);
     T = lens.tok[s + 1] - lens.tok[s];
@@ -89,7 +90,6 @@ __global__ void __launch_bounds__(256) k_append_chunk(Ctx c, int layer, const ui
   const int pop_off = block_excl_scan(pop, s_scan, pops);
   const int push_off = block_excl_scan(push, s_scan, pushes);
   if (s < c.batch) { s_pop[s] = pop_off; s_push[s] = push_off; }
-  const int top = __ldcg(c.ctrl + CTRL_FREE_TOP);
   const bool exhausted = pops > top;
   if (blockIdx.x == 0) {
     if (bad) set_status(c, (unsigned)bad);
@@ -97,9 +97,9 @@ __global__ void __launch_bounds__(256) k_append_chunk(Ctx c, int layer, const ui
   }
   __syncthreads();
   if (!exhausted) {
-    const long long tasks = (long long)lens.tok[c.batch] * c.Hkv;
-    for (long long t = (long long)blockIdx.x * 8 + warp; t < tasks; t += (long long)gridDim.x * 8) {
-      const int row = (int)(t / c.Hkv), h = (int)(t - (long long)row * c.Hkv);
+    const int tasks = lens.tok[c.batch] * c.Hkv;   // (at most 2^24 x 32)
+    for (int t = blockIdx.x * 8 + warp; t < tasks; t += gridDim.x * 8) {
+      const int row = t / c.Hkv, h = t - row * c.Hkv;
       int lo = 0, hi = c.batch;   // the sequence of the row: the last one that starts at or before it
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -182,7 +182,7 @@ struct ChunkItem {
   int pa0, pa1;    // pages of the sinks ...
   int pb0, pb1;    // ... and of the rest that this CTA takes
   int part;        // -1: the whole item is here; 0 / 1: the slot for the partial result
-  int pad[2];
+  int w0, e1;      // outside [0, a) and [w0, e1) no token of the item sees a slot
 };
 
 // The key tiles of an item: up to TP pages each, those of the sinks first.
@@ -686,14 +686,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       // stored positions show to be hidden from every token.
       int pa0 = min(off, b.r.sp), pa1 = min(off + take, b.r.sp);
       int pb0 = b.r.b0 + max(off - b.r.sp, 0), pb1 = b.r.b0 + max(off + take - b.r.sp, 0);
-      int na = 0;
+      int na = 0, first = 0;
       if (W) {
         na = S ? slot_sinks(c, ptrow, b.n, S) : 0;
         // Where the first token's window begins, then the others': a window that begins d positions later begins at most d
         // slots later, so the positions of those slots decide, read together (a search of its own for a token whose
         // window is further off: a chunk with gaps in its positions).
         const int p_first = slot_pos(c, ptrow, e0 - 1), lo0 = max(0, e0 - W), start = window_start(p_first, W);
-        const int first = slot_pos(c, ptrow, lo0) >= start ? lo0 : slot_lower_bound_warp(c, ptrow, lo0 + 1, e0, start);
+        first = slot_pos(c, ptrow, lo0) >= start ? lo0 : slot_lower_bound_warp(c, ptrow, lo0 + 1, e0, start);
         __syncwarp();
         for (int i = lane; i < 256 && first + i < b.n; i += 32) Pos[i] = slot_pos(c, ptrow, first + i);
         __syncwarp();
@@ -730,7 +730,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
         x->head = head; x->seg = seg;
         x->row0 = a.lens.tok[b.s] + b.j0;
         x->ntok[0] = nt0; x->ntok[1] = ntok - nt0;
-        x->e0 = e0; x->n = b.n; x->a = na;
+        x->e0 = e0; x->n = b.n; x->a = na; x->w0 = first; x->e1 = e0 + ntok - 1;
         x->pa0 = pa0; x->pa1 = pa1; x->pb0 = pb0; x->pb1 = pb1;
         x->part = part;
         if (part == 1) {   // for the merge, with the last CTA that the item reaches
@@ -878,12 +878,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
             umma_commit_if(on, smem_u32(&s_full[t]));
           }
         } else {
-          // Rows of the last page past the segment's end hold whatever the page held before: P is zero there, but zero
-          // times an infinity is not, so they are cleared.
-          const int r0 = x.n - tl.first(i) * kPage;
-          if (r0 < np * kPage) {
-            for (int e = lane; e < (np * kPage - r0) * NQ * 8; e += 32) {
-              const int row = r0 + e / (NQ * 8), ch = e % (NQ * 8);
+          // Rows that no token of the item sees (pairs outside every window; past the segment's end whatever the page held
+          // before) are cleared: P is zero there, but zero times an infinity is not.
+          const int s0 = tl.first(i) * kPage, s1 = s0 + np * kPage;
+          if (!((s0 >= x.w0 && s1 <= x.e1) || s1 <= min(x.a, x.e1))) {
+            for (int e = lane; e < np * kPage * NQ * 8; e += 32) {
+              const int row = e / (NQ * 8), ch = e % (NQ * 8), at = s0 + row;
+              if (at < x.e1 && (at < x.a || at >= x.w0)) continue;
               *reinterpret_cast<uint4 *>(Vt + slot * SM::kKv + (size_t)((row / kPage * NQ + (ch >> 3)) * kPage + row % kPage) * 128 +
                                          (ch & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
             }
@@ -952,40 +953,46 @@ __global__ void __launch_bounds__(256) k_chunk_merge(Ctx c, const __grid_constan
       const int cta = two ? p >> 1 : p;
       return (size_t)((cf + cta) * 2 + (cta == 0 ? 1 : 0)) * 256 + prow + (two ? (p & 1) * kChunkRows : 0);
     };
-    float M = -INFINITY, L = 0.f;
-    for (int p = lane; p < parts; p += 32) M = fmaxf(M, __ldcg(ml + row_of(p)).x);
+    // Statistics of 32 parts, one per lane, and the rows of the first eight are asked for together: one round trip to L2 for
+    // most items.  A part that saw nothing of the row may not have been written: whatever was read counts for nothing.
+    auto row = [&](int p, float (&w)[D / 32]) {
+      const float *o = c.chunk_part + row_of(p) * D + lane * (D / 32);
+      if (D == 128) {
+        const float4 x4 = __ldcg(reinterpret_cast<const float4 *>(o));
+        w[0] = x4.x; w[1] = x4.y; w[D / 32 - 2] = x4.z; w[D / 32 - 1] = x4.w;
+      } else {
+        const float2 x2 = __ldcg(reinterpret_cast<const float2 *>(o));
+        w[0] = x2.x; w[1] = x2.y;
+      }
+    };
+    auto stats = [&](int p) { return p < parts ? __ldcg(ml + row_of(p)) : make_float2(-INFINITY, 0.f); };
+    float2 x = stats(lane);
+    float w[8][D / 32];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < parts) row(i, w[i]);
+    float M = x.x, L = 0.f;
+    for (int p = 32 + lane; p < parts; p += 32) M = fmaxf(M, stats(p).x);
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
     float acc[D / 32];
 #pragma unroll
     for (int j = 0; j < D / 32; ++j) acc[j] = 0.f;
-    for (int p0 = 0; p0 < parts; p0 += 32) {
-      const float2 x = p0 + lane < parts ? __ldcg(ml + row_of(p0 + lane)) : make_float2(-INFINITY, 0.f);
+    for (int p0 = 0; p0 < parts; p0 += 8) {
+      if (p0 > 0) {
+        if (p0 % 32 == 0) x = stats(p0 + lane);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (p0 + i < parts) row(p0 + i, w[i]);
+      }
       const float f = x.x == -INFINITY ? 0.f : ex2((x.x - M) * a.scale_log2);
-      L += f * x.y;
-      const int cnt = min(32, parts - p0);
-      // Eight parts' rows are asked for before the first is used.  One that saw nothing of the row may not have been
-      // written: whatever was read there counts for nothing.
-      for (int i0 = 0; i0 < cnt; i0 += 8) {
-        float w[8][D / 32];
+      if (p0 % 32 == 0) L += f * x.y;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float *o = c.chunk_part + row_of(p0 + min(i0 + i, cnt - 1)) * D + lane * (D / 32);
-          if (D == 128) {
-            const float4 x4 = __ldcg(reinterpret_cast<const float4 *>(o));
-            w[i][0] = x4.x; w[i][1] = x4.y; w[i][D / 32 - 2] = x4.z; w[i][D / 32 - 1] = x4.w;
-          } else {
-            const float2 x2 = __ldcg(reinterpret_cast<const float2 *>(o));
-            w[i][0] = x2.x; w[i][1] = x2.y;
-          }
-        }
+      for (int i = 0; i < 8; ++i) {
+        const float fi = __shfl_sync(0xffffffffu, f, (p0 + i) & 31);
+        const bool on = p0 + i < parts && fi != 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float fi = __shfl_sync(0xffffffffu, i0 + i < cnt ? f : 0.f, min(i0 + i, 31));
-          const bool on = i0 + i < cnt && fi != 0.f;
-#pragma unroll
-          for (int j = 0; j < D / 32; ++j) acc[j] = on ? fmaf(fi, w[i][j], acc[j]) : acc[j];
-        }
+        for (int j = 0; j < D / 32; ++j) acc[j] = on ? fmaf(fi, w[i][j], acc[j]) : acc[j];
       }
     }
 #pragma unroll

@@ -439,11 +439,11 @@ __global__ void __launch_bounds__(kCfThreads, 1) k_chunk_features(Ctx c, const _
         tc_fence_after();
         if (there) {
           const uint32_t d = td + buf * 128;
-          umma_bf16_if(on, d, ke, be, idesc, 0);
 #pragma unroll
           for (int ks = 0; ks < D / 16; ++ks) {
             const uint64_t o = (uint64_t)(((ks >> 2) * 128 * 128 + (ks & 3) * 32) >> 4);
-            umma_bf16_if(on, d, ad + o, bd + o, idesc, 1);
+            umma_bf16_if(on, d, ad + o, bd + o, idesc, ks > 0);
+            if (ks == D / 32 - 1) umma_bf16_if(on, d, ke, be, idesc, 1);   // half-way: the partial sums of the large weights stay smallest
           }
         }
         umma_commit_if(on, smem_u32(&acc_full[t * 2 + buf]));

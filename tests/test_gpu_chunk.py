@@ -264,6 +264,78 @@ def test_chunk_attention_ignores_what_freed_pages_held():
     run_chunk(c, [0, 1], window=3, sinks=2)
 
 
+@pytest.mark.parametrize("D,T", [(128, 9), (64, 200)])
+def test_chunk_attention_ignores_what_no_query_sees(D, T):
+    # Infinities and NaN in keys and values that lie outside the window of every query of the chunk.
+    c = Case(2, 4, D, [0, 0])
+    n, window, sinks = [333, 90], 20, 5
+    for s in range(2):
+        k, v = c.rand(n[s], 2), c.rand(n[s], 2)
+        hidden = slice(sinks, n[s] - window + 1)
+        k[hidden][::2], k[hidden][1::2], v[hidden][::2], v[hidden][1::2] = math.inf, math.nan, math.nan, -math.inf
+        lens = [n[s] if i == s else 0 for i in range(2)]
+        c.cache.append_chunk(0, k, v, lens)
+        k[hidden], v[hidden] = 0, 0
+        c.extend(k, v, lens)
+    run_chunk(c, [T, 3], window, sinks)
+
+
+def test_chunks_of_two_caches_on_two_streams():
+    cases = [Case(2, 4, 128, [700, 90], seed=s) for s in range(2)]
+    streams = [torch.cuda.Stream() for _ in cases]
+    lens, calls = [60, 7], []
+    torch.cuda.synchronize()
+    for c in cases:
+        calls.append([c.chunk(lens) for _ in range(4)])
+    torch.cuda.synchronize()
+    results = [[], []]
+    for step in range(4):
+        for i, c in enumerate(cases):
+            with torch.cuda.stream(streams[i]):
+                k, v, q = calls[i][step]
+                lse = torch.empty(q.shape[:2], device="cuda")
+                results[i].append((c.cache.append_chunk_attn(0, k, v, q, lens, lse=lse), lse))
+    torch.cuda.synchronize()
+    for i, c in enumerate(cases):
+        for (k, v, q), (out, lse) in zip(calls[i], results[i]):
+            c.extend(k, v, lens)
+            c.check_chunk(out, lse, q, lens)
+        assert c.status() == 0
+
+
+def test_chunk_attention_on_pages_past_four_gigabytes():
+    # 16 sequences of 65536 pairs on eight heads take 4.5 GB of pages; the last one's lie behind 2^32 bytes.
+    Hkv, D, n = 8, 128, 65536
+    cache = binding.Cache(1, Hkv, 1, D, 17, 16, n, num_pages=17 * Hkv * (n // 16) - 8 * 3000)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(5)
+    k = torch.randn((Hkv, n, D), generator=gen, device="cuda").to(torch.bfloat16)
+    v = torch.randn((Hkv, n, D), generator=gen, device="cuda").to(torch.bfloat16)
+    for s in range(16):
+        cache.prefill(0, s, k, v)
+    c = Case(Hkv, 1, D, [0], seed=8)   # (its own small cache is not used)
+    c.cache, c.batch = cache, 17
+    c.seqs = [ref.Seq(Hkv, D, 6) for _ in range(17)]
+    for h in range(Hkv):
+        c.seqs[15].k[h], c.seqs[15].v[h] = k[h], v[h]
+        c.seqs[15].pos[h] = torch.arange(n, dtype=torch.int32, device="cuda")
+    keep = [n] * 15 + [n - 40, 0]
+    lens = [0] * 15 + [40, 300]
+    kn, vn, q = c.chunk(lens)
+    lse = torch.empty(q.shape[:2], device="cuda")
+    out = cache.append_chunk_attn(0, kn, vn, q, lens, keep_lens=keep, lse=lse)
+    c.seqs[15].extend(kn[:40], vn[:40], keep=n - 40)
+    c.seqs[16].extend(kn[40:], vn[40:])
+    assert cache.device_status()[0] == 0
+    c.check_chunk(out, lse, q, lens)
+    cache.chunk_features(0, q, lse, lens)
+    assert bool(torch.isfinite(cache.export_features(0, 15)).all())
+    out = cache.decode_attn_window(0, q[:17].contiguous(), 5000, 4)
+    o, _, _, tol, _ = ref.attend(q[15:16, 3], c.seqs[15].k[3], c.seqs[15].v[3],
+                                 ref.seen(c.seqs[15].pos[3], torch.tensor([n - 1], device="cuda"), c.seqs[15].pos[3][-1:], 5000, 4), D ** -0.5)
+    assert bool(((out[15:16, 3].double() - o).abs() <= tol).all())
+
+
 def test_chunk_attention_reproducible_and_independent_of_the_split():
     c = Case(2, 4, 128, [3000, 20])
     lens = [100, 33]
