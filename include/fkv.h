@@ -271,7 +271,7 @@ int fkv_decode_step(fkv_cache *c, const void *k, const void *v, const int32_t *p
  * fkv_decode_attn / fkv_append_decode_attn of a layer whose queries see only part of the retained set: a query of
  * position p sees the pairs of positions (p - window, p] and those of positions below `sinks` (the first tokens, that
  * stay visible).  Positions are the stored ones, so a window means the same before and after an eviction.  window >= 1,
- * sinks >= 0 (else FKV_ERR_INVALID_ARG).  The rest is as in the calls without a window, but that the query is NOT put on
+ * sinks >= 0, and k, v, q and out 16-byte aligned (else FKV_ERR_INVALID_ARG).  The rest is as in the calls without a window, but that the query is NOT put on
  * record for the attention features (they describe attention over the whole retained set).
  *
  * Positions must grow from pair to pair of a segment, and k and v must be finite where some of the queries of a call see a

@@ -263,11 +263,30 @@ class Cache:
         return out
 
     # -- sliding windows and sinks
+    def _check_place(self, *tensors):
+        """The kernels run on the cache's device, on its current stream: a tensor elsewhere would fault there."""
+        dev = self.workspace.device
+        if torch.cuda.current_device() != dev.index:
+            raise ValueError(f"the cache is on {dev}, the current device is cuda:{torch.cuda.current_device()}")
+        for t in tensors:
+            if t is not None and t.device != dev:
+                raise ValueError(f"the cache is on {dev}, a tensor on {t.device}")
+
+    def _check_step(self, k, v, q, out, pos):
+        c = self.cfg
+        kv = c.max_batch * c.num_kv_heads * c.head_dim
+        for name, t, want in (("k", k, kv), ("v", v, kv), ("q", q, kv * c.group_size), ("out", out, kv * c.group_size),
+                              ("pos", pos, c.max_batch)):
+            if t is not None and t.numel() != want:
+                raise ValueError(f"{name}: expected {want} elements, got {t.numel()}")
+        self._check_place(k, v, q, out, pos)
+
     def decode_attn_window(self, layer, q, window, sinks=0, q_pos=None, out=None, scale=0.0):
         """decode_attn over the last `window` positions up to the query's and the positions below `sinks`.
         q_pos [batch] int32: positions of the queries (None: the last pair's)."""
         if out is None:
             out = torch.empty_like(q)
+        self._check_step(None, None, q, out, q_pos)
         _check(lib().fkv_decode_attn_window(self._h, layer, _ptr(q, torch.bfloat16), _ptr(q_pos, torch.int32), window, sinks,
                                             _ptr(out, torch.bfloat16), scale, _stream()), "fkv_decode_attn_window")
         return out
@@ -276,6 +295,7 @@ class Cache:
         """append(k, v) then decode_attn_window(q) on one layer, as one launch."""
         if out is None:
             out = torch.empty_like(q)
+        self._check_step(k, v, q, out, pos)
         keep, m = _mask(seq_mask, self.cfg.max_batch)
         _check(lib().fkv_append_decode_attn_window(self._h, layer, _ptr(k, torch.bfloat16), _ptr(v, torch.bfloat16),
                                                    _ptr(pos, torch.int32), m, _ptr(q, torch.bfloat16), window, sinks,
@@ -291,6 +311,7 @@ class Cache:
             want = (total, heads) if name == "lse" else (total,) if name == "pos" else (total, heads, c.head_dim)
             if t is not None and tuple(t.shape) != want:
                 raise ValueError(f"{name}: expected shape {want}, got {tuple(t.shape)}")
+        self._check_place(*tensors.values())
 
     def append_chunk(self, layer, k, v, chunk_lens, pos=None, keep_lens=None):
         """Store chunk_lens[s] new pairs behind the first keep_lens[s] pairs of every sequence (None: behind all)."""
@@ -337,6 +358,7 @@ class Cache:
             out = torch.empty(shape, dtype=torch.float32, device="cuda")
         elif tuple(out.shape) != shape:
             raise ValueError(f"out: expected shape {shape}, got {tuple(out.shape)}")
+        self._check_place(out)
         _check(lib().fkv_export_features(self._h, layer, seq, _ptr(out, torch.float32), _stream()), "fkv_export_features")
         return out
 

@@ -564,11 +564,11 @@ cudaError_t launch_waiting(void (*kern)(P...), dim3 grid, int threads, size_t sm
   return cudaLaunchKernelEx(&cfg, kern, std::forward<A>(args)...);
 }
 
-int check_append_chunk(const fkv_cache *c, int layer, const void *k, const void *v, const int32_t *keep_lens,
-                       const int32_t *chunk_lens, ChunkLens &lens) {
+int check_append_chunk(const fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos,
+                       const int32_t *keep_lens, const int32_t *chunk_lens, ChunkLens &lens) {
   if (!c || !layer_ok(c, layer) || !chunk_lens || !make_lens(c, chunk_lens, lens)) return FKV_ERR_INVALID_ARG;
   const int batch = c->cfg.max_batch;
-  if (lens.tok[batch] > 0 && (!k || !v || !aligned(k, 16) || !aligned(v, 16))) return FKV_ERR_INVALID_ARG;
+  if (lens.tok[batch] > 0 && (!k || !v || !aligned(k, 16) || !aligned(v, 16) || !aligned(pos, 4))) return FKV_ERR_INVALID_ARG;
   for (int s = 0; s < batch; ++s) {
     const int n = c->h_len[(size_t)layer * batch + s], keep = keep_lens ? keep_lens[s] : n;
     if (keep < 0 || keep > n) return FKV_ERR_INVALID_ARG;
@@ -1066,7 +1066,7 @@ int fkv_decode_step(fkv_cache *c, const void *k, const void *v, const int32_t *p
 int fkv_append_chunk(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos, const int32_t *keep_lens,
                      const int32_t *chunk_lens, void *stream) {
   ChunkLens lens;
-  if (int e = check_append_chunk(c, layer, k, v, keep_lens, chunk_lens, lens)) return e;
+  if (int e = check_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens)) return e;
   return launch_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens, (cudaStream_t)stream);
 }
 
@@ -1074,7 +1074,7 @@ int fkv_chunk_attn(fkv_cache *c, int layer, const void *q, const int32_t *chunk_
                    void *out, float *lse_out, void *stream) {
   ChunkLens lens;
   if (int e = check_chunk(c, layer, q, chunk_lens, window, sinks, scale, lens)) return e;
-  if (lens.tok[c->cfg.max_batch] > 0 && (!out || !aligned(out, 16))) return FKV_ERR_INVALID_ARG;
+  if (lens.tok[c->cfg.max_batch] > 0 && (!out || !aligned(out, 16) || !aligned(lse_out, 4))) return FKV_ERR_INVALID_ARG;
   if (!chunk_is_stored(c, layer, chunk_lens)) return FKV_ERR_INVALID_ARG;
   return launch_chunk_attend(c, layer, q, chunk_lens, lens, window, sinks, scale, out, lse_out, (cudaStream_t)stream);
 }
@@ -1084,8 +1084,9 @@ int fkv_append_chunk_attn(fkv_cache *c, int layer, const void *k, const void *v,
                           float *lse_out, void *stream) {
   ChunkLens lens;
   if (int e = check_chunk(c, layer, q, chunk_lens, window, sinks, scale, lens)) return e;
-  if (int e = check_append_chunk(c, layer, k, v, keep_lens, chunk_lens, lens)) return e;
-  if (lens.tok[c->cfg.max_batch] > 0 && (!out || !aligned(out, 16))) return FKV_ERR_INVALID_ARG;
+  if (int e = check_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens)) return e;
+  if (lens.tok[c->cfg.max_batch] > 0 && (!out || !aligned(out, 16) || !aligned(lse_out, 4))) return FKV_ERR_INVALID_ARG;
+  if (int e = ensure_page_rows_map(c)) return e;   // (what can fail does so before anything is stored)
   if (int e = launch_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens, (cudaStream_t)stream)) return e;
   return launch_chunk_attend(c, layer, q, chunk_lens, lens, window, sinks, scale, out, lse_out, (cudaStream_t)stream);
 }
@@ -1102,6 +1103,7 @@ int fkv_chunk_features(fkv_cache *c, int layer, const void *q, const float *lse,
 int fkv_decode_attn_window(fkv_cache *c, int layer, const void *q, const int32_t *q_pos, int32_t window, int32_t sinks, void *out,
                            float scale, void *stream) {
   if (!c || !layer_ok(c, layer) || !q || !out || window < 1 || sinks < 0) return FKV_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(q_pos, 4)) return FKV_ERR_INVALID_ARG;
   Window w;
   w.window = window; w.sinks = sinks; w.q_pos = q_pos;
   return launch_attend(c, layer, q, out, scale, nullptr, nullptr, nullptr, make_mask(c, nullptr), false, (cudaStream_t)stream, w);
@@ -1111,6 +1113,7 @@ int fkv_append_decode_attn_window(fkv_cache *c, int layer, const void *k, const 
                                   const uint64_t *seq_mask, const void *q, int32_t window, int32_t sinks, void *out, float scale,
                                   void *stream) {
   if (!c || !layer_ok(c, layer) || !k || !v || !q || !out || window < 1 || sinks < 0) return FKV_ERR_INVALID_ARG;
+  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(q, 16) || !aligned(out, 16) || !aligned(pos, 4)) return FKV_ERR_INVALID_ARG;
   const int batch = c->cfg.max_batch;
   const SeqMask m = make_mask(c, seq_mask);
   for (int s = 0; s < batch; ++s)
@@ -1124,7 +1127,7 @@ int fkv_export_features(fkv_cache *c, int layer, int seq, float *feat, void *str
   if (!c || !layer_ok(c, layer) || seq < 0 || seq >= c->cfg.max_batch) return FKV_ERR_INVALID_ARG;
   const int n = c->h_len[(size_t)layer * c->cfg.max_batch + seq];
   if (n == 0) return FKV_OK;   // (an empty tensor may have no address)
-  if (!feat) return FKV_ERR_INVALID_ARG;
+  if (!feat || !aligned(feat, 4)) return FKV_ERR_INVALID_ARG;
   k_export_features<<<dim3((n + 7) / 8, c->cfg.num_kv_heads), 256, 0, (cudaStream_t)stream>>>(c->ctx, layer, seq, n, feat);
   FKV_LAUNCHED(c);
   return FKV_OK;

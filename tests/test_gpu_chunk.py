@@ -568,3 +568,32 @@ def test_refusals():
         c.cache.chunk_attn(0, q, [3, 2], lse=lse.double())
     c.check_stored()   # nothing was stored by a refused call
     assert c.status() == 0
+
+
+def test_misaligned_tensors_are_refused():
+    c = Case(2, 4, 64, [20, 10], cap=64)
+    lib, h, st = binding.lib(), c.cache._h, ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    k, v, q = c.chunk([3, 2])
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device="cuda")
+    pos, feat = torch.arange(100, 105, dtype=torch.int32, device="cuda"), torch.zeros(2, 20, 24, device="cuda")
+    lens = (ctypes.c_int32 * 2)(3, 2)
+    p = lambda t, off=0: ctypes.c_void_p(t.data_ptr() + off)  # noqa: E731
+    good = dict(k=p(k), v=p(v), q=p(q), out=p(out), pos=p(pos), lse=p(lse))
+
+    def calls(**x):
+        return (lib.fkv_append_chunk(h, 0, x["k"], x["v"], x["pos"], None, lens, st) if not {"q", "out", "lse"} & set(x["bad"]) else -1,
+                lib.fkv_append_chunk_attn(h, 0, x["k"], x["v"], x["pos"], None, lens, x["q"], 0, 0, 0.0, x["out"], x["lse"], st),
+                lib.fkv_append_decode_attn_window(h, 0, x["k"], x["v"], x["pos"], None, x["q"], 4, 0, x["out"], 0.0, st)
+                if "lse" not in x["bad"] else -1)
+
+    for name, offs in [("k", (2, 8)), ("v", (2, 8)), ("q", (2, 8)), ("out", (2, 8)), ("pos", (1, 2)), ("lse", (1, 2))]:
+        for off in offs:
+            assert calls(**{**good, name: ctypes.c_void_p(good[name].value + off)}, bad=[name]) == (-1, -1, -1), (name, off)
+    for off in (2, 8):
+        assert lib.fkv_decode_attn_window(h, 0, p(q, off), None, 4, 0, p(out), 0.0, st) == -1
+        assert lib.fkv_decode_attn_window(h, 0, p(q), None, 4, 0, p(out, off), 0.0, st) == -1
+    assert lib.fkv_decode_attn_window(h, 0, p(q), p(pos, 2), 4, 0, p(out), 0.0, st) == -1
+    assert lib.fkv_chunk_attn(h, 0, p(q), lens, 0, 0, 0.0, p(out), p(lse, 2), st) == -1
+    assert lib.fkv_export_features(h, 0, 0, p(feat, 2), st) == -1
+    c.check_stored()
+    assert c.status() == 0 and not out.any() and not lse.any() and not feat.any()
