@@ -635,11 +635,11 @@ int launch_chunk_attend_t(fkv_cache *c, const CUtensorMap &tmq, const ChunkArgs 
   FKV_CUDA(launch_waiting(k_chunk_attend<D>, dim3(grid), kChunkThreads, smem, st, c->ctx, c->page_rows, c->page_parts, tmq, a));
   ++c->launches;
   if (grid > 1) {   // (a single CTA cuts nothing)
-    // A warp per query row of the largest item.
+    // A warp per query row of the largest item, or per 8 rows x 16 channels.
     int longest = 0;
     for (int s = 0; s < c->cfg.max_batch; ++s) longest = std::max(longest, a.lens.tok[s + 1] - a.lens.tok[s]);
-    const int G = c->cfg.group_size, rows = std::min(longest, 2 * (kChunkRows / G)) * G;
-    FKV_CUDA(launch_waiting(k_chunk_merge<D>, dim3(grid, (rows + 7) / 8), 256, 0, st, c->ctx, a));
+    const int G = c->cfg.group_size, tile = kChunkRows / G, rows = std::min(longest, 2 * tile) * G;
+    FKV_CUDA(launch_waiting(longest <= tile ? k_chunk_merge<D, true> : k_chunk_merge<D, false>, dim3(grid, (rows + 7) / 8), 256, 0, st, c->ctx, a));
     ++c->launches;
   }
   return FKV_OK;

@@ -507,10 +507,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       // Both streams of one query tile: where the item goes on elsewhere the merge takes both results, else they meet here.
       const bool join = x.kind == 2 && nt > 1 && x.part < 0;
       const size_t orow = ((size_t)(x.row0 + tj) * c.Hkv + x.head) * G + hq;
-      const size_t prow = (size_t)(blockIdx.x * 2 + max(x.part, 0)) * 256 + t * kChunkRows + R;
+      const int pslot = blockIdx.x * 2 + max(x.part, 0), prow = t * kChunkRows + R;
       float f0 = 1.f, f1 = 0.f;   // weights of the two streams' results
       const bool writes = live && (x.kind == 1 || t == 0 || x.part >= 0);
-      float *part = c.chunk_part + prow * D;
       __nv_bfloat16 *out = a.out + orow * D;
       // 16 columns at a time: short calls end here, and code that runs for the first time costs more than its arithmetic.
 #pragma unroll 1
@@ -550,9 +549,12 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
         }
         if (!writes) continue;
         if (x.part >= 0) {
-          if (has) {
+          if (has) {   // (the two layouts: see k_chunk_merge)
+            const int step = x.kind == 1 ? 256 * 4 : 4;
+            float *part = c.chunk_part + pslot * (256 * D) + prow * (x.kind == 1 ? 4 : D) + q / 4 * step;
 #pragma unroll
-            for (int j = 0; j < 16; j += 4) __stcg(reinterpret_cast<uint4 *>(part + q + j), make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]));
+            for (int j = 0; j < 4; ++j)
+              __stcg(reinterpret_cast<uint4 *>(part + j * step), make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]));
           }
         } else {
           const float inv = l == 0.f ? 0.f : 1.f / l;   // a row that sees nothing gives zeros
@@ -574,7 +576,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       if (writes) {
         // (a row whose scores are all NaN has found no maximum, but must not count as one that saw nothing)
         if (x.part >= 0)
-          __stcg(reinterpret_cast<float2 *>(c.chunk_ml) + prow, make_float2(l != l ? 0.f : m, l));
+          __stcg(reinterpret_cast<float2 *>(c.chunk_ml) + pslot * 256 + prow, make_float2(l != l ? 0.f : m, l));
         else if (a.lse)
           a.lse[orow] = l == 0.f ? -INFINITY : fmaf(m, a.scale, logf(l));
       }
@@ -930,10 +932,17 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
   if (warp == 3) tmem_dealloc(tmem_base, 512);
 }
 
-// Joins the partial results of the items that cuts go through: grid (CTAs of the attention launch, row groups), a warp
-// per query row.  CTA x looks after the item that CTA x of the attention left open: its own part, and those of the CTAs up
-// to the last one that the item reached.
-template <int D>
+// Joins the partial results of the items that cuts go through: grid (CTAs of the attention launch, row groups).  CTA x
+// looks after the item that CTA x of the attention left open: its own part, and those of the CTAs up to the last one that
+// the item reached.  Items come in two forms:
+//   two query tiles (more than 128 rows, a few parts).  A thread of the attention has a row, and 32 rows of 512 bytes are 32
+//   lines to a store (9000 cycles for an item's end, 4000 like this): a slot holds [D / 4][256 rows][4 channels], and a warp
+//   here takes 8 rows x 16 channels.  (256 tokens at 8K: 65 us for both kernels with the form below, 59 with this one.)
+//   one query tile (few rows, with drafts over a long cache in many parts; both streams leave one).  A slot holds [256
+//   rows][D], and a warp here takes a row.  (5 drafts at 8K: 27 us for both kernels with the form above, 25 with this one.)
+// SHORT: a launch whose items all have one tile has no code for the other form (with it, that takes 1.7 us longer).
+// A part that saw nothing of a row may not have been written: whatever was read counts for nothing.
+template <int D, bool SHORT>
 __global__ void __launch_bounds__(256) k_chunk_merge(Ctx c, const __grid_constant__ ChunkArgs a) {
   griddep_wait();
   griddep_launch();
@@ -941,68 +950,111 @@ __global__ void __launch_bounds__(256) k_chunk_merge(Ctx c, const __grid_constan
   const int cl = __ldcg(info);
   if (cl < 0) return;
   const int cf = blockIdx.x, head = __ldcg(info + 1), row0 = __ldcg(info + 2), G = c.G, TPT = kChunkRows / G;
-  const int nt0 = __ldcg(info + 3), ntok = nt0 + __ldcg(info + 4), lane = threadIdx.x & 31;
-  const bool two = ntok == nt0;
-  const int parts = (cl + 1 - cf) * (two ? 2 : 1);
-  const float2 *ml = reinterpret_cast<const float2 *>(c.chunk_ml);
-  for (int r = blockIdx.y * 8 + (threadIdx.x >> 5); r < ntok * G; r += gridDim.y * 8) {
+  const int nt0 = __ldcg(info + 3), ntok = nt0 + __ldcg(info + 4), lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rows = ntok * G;
+  // Slot 1 of CTA cf, then slots 0 of the CTAs behind it.
+  const float *part = c.chunk_part + (size_t)(2 * cf + 1) * 256 * D;
+  const float2 *ml = reinterpret_cast<const float2 *>(c.chunk_ml) + (2 * cf + 1) * 256;
+  auto slot_of = [](int cta) { return 2 * cta - (cta > 0 ? 1 : 0); };
+  if (SHORT || ntok == nt0) {
+    const int parts = (cl + 1 - cf) * 2;   // part p: of CTA cf + p / 2 and stream p % 2
+    for (int r = blockIdx.y * 8 + warp; r < rows; r += gridDim.y * 8) {
+      auto row_of = [&](int p) { return slot_of(p >> 1) * 256 + (p & 1) * kChunkRows + r; };
+      // Statistics of 32 parts, one per lane, and the rows of the first eight are asked for together: one round trip to L2 for
+      // most items.
+      auto row = [&](int p, float (&w)[D / 32]) {
+        const float *o = part + row_of(p) * D + lane * (D / 32);
+        if (D == 128) {
+          const float4 x4 = __ldcg(reinterpret_cast<const float4 *>(o));
+          w[0] = x4.x; w[1] = x4.y; w[D / 32 - 2] = x4.z; w[D / 32 - 1] = x4.w;
+        } else {
+          const float2 x2 = __ldcg(reinterpret_cast<const float2 *>(o));
+          w[0] = x2.x; w[1] = x2.y;
+        }
+      };
+      auto stats = [&](int p) { return p < parts ? __ldcg(ml + row_of(p)) : make_float2(-INFINITY, 0.f); };
+      float2 x = stats(lane);
+      float w[8][D / 32];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < parts) row(i, w[i]);
+      float M = x.x, L = 0.f;
+      for (int p = 32 + lane; p < parts; p += 32) M = fmaxf(M, stats(p).x);
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+      float acc[D / 32];
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) acc[j] = 0.f;
+      for (int p0 = 0; p0 < parts; p0 += 8) {
+        if (p0 > 0) {
+          if (p0 % 32 == 0) x = stats(p0 + lane);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (p0 + i < parts) row(p0 + i, w[i]);
+        }
+        const float f = x.x == -INFINITY ? 0.f : ex2((x.x - M) * a.scale_log2);
+        if (p0 % 32 == 0) L += f * x.y;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float fi = __shfl_sync(0xffffffffu, f, (p0 + i) & 31);
+          const bool on = p0 + i < parts && fi != 0.f;
+#pragma unroll
+          for (int j = 0; j < D / 32; ++j) acc[j] = on ? fmaf(fi, w[i][j], acc[j]) : acc[j];
+        }
+      }
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+      const float inv = L == 0.f ? 0.f : 1.f / L;
+      const size_t orow = ((size_t)(row0 + r / G) * c.Hkv + head) * G + r % G;
+      uint32_t *dst = reinterpret_cast<uint32_t *>(a.out + orow * D) + lane * (D / 64);
+      dst[0] = pack_bf16(acc[0] * inv, acc[1] * inv);
+      if (D == 128) dst[1] = pack_bf16(acc[D / 32 - 2] * inv, acc[D / 32 - 1] * inv);
+      if (a.lse && lane == 0) a.lse[orow] = L == 0.f ? -INFINITY : fmaf(M, a.scale, logf(L));
+    }
+    return;
+  }
+  const int parts = cl + 1 - cf;
+  for (int u = blockIdx.y * 8 + warp; u < (rows + 7) / 8 * (D / 16); u += gridDim.y * 8) {
+    const int r = u / (D / 16) * 8 + (lane >> 2), ch = u % (D / 16) * 4 + (lane & 3);   // a lane: 4 channels of a row
     const int tj = r / G, hq = r - tj * G;
-    const int prow = tj < nt0 ? tj * G + hq : kChunkRows + (tj - TPT) * G + hq;   // row inside a CTA's slot
-    // Part p: of CTA cf + p, or, where two streams worked on one query tile, of CTA cf + p / 2 and stream p % 2.
-    auto row_of = [&](int p) {
-      const int cta = two ? p >> 1 : p;
-      return (size_t)((cf + cta) * 2 + (cta == 0 ? 1 : 0)) * 256 + prow + (two ? (p & 1) * kChunkRows : 0);
-    };
-    // Statistics of 32 parts, one per lane, and the rows of the first eight are asked for together: one round trip to L2 for
-    // most items.  A part that saw nothing of the row may not have been written: whatever was read counts for nothing.
-    auto row = [&](int p, float (&w)[D / 32]) {
-      const float *o = c.chunk_part + row_of(p) * D + lane * (D / 32);
-      if (D == 128) {
-        const float4 x4 = __ldcg(reinterpret_cast<const float4 *>(o));
-        w[0] = x4.x; w[1] = x4.y; w[D / 32 - 2] = x4.z; w[D / 32 - 1] = x4.w;
-      } else {
-        const float2 x2 = __ldcg(reinterpret_cast<const float2 *>(o));
-        w[0] = x2.x; w[1] = x2.y;
-      }
-    };
-    auto stats = [&](int p) { return p < parts ? __ldcg(ml + row_of(p)) : make_float2(-INFINITY, 0.f); };
-    float2 x = stats(lane);
-    float w[8][D / 32];
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < parts) row(i, w[i]);
-    float M = x.x, L = 0.f;
-    for (int p = 32 + lane; p < parts; p += 32) M = fmaxf(M, stats(p).x);
-#pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    float acc[D / 32];
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j) acc[j] = 0.f;
-    for (int p0 = 0; p0 < parts; p0 += 8) {
-      if (p0 > 0) {
-        if (p0 % 32 == 0) x = stats(p0 + lane);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (p0 + i < parts) row(p0 + i, w[i]);
-      }
-      const float f = x.x == -INFINITY ? 0.f : ex2((x.x - M) * a.scale_log2);
-      if (p0 % 32 == 0) L += f * x.y;
+    const int prow = tj < nt0 ? r : kChunkRows + (tj - TPT) * G + hq;   // row inside a slot
+    const float *o = part + (ch * 256 + prow) * 4;
+    float M = -INFINITY, L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int p0 = 0; p0 < parts; p0 += 8) {   // eight parts are asked for together
+      float2 x[8];
+      float4 w[8];
+      float Mn = M;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float fi = __shfl_sync(0xffffffffu, f, (p0 + i) & 31);
-        const bool on = p0 + i < parts && fi != 0.f;
+        x[i] = make_float2(-INFINITY, 0.f);
+        if (p0 + i < parts && r < rows) {
+          x[i] = __ldcg(ml + slot_of(p0 + i) * 256 + prow);
+          w[i] = __ldcg(reinterpret_cast<const float4 *>(o + slot_of(p0 + i) * (256 * D)));
+        }
+      }
 #pragma unroll
-        for (int j = 0; j < D / 32; ++j) acc[j] = on ? fmaf(fi, w[i][j], acc[j]) : acc[j];
+      for (int i = 0; i < 8; ++i) Mn = fmaxf(Mn, x[i].x);
+      const float f0 = M == -INFINITY ? 0.f : ex2((M - Mn) * a.scale_log2);
+      M = Mn;
+      L *= f0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] *= f0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (x[i].x == -INFINITY) continue;
+        const float f = ex2((x[i].x - M) * a.scale_log2);
+        L = fmaf(f, x[i].y, L);
+        acc[0] = fmaf(f, w[i].x, acc[0]);
+        acc[1] = fmaf(f, w[i].y, acc[1]);
+        acc[2] = fmaf(f, w[i].z, acc[2]);
+        acc[3] = fmaf(f, w[i].w, acc[3]);
       }
     }
-#pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) L += __shfl_xor_sync(0xffffffffu, L, o);
+    if (r >= rows) continue;
     const float inv = L == 0.f ? 0.f : 1.f / L;
     const size_t orow = ((size_t)(row0 + tj) * c.Hkv + head) * G + hq;
-    uint32_t *dst = reinterpret_cast<uint32_t *>(a.out + orow * D) + lane * (D / 64);
-    dst[0] = pack_bf16(acc[0] * inv, acc[1] * inv);
-    if (D == 128) dst[1] = pack_bf16(acc[D / 32 - 2] * inv, acc[D / 32 - 1] * inv);
-    if (a.lse && lane == 0) a.lse[orow] = L == 0.f ? -INFINITY : fmaf(M, a.scale, logf(L));
+    *reinterpret_cast<uint2 *>(a.out + orow * D + ch * 4) = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv));
+    if (a.lse && ch == 0) a.lse[orow] = L == 0.f ? -INFINITY : fmaf(M, a.scale, logf(L));
   }
 }
 
