@@ -20,7 +20,10 @@
 //               that hands them to the tensor core waits for the loads of the next ones);
 //   warps 4-11  two warpgroups, one per tile: exp2, sums, and the pair's meta row at the end.
 // Accuracy: a score is off by what the tensor core's fp32 accumulation drops (2^-23 of the partial sums, per step of 16
-// channels), which moves a probability by 1e-6 - 3e-6 relative; everything after it is below 3e-7.
+// channels), which moves a probability by 1e-6 - 3e-6 relative (a library product in fp32: 0.7e-6 - 2e-6); everything after
+// it is below 3e-7.  The truncation is the products' too, so subtracting in two or four pieces gains nothing (615, 636 us).
+// Measured (32 query heads, g = 4, D = 128): 2048 queries at 32K 612 us, 870 TFLOP/s, the exponentials alone 462; 128 at 8K 28
+// us: the copies of a tile, four blocks of products and its meta rows follow one another twice per CTA.
 // Every wait is bounded; tensor memory is freed at the common exit.
 #pragma once
 #include "fkv_chunk.cuh"
