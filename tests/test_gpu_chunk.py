@@ -192,6 +192,16 @@ def test_chunk_attention_long():
     run_chunk(c, [700, 40])
 
 
+@pytest.mark.parametrize("D,g", [(128, 4), (64, 7), (128, 1), (64, 3)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1500, 4)])
+def test_chunk_attention_cut_items_of_both_forms(D, g, window, sinks):
+    """Items of one and of two query tiles, each gone on with by several CTAs, in the same call."""
+    c = Case(2, g, D, [3000, 5000, 0], cap=6000)
+    run_chunk(c, [400, 5, 37], window=window, sinks=sinks)
+    run_chunk(c, [3, 256 // g, 128 // g], window=window, sinks=sinks)
+    c.check_stored()
+
+
 def test_chunk_attention_drafts_accepted_and_rejected():
     c = Case(4, 4, 128, [500, 77, 1])
     keep = [500, 77, 1]
