@@ -14,14 +14,14 @@
 // batch looks like (one long sequence, many short ones, drafts of a few tokens over long caches).  An item that a cut
 // goes through leaves partial results (O, m, l) which k_chunk_merge joins.
 //   warp 0      tensor copies (TMA) of the item's query tiles and of K, page by page (one copy = 16 rows x 64 channels; the
-//               page record's swizzle is the shared-memory swizzle), into a ring of key tiles of up to eight pages;
+//               page record's swizzle is the shared-memory swizzle), into a ring of key tiles of five pages (D = 64: six);
 //   warp 1      one lane issues tcgen05.mma S = Q K^T (K-major operands) into tensor memory;
 //   warp 3      ... and O += P V with P read from tensor memory and V as an MN-major operand (channels run along its
 //               rows: no transpose anywhere);
 //   warp 2      walks the items ahead of the others, searches the positions, and copies V (one copy = a page's 16 rows): a
 //               warp issues a copy per 80 - 100 cycles, so one for K and V would not keep up;
 //   warps 4-11  two warpgroups, each with a stream of its own (S and O accumulators): thread = query row; running
-//               maximum, exp2, row sum in fp32, P rounded to bf16 into the columns of S.  O is rescaled only when the
+//               maximum, exp2, row sum in fp32, P rounded to bf16 into columns of its own.  O is rescaled only when the
 //               maximum has grown by more than 2^24: until then P is at most 2^24, which bf16 holds as exactly as 1.
 // Measured (attention and merge, back to back; 32 query heads, g = 4, D = 128): 2048 tokens at 32K 1.04 ms = 1020 TFLOP/s, where
 // the tensor core and the exponentials, 1 : 1 in cycles, hold each other up; 256 tokens at 8K 59.7 us, 34 of them at that rate
