@@ -97,12 +97,19 @@ __device__ __forceinline__ uint64_t umma_desc_k16(uint32_t smem_addr) {
 // Byte offset of row r's first 8 channels in such a tile.
 __device__ __forceinline__ int k16_row(int r) { return (r >> 3) * 256 + (r & 7) * 16; }
 
-// 2^x of two values on the FMA pipe for x <= 0 (below -126 it stays there, about 1e-38): x = n + r with n the nearest integer,
-// found by adding 1.5 * 2^23, and the minimax polynomial of degree 5 for 2^r on [-1/2, 1/2] (relative error, Remez
-// exchange: 7.5e-8, 2.1e-7 as evaluated in fp32).  n goes into the exponent by an integer addition.
+// The larger one, or NaN if one of them is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+// 2^x of two values on the FMA pipe for x <= 0: x = n + r with n the nearest integer, found by adding 1.5 * 2^23, and the
+// minimax polynomial of degree 5 for 2^r on [-1/2, 1/2] (relative error, Remez exchange: 7.5e-8, 2.1e-7 as evaluated in
+// fp32), times 2^n, which is n added to the exponent of 1.  x below -127 counts as -127, whose 2^n is then zero: so a
+// masked score, -infinity, gives exactly 0, and NaN stays NaN (n added to the polynomial's own exponent would lose both).
 __device__ __forceinline__ float2 ex2_fma(float2 x) {
-  x.x = fmaxf(x.x, -126.f);
-  x.y = fmaxf(x.y, -126.f);
+  x.x = max_nan(x.x, -127.f);
+  x.y = max_nan(x.y, -127.f);
   const float2 t = __fadd2_rn(x, make_float2(12582912.f, 12582912.f));
   const float2 r = __ffma2_rn(__fadd2_rn(t, make_float2(-12582912.f, -12582912.f)), make_float2(-1.f, -1.f), x);
   float2 p = __ffma2_rn(make_float2(1.327647245e-3f, 1.327647245e-3f), r, make_float2(9.675540961e-3f, 9.675540961e-3f));
@@ -110,8 +117,8 @@ __device__ __forceinline__ float2 ex2_fma(float2 x) {
   p = __ffma2_rn(p, r, make_float2(2.402212024e-1f, 2.402212024e-1f));
   p = __ffma2_rn(p, r, make_float2(6.931469440e-1f, 6.931469440e-1f));
   p = __ffma2_rn(p, r, make_float2(1.000000119f, 1.000000119f));
-  return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)),
-                     __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
+  return __fmul2_rn(p, make_float2(__int_as_float((__float_as_int(t.x) << 23) + 0x3f800000),
+                                   __int_as_float((__float_as_int(t.y) << 23) + 0x3f800000)));
 }
 // The columns outside [lo, hi) of the 32 from c0 become -infinity, in tensor memory (for the few blocks at an edge).
 __device__ __forceinline__ void cf_mask(uint32_t ta, int c0, int lo, int hi) {
@@ -475,7 +482,7 @@ __global__ void __launch_bounds__(kCfThreads, 1) k_chunk_features(Ctx c, const _
       const int slot = x.pg0 * kPage + t * 128 + R;
       const bool live = slot < x.n;
       float *frow = nullptr;
-      int jlo = INT_MAX, jhi = 0;   // the tokens that see this pair
+      int jlo = x.T, jhi = 0;   // the tokens that see this pair (none, for a slot past the end)
       if (live) {
         const int *ptrow = c.pt + (size_t)x.seg * c.max_pages;
         frow = meta_row(c, c.pool + (size_t)__ldcg(ptrow + slot / kPage) * c.page_bytes, slot % kPage);
