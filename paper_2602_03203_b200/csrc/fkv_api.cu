@@ -580,16 +580,13 @@ int check_append_chunk(const fkv_cache *c, int layer, const void *k, const void 
 int launch_append_chunk(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos, const int32_t *keep_lens,
                         const int32_t *chunk_lens, const ChunkLens &lens, cudaStream_t st) {
   const int batch = c->cfg.max_batch;
+  // (A roll-back to the lengths that the host knows is launched all the same: replayed, it meets others.)
+  if (lens.tok[batch] == 0 && !keep_lens) return FKV_OK;
   ChunkKeep keep = {};
-  bool any = lens.tok[batch] > 0;
   if (keep_lens) {
     keep.use = 1;
-    for (int s = 0; s < batch; ++s) {
-      keep.keep[s] = keep_lens[s];
-      any = any || keep_lens[s] != c->h_len[(size_t)layer * batch + s];
-    }
+    for (int s = 0; s < batch; ++s) keep.keep[s] = keep_lens[s];
   }
-  if (!any) return FKV_OK;
   // A warp per pair, up to four CTAs of eight warps on every SM: more pairs than that go round.
   const long long tasks = (long long)lens.tok[batch] * c->cfg.num_kv_heads;
   const int grid = (int)std::max<long long>(1, std::min<long long>((tasks + 7) / 8, 4LL * c->sm_count));
