@@ -300,8 +300,9 @@ int fkv_append_decode_attn_window(fkv_cache *c, int layer, const void *k, const 
  * chunk_lens all 0 the call only rolls back, and k, v may be NULL), or NULL: all.  pos: dev [tokens] int32, or NULL: the
  * positions after the last pair that stays (from 0 for an empty segment).  The feature rows of the new pairs are zero.
  * Decode queries on record (feature_window) whose tokens are dropped leave the record; a record that has wrapped starts
- * over then.  FKV_ERR_CAPACITY if a sequence would exceed max_tokens_per_head.  If the pool runs out of pages nothing is
- * stored (FKV_DEV_POOL_EXHAUSTED).
+ * over then.  FKV_ERR_CAPACITY if a sequence would exceed max_tokens_per_head.  Pages that the call returns serve the growth
+ * of its other sequences; if these and the free ones are too few, the whole call, roll-backs included, does nothing
+ * (FKV_DEV_POOL_EXHAUSTED; what fkv_append_chunk_attn writes to out and lse_out is then of no meaning).
  *
  * fkv_chunk_attn: attention of a chunk's queries, the chunk's pairs being the last chunk_lens[s] pairs of their segments:
  *     out[j] = sum_i softmax_i(scale <q_j, k_i>) v_i,   lse_out[j] = ln sum_i exp(scale <q_j, k_i>),

@@ -59,10 +59,11 @@ struct ChunkKeep {
 
 // ---------------------------------------------------------------- storing the chunk
 // Every CTA works the page arithmetic out for itself (one thread per sequence, two prefix sums): pages to take from the
-// free stack where a sequence grows past its last page, pages to return where it shrinks.  A warp stores one pair.  The
-// last CTA to finish returns pages, moves the stack top and the lengths and takes rolled-back queries off the record.
-// A sequence that the device finds past its capacity or shorter than `keep` is skipped; without enough free pages the
-// whole call is.
+// free stack where a sequence grows past its last page, pages to return where it shrinks.  Growth that the stack does not
+// cover is served from the returned pages, in their order: nothing reads their pairs any more.  A warp stores one pair.  The
+// last CTA to finish returns what is left, moves the stack top and the lengths and takes rolled-back queries off the record.
+// A sequence that the device finds past its capacity or shorter than `keep` is skipped; without enough pages, free and
+// returned together, the whole call is.
 // Bound: bytes (8 D a pair, read and written); 6.8 us for 5 tokens, 7.2 us for 256 (a launch and four dependent reads: length,
 // page, last position, free stack).
 __global__ void __launch_bounds__(256) k_append_chunk(Ctx c, int layer, const uint8_t *k, const uint8_t *v, const int32_t *pos,
@@ -96,12 +97,19 @@ __global__ void __launch_bounds__(256) k_append_chunk(Ctx c, int layer, const ui
   const int pop_off = block_excl_scan(pop, s_scan, pops);
   const int push_off = block_excl_scan(push, s_scan, pushes);
   if (s < c.batch) { s_pop[s] = pop_off; s_push[s] = push_off; }
-  const bool exhausted = pops > top;
+  const bool exhausted = pops > top + pushes;
   if (blockIdx.x == 0) {
     if (bad) set_status(c, (unsigned)bad);
     if (exhausted && tid == 0) set_status(c, kDevPoolExhausted);
   }
   __syncthreads();
+  // Pages that sequence q returns: of every head the same number, behind the pages that hold what stays.
+  auto pages_kept = [&](int q) { return (s_keep[q] + lens.tok[q + 1] - lens.tok[q] + kPage - 1) / kPage; };
+  auto pages_old = [&](int q) { return (s_old[q] + kPage - 1) / kPage; };
+  auto returned = [&](int q, int i) {   // the i-th of them
+    const int kept = pages_kept(q), cnt = pages_old(q) - kept, h = i / cnt;
+    return __ldcg(c.pt + (size_t)seg_of(c, layer, q, h) * c.max_pages + kept + i - h * cnt);
+  };
   if (!exhausted) {
     const int tasks = lens.tok[c.batch] * c.Hkv;   // (at most 2^24 x 32)
     for (int t = blockIdx.x * 8 + warp; t < tasks; t += gridDim.x * 8) {
@@ -121,7 +129,17 @@ __global__ void __launch_bounds__(256) k_append_chunk(Ctx c, int layer, const ui
       if (pg < np_old) {
         pid = __ldcg(ptrow + pg);
       } else {
-        pid = __ldcg(c.free_stack + top - 1 - (s_pop[lo] + h * grow + pg - np_old));
+        const int x = s_pop[lo] + h * grow + pg - np_old;   // the x-th page that the call takes
+        if (x < top) {
+          pid = __ldcg(c.free_stack + top - 1 - x);
+        } else {
+          int q = 0, end = c.batch;   // the sequence that returns page x - top: the last one whose pages begin at or before it
+          while (end - q > 1) {
+            const int mid = (q + end) >> 1;
+            if (s_push[mid] <= x - top) q = mid; else end = mid;
+          }
+          pid = returned(q, x - top - s_push[q]);
+        }
         if (lane == 0 && (slot % kPage == 0 || j == 0)) ptrow[pg] = pid;
       }
       int32_t pdef = j;
@@ -142,14 +160,14 @@ __global__ void __launch_bounds__(256) k_append_chunk(Ctx c, int layer, const ui
   __threadfence();
   if (tid == 0) c.ctrl[CTRL_CHUNK_TICKET] = 0;
   if (exhausted) return;
-  // Freed pages go where the taken ones came from and above (every CTA has read those entries by now).
+  // Returned pages go where the taken ones came from and above (every CTA has read those entries by now); the ones that
+  // would go below the stack are those that were taken again.
   for (int q = 0; q < c.batch; ++q) {
     if (s_keep[q] < 0) continue;
-    const int np_new = (s_keep[q] + lens.tok[q + 1] - lens.tok[q] + kPage - 1) / kPage;
-    const int cnt = (s_old[q] + kPage - 1) / kPage - np_new;
-    for (int i = tid; i < cnt * c.Hkv; i += blockDim.x) {
-      const int h = i / cnt, p = i - h * cnt;
-      c.free_stack[top - pops + s_push[q] + i] = __ldcg(c.pt + (size_t)seg_of(c, layer, q, h) * c.max_pages + np_new + p);
+    const int cnt = (pages_old(q) - pages_kept(q)) * c.Hkv;
+    for (int i = tid; i < cnt; i += blockDim.x) {
+      const int at = top - pops + s_push[q] + i;
+      if (at >= 0) c.free_stack[at] = returned(q, i);
     }
   }
   if (tid == 0) c.ctrl[CTRL_FREE_TOP] = top - pops + pushes;

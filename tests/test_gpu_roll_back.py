@@ -1,7 +1,9 @@
-"""Roll-backs of chunks in captured graphs."""
+"""Roll-backs of chunks: in captured graphs, and in a pool without free pages."""
 import pytest
 import torch
 
+import chunk_ref as ref
+from paper_2602_03203_b200 import binding
 from test_gpu_chunk import Case
 
 pytestmark = pytest.mark.gpu
@@ -26,3 +28,45 @@ def test_a_captured_roll_back_to_the_length_at_capture_rolls_every_replay_back()
     c.extend(k, v, lens)
     c.check_stored()
     assert c.cache.device_status() == (0, total - used_pages(c))
+
+
+@pytest.mark.parametrize("spare", [0, 2, 3])
+def test_pages_that_a_call_returns_serve_its_own_growth(spare):
+    # Two sequences shrink and two grow in one call; the pool has `spare` free pages, fewer than the growth takes.
+    Hkv = 2
+    c = Case(Hkv, 4, 64, [48, 17, 40, 16], cap=160, num_pages=(3 + 2 + 3 + 1) * Hkv + spare)
+    assert c.cache.device_status() == (0, spare)
+    keep, lens = [10, 17, 2, 16], [0, 32, 5, 30]      # pages a head: 3 -> 1, 2 -> 4, 3 -> 1, 1 -> 3
+    k, v, q = c.chunk(lens)
+    lse = torch.empty(q.shape[:2], device="cuda")
+    out = c.cache.append_chunk_attn(0, k, v, q, lens, keep_lens=keep, lse=lse)
+    c.extend(k, v, lens, keep=keep)
+    assert c.cache.device_status() == (0, spare)
+    c.check_stored()
+    c.check_chunk(out, lse, q, lens)
+    # A net demand of exactly what is free, then of more: refused as a whole, nothing lost.
+    keep, lens = [10, 49, 7, 46], [32 if spare else 0, 0, 0, 0]
+    if spare == 2:
+        lens[0] = 22
+        k, v, q = c.chunk(lens)
+        c.cache.append_chunk(0, k, v, lens, keep_lens=keep)
+        c.extend(k, v, lens, keep=keep)
+        assert c.cache.device_status() == (0, 0)
+    free = c.cache.device_status()[1]
+    keep = [len(c.seqs[0]), 48, 7, 46]                 # a page a head comes back ...
+    lens = [0, 0, 0, 16 * (free // Hkv) + 35]          # ... and one more than it and the free ones is wanted
+    k, v, q = c.chunk(lens)
+    c.cache.append_chunk(0, k, v, lens, keep_lens=keep)
+    assert c.cache.device_status() == (binding.DEV_POOL_EXHAUSTED, free)
+    c.cache.sync_lengths()
+    c.check_stored()
+    c.cache.append_chunk(0, None, None, [0] * 4, keep_lens=[0] * 4)
+    assert c.cache.device_status() == (0, (3 + 2 + 3 + 1) * Hkv + spare)
+    # No page is on the stack twice: the whole pool is taken again and holds what was stored.
+    c.seqs = [ref.Seq(Hkv, 64, 24) for _ in range(4)]
+    lens = [16 * ((9 * Hkv + spare) // Hkv // 4)] * 4
+    k, v, q = c.chunk(lens)
+    c.cache.append_chunk(0, k, v, lens)
+    c.extend(k, v, lens)
+    c.check_stored()
+    assert c.status() == 0
