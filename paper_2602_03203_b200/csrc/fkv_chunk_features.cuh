@@ -329,7 +329,7 @@ __global__ void __launch_bounds__(kCfThreads, 1) k_chunk_features(Ctx c, const _
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int t = T - kCfQueries * (am + 1) + lane * 4 + i;   // (negative in the oldest block)
-          l[i] = t >= 0 && aj < j0 + nj ? __ldg(lse + (size_t)t * Hq + aj) : 0.f;
+          l[i] = t >= 0 && aj < j0 + nj ? __ldcg(lse + (size_t)t * Hq + aj) : 0.f;   // (the launch before may still have been writing them as this one began: not the read-only path)
         }
         if (++am == m0 + blocks) { am = m0; ++aj; }
       };
