@@ -493,6 +493,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
           chunk_weights<TP>(v, a.scale_log2, m == -INFINITY ? 0.f : m * a.scale_log2, tp, wait_products, lt, mx);
           const bool grow = mx > m && (mx - m) * a.scale_log2 > kChunkGrow;
           if (__any_sync(0xffffffffu, grow)) {
+            tmem_st_wait();   // stores to tensor memory are asynchronous: P's first values land before its second ones set out
             const float f = grow ? ex2((m - mx) * a.scale_log2) : 1.f;
             if (grow) m = mx;
             l *= f;
