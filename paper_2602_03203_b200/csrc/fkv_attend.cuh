@@ -429,6 +429,10 @@ __global__ void __launch_bounds__((NCW + 1) * 32, NCW <= 4 ? 3 : 1) k_attend(Ctx
     }
     // The new pair, one 16-byte chunk per lane (K chunks, then V chunks), for the warp that gets its page.
     const bool mine_new = tail && (npg - 1) % NCW == warp;
+    // The page that this warp completes before it is read: the one the new pair goes to; without a window also the last one
+    // if it is not full.  Pairs that a query does not see get p = 0, but zero times an infinity is not zero: their V rows are
+    // cleared.  (Looked at once, ahead of the loop: the same comparison page by page costs 0.5 % of a large batch's step.)
+    const int last_i = (npg - 1) % NCW == warp && (tail || (!WIN && pg1 == npages && n % kPage != 0)) ? npg - 1 : -1;
     uint4 newrow = make_uint4(0u, 0u, 0u, 0u);
     if (mine_new && lane < 2 * NCH) {
       const size_t row = (size_t)seq * c.Hkv + head;
@@ -443,24 +447,31 @@ __global__ void __launch_bounds__((NCW + 1) * 32, NCW <= 4 ? 3 : 1) k_attend(Ctx
       const int slot_i = i % SLOTS;
       if (!mbar_wait(smem_u32(&bars[slot_i]), (i / SLOTS) & 1)) { set_status(c, kDevWaitTimeout); break; }
       uint8_t *page = smem + (size_t)slot_i * PAGE_KV;
-      if (mine_new && i == npg - 1) {
-        if (fresh) {   // no copy was issued for a brand-new page: its other rows must still be finite
-          for (int j = lane; j < PAGE_KV / 16; j += 32) reinterpret_cast<uint4 *>(page)[j] = make_uint4(0u, 0u, 0u, 0u);
-          __syncwarp();
-        }
-        if (lane < 2 * NCH)
-          *reinterpret_cast<uint4 *>(page + (lane < NCH ? 0 : 2 * D) + kv_chunk_off(n_old % kPage, lane % NCH, D)) =
-              newrow;
-        __syncwarp();
-      }
       const int slot0 = page_of(pg0 + i) * kPage;
       auto seen = [&](int slot) { return WIN ? slot < wa || (slot >= wb && slot < we) : slot < n; };
+      if (i == last_i) {
+        if (mine_new) {
+          if (fresh) {   // no copy was issued for a brand-new page: what shared memory held there is not read
+            for (int j = lane; j < PAGE_KV / 16; j += 32) reinterpret_cast<uint4 *>(page)[j] = make_uint4(0u, 0u, 0u, 0u);
+            __syncwarp();
+          }
+          if (lane < 2 * NCH)
+            *reinterpret_cast<uint4 *>(page + (lane < NCH ? 0 : 2 * D) + kv_chunk_off(n_old % kPage, lane % NCH, D)) =
+                newrow;
+        }
+        if (!WIN) {   // what the page holds behind the last pair (of an earlier owner, or of drafts that were rejected)
+#pragma unroll 1
+          for (int j = (n - slot0) * NCH + lane; j < kPage * NCH; j += 32)
+            *reinterpret_cast<uint4 *>(page + 2 * D + kv_chunk_off(j / NCH, j % NCH, D)) = make_uint4(0u, 0u, 0u, 0u);
+          fence_proxy_async();   // (the next copy into this slot comes after these writes)
+        }
+        __syncwarp();
+      }
       if (WIN && !__all_sync(0xffffffffu, seen(slot0 + (lane & 15)))) {
-        // Hidden rows get p = 0, but zero times an infinity is not zero: their V rows are cleared.
         for (int j = lane; j < kPage * NCH; j += 32)
           if (!seen(slot0 + j / NCH))
             *reinterpret_cast<uint4 *>(page + 2 * D + kv_chunk_off(j / NCH, j % NCH, D)) = make_uint4(0u, 0u, 0u, 0u);
-        fence_proxy_async();   // (the next copy into this slot comes after these writes)
+        fence_proxy_async();
         __syncwarp();
       }
       const uint32_t kbase = smem_u32(page), vbase = kbase + 2 * D;

@@ -1,4 +1,6 @@
-"""Roll-backs of chunks: in captured graphs, and in a pool without free pages."""
+"""Roll-backs of chunks: in captured graphs, in a pool without free pages, and what rejected drafts leave behind."""
+import math
+
 import pytest
 import torch
 
@@ -70,3 +72,52 @@ def test_pages_that_a_call_returns_serve_its_own_growth(spare):
     c.extend(k, v, lens)
     c.check_stored()
     assert c.status() == 0
+
+
+@pytest.mark.parametrize("D,g,n", [(128, 4, 35), (64, 2, 3000), (128, 7, 1), (64, 8, 16)])
+def test_infinities_of_rejected_drafts_do_not_reach_decode_steps(D, g, n):
+    # A decode step reads the last page whole: rows behind the last pair hold what was rolled back.
+    c = Case(2, g, D, [n, n + 9], cap=n + 60)
+    bad = c.rand(12, 2)
+    bad[::2], bad[1::2] = math.inf, math.nan
+    c.cache.append_chunk(0, bad, bad, [6, 6])
+    c.cache.append_chunk(0, None, None, [0, 0], keep_lens=[n, n + 9])
+
+    def check(out, q):
+        for s, seq in enumerate(c.seqs):
+            m = len(seq)
+            ok = torch.ones((1, m), dtype=torch.bool, device="cuda")
+            for hq in range(2 * g):
+                o, _, _, tol, _ = ref.attend(q[s:s + 1, hq], seq.k[hq // g], seq.v[hq // g], ok, D ** -0.5)
+                d = (out[s:s + 1, hq].double() - o).abs()
+                assert bool((d <= tol).all()), (s, hq, float(d.max()))
+
+    q = c.rand(2, 2 * g)
+    check(c.cache.decode_attn(0, q), q)
+    for _ in range(2):
+        k, v, q = c.rand(2, 2), c.rand(2, 2), c.rand(2, 2 * g)
+        out = c.cache.append_decode_attn(0, k, v, q)
+        c.extend(k, v, [1, 1])
+        check(out, q)
+    k, v, q = c.rand(2, 2), c.rand(2, 2), c.rand(2, 2 * g)
+    out = c.cache.decode_step(k[None], v[None], q[None])[0]
+    c.extend(k, v, [1, 1])
+    check(out, q)
+    c.check_stored()
+    assert c.status() == 0
+
+
+def test_infinities_in_a_page_of_another_sequence_do_not_reach_decode_steps():
+    # The same with a page that another sequence held before.
+    c = Case(1, 4, 128, [0, 0], num_pages=4, cap=64)
+    bad = torch.full((60, 1, 128), math.inf, dtype=torch.bfloat16, device="cuda")
+    c.cache.append_chunk(0, bad, bad, [60, 0])
+    c.cache.append_chunk(0, None, None, [0, 0], keep_lens=[0, 0])
+    k, v = c.rand(21, 1), c.rand(21, 1)
+    c.cache.prefill(0, 1, k.transpose(0, 1).contiguous(), v.transpose(0, 1).contiguous())
+    q = c.rand(2, 4)
+    out = c.cache.decode_attn(0, q)
+    assert bool((out[0] == 0).all())
+    for h in range(4):
+        o, _, _, tol, _ = ref.attend(q[1:2, h], k[:, 0], v[:, 0], torch.ones((1, 21), dtype=torch.bool, device="cuda"), 128 ** -0.5)
+        assert bool(((out[1:2, h].double() - o).abs() <= tol).all())
