@@ -334,8 +334,11 @@ int fkv_append_chunk_attn(fkv_cache *c, int layer, const void *k, const void *v,
  * P_ji = exp(scale <q_j, k_i> - lse_j) for the pairs that query j sees and 0 for the others, the features of EVERY pair of
  * the sequences with tokens become, per query head, the means of P over the chunk's last 8 / 16 / 32 queries (fewer queries
  * still divide by 8 / 16 / 32) and over the whole chunk, previous sum + the latter, 0.9 * previous decayed sum + the latter:
- * one chunk of the recurrence described at fkv_update_features.  Needs no feature_window; decode queries on record are
- * neither used nor dropped.  Errors as fkv_chunk_attn.
+ * one chunk of the recurrence described at fkv_update_features.  A chunk counts as one whatever its length: the sums
+ * grow by its MEAN, so a prompt in two chunks adds two means, and a chunk of a few drafts weighs as much as one of
+ * thousands of tokens.  Needs no feature_window.  Decode queries that are on record (feature_window) for a sequence with
+ * tokens came before the chunk: they are a chunk of their own, applied first, as fkv_update_features would, and leave the
+ * record.  Errors as fkv_chunk_attn.
  */
 int fkv_chunk_features(fkv_cache *c, int layer, const void *q, const float *lse, const int32_t *chunk_lens, int32_t window,
                        int32_t sinks, float scale, void *stream);

@@ -945,7 +945,7 @@ static int evict_impl(fkv_cache *c, int layer, const float *noise, int noise_str
   cudaStream_t st = (cudaStream_t)stream;
   const bool tm = c->timing;
   if (tm) FKV_CUDA(cudaEventRecord(c->ev[0], st));
-  k_plan<<<1, 1024, 0, st>>>(c->ctx, l0, l1, PLAN_EVICT, kScorePPS * kPage, nullptr);
+  k_plan<<<1, 1024, 0, st>>>(c->ctx, l0, l1, PLAN_EVICT, kScorePPS * kPage, nullptr, SeqMask{});
   FKV_LAUNCHED(c);
   if (tm) FKV_CUDA(cudaEventRecord(c->ev[6], st));
   if (c->cfg.feature_window > 0 && c->feature_scale > 0.f) {   // refresh a_n from the chunk's recorded queries first
@@ -1014,7 +1014,7 @@ int fkv_score_rkv(fkv_cache *c, int layer, float lambda_attn, float lambda_sim, 
   }
   if (tiles == 0) return FKV_OK;
   cudaStream_t st = (cudaStream_t)stream;
-  k_plan<<<1, 1024, 0, st>>>(c->ctx, layer, layer + 1, PLAN_SCORE_ALL, kScorePPS * kPage, nullptr);
+  k_plan<<<1, 1024, 0, st>>>(c->ctx, layer, layer + 1, PLAN_SCORE_ALL, kScorePPS * kPage, nullptr, SeqMask{});
   FKV_LAUNCHED(c);
   return launch_rkv(c, scores_out, layer * batch * Hkv, max_old, batch * Hkv, tiles, lambda_attn, lambda_sim, st);
 }
@@ -1094,7 +1094,24 @@ int fkv_chunk_features(fkv_cache *c, int layer, const void *q, const float *lse,
   if (int e = check_chunk(c, layer, q, chunk_lens, window, sinks, scale, lens)) return e;
   if (lens.tok[c->cfg.max_batch] > 0 && (!lse || !aligned(lse, 4))) return FKV_ERR_INVALID_ARG;
   if (!chunk_is_stored(c, layer, chunk_lens)) return FKV_ERR_INVALID_ARG;
-  return launch_chunk_features(c, layer, q, lse, chunk_lens, lens, window, sinks, scale, (cudaStream_t)stream);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (lens.tok[c->cfg.max_batch] > 0 && c->cfg.feature_window > 0 && c->feature_scale > 0.f) {
+    // Decode queries on record came before the chunk: they move the features on first, and the chunk's kernel then takes
+    // them off the record.
+    if (int e = ensure_page_rows_map(c)) return e;   // (what can fail does so before anything is changed)
+    SeqMask seqs = {};
+    seqs.use = 1;
+    int max_old = 0;
+    for (int s = 0; s < c->cfg.max_batch; ++s)
+      if (chunk_lens[s] > 0) {
+        seqs.w[s / 64] |= 1ull << (s % 64);
+        max_old = std::max(max_old, c->h_len[(size_t)layer * c->cfg.max_batch + s]);
+      }
+    k_plan<<<1, 1024, 0, st>>>(c->ctx, layer, layer + 1, PLAN_RECORD, kScorePPS * kPage, nullptr, seqs);
+    FKV_LAUNCHED(c);
+    if (int e = launch_features(c, max_old, c->cfg.max_batch * c->cfg.num_kv_heads, st)) return e;
+  }
+  return launch_chunk_features(c, layer, q, lse, chunk_lens, lens, window, sinks, scale, st);
 }
 
 int fkv_decode_attn_window(fkv_cache *c, int layer, const void *q, const int32_t *q_pos, int32_t window, int32_t sinks, void *out,
@@ -1139,7 +1156,7 @@ int fkv_update_features(fkv_cache *c, int layer, void *stream) {
   for (int s = 0; s < batch; ++s) max_old = std::max(max_old, c->h_len[(size_t)layer * batch + s]);
   if (max_old == 0) return FKV_OK;
   cudaStream_t st = (cudaStream_t)stream;
-  k_plan<<<1, 1024, 0, st>>>(c->ctx, layer, layer + 1, PLAN_SCORE_ALL, kScorePPS * kPage, nullptr);
+  k_plan<<<1, 1024, 0, st>>>(c->ctx, layer, layer + 1, PLAN_SCORE_ALL, kScorePPS * kPage, nullptr, SeqMask{});
   FKV_LAUNCHED(c);
   return launch_features(c, max_old, batch * Hkv, st);
 }
@@ -1160,7 +1177,7 @@ int fkv_score(fkv_cache *c, int layer, float *scores_out, void *stream) {
     tiles += (long long)Hkv * ((c->h_len[(size_t)layer * batch + s] + kScorePPS * kPage - 1) / (kScorePPS * kPage));
   if (tiles == 0) return FKV_OK;
   cudaStream_t st = (cudaStream_t)stream;
-  k_plan<<<1, 1024, 0, st>>>(c->ctx, layer, layer + 1, PLAN_SCORE_ALL, kScorePPS * kPage, nullptr);
+  k_plan<<<1, 1024, 0, st>>>(c->ctx, layer, layer + 1, PLAN_SCORE_ALL, kScorePPS * kPage, nullptr, SeqMask{});
   FKV_LAUNCHED(c);
   return launch_score_any(c, scores_out, layer * batch * Hkv, (int)tiles, st);
 }
@@ -1175,7 +1192,7 @@ static int select_impl(fkv_cache *c, int layer, const float *scores_in, const fl
         return FKV_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)stream;
   FKV_CUDA(cudaMemsetAsync(kept_count_out, 0, (size_t)batch * Hkv * 4, st));
-  k_plan<<<1, 1024, 0, st>>>(c->ctx, layer, layer + 1, PLAN_SELECT, kScorePPS * kPage, nullptr);
+  k_plan<<<1, 1024, 0, st>>>(c->ctx, layer, layer + 1, PLAN_SELECT, kScorePPS * kPage, nullptr, SeqMask{});
   FKV_LAUNCHED(c);
   int max_old = 0;
   for (int s = 0; s < batch; ++s) max_old = std::max(max_old, c->h_len[(size_t)layer * batch + s]);
@@ -1211,7 +1228,7 @@ int fkv_compact(fkv_cache *c, int layer, const int32_t *idx, const int32_t *kept
   for (int s = 0; s < batch; ++s) maxn = std::max(maxn, c->h_len[(size_t)layer * batch + s]);
   if (maxn == 0) return FKV_OK;
   cudaStream_t st = (cudaStream_t)stream;
-  k_plan<<<1, 1024, 0, st>>>(c->ctx, layer, layer + 1, PLAN_COMPACT, kScorePPS * kPage, kept_count);
+  k_plan<<<1, 1024, 0, st>>>(c->ctx, layer, layer + 1, PLAN_COMPACT, kScorePPS * kPage, kept_count, SeqMask{});
   FKV_LAUNCHED(c);
   k_fill_pt_new<<<batch * Hkv, 256, 0, st>>>(c->ctx, layer * batch * Hkv, batch * Hkv);
   FKV_LAUNCHED(c);

@@ -147,10 +147,11 @@ __global__ void k_append(Ctx c, int layer, const uint8_t *k, const uint8_t *v, c
 // compacts - one batch of fresh pages per segment, reserved at the top of the
 // free stack (offset pad0 of its plan entry).  Everything later kernels need comes from
 // here, so the host never reads a length back.
-enum { PLAN_EVICT = 0, PLAN_SCORE_ALL = 1, PLAN_SELECT = 2, PLAN_COMPACT = 3 };
+// PLAN_RECORD: the segments of the sequences in `seqs` that have decode queries on record.
+enum { PLAN_EVICT = 0, PLAN_SCORE_ALL = 1, PLAN_SELECT = 2, PLAN_COMPACT = 3, PLAN_RECORD = 4 };
 
 __global__ void __launch_bounds__(1024) k_plan(Ctx c, int l0, int l1, int mode, int tile_pairs,
-                                                const int32_t *kept_count /* PLAN_COMPACT: [batch][Hkv] */) {
+                                                const int32_t *kept_count /* PLAN_COMPACT: [batch][Hkv] */, SeqMask seqs) {
   __shared__ int s_scan[33];
   __shared__ int s_fail;
   const int seg0 = l0 * c.batch * c.Hkv, nseg = (l1 - l0) * c.batch * c.Hkv;
@@ -171,6 +172,7 @@ __global__ void __launch_bounds__(1024) k_plan(Ctx c, int l0, int l1, int mode, 
       k = n_new - r;
       active = (mode == PLAN_EVICT || mode == PLAN_COMPACT) && n_new < n;
       is_work = (mode == PLAN_EVICT || mode == PLAN_COMPACT) ? active : n > 0;
+      if (mode == PLAN_RECORD) is_work = is_work && seqs.has(seq) && c.hist_cnt[ls] > 0;
       tiles = is_work ? (n + tile_pairs - 1) / tile_pairs : 0;
     }
     const int new_pages = active ? (n_new + kPage - 1) / kPage : 0;

@@ -196,7 +196,10 @@ __global__ void __launch_bounds__(kCfThreads, 1) k_chunk_features(Ctx c, const _
     for (int s = lane; s < batch; s += 32) {
       const int n = __ldcg(c.len + a.layer * batch + s);
       Len[s] = n;
-      if (blockIdx.x == 0 && n < a.lens.tok[s + 1] - a.lens.tok[s]) set_status(c, kDevBadIndex);
+      const int T = a.lens.tok[s + 1] - a.lens.tok[s];
+      if (blockIdx.x == 0 && n < T) set_status(c, kDevBadIndex);
+      // The record of decode queries has been used by the launch before (fkv_chunk_features) and starts over.
+      if (blockIdx.x == 0 && T > 0 && c.hist_w) c.hist_cnt[a.layer * batch + s] = 0;
     }
     __syncwarp();
     int NB = 0;   // pairs of tiles of the sequences that take part
