@@ -7,6 +7,7 @@ library has not been built, or no CUDA device is present, calls raise.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from typing import Optional
 
@@ -103,12 +104,21 @@ def _mask(seq_mask, max_batch):
     return arr, ctypes.cast(arr, ctypes.c_void_p)
 
 
+def _check_i32(**ints):
+    """Integers that the library takes as int32_t: ctypes would cut larger ones off without a word."""
+    for name, x in ints.items():
+        if not -2 ** 31 <= operator.index(x) < 2 ** 31:
+            raise ValueError(f"{name}: {x} does not fit 32 bits")
+
+
 def _lens(x, max_batch, what):
     """A list of max_batch integers as the host array the library reads (NULL for None)."""
     if x is None:
         return None
     if len(x) != max_batch:
         raise ValueError(f"{what}: expected {max_batch} entries, one per sequence, got {len(x)}")
+    _check_i32(**{what: min(x)})
+    _check_i32(**{what: max(x)})
     return (ctypes.c_int32 * max_batch)(*x)
 
 
@@ -284,6 +294,7 @@ class Cache:
     def decode_attn_window(self, layer, q, window, sinks=0, q_pos=None, out=None, scale=0.0):
         """decode_attn over the last `window` positions up to the query's and the positions below `sinks`.
         q_pos [batch] int32: positions of the queries (None: the last pair's)."""
+        _check_i32(layer=layer, window=window, sinks=sinks)
         if out is None:
             out = torch.empty_like(q)
         self._check_step(None, None, q, out, q_pos)
@@ -293,6 +304,7 @@ class Cache:
 
     def append_decode_attn_window(self, layer, k, v, q, window, sinks=0, out=None, pos=None, seq_mask=0, scale=0.0):
         """append(k, v) then decode_attn_window(q) on one layer, as one launch."""
+        _check_i32(layer=layer, window=window, sinks=sinks)
         if out is None:
             out = torch.empty_like(q)
         self._check_step(k, v, q, out, pos)
@@ -315,6 +327,7 @@ class Cache:
 
     def append_chunk(self, layer, k, v, chunk_lens, pos=None, keep_lens=None):
         """Store chunk_lens[s] new pairs behind the first keep_lens[s] pairs of every sequence (None: behind all)."""
+        _check_i32(layer=layer)
         self._check_chunk(chunk_lens, k=k, v=v, pos=pos)
         lens, keep = _lens(chunk_lens, self.cfg.max_batch, "chunk_lens"), _lens(keep_lens, self.cfg.max_batch, "keep_lens")
         _check(lib().fkv_append_chunk(self._h, layer, _ptr(k, torch.bfloat16), _ptr(v, torch.bfloat16), _ptr(pos, torch.int32),
@@ -323,6 +336,7 @@ class Cache:
     def chunk_attn(self, layer, q, chunk_lens, window=0, sinks=0, out=None, lse=None, scale=0.0):
         """Attention of the queries q [tokens][Hq][D] of the last chunk_lens[s] pairs of every sequence, each over the pairs
         up to its own; lse [tokens][Hq] fp32, if given, gets the log-sum-exp of the scores."""
+        _check_i32(layer=layer, window=window, sinks=sinks)
         if out is None:
             out = torch.empty_like(q)
         self._check_chunk(chunk_lens, q=q, out=out, lse=lse)
@@ -334,6 +348,7 @@ class Cache:
     def append_chunk_attn(self, layer, k, v, q, chunk_lens, pos=None, keep_lens=None, window=0, sinks=0, out=None, lse=None,
                           scale=0.0):
         """append_chunk(k, v) then chunk_attn(q) in one call."""
+        _check_i32(layer=layer, window=window, sinks=sinks)
         if out is None:
             out = torch.empty_like(q)
         self._check_chunk(chunk_lens, k=k, v=v, q=q, out=out, lse=lse, pos=pos)
@@ -346,6 +361,7 @@ class Cache:
 
     def chunk_features(self, layer, q, lse, chunk_lens, window=0, sinks=0, scale=0.0):
         """Features of all pairs from the queries of a chunk and the log-sum-exp that chunk_attn gave for them."""
+        _check_i32(layer=layer, window=window, sinks=sinks)
         self._check_chunk(chunk_lens, q=q, lse=lse)
         _check(lib().fkv_chunk_features(self._h, layer, _ptr(q, torch.bfloat16), _ptr(lse, torch.float32),
                                         _lens(chunk_lens, self.cfg.max_batch, "chunk_lens"), window, sinks, scale, _stream()),
@@ -353,6 +369,7 @@ class Cache:
 
     def export_features(self, layer, seq, out=None):
         """The features of one (layer, sequence): [Hkv][n][6 g] fp32."""
+        _check_i32(layer=layer, seq=seq)
         shape = (self.cfg.num_kv_heads, self.lengths(layer)[seq], self.feat_dim)
         if out is None:
             out = torch.empty(shape, dtype=torch.float32, device="cuda")
