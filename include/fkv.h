@@ -338,7 +338,8 @@ int fkv_append_chunk_attn(fkv_cache *c, int layer, const void *k, const void *v,
  * grow by its MEAN, so a prompt in two chunks adds two means, and a chunk of a few drafts weighs as much as one of
  * thousands of tokens.  Needs no feature_window.  Decode queries that are on record (feature_window) for a sequence with
  * tokens came before the chunk: they are a chunk of their own, applied first, as fkv_update_features would, and leave the
- * record.  Errors as fkv_chunk_attn.
+ * record.  (A captured call takes the scale of the decode calls made before it was captured, and one captured before the first
+ * of them leaves the record as it is.)  Errors as fkv_chunk_attn.
  */
 int fkv_chunk_features(fkv_cache *c, int layer, const void *q, const float *lse, const int32_t *chunk_lens, int32_t window,
                        int32_t sinks, float scale, void *stream);

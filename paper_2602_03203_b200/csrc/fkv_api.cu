@@ -682,11 +682,12 @@ int launch_chunk_features_t(fkv_cache *c, const CUtensorMap &tmq, ChunkFeatArgs 
 }
 
 int launch_chunk_features(fkv_cache *c, int layer, const void *q, const float *lse, const int32_t *chunk_lens, const ChunkLens &lens,
-                          int window, int sinks, float scale, cudaStream_t st) {
+                          int window, int sinks, float scale, bool record_used, cudaStream_t st) {
   const int batch = c->cfg.max_batch, D = c->cfg.head_dim;
   if (lens.tok[batch] == 0) return FKV_OK;
   if (int e = ensure_page_rows_map(c)) return e;
   ChunkFeatArgs a;
+  a.record_used = record_used ? 1 : 0;
   a.layer = layer; a.window = window; a.sinks = window ? sinks : 0;
   if (scale == 0.f) scale = 1.f / sqrtf((float)D);
   a.scale_log2 = scale * 1.4426950408889634f;
@@ -1095,7 +1096,8 @@ int fkv_chunk_features(fkv_cache *c, int layer, const void *q, const float *lse,
   if (lens.tok[c->cfg.max_batch] > 0 && (!lse || !aligned(lse, 4))) return FKV_ERR_INVALID_ARG;
   if (!chunk_is_stored(c, layer, chunk_lens)) return FKV_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)stream;
-  if (lens.tok[c->cfg.max_batch] > 0 && c->cfg.feature_window > 0 && c->feature_scale > 0.f) {
+  const bool record = lens.tok[c->cfg.max_batch] > 0 && c->cfg.feature_window > 0 && c->feature_scale > 0.f;
+  if (record) {
     // Decode queries on record came before the chunk: they move the features on first, and the chunk's kernel then takes
     // them off the record.
     if (int e = ensure_page_rows_map(c)) return e;   // (what can fail does so before anything is changed)
@@ -1111,7 +1113,7 @@ int fkv_chunk_features(fkv_cache *c, int layer, const void *q, const float *lse,
     FKV_LAUNCHED(c);
     if (int e = launch_features(c, max_old, c->cfg.max_batch * c->cfg.num_kv_heads, st)) return e;
   }
-  return launch_chunk_features(c, layer, q, lse, chunk_lens, lens, window, sinks, scale, st);
+  return launch_chunk_features(c, layer, q, lse, chunk_lens, lens, window, sinks, scale, record, st);
 }
 
 int fkv_decode_attn_window(fkv_cache *c, int layer, const void *q, const int32_t *q_pos, int32_t window, int32_t sinks, void *out,

@@ -39,6 +39,7 @@ struct ChunkFeatArgs {
   float scale_log2;
   float inv_hi, inv_lo;   // 1 / scale in two parts
   int nk, nq;          // pairs of K tiles and blocks of queries in shared memory
+  int record_used;     // the launch before has applied the record of decode queries of the sequences with tokens
   const float *lse;    // [tokens][Hkv * g]
   ChunkLens lens;
 };
@@ -198,8 +199,7 @@ __global__ void __launch_bounds__(kCfThreads, 1) k_chunk_features(Ctx c, const _
       Len[s] = n;
       const int T = a.lens.tok[s + 1] - a.lens.tok[s];
       if (blockIdx.x == 0 && n < T) set_status(c, kDevBadIndex);
-      // The record of decode queries has been used by the launch before (fkv_chunk_features) and starts over.
-      if (blockIdx.x == 0 && T > 0 && c.hist_w) c.hist_cnt[a.layer * batch + s] = 0;
+      if (blockIdx.x == 0 && T > 0 && a.record_used) c.hist_cnt[a.layer * batch + s] = 0;   // it starts over
     }
     __syncwarp();
     int NB = 0;   // pairs of tiles of the sequences that take part
@@ -332,7 +332,8 @@ __global__ void __launch_bounds__(kCfThreads, 1) k_chunk_features(Ctx c, const _
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int t = T - kCfQueries * (am + 1) + lane * 4 + i;   // (negative in the oldest block)
-          l[i] = t >= 0 && aj < j0 + nj ? __ldcg(lse + (size_t)t * Hq + aj) : 0.f;   // (the launch before may still have been writing them as this one began: not the read-only path)
+          // (not the read-only path: the launch before may still have been writing them as this one began)
+          l[i] = t >= 0 && aj < j0 + nj ? __ldcg(lse + (size_t)t * Hq + aj) : 0.f;
         }
         if (++am == m0 + blocks) { am = m0; ++aj; }
       };

@@ -100,3 +100,21 @@ def test_record_and_chunk_in_a_graph():
     assert torch.equal(once, d.cache.export_features(0, 0))
     graph.replay()
     check_features(c, q, [20], [once])   # the record was used once
+
+
+def test_a_call_captured_before_the_first_decode_step_leaves_the_record():
+    c, d = (Case(2, 2, 64, [50], feature_window=8, cap=200) for _ in range(2))
+    k, v, q = c.chunk([5])
+    lse = torch.empty(q.shape[:2], device="cuda")
+    for x in (c, d):
+        x.cache.append_chunk_attn(0, k, v, q, [5], lse=lse)
+        x.extend(k, v, [5])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.cache.chunk_features(0, q, lse, [5])
+    decode((c, d), [(c.rand(1, 2), c.rand(1, 2), c.rand(1, 4)) for _ in range(3)])
+    graph.replay()   # (of the last five pairs as they are now; its sums do not matter here)
+    for x in (c, d):
+        x.cache.update_features(0)
+    got, want = (x.cache.export_features(0, 0).unflatten(2, (2, 6)) for x in (c, d))
+    assert torch.equal(got[..., :4], want[..., :4])   # the windows and the mean of the three decode queries
