@@ -59,7 +59,7 @@ typedef enum {
 #define FKV_DEV_POOL_EXHAUSTED 1u /* no free page: the step that needed it was skipped */
 #define FKV_DEV_CAPACITY 2u       /* append past max_tokens_per_head was skipped */
 #define FKV_DEV_WAIT_TIMEOUT 4u   /* a bounded wait in a kernel ran out */
-#define FKV_DEV_BAD_INDEX 8u      /* fkv_compact was given an index outside the segment */
+#define FKV_DEV_BAD_INDEX 8u      /* fkv_compact was given an index outside the segment; a replayed chunk call met a shorter one */
 
 /* Scorer activation sigma.  The paper does not name it (Appendix B.1); ReLU is the default. */
 enum { FKV_ACT_RELU = 0, FKV_ACT_SILU = 1, FKV_ACT_GELU_TANH = 2, FKV_ACT_SIGMOID = 3 };
@@ -88,7 +88,8 @@ typedef struct {
                                   maintain the features */
 } fkv_config;
 
-/* Bytes of device workspace fkv_init_cache needs for this config. */
+/* Bytes of device workspace fkv_init_cache needs for this config (39 MB of them, 20 with head_dim 64, for the partial results
+ * of fkv_chunk_attn, whatever the shape of the cache). */
 int fkv_workspace_bytes(const fkv_config *cfg, size_t *bytes);
 
 /*
@@ -271,11 +272,13 @@ int fkv_decode_step(fkv_cache *c, const void *k, const void *v, const int32_t *p
  * fkv_decode_attn / fkv_append_decode_attn of a layer whose queries see only part of the retained set: a query of
  * position p sees the pairs of positions (p - window, p] and those of positions below `sinks` (the first tokens, that
  * stay visible).  Positions are the stored ones, so a window means the same before and after an eviction.  window >= 1,
- * sinks >= 0, and k, v, q and out 16-byte aligned (else FKV_ERR_INVALID_ARG).  The rest is as in the calls without a window, but that the query is NOT put on
- * record for the attention features (they describe attention over the whole retained set).
+ * sinks >= 0, and k, v, q and out 16-byte aligned (else FKV_ERR_INVALID_ARG).  The rest is as in the calls without a
+ * window, but that the query is NOT put on record for the attention features (those describe attention over the whole
+ * retained set).  A windowed layer that wants features while it decodes takes its tokens as chunks of one: fkv_append_chunk_attn,
+ * which gives the log-sum-exp, and fkv_chunk_features.
  *
- * Positions must grow from pair to pair of a segment, and k and v must be finite where some of the queries of a call see a
- * pair and others do not.
+ * Positions must not be negative and must grow from pair to pair of a segment, and k and v must be finite where some of the
+ * queries of a call see a pair and others do not.
  *
  * fkv_decode_attn_window: q_pos dev [max_batch] int32 positions of the queries (pairs of later positions are not seen), or
  * NULL: the position of the last pair.  A query that sees no pair gets zeros.  fkv_append_decode_attn_window: the query's

@@ -194,11 +194,13 @@ __device__ __forceinline__ void merge_partials(const float *part, int nact, int 
 // it - no partial leaves the SMs and no ticket is taken.  For launches that run on their own (the per-layer entry
 // points at small batch), where the merge's round trips to L2 are a sixth of the launch.
 // WIN: the query sees the pairs of the last `window` positions up to its own and those of the first `sinks` positions.
-// Positions grow with the slot, so these are slots [0, wa) and [wb, we), found by looking at three stored positions (a
-// search only where positions are missing); the CTAs share out the pages that hold them, and no other page is read.
+// Positions grow with the slot, so these are slots [0, wa) and [wb, we), found by looking at three stored positions (and by a
+// search where positions are missing; also, one round of it, in a step that appends, since the place that is looked at
+// leaves the new pair out); the CTAs share out the pages that hold them, and no other page is read.
 // Windowed launches leave no query record: the features describe attention over the whole retained set.
 // Bound: bytes, 4 D per pair seen and KV head (64 sequences, window 4096, g = 4, D = 128: 180 us = 6.0 TB/s), below some 20 MB
-// the latency of a dependent launch and of the search (one sequence 8.7 us, 16.8 MB).
+// the latency of a dependent launch and of the looks (one sequence, 16.8 MB, back to back: 8.8 us, 10.5 when it appends; the
+// plain step over as many pairs 8.0 and 8.8).
 template <int D, int NCW, int SLOTS, bool CLUSTER, bool WIN>
 __global__ void __launch_bounds__((NCW + 1) * 32, NCW <= 4 ? 3 : 1) k_attend(Ctx c, AttendArgs a) {
   constexpr int KSQ = D / 16;  // k-steps of K Q^T

@@ -23,10 +23,11 @@
 //   warps 4-11  two warpgroups, each with a stream of its own (S and O accumulators): thread = query row; running
 //               maximum, exp2, row sum in fp32, P rounded to bf16 into columns of its own.  O is rescaled only when the
 //               maximum has grown by more than 2^24: until then P is at most 2^24, which bf16 holds as exactly as 1.
-// Measured (attention and merge, back to back; 32 query heads, g = 4, D = 128): 2048 tokens at 32K 1.04 ms = 1020 TFLOP/s, where
-// the tensor core and the exponentials, 1 : 1 in cycles, hold each other up; 256 tokens at 8K 59.7 us, 34 of them at that rate
-// and the rest the start, the items' ends and the merge; 16 sequences with a few drafts over long caches 87.7 us = 4.8 TB/s
-// with it all, the pages themselves at 6.1 TB/s; 5 drafts at 8K 26.3 us, latency.
+// Measured (attention and merge, back to back; 32 query heads, g = 4, D = 128): 2048 tokens at 32K 1.00 ms = 1065 TFLOP/s for the
+// first 0.1 s, 1.15 - 1.21 ms (880 - 925) once the card's power limit holds the clock at 1.5 GHz; the tensor core and the
+// exponentials, 1 : 1 in cycles, hold each other up.  256 tokens at 8K 60 us, 33 of them at that rate and the rest the start, the
+// items' ends and the merge; 16 sequences with a few drafts over long caches 88 us = 4.8 TB/s with it all, the pages
+// themselves at 6.1 TB/s; 5 drafts at 8K 26 us, latency.
 // The streams are the item's two query tiles; an item with one tile gives its key tiles to the streams in turn, and the
 // streams' results are joined through shared memory.
 // Every wait is bounded; tensor memory is freed at the common exit.
@@ -64,8 +65,8 @@ struct ChunkKeep {
 // last CTA to finish returns what is left, moves the stack top and the lengths and takes rolled-back queries off the record.
 // A sequence that the device finds past its capacity or shorter than `keep` is skipped; without enough pages, free and
 // returned together, the whole call is.
-// Bound: bytes (8 D a pair, read and written); 6.8 us for 5 tokens, 7.2 us for 256 (a launch and four dependent reads: length,
-// page, last position, free stack).
+// Bound: bytes (8 D a pair and KV head, read and written); back to back 4.7 us for 5 tokens, 5.3 for 256, 12.7 for 2048 on 8 heads
+// (a launch and four dependent reads: length, page, last position, free stack).
 __global__ void __launch_bounds__(256) k_append_chunk(Ctx c, int layer, const uint8_t *k, const uint8_t *v, const int32_t *pos,
                                                       const __grid_constant__ ChunkLens lens,
                                                       const __grid_constant__ ChunkKeep keep) {

@@ -4,9 +4,10 @@
 // per query head and pair the means of P over the chunk's last 8 / 16 / 32 queries and over the whole chunk, and the two
 // running sums moved on by the latter, as k_features does for decode queries.
 //
-// Bound: 2 D flops and one exp2 per (query head, seen pair).  The special-function pipe takes 1024 cycles for a block of
+// Bound: 2 D flops and one exp2 per (query head, seen pair).  The special-function pipe would take 1024 cycles for a block of
 // 128 pairs x 128 queries and the tensor core 512, so the exponentials are what the kernel is built around: a quarter is
-// computed on the FMA pipe, and nothing but a multiplication, the exponential and an addition is left per score.  The
+// computed on the FMA pipe (768 cycles are left on the other), and nothing but a multiplication, the exponential and an
+// addition is left per score.  The
 // log-sum-exp is subtracted by the tensor core: one more step of 16 channels, in which a key holds 1, 1, 1, 0, ... and a
 // query -lse / scale as three bf16 values (rounding, and twice the rounding of what is left: 27 bits).
 //
@@ -20,10 +21,13 @@
 //               that hands them to the tensor core waits for the loads of the next ones);
 //   warps 4-11  two warpgroups, one per tile: exp2, sums, and the pair's meta row at the end.
 // Accuracy: a score is off by what the tensor core's fp32 accumulation drops (2^-23 of the partial sums, per step of 16
-// channels), which moves a probability by 1e-6 - 3e-6 relative (a library product in fp32: 0.7e-6 - 2e-6); everything after
-// it is below 3e-7.  The truncation is the products' too, so subtracting in two or four pieces gains nothing (615, 636 us).
-// Measured (32 query heads, g = 4, D = 128): 2048 queries at 32K 612 us, 870 TFLOP/s, the exponentials alone 462; 128 at 8K 28
-// us: the copies of a tile, four blocks of products and its meta rows follow one another twice per CTA.
+// channels), which moves a probability by 1e-6 - 3e-6 relative, 1.3 - 2.5 times what a library product in fp32 does on the
+// same inputs, for some 3 - 4 times; everything after it is below 3e-7.  The truncation is the products' too, so subtracting in
+// two or four pieces gains nothing, and costs 1 - 4 % of the time.
+// Measured (32 query heads, g = 4, D = 128): 2048 queries at 32K 0.59 ms, 900 TFLOP/s, for the first 0.1 s, 0.64 - 0.68 ms once
+// the card's power limit holds the clock at 1.7 GHz; the three quarters of the exponentials on the special-function pipe are
+// 0.35 ms of it, the products 0.32 ms: neither pipe alone bounds it.  128 at 8K 27 us: the copies of a tile, four blocks of products
+// and its meta rows follow one another twice per CTA.
 // Every wait is bounded; tensor memory is freed at the common exit.
 #pragma once
 #include "fkv_chunk.cuh"
@@ -142,7 +146,7 @@ __device__ __forceinline__ float cf_sum8(const uint32_t (&v)[32], int g, float s
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const float2 z = __fmul2_rn(make_float2(__uint_as_float(v[8 * g + 2 * j]), __uint_as_float(v[8 * g + 2 * j + 1])), sc);
-    if (j == 0) x[j] = ex2_fma(z);   // (2048 queries at 32K: none 642 us, an eighth 616, a quarter 612, a half 641)
+    if (j == 0) x[j] = ex2_fma(z);   // (2048 queries at 32K, first 0.1 s: none 646 us, an eighth 623, a quarter 586, a half 690)
     else x[j] = make_float2(ex2(z.x), ex2(z.y));
   }
   const float2 y = __fadd2_rn(__fadd2_rn(x[0], x[1]), __fadd2_rn(x[2], x[3]));
