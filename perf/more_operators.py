@@ -330,8 +330,8 @@ def _step(st):
             x[seq, :, st["stored"][seq] + j] = new[packed]
             outs.append(torch.zeros_like(new))
             outs[-1][: len(seq)] = x[seq, :, st["stored"][seq] + j]
-    pos = torch.zeros_like(st["parents"])
-    pos[: len(seq)] = own_pos[packed].to(torch.int32)
+    pos = st["parents"].new_zeros((len(own_pos), c["kv_heads"]))
+    pos[: len(seq)] = own_pos[packed, None].to(torch.int32)
     return outs + [pos, path, count, tokens, count + st["stored"].to(torch.int32)]
 
 
@@ -361,7 +361,7 @@ def run(st):
         cache.sync_lengths()   # the host reads how far every sequence has come
         now = cache.lengths(0)
         accepted = [m - n for m, n in zip(now, st["keep"])]
-        m, pos = sum(accepted), torch.zeros_like(st["parents"])
+        m, pos = sum(accepted), st["parents"].new_zeros((len(st["parents"]), c["kv_heads"]))
         for i in range(c["layers"]):   # (as many rows as there are nodes, zeros behind the accepted ones)
             k, v = torch.zeros_like(st["k_new"][i]), torch.zeros_like(st["v_new"][i])
             cache.export_chunk(i, accepted, (k[:m], v[:m], None, pos[:m]))
@@ -380,7 +380,7 @@ def run(st):
     slot = torch.arange(len(seq), device="cuda") - (new.cumsum(0) - new)[seq]
     outs = []
     for i in range(c["layers"]):
-        outs += [x[i][src][seq, :, slot] for x in (st["k"], st["v"], st["f"])] + [st["pos"][src][seq, slot]]
+        outs += [x[i][src][seq, :, slot] for x in (st["k"], st["v"], st["f"])] + [st["pos"][src][seq, slot, None].expand(-1, c["kv_heads"])]
     return outs
 
 
