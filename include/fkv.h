@@ -59,7 +59,8 @@ typedef enum {
 #define FKV_DEV_POOL_EXHAUSTED 1u /* no free page: the step that needed it was skipped */
 #define FKV_DEV_CAPACITY 2u       /* append past max_tokens_per_head was skipped */
 #define FKV_DEV_WAIT_TIMEOUT 4u   /* a bounded wait in a kernel ran out */
-#define FKV_DEV_BAD_INDEX 8u      /* fkv_compact was given an index outside the segment; a replayed chunk call met a shorter one */
+#define FKV_DEV_BAD_INDEX 8u      /* fkv_compact was given an index outside the segment; a replayed chunk call met a shorter one;
+                                   a tree's parents or path are out of order */
 
 /* Scorer activation sigma.  The paper does not name it (Appendix B.1); ReLU is the default. */
 enum { FKV_ACT_RELU = 0, FKV_ACT_SILU = 1, FKV_ACT_GELU_TANH = 2, FKV_ACT_SIGMOID = 3 };
@@ -346,6 +347,99 @@ int fkv_append_chunk_attn(fkv_cache *c, int layer, const void *k, const void *v,
  */
 int fkv_chunk_features(fkv_cache *c, int layer, const void *q, const float *lse, const int32_t *chunk_lens, int32_t window,
                        int32_t sinks, float scale, void *stream);
+
+/*
+ * ---- draft trees of a speculative decoder ----
+ *
+ * The drafts of a step as a tree: node 0 is its root, in general the token that the step before gave, whose pair is not stored yet;
+ * every other node is a guess for the token after its parent.  A tree's nodes are packed like the tokens of a chunk (above), in any
+ * order in which parents come before their children; tree_lens: host [max_batch], the nodes of every sequence's tree, at most
+ * FKV_TREE_NODES each (0: the sequence takes no part).  One step:
+ *     fkv_tree_masks(parents) -> masks
+ *     for every layer:  fkv_append_tree_attn(k, v, q, masks) -> out, lse
+ *     fkv_verify_tree(target's probabilities) -> path, path_len, tokens
+ *     fkv_commit_tree(path, path_len)                 (all layers)
+ * and the last one of `tokens` is the root of the next step's tree.  Everything only enqueues kernels and may be captured.
+ *
+ * fkv_tree_masks: parents dev [tokens] int32, a node's parent as an index inside its own tree (smaller than its own), or -1 for a root
+ * (there may be several: children of the last stored pair).  masks: dev [tokens][FKV_TREE_WORDS] uint32, 16-byte aligned; bit i of
+ * node j's mask (bit i % 32 of word i / 32) says that j sees node i: its ancestors and itself.  A parent that is not before its
+ * node sets FKV_DEV_BAD_INDEX and counts as -1.
+ *
+ * fkv_append_tree: fkv_append_chunk for the nodes of trees.  pos NULL: a node's position is one more than its parent's, a root's the
+ * one after the last pair that stays; given positions must be behind that of the last pair that stays.
+ * fkv_tree_attn: fkv_chunk_attn for the nodes of trees, which are the last tree_lens[s] pairs of their segments: a node sees the pairs
+ * ahead of the tree as a chunk's token does (with window > 0 those inside the window of its own position, and the sinks), and the pairs
+ * of the tree that its mask names up to its own (other masks than fkv_tree_masks writes are welcome; a node that sees nothing gets
+ * zeros, and -infinity as its log-sum-exp).  A window must not be shorter than the longest tree, so that it holds every ancestor.
+ * k and v of a tree must be finite.  fkv_append_tree_attn: the two calls in one.  Errors and stream capture as for the chunk calls.
+ *
+ * fkv_verify_tree: which drafts stand, and the token after them, so that every token is distributed as the target says (speculative
+ * sampling; siblings are tried in the order of their indices).  Per sequence, from a = node 0 with R = p = target[a]:
+ *     for every child c of a, x = tokens[c]:
+ *         accepted if u_accept[c] * draft[a][x] < R[x]:  go on at a = c with R = target[c];
+ *         else R = max(R - draft[a], 0) / sum(max(R - draft[a], 0)),  or R = target[a] where that sum is 0;
+ *     no child left: the next token is the first one whose running sum of R exceeds u_sample[s] times the whole sum.
+ * draft NULL: the drafts are no samples but a choice (the likeliest tokens of a draft head): child c is accepted if u_accept[c] * m <
+ * target[a][x], m = 1 less the probabilities of the siblings that were rejected; a rejection takes x out of R (a rejected token that
+ * comes again has probability 0).
+ * tokens, parents: dev [tokens] int32 (tokens[node 0] is not read; nodes that node 0 does not lead to are never reached; one whose token
+ * is outside the vocabulary is passed over).  target, draft: dev [tokens][vocab] of dtype FKV_F32 or FKV_BF16, rows target_stride and
+ * draft_stride elements apart (row a: the token after node a); taken as they are, not normalised, NaN and negative ones as 0.
+ * u_accept: dev [tokens] fp32 (entry 0 of a tree is not read), u_sample: dev [max_batch] fp32, uniform in [0, 1): the library draws no
+ * random numbers itself.  vocab at most 2^20.
+ * path: dev [max_batch][path_stride] int32, the accepted nodes from node 0 down, -1 behind them; path_len: dev [max_batch] int32, their
+ * number (at least 1, 0 without a tree); tokens_out: dev [max_batch][path_stride] int32, the path_len tokens that the step gives: those of
+ * the accepted nodes behind node 0, then the next one (-1 if R is zero everywhere), -1 behind them.  path_stride is at least the longest tree.
+ * Arithmetic in fp64.  Same inputs give same results, in any batch.
+ * fkv_verify_tree_greedy: the same at temperature 0: choice dev [tokens] int32 is the target's own token after every node, a child is
+ * accepted if it is that token (of several the first one), and the next token is the choice of the last accepted node.
+ *
+ * fkv_commit_tree: of every sequence's last tree_lens[s] pairs (its tree's) those of path[s][0 .. path_len[s]) move together behind the
+ * pairs ahead of the tree, the others are dropped and their pages returned, in one layer or (FKV_ALL_LAYERS) in all.  path and path_len:
+ * dev, as fkv_verify_tree writes them: ascending indices inside the tree; path_len[s] = 0 drops the whole tree.  A path that is not, or
+ * a tree longer than its segment, sets FKV_DEV_BAD_INDEX and leaves the sequence as it is.  What a pair holds moves with it, so
+ * fkv_chunk_features may follow with the path's queries and log-sum-exps.  Decode queries on record that saw pairs of the tree leave the
+ * record.  The new lengths are known to the device alone: call fkv_sync_lengths before any call that goes by the host's (until then the
+ * host's are those with the whole trees; fkv_append_tree and fkv_append_chunk with keep_lens may follow at once).
+ */
+#define FKV_TREE_NODES 256
+#define FKV_TREE_WORDS (FKV_TREE_NODES / 32)
+enum { FKV_F32 = 0, FKV_BF16 = 1 };
+int fkv_tree_masks(fkv_cache *c, const int32_t *parents, const int32_t *tree_lens, uint32_t *masks, void *stream);
+int fkv_append_tree(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos, const int32_t *keep_lens,
+                    const int32_t *tree_lens, const uint32_t *masks, void *stream);
+int fkv_tree_attn(fkv_cache *c, int layer, const void *q, const int32_t *tree_lens, const uint32_t *masks, int32_t window,
+                  int32_t sinks, float scale, void *out, float *lse_out, void *stream);
+int fkv_append_tree_attn(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos, const int32_t *keep_lens,
+                         const int32_t *tree_lens, const uint32_t *masks, const void *q, int32_t window, int32_t sinks,
+                         float scale, void *out, float *lse_out, void *stream);
+int fkv_verify_tree(fkv_cache *c, const int32_t *tokens, const int32_t *parents, const int32_t *tree_lens, const void *target,
+                    int64_t target_stride, const void *draft, int64_t draft_stride, int32_t dtype, int32_t vocab,
+                    const float *u_accept, const float *u_sample, int32_t *path, int32_t *path_len, int32_t *tokens_out,
+                    int32_t path_stride, void *stream);
+int fkv_verify_tree_greedy(fkv_cache *c, const int32_t *tokens, const int32_t *parents, const int32_t *tree_lens,
+                           const int32_t *choice, int32_t *path, int32_t *path_len, int32_t *tokens_out, int32_t path_stride,
+                           void *stream);
+int fkv_commit_tree(fkv_cache *c, int layer, const int32_t *tree_lens, const int32_t *path, const int32_t *path_len,
+                    int32_t path_stride, void *stream);
+
+/*
+ * ---- sequences that are copied, change places or end ----
+ * fkv_fork: every sequence s becomes, in all layers, what sequence from[s] was before the call (from[s] = s: it stays as it is; -1: it
+ * is emptied and its pages are returned): a prompt for several samples, beams that change places, requests that end, in any mixture.
+ * from: host [max_batch], read before the call returns; entries outside [-1, max_batch) are FKV_ERR_INVALID_ARG.  Everything a sequence
+ * holds goes with it: pairs, features, positions, decode queries on record, its budget (an emptied place keeps its own).  Sequences never
+ * share pages (each keeps features of its own in them): of a sequence that goes away while others become what it was, one takes the pages
+ * over and the others get copies.  The pages of sequences that go away serve the copies; if these and the free ones are too few the
+ * whole call does nothing (FKV_DEV_POOL_EXHAUSTED).  Only enqueues kernels; a replayed call does the same to what it finds.
+ *
+ * fkv_export_chunk: dense copy of the last chunk_lens[s] pairs of every sequence of a layer, packed, the inverse of fkv_append_chunk:
+ * k, v dev [tokens][Hkv][D] bf16 (16-byte aligned), feat dev [tokens][Hkv][F] fp32, pos dev [tokens][Hkv] int32 (after an eviction the
+ * heads keep pairs of different positions); any may be NULL.  FKV_ERR_INVALID_ARG if a chunk is longer than its segment.
+ */
+int fkv_fork(fkv_cache *c, const int32_t *from, void *stream);
+int fkv_export_chunk(fkv_cache *c, int layer, const int32_t *chunk_lens, void *k, void *v, float *feat, int32_t *pos, void *stream);
 
 /* ---- staged entry points: one kernel each, for per-step checks ---- */
 

@@ -29,7 +29,10 @@ EXPORTS = ["fkv_workspace_bytes", "fkv_init_cache", "fkv_destroy", "fkv_reset", 
            "fkv_launch_count", "fkv_last_cuda_error", "fkv_sync_lengths", "fkv_set_timing", "fkv_get_evict_timing",
            "fkv_decode_step", "fkv_decode_attn_dense_noalloc", "fkv_append_decode_attn", "fkv_evict_sampled", "fkv_select_sampled", "fkv_update_features", "fkv_evict_by_feature", "fkv_golden_steps", "fkv_golden_eviction", "fkv_golden_select",
            "fkv_evict_rkv", "fkv_score_rkv", "fkv_append_chunk", "fkv_chunk_attn", "fkv_append_chunk_attn",
-           "fkv_decode_attn_window", "fkv_append_decode_attn_window", "fkv_export_features", "fkv_chunk_features"]
+           "fkv_decode_attn_window", "fkv_append_decode_attn_window", "fkv_export_features", "fkv_chunk_features",
+           "fkv_tree_masks", "fkv_append_tree", "fkv_tree_attn", "fkv_append_tree_attn", "fkv_verify_tree",
+           "fkv_verify_tree_greedy", "fkv_commit_tree", "fkv_fork", "fkv_export_chunk"]
+TREE_NODES, TREE_WORDS = 256, 8   # most nodes of a draft tree, words of a node's mask
 
 
 class FkvConfig(ctypes.Structure):
@@ -57,7 +60,7 @@ def lib():
         for name in EXPORTS:
             getattr(_lib, name).restype = ctypes.c_int
         _lib.fkv_last_cuda_error.restype = ctypes.c_char_p
-        vp, i32, u64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64, ctypes.c_float
+        vp, i32, u64, f32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64, ctypes.c_float, ctypes.c_int64
         # Declared argument types for the per-token calls: plain ints and floats are converted by ctypes itself.
         _lib.fkv_append.argtypes = [vp, i32, vp, vp, vp, vp, vp]
         _lib.fkv_decode_attn.argtypes = [vp, i32, vp, vp, f32, vp]
@@ -70,6 +73,15 @@ def lib():
         _lib.fkv_chunk_features.argtypes = [vp, i32, vp, vp, vp, i32, i32, f32, vp]
         _lib.fkv_decode_attn_window.argtypes = [vp, i32, vp, vp, i32, i32, vp, f32, vp]
         _lib.fkv_append_decode_attn_window.argtypes = [vp, i32, vp, vp, vp, vp, vp, i32, i32, vp, f32, vp]
+        _lib.fkv_tree_masks.argtypes = [vp, vp, vp, vp, vp]
+        _lib.fkv_append_tree.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp]
+        _lib.fkv_tree_attn.argtypes = [vp, i32, vp, vp, vp, i32, i32, f32, vp, vp, vp]
+        _lib.fkv_append_tree_attn.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp, i32, i32, f32, vp, vp, vp]
+        _lib.fkv_verify_tree.argtypes = [vp, vp, vp, vp, vp, i64, vp, i64, i32, i32, vp, vp, vp, vp, vp, i32, vp]
+        _lib.fkv_verify_tree_greedy.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, vp]
+        _lib.fkv_commit_tree.argtypes = [vp, i32, vp, vp, vp, i32, vp]
+        _lib.fkv_fork.argtypes = [vp, vp, vp]
+        _lib.fkv_export_chunk.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp]
     return _lib
 
 
@@ -320,7 +332,8 @@ class Cache:
         total, c = sum(chunk_lens), self.cfg
         for name, t in tensors.items():
             heads = c.num_kv_heads * (1 if name in ("k", "v") else c.group_size)
-            want = (total, heads) if name == "lse" else (total,) if name == "pos" else (total, heads, c.head_dim)
+            want = ((total, heads) if name == "lse" else (total,) if name in ("pos", "parents") else
+                    (total, TREE_WORDS) if name == "masks" else (total, heads, c.head_dim))
             if t is not None and tuple(t.shape) != want:
                 raise ValueError(f"{name}: expected shape {want}, got {tuple(t.shape)}")
         self._check_place(*tensors.values())
@@ -377,6 +390,136 @@ class Cache:
             raise ValueError(f"out: expected shape {shape}, got {tuple(out.shape)}")
         self._check_place(out)
         _check(lib().fkv_export_features(self._h, layer, seq, _ptr(out, torch.float32), _stream()), "fkv_export_features")
+        return out
+
+    # -- draft trees: nodes are packed like the tokens of a chunk, parents ahead of their children, node 0 the root
+    def tree_masks(self, parents, tree_lens, out=None):
+        """Which nodes of its tree every node sees, its ancestors and itself, as bits: int32 [nodes][8].  parents [nodes] int32: the
+        parent's index inside the tree, -1 for a root."""
+        if out is None:
+            out = torch.empty((parents.shape[0], TREE_WORDS), dtype=torch.int32, device=parents.device)
+        self._check_chunk(tree_lens, parents=parents, masks=out)
+        _check(lib().fkv_tree_masks(self._h, _ptr(parents, torch.int32), _lens(tree_lens, self.cfg.max_batch, "tree_lens"),
+                                    _ptr(out, torch.int32), _stream()), "fkv_tree_masks")
+        return out
+
+    def append_tree(self, layer, k, v, tree_lens, masks, pos=None, keep_lens=None):
+        """append_chunk for the nodes of draft trees (a node's position is one behind its parent's)."""
+        _check_i32(layer=layer)
+        self._check_chunk(tree_lens, k=k, v=v, pos=pos, masks=masks)
+        lens, keep = _lens(tree_lens, self.cfg.max_batch, "tree_lens"), _lens(keep_lens, self.cfg.max_batch, "keep_lens")
+        _check(lib().fkv_append_tree(self._h, layer, _ptr(k, torch.bfloat16), _ptr(v, torch.bfloat16), _ptr(pos, torch.int32), keep,
+                                     lens, _ptr(masks, torch.int32), _stream()), "fkv_append_tree")
+
+    def tree_attn(self, layer, q, tree_lens, masks, window=0, sinks=0, out=None, lse=None, scale=0.0):
+        """chunk_attn for the nodes of draft trees: over the pairs ahead of the tree and those of it that the masks name."""
+        _check_i32(layer=layer, window=window, sinks=sinks)
+        if out is None:
+            out = torch.empty_like(q)
+        self._check_chunk(tree_lens, q=q, out=out, lse=lse, masks=masks)
+        _check(lib().fkv_tree_attn(self._h, layer, _ptr(q, torch.bfloat16), _lens(tree_lens, self.cfg.max_batch, "tree_lens"),
+                                   _ptr(masks, torch.int32), window, sinks, scale, _ptr(out, torch.bfloat16),
+                                   _ptr(lse, torch.float32), _stream()), "fkv_tree_attn")
+        return out
+
+    def append_tree_attn(self, layer, k, v, q, tree_lens, masks, pos=None, keep_lens=None, window=0, sinks=0, out=None, lse=None,
+                         scale=0.0):
+        """append_tree(k, v) then tree_attn(q) in one call."""
+        _check_i32(layer=layer, window=window, sinks=sinks)
+        if out is None:
+            out = torch.empty_like(q)
+        self._check_chunk(tree_lens, k=k, v=v, q=q, out=out, lse=lse, pos=pos, masks=masks)
+        lens, keep = _lens(tree_lens, self.cfg.max_batch, "tree_lens"), _lens(keep_lens, self.cfg.max_batch, "keep_lens")
+        _check(lib().fkv_append_tree_attn(self._h, layer, _ptr(k, torch.bfloat16), _ptr(v, torch.bfloat16), _ptr(pos, torch.int32),
+                                          keep, lens, _ptr(masks, torch.int32), _ptr(q, torch.bfloat16), window, sinks, scale,
+                                          _ptr(out, torch.bfloat16), _ptr(lse, torch.float32), _stream()), "fkv_append_tree_attn")
+        return out
+
+    def _verified(self, tree_lens, out, device, **nodes):
+        """The checked inputs' results: path [batch][nodes], path_len [batch] and tokens [batch][nodes], int32."""
+        batch, total = self.cfg.max_batch, sum(tree_lens)
+        for name, t in nodes.items():
+            if t is not None and tuple(t.shape) != (total,):
+                raise ValueError(f"{name}: expected shape {(total,)}, got {tuple(t.shape)}")
+        if out is None:
+            width = max(1, max(tree_lens))
+            out = tuple(torch.empty(s, dtype=torch.int32, device=device) for s in ((batch, width), (batch,), (batch, width)))
+        path, path_len, tokens = out
+        if path.dim() != 2 or path.shape[0] != batch or tokens.shape != path.shape or tuple(path_len.shape) != (batch,):
+            raise ValueError(f"out: expected shapes ({batch}, n), ({batch},), ({batch}, n), got {[tuple(t.shape) for t in out]}")
+        self._check_place(*nodes.values(), *out)
+        return out
+
+    def verify_tree(self, tokens, parents, tree_lens, target, u_accept, u_sample, draft=None, out=None):
+        """Which drafts stand and the token after them (speculative sampling with the caller's uniform numbers).  target and draft
+        [nodes][vocab] fp32 or bf16, the probabilities of the token after every node (draft None: the drafts are the draft head's
+        choice, not samples); tokens, parents [nodes] int32, u_accept [nodes], u_sample [batch] fp32.
+        Returns (path [batch][n], path_len [batch], tokens [batch][n]) with n = the longest tree."""
+        lens = _lens(tree_lens, self.cfg.max_batch, "tree_lens")
+        path, path_len, given = self._verified(tree_lens, out, tokens.device, tokens=tokens, parents=parents, u_accept=u_accept)
+        total, dtype = sum(tree_lens), target.dtype
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"target: expected float32 or bfloat16, got {dtype}")
+        rows = []
+        for name, t in (("target", target), ("draft", draft)):
+            if t is None:
+                rows += [None, 0]
+                continue
+            if t.dim() != 2 or t.shape[0] != total or t.shape[1] != target.shape[1] or t.dtype is not dtype:
+                raise ValueError(f"{name}: expected {dtype} [{total}][vocab], got {t.dtype} {tuple(t.shape)}")
+            if t.numel() and t.stride(1) != 1 and t.shape[1] > 1:
+                raise ValueError(f"{name}: a row's elements must be next to one another")
+            rows += [ctypes.c_void_p(t.data_ptr()), max(t.stride(0), t.shape[1]) if total < 2 else t.stride(0)]
+        if tuple(u_sample.shape) != (self.cfg.max_batch,):
+            raise ValueError(f"u_sample: expected shape {(self.cfg.max_batch,)}, got {tuple(u_sample.shape)}")
+        self._check_place(target, draft, u_sample)
+        _check(lib().fkv_verify_tree(self._h, _ptr(tokens, torch.int32), _ptr(parents, torch.int32), lens, *rows,
+                                     0 if dtype is torch.float32 else 1, target.shape[1], _ptr(u_accept, torch.float32),
+                                     _ptr(u_sample, torch.float32), _ptr(path, torch.int32), _ptr(path_len, torch.int32),
+                                     _ptr(given, torch.int32), path.shape[1], _stream()), "fkv_verify_tree")
+        return path, path_len, given
+
+    def verify_tree_greedy(self, tokens, parents, tree_lens, choice, out=None):
+        """verify_tree at temperature 0: choice [nodes] int32 is the target's own token after every node."""
+        lens = _lens(tree_lens, self.cfg.max_batch, "tree_lens")
+        path, path_len, given = self._verified(tree_lens, out, tokens.device, tokens=tokens, parents=parents, choice=choice)
+        _check(lib().fkv_verify_tree_greedy(self._h, _ptr(tokens, torch.int32), _ptr(parents, torch.int32), lens,
+                                            _ptr(choice, torch.int32), _ptr(path, torch.int32), _ptr(path_len, torch.int32),
+                                            _ptr(given, torch.int32), path.shape[1], _stream()), "fkv_verify_tree_greedy")
+        return path, path_len, given
+
+    def commit_tree(self, tree_lens, path, path_len, layer=ALL_LAYERS):
+        """The accepted nodes' pairs move together behind the pairs ahead of the tree, the others are dropped.  The host learns the
+        new lengths by sync_lengths()."""
+        _check_i32(layer=layer)
+        batch = self.cfg.max_batch
+        if path.dim() != 2 or path.shape[0] != batch or tuple(path_len.shape) != (batch,):
+            raise ValueError(f"path, path_len: expected shapes ({batch}, n), ({batch},), got {tuple(path.shape)}, {tuple(path_len.shape)}")
+        self._check_place(path, path_len)
+        _check(lib().fkv_commit_tree(self._h, layer, _lens(tree_lens, batch, "tree_lens"), _ptr(path, torch.int32),
+                                     _ptr(path_len, torch.int32), path.shape[1], _stream()), "fkv_commit_tree")
+
+    # -- sequences that are copied, change places or end
+    def fork(self, source):
+        """Sequence s becomes what sequence source[s] was, in all layers (s itself: it stays; -1: it is emptied)."""
+        self._check_place()
+        _check(lib().fkv_fork(self._h, _lens(source, self.cfg.max_batch, "source"), _stream()), "fkv_fork")
+
+    def export_chunk(self, layer, chunk_lens, out=None):
+        """Dense copy of the last chunk_lens[s] pairs of every sequence: k, v [tokens][Hkv][D], features [tokens][Hkv][6 g], positions
+        [tokens][Hkv].  out: four such tensors (None: not wanted)."""
+        _check_i32(layer=layer)
+        total, c = sum(chunk_lens), self.cfg
+        shapes = [(total, c.num_kv_heads, n) for n in (c.head_dim, c.head_dim, self.feat_dim)] + [(total, c.num_kv_heads)]
+        types = (torch.bfloat16, torch.bfloat16, torch.float32, torch.int32)
+        if out is None:
+            out = tuple(torch.empty(s, dtype=t, device=self.workspace.device) for s, t in zip(shapes, types))
+        for t, s in zip(out, shapes):
+            if t is not None and tuple(t.shape) != s:
+                raise ValueError(f"out: expected shape {s}, got {tuple(t.shape)}")
+        self._check_place(*out)
+        _check(lib().fkv_export_chunk(self._h, layer, _lens(chunk_lens, c.max_batch, "chunk_lens"),
+                                      *(_ptr(t, d) for t, d in zip(out, types)), _stream()), "fkv_export_chunk")
         return out
 
     # -- staged entry points

@@ -23,10 +23,13 @@
 #include "fkv_compact.cuh"
 #include "fkv_dev.cuh"
 #include "fkv_features.cuh"
+#include "fkv_fork.cuh"
 #include "fkv_golden.cuh"
 #include "fkv_rkv.cuh"
 #include "fkv_score.cuh"
 #include "fkv_select.cuh"
+#include "fkv_tree.cuh"
+#include "fkv_verify.cuh"
 
 using namespace fkv;
 
@@ -577,8 +580,9 @@ int check_append_chunk(const fkv_cache *c, int layer, const void *k, const void 
   return FKV_OK;
 }
 
+// masks: of a draft tree, else NULL.
 int launch_append_chunk(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos, const int32_t *keep_lens,
-                        const int32_t *chunk_lens, const ChunkLens &lens, cudaStream_t st) {
+                        const int32_t *chunk_lens, const ChunkLens &lens, const uint32_t *masks, cudaStream_t st) {
   const int batch = c->cfg.max_batch;
   // (A roll-back to the lengths that the host knows is launched all the same: replayed, it meets others.)
   if (lens.tok[batch] == 0 && !keep_lens) return FKV_OK;
@@ -590,7 +594,8 @@ int launch_append_chunk(fkv_cache *c, int layer, const void *k, const void *v, c
   // A warp per pair, up to four CTAs of eight warps on every SM: more pairs than that go round.
   const long long tasks = (long long)lens.tok[batch] * c->cfg.num_kv_heads;
   const int grid = (int)std::max<long long>(1, std::min<long long>((tasks + 7) / 8, 4LL * c->sm_count));
-  FKV_CUDA(launch_waiting(k_append_chunk, dim3(grid), 256, 0, st, c->ctx, layer, (const uint8_t *)k, (const uint8_t *)v, pos, lens, keep));
+  FKV_CUDA(launch_waiting(masks ? k_append_chunk<true> : k_append_chunk<false>, dim3(grid), 256, 0, st, c->ctx, layer, (const uint8_t *)k,
+                          (const uint8_t *)v, pos, lens, keep, masks));
   ++c->launches;
   for (int s = 0; s < batch; ++s) {
     int &n = c->h_len[(size_t)layer * batch + s];
@@ -623,13 +628,13 @@ int query_map(const fkv_cache *c, const void *q, int tokens, int box_heads, int 
   return tensor_map(map, const_cast<void *>(q), 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-template <int D>
+template <int D, bool TREE>
 int launch_chunk_attend_t(fkv_cache *c, const CUtensorMap &tmq, const ChunkArgs &a, int grid, cudaStream_t st) {
   constexpr size_t smem = ChunkSmem<D>::bytes();
   static_assert(smem <= kMaxSmem, "one CTA's shared memory");
   static SmemOptIn opt_in;
-  FKV_CUDA(opt_in.ensure(k_chunk_attend<D>, smem));
-  FKV_CUDA(launch_waiting(k_chunk_attend<D>, dim3(grid), kChunkThreads, smem, st, c->ctx, c->page_rows, c->page_parts, tmq, a));
+  FKV_CUDA(opt_in.ensure(k_chunk_attend<D, TREE>, smem));
+  FKV_CUDA(launch_waiting(k_chunk_attend<D, TREE>, dim3(grid), kChunkThreads, smem, st, c->ctx, c->page_rows, c->page_parts, tmq, a));
   ++c->launches;
   if (grid > 1) {   // (a single CTA cuts nothing)
     // A warp per query row of the largest item, or per 8 rows x 16 channels.
@@ -643,7 +648,7 @@ int launch_chunk_attend_t(fkv_cache *c, const CUtensorMap &tmq, const ChunkArgs 
 }
 
 int launch_chunk_attend(fkv_cache *c, int layer, const void *q, const int32_t *chunk_lens, const ChunkLens &lens, int window,
-                        int sinks, float scale, void *out, float *lse, cudaStream_t st) {
+                        int sinks, float scale, void *out, float *lse, const uint32_t *masks, cudaStream_t st) {
   const int batch = c->cfg.max_batch, D = c->cfg.head_dim, G = c->cfg.group_size;
   if (lens.tok[batch] == 0) return FKV_OK;
   if (int e = ensure_page_rows_map(c)) return e;
@@ -651,7 +656,7 @@ int launch_chunk_attend(fkv_cache *c, int layer, const void *q, const int32_t *c
   a.layer = layer; a.window = window; a.sinks = window ? sinks : 0;
   a.scale = scale == 0.f ? 1.f / sqrtf((float)D) : scale;
   a.scale_log2 = a.scale * 1.4426950408889634f;
-  a.out = (__nv_bfloat16 *)out; a.lse = lse; a.lens = lens;
+  a.out = (__nv_bfloat16 *)out; a.lse = lse; a.masks = masks; a.lens = lens;
   CUtensorMap tmq;
   const int tokens_per_tile = kChunkRows / G, block = 2 * tokens_per_tile;
   if (int e = query_map(c, q, lens.tok[batch], G, tokens_per_tile, &tmq)) return e;
@@ -664,7 +669,8 @@ int launch_chunk_attend(fkv_cache *c, int layer, const void *q, const int32_t *c
   pages *= c->cfg.num_kv_heads;
   const int most = std::min(kChunkCtas, c->sm_count);
   const int grid = (int)std::max<long long>(1, std::min<long long>(most, (pages + kChunkMinPages - 1) / kChunkMinPages));
-  return D == 128 ? launch_chunk_attend_t<128>(c, tmq, a, grid, st) : launch_chunk_attend_t<64>(c, tmq, a, grid, st);
+  if (masks) return D == 128 ? launch_chunk_attend_t<128, true>(c, tmq, a, grid, st) : launch_chunk_attend_t<64, true>(c, tmq, a, grid, st);
+  return D == 128 ? launch_chunk_attend_t<128, false>(c, tmq, a, grid, st) : launch_chunk_attend_t<64, false>(c, tmq, a, grid, st);
 }
 
 template <int D>
@@ -702,6 +708,119 @@ int launch_chunk_features(fkv_cache *c, int layer, const void *q, const float *l
   units *= c->cfg.num_kv_heads * c->cfg.group_size;
   const int grid = (int)std::max<long long>(1, std::min<long long>(c->sm_count, units));
   return D == 128 ? launch_chunk_features_t<128>(c, tmq, a, grid, st) : launch_chunk_features_t<64>(c, tmq, a, grid, st);
+}
+
+// ---------------------------------------------------------------- draft trees
+// Lengths of trees: at most kTreeNodes each, and a window (if any) holds every ancestor.
+bool trees_ok(const fkv_cache *c, const int32_t *tree_lens, int window) {
+  for (int s = 0; s < c->cfg.max_batch; ++s)
+    if (tree_lens[s] > kTreeNodes || (window > 0 && tree_lens[s] > window)) return false;
+  return true;
+}
+
+// A cluster of CTAs per sequence: as many as keep the card at about one CTA per SM, so that a single sequence's rows are read by
+// eight SMs and a large batch's by all of them.
+template <class T, bool Q>
+int launch_verify_t(fkv_cache *c, const VerifyArgs &a, cudaStream_t st) {
+  int cs = 1;
+  while (cs < kVerMaxCluster && cs * 2 * c->cfg.max_batch <= c->sm_count) cs *= 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(c->cfg.max_batch * cs);
+  cfg.blockDim = dim3(kVerThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = cs; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  FKV_CUDA(cudaLaunchKernelEx(&cfg, k_verify_tree<T, Q>, c->ctx, a));
+  ++c->launches;
+  return FKV_OK;
+}
+
+int check_verify(const fkv_cache *c, const int32_t *tokens, const int32_t *parents, const int32_t *tree_lens, const int32_t *path,
+                 const int32_t *path_len, const int32_t *tokens_out, int32_t stride, VerifyArgs &a) {
+  if (!c || !tree_lens || !make_lens(c, tree_lens, a.lens) || !trees_ok(c, tree_lens, 0)) return FKV_ERR_INVALID_ARG;
+  const int total = a.lens.tok[c->cfg.max_batch];
+  if (!path || !path_len || !tokens_out || stride < 1 || !aligned(path, 4) || !aligned(path_len, 4) || !aligned(tokens_out, 4))
+    return FKV_ERR_INVALID_ARG;
+  if (total > 0 && (!tokens || !parents || !aligned(tokens, 4) || !aligned(parents, 4))) return FKV_ERR_INVALID_ARG;
+  for (int s = 0; s < c->cfg.max_batch; ++s)
+    if (tree_lens[s] > stride) return FKV_ERR_INVALID_ARG;
+  return FKV_OK;
+}
+
+// ---------------------------------------------------------------- forks
+// What every sequence does, from where each comes; false if nothing changes.
+bool make_fork(const fkv_cache *c, const int32_t *from, ForkMap &m, ForkOps &ops) {
+  const int batch = c->cfg.max_batch;
+  bool any = false;
+  for (int s = 0; s < kMaxBatch; ++s) {
+    m.from[s] = (short)s;
+    m.first[s] = m.next[s] = -1;
+    m.what[s] = 0;
+    ops.emptied[s] = 0;
+  }
+  bool moved[kMaxBatch] = {};   // whose pages have been handed over
+  for (int s = 0; s < batch; ++s) {
+    const int r = from[s];
+    m.from[s] = (short)r;
+    if (r == s) continue;
+    any = true;
+    m.what[s] = FORK_CHANGES;
+    if (r < 0) {
+      ops.emptied[s] = 1;
+    } else if (from[r] != r && !moved[r]) {
+      moved[r] = true;
+      m.what[s] |= FORK_MOVES;
+    }
+  }
+  for (int s = batch - 1; s >= 0; --s) {
+    if (!(m.what[s] & FORK_CHANGES)) continue;
+    if (!moved[s]) m.what[s] |= FORK_FREED;
+    if (m.from[s] >= 0 && !(m.what[s] & FORK_MOVES)) {
+      m.next[s] = m.first[m.from[s]];
+      m.first[m.from[s]] = (short)s;
+    }
+  }
+  // The record's copies in an order in which no value is overwritten before it is used.
+  ops.n = 0;
+  int src[kMaxBatch], uses[kForkAside + 1] = {}, ready[kMaxBatch], nready = 0;
+  std::fill(src, src + kMaxBatch, -1);
+  for (int s = 0; s < batch; ++s)
+    if ((m.what[s] & FORK_CHANGES) && m.from[s] >= 0) {
+      src[s] = m.from[s];
+      ++uses[src[s]];
+    }
+  auto emit = [&](int d, int s) {
+    ops.dst[ops.n] = (short)d;
+    ops.src[ops.n] = (short)s;
+    ++ops.n;
+  };
+  auto run_ready = [&]() {
+    while (nready > 0) {
+      const int d = ready[--nready], s = src[d];
+      emit(d, s);
+      src[d] = -1;
+      if (--uses[s] == 0 && s < batch && src[s] >= 0) ready[nready++] = s;
+    }
+  };
+  for (int s = 0; s < batch; ++s)
+    if (src[s] >= 0 && uses[s] == 0) ready[nready++] = s;
+  run_ready();
+  for (int s = 0; s < batch; ++s) {   // what is left are cycles: one element aside, and the rest follows
+    if (src[s] < 0) continue;
+    emit(kForkAside, s);
+    for (int d = 0; d < batch; ++d)
+      if (src[d] == s) src[d] = kForkAside;
+    uses[kForkAside] = uses[s];
+    uses[s] = 0;
+    ready[nready++] = s;
+    run_ready();
+  }
+  return any;
 }
 
 }  // namespace
@@ -1065,7 +1184,7 @@ int fkv_append_chunk(fkv_cache *c, int layer, const void *k, const void *v, cons
                      const int32_t *chunk_lens, void *stream) {
   ChunkLens lens;
   if (int e = check_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens)) return e;
-  return launch_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens, (cudaStream_t)stream);
+  return launch_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens, nullptr, (cudaStream_t)stream);
 }
 
 int fkv_chunk_attn(fkv_cache *c, int layer, const void *q, const int32_t *chunk_lens, int32_t window, int32_t sinks, float scale,
@@ -1074,7 +1193,7 @@ int fkv_chunk_attn(fkv_cache *c, int layer, const void *q, const int32_t *chunk_
   if (int e = check_chunk(c, layer, q, chunk_lens, window, sinks, scale, lens)) return e;
   if (lens.tok[c->cfg.max_batch] > 0 && (!out || !aligned(out, 16) || !aligned(lse_out, 4))) return FKV_ERR_INVALID_ARG;
   if (!chunk_is_stored(c, layer, chunk_lens)) return FKV_ERR_INVALID_ARG;
-  return launch_chunk_attend(c, layer, q, chunk_lens, lens, window, sinks, scale, out, lse_out, (cudaStream_t)stream);
+  return launch_chunk_attend(c, layer, q, chunk_lens, lens, window, sinks, scale, out, lse_out, nullptr, (cudaStream_t)stream);
 }
 
 int fkv_append_chunk_attn(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos, const int32_t *keep_lens,
@@ -1085,8 +1204,8 @@ int fkv_append_chunk_attn(fkv_cache *c, int layer, const void *k, const void *v,
   if (int e = check_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens)) return e;
   if (lens.tok[c->cfg.max_batch] > 0 && (!out || !aligned(out, 16) || !aligned(lse_out, 4))) return FKV_ERR_INVALID_ARG;
   if (int e = ensure_page_rows_map(c)) return e;   // (what can fail does so before anything is stored)
-  if (int e = launch_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens, (cudaStream_t)stream)) return e;
-  return launch_chunk_attend(c, layer, q, chunk_lens, lens, window, sinks, scale, out, lse_out, (cudaStream_t)stream);
+  if (int e = launch_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens, nullptr, (cudaStream_t)stream)) return e;
+  return launch_chunk_attend(c, layer, q, chunk_lens, lens, window, sinks, scale, out, lse_out, nullptr, (cudaStream_t)stream);
 }
 
 int fkv_chunk_features(fkv_cache *c, int layer, const void *q, const float *lse, const int32_t *chunk_lens, int32_t window,
@@ -1114,6 +1233,142 @@ int fkv_chunk_features(fkv_cache *c, int layer, const void *q, const float *lse,
     if (int e = launch_features(c, max_old, c->cfg.max_batch * c->cfg.num_kv_heads, st)) return e;
   }
   return launch_chunk_features(c, layer, q, lse, chunk_lens, lens, window, sinks, scale, record, st);
+}
+
+int fkv_tree_masks(fkv_cache *c, const int32_t *parents, const int32_t *tree_lens, uint32_t *masks, void *stream) {
+  ChunkLens lens;
+  if (!c || !tree_lens || !make_lens(c, tree_lens, lens) || !trees_ok(c, tree_lens, 0)) return FKV_ERR_INVALID_ARG;
+  if (lens.tok[c->cfg.max_batch] == 0) return FKV_OK;
+  if (!parents || !masks || !aligned(parents, 4) || !aligned(masks, 16)) return FKV_ERR_INVALID_ARG;
+  FKV_CUDA(launch_waiting(k_tree_masks, dim3(c->cfg.max_batch), kTreeNodes, 0, (cudaStream_t)stream, c->ctx, lens, parents, masks));
+  ++c->launches;
+  return FKV_OK;
+}
+
+static int check_tree(const fkv_cache *c, const int32_t *tree_lens, const ChunkLens &lens, const uint32_t *masks, int window) {
+  if (!trees_ok(c, tree_lens, window)) return FKV_ERR_INVALID_ARG;
+  return lens.tok[c->cfg.max_batch] > 0 && (!masks || !aligned(masks, 4)) ? FKV_ERR_INVALID_ARG : FKV_OK;
+}
+
+int fkv_append_tree(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos, const int32_t *keep_lens,
+                    const int32_t *tree_lens, const uint32_t *masks, void *stream) {
+  ChunkLens lens;
+  if (int e = check_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens)) return e;
+  if (int e = check_tree(c, tree_lens, lens, masks, 0)) return e;
+  return launch_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens, masks, (cudaStream_t)stream);
+}
+
+int fkv_tree_attn(fkv_cache *c, int layer, const void *q, const int32_t *tree_lens, const uint32_t *masks, int32_t window, int32_t sinks,
+                  float scale, void *out, float *lse_out, void *stream) {
+  ChunkLens lens;
+  if (int e = check_chunk(c, layer, q, tree_lens, window, sinks, scale, lens)) return e;
+  if (int e = check_tree(c, tree_lens, lens, masks, window)) return e;
+  if (lens.tok[c->cfg.max_batch] > 0 && (!out || !aligned(out, 16) || !aligned(lse_out, 4))) return FKV_ERR_INVALID_ARG;
+  if (!chunk_is_stored(c, layer, tree_lens)) return FKV_ERR_INVALID_ARG;
+  return launch_chunk_attend(c, layer, q, tree_lens, lens, window, sinks, scale, out, lse_out, masks, (cudaStream_t)stream);
+}
+
+int fkv_append_tree_attn(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos, const int32_t *keep_lens,
+                         const int32_t *tree_lens, const uint32_t *masks, const void *q, int32_t window, int32_t sinks, float scale,
+                         void *out, float *lse_out, void *stream) {
+  ChunkLens lens;
+  if (int e = check_chunk(c, layer, q, tree_lens, window, sinks, scale, lens)) return e;
+  if (int e = check_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens)) return e;
+  if (int e = check_tree(c, tree_lens, lens, masks, window)) return e;
+  if (lens.tok[c->cfg.max_batch] > 0 && (!out || !aligned(out, 16) || !aligned(lse_out, 4))) return FKV_ERR_INVALID_ARG;
+  if (int e = ensure_page_rows_map(c)) return e;   // (what can fail does so before anything is stored)
+  if (int e = launch_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens, masks, (cudaStream_t)stream)) return e;
+  return launch_chunk_attend(c, layer, q, tree_lens, lens, window, sinks, scale, out, lse_out, masks, (cudaStream_t)stream);
+}
+
+int fkv_verify_tree(fkv_cache *c, const int32_t *tokens, const int32_t *parents, const int32_t *tree_lens, const void *target,
+                    int64_t target_stride, const void *draft, int64_t draft_stride, int32_t dtype, int32_t vocab, const float *u_accept,
+                    const float *u_sample, int32_t *path, int32_t *path_len, int32_t *tokens_out, int32_t path_stride, void *stream) {
+  VerifyArgs a;
+  if (int e = check_verify(c, tokens, parents, tree_lens, path, path_len, tokens_out, path_stride, a)) return e;
+  if (dtype != FKV_F32 && dtype != FKV_BF16) return FKV_ERR_INVALID_ARG;
+  const int size = dtype == FKV_F32 ? 4 : 2;
+  if (vocab < 1 || vocab > kVerMaxVocab || target_stride < vocab || (draft && draft_stride < vocab)) return FKV_ERR_INVALID_ARG;
+  if (!aligned(target, size) || !aligned(draft, size) || !aligned(u_accept, 4) || !aligned(u_sample, 4)) return FKV_ERR_INVALID_ARG;
+  if (a.lens.tok[c->cfg.max_batch] > 0 && (!target || !u_accept || !u_sample)) return FKV_ERR_INVALID_ARG;
+  a.target = target; a.draft = draft; a.target_stride = target_stride; a.draft_stride = draft_stride;
+  a.tokens = tokens; a.parents = parents; a.u_accept = u_accept; a.u_sample = u_sample;
+  a.path = path; a.path_len = path_len; a.out = tokens_out; a.vocab = vocab; a.stride = path_stride;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (dtype == FKV_F32) return draft ? launch_verify_t<float, true>(c, a, st) : launch_verify_t<float, false>(c, a, st);
+  return draft ? launch_verify_t<__nv_bfloat16, true>(c, a, st) : launch_verify_t<__nv_bfloat16, false>(c, a, st);
+}
+
+int fkv_verify_tree_greedy(fkv_cache *c, const int32_t *tokens, const int32_t *parents, const int32_t *tree_lens, const int32_t *choice,
+                           int32_t *path, int32_t *path_len, int32_t *tokens_out, int32_t path_stride, void *stream) {
+  VerifyArgs a = {};
+  if (int e = check_verify(c, tokens, parents, tree_lens, path, path_len, tokens_out, path_stride, a)) return e;
+  if (a.lens.tok[c->cfg.max_batch] > 0 && (!choice || !aligned(choice, 4))) return FKV_ERR_INVALID_ARG;
+  a.tokens = tokens; a.parents = parents; a.path = path; a.path_len = path_len; a.out = tokens_out; a.stride = path_stride;
+  FKV_CUDA(launch_waiting(k_verify_greedy, dim3(c->cfg.max_batch), 32, 0, (cudaStream_t)stream, c->ctx, a, choice));
+  ++c->launches;
+  return FKV_OK;
+}
+
+int fkv_commit_tree(fkv_cache *c, int layer, const int32_t *tree_lens, const int32_t *path, const int32_t *path_len, int32_t path_stride,
+                    void *stream) {
+  ChunkLens lens;
+  if (!c || (layer != FKV_ALL_LAYERS && !layer_ok(c, layer)) || !tree_lens || !make_lens(c, tree_lens, lens) || !trees_ok(c, tree_lens, 0))
+    return FKV_ERR_INVALID_ARG;
+  if (lens.tok[c->cfg.max_batch] == 0) return FKV_OK;
+  if (!path || !path_len || path_stride < 1 || !aligned(path, 4) || !aligned(path_len, 4)) return FKV_ERR_INVALID_ARG;
+  const int l0 = layer == FKV_ALL_LAYERS ? 0 : layer, nl = layer == FKV_ALL_LAYERS ? c->cfg.num_layers : 1;
+  for (int l = l0; l < l0 + nl; ++l)
+    if (!chunk_is_stored(c, l, tree_lens)) return FKV_ERR_INVALID_ARG;
+  if (nl > 65535) return FKV_ERR_INVALID_ARG;   // (the grid's second dimension)
+  FKV_CUDA(launch_waiting(k_commit_tree, dim3(c->cfg.max_batch, nl), 1024, 0, (cudaStream_t)stream, c->ctx, l0, lens, path, path_len, path_stride));
+  ++c->launches;
+  return FKV_OK;
+}
+
+int fkv_export_chunk(fkv_cache *c, int layer, const int32_t *chunk_lens, void *k, void *v, float *feat, int32_t *pos, void *stream) {
+  ChunkLens lens;
+  if (!c || !layer_ok(c, layer) || !chunk_lens || !make_lens(c, chunk_lens, lens)) return FKV_ERR_INVALID_ARG;
+  if (!chunk_is_stored(c, layer, chunk_lens)) return FKV_ERR_INVALID_ARG;
+  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(feat, 4) || !aligned(pos, 4)) return FKV_ERR_INVALID_ARG;
+  const long long tasks = (long long)lens.tok[c->cfg.max_batch] * c->cfg.num_kv_heads;
+  if (tasks == 0 || (!k && !v && !feat && !pos)) return FKV_OK;
+  const int grid = (int)std::min<long long>((tasks + 7) / 8, 8LL * c->sm_count);
+  FKV_CUDA(launch_waiting(k_export_chunk, dim3(grid), 256, 0, (cudaStream_t)stream, c->ctx, layer, lens, (uint8_t *)k, (uint8_t *)v, feat, pos));
+  ++c->launches;
+  return FKV_OK;
+}
+
+int fkv_fork(fkv_cache *c, const int32_t *from, void *stream) {
+  if (!c || !from) return FKV_ERR_INVALID_ARG;
+  const int batch = c->cfg.max_batch, L = c->cfg.num_layers;
+  for (int s = 0; s < batch; ++s)
+    if (from[s] < -1 || from[s] >= batch) return FKV_ERR_INVALID_ARG;
+  ForkMap m;
+  ForkOps ops;
+  if (!make_fork(c, from, m, ops)) return FKV_OK;
+  cudaStream_t st = (cudaStream_t)stream;
+  FKV_CUDA(launch_waiting(k_fork_plan, dim3(1), 1024, 0, st, c->ctx, m));
+  ++c->launches;
+  FKV_CUDA(launch_waiting(k_fork_copy, dim3(2 * c->sm_count), 256, 0, st, c->ctx, m));
+  ++c->launches;
+  FKV_CUDA(launch_waiting(k_fork_commit, dim3(L * batch), 256, 0, st, c->ctx, m));
+  ++c->launches;
+  if (c->cfg.feature_window > 0) {
+    const size_t words = (size_t)c->ctx.hist_wp * c->cfg.num_kv_heads * c->cfg.group_size * c->cfg.head_dim / 8;
+    FKV_CUDA(launch_waiting(k_fork_record, dim3((unsigned)((words + 255) / 256), L), 256, 0, st, c->ctx, ops));
+    ++c->launches;
+  }
+  int old[kMaxBatch];
+  for (int l = 0; l < L; ++l) {
+    int *h = &c->h_len[(size_t)l * batch];
+    std::copy(h, h + batch, old);
+    for (int s = 0; s < batch; ++s) h[s] = from[s] < 0 ? 0 : old[from[s]];
+  }
+  std::copy(c->h_budget.begin(), c->h_budget.end(), old);
+  for (int s = 0; s < batch; ++s)
+    if (from[s] >= 0) c->h_budget[s] = old[from[s]];
+  return FKV_OK;
 }
 
 int fkv_decode_attn_window(fkv_cache *c, int layer, const void *q, const int32_t *q_pos, int32_t window, int32_t sinks, void *out,

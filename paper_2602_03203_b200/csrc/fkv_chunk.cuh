@@ -47,6 +47,8 @@ constexpr int kChunkRows = 128;       // query rows of a tile = M of the mma
 constexpr int kChunkMinPages = 8;     // least work of a CTA
 constexpr int kChunkInfo = 8;         // words that describe a CTA's unfinished item to the merge
 constexpr float kChunkGrow = 24.f;    // log2 of the growth of a row's maximum that O is rescaled for
+constexpr int kTreeNodes = 256;       // most nodes of a draft tree
+constexpr int kTreeWords = kTreeNodes / 32;   // words of a node's mask: bit i says that it sees node i
 constexpr int kChunkItems = 3;        // items in use: being finished, being worked on, being read ahead
 
 // Prefix sums of the chunk lengths over the sequences, and the pairs that stay (use == 0: all of them).
@@ -67,9 +69,12 @@ struct ChunkKeep {
 // returned together, the whole call is.
 // Bound: bytes (8 D a pair and KV head, read and written); back to back 4.7 us for 5 tokens, 5.3 for 256, 12.7 for 2048 on 8 heads
 // (a launch and four dependent reads: length, page, last position, free stack).
+// TREE: the chunk is a draft tree (kernel 10); a node's position is one behind its parent's, so it follows from the number
+// of its ancestors in `masks`.
+template <bool TREE>
 __global__ void __launch_bounds__(256) k_append_chunk(Ctx c, int layer, const uint8_t *k, const uint8_t *v, const int32_t *pos,
                                                       const __grid_constant__ ChunkLens lens,
-                                                      const __grid_constant__ ChunkKeep keep) {
+                                                      const __grid_constant__ ChunkKeep keep, const uint32_t *masks) {
   static_assert(kMaxBatch <= 256, "one thread per sequence");
   __shared__ int s_scan[33];
   __shared__ int s_keep[kMaxBatch], s_old[kMaxBatch], s_pop[kMaxBatch], s_push[kMaxBatch];
@@ -144,9 +149,10 @@ __global__ void __launch_bounds__(256) k_append_chunk(Ctx c, int layer, const ui
         if (lane == 0 && (slot % kPage == 0 || j == 0)) ptrow[pg] = pid;
       }
       int32_t pdef = j;
+      if (TREE && !pos) pdef = (int)__reduce_add_sync(0xffffffffu, lane < kTreeWords ? __popc(__ldcg(masks + (size_t)row * kTreeWords + lane)) : 0) - 1;
       if (!pos && kp_s > 0) {   // the position after the last pair that stays
         const uint8_t *prev = c.pool + (size_t)__ldcg(ptrow + (kp_s - 1) / kPage) * c.page_bytes;
-        pdef = __ldcg(reinterpret_cast<const int32_t *>(meta_row(c, prev, (kp_s - 1) % kPage)) + c.F) + 1 + j;
+        pdef = __ldcg(reinterpret_cast<const int32_t *>(meta_row(c, prev, (kp_s - 1) % kPage)) + c.F) + 1 + pdef;
       }
       const size_t at = ((size_t)row * c.Hkv + h) * c.D * 2;
       move_row<0>(c, c.pool + (size_t)pid * c.page_bytes, slot % kPage, const_cast<uint8_t *>(k) + at,
@@ -192,6 +198,7 @@ struct ChunkArgs {
   float scale, scale_log2;
   __nv_bfloat16 *out;   // [tokens][Hkv * g][D]
   float *lse;           // [tokens][Hkv * g] or null
+  const uint32_t *masks;   // TREE: [tokens][kTreeWords]
   ChunkLens lens;
 };
 
@@ -202,7 +209,7 @@ struct ChunkItem {
   int row0;        // packed index of the first token
   int ntok[2];     // tokens of the two tiles
   int e0;          // slots up to and with the first token's own
-  int n;           // pairs of the segment
+  int base;        // pairs ahead of the chunk's own
   int a;           // slots [0, a) are sinks
   int pa0, pa1;    // pages of the sinks ...
   int pb0, pb1;    // ... and of the rest that this CTA takes
@@ -379,7 +386,9 @@ __device__ __forceinline__ bool mbar_sleep_warp(uint32_t bar, uint32_t parity) {
   return __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
 }
 
-template <int D>
+// TREE: the chunk is a draft tree.  Its nodes see the pairs ahead of it as the tokens of a chunk do; of the tree's own pairs
+// a node sees those that its mask names, up to its own.
+template <int D, bool TREE>
 __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const __grid_constant__ CUtensorMap tmk,
                                                                    const __grid_constant__ CUtensorMap tmv,
                                                                    const __grid_constant__ CUtensorMap tmq,
@@ -457,6 +466,18 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       for (int i = i0; i < nt; i += step) {
         const int p0 = tl.first(i), cols = tl.pages(i) * kPage;
         const int hi = min(cols, e - p0 * kPage), lo = wlo - p0 * kPage, na = x.a - p0 * kPage;
+        // The tile's bits of the row's mask: ones for pairs ahead of the tree.
+        uint32_t tree[3] = {~0u, ~0u, ~0u};
+        const bool in_tree = TREE && p0 * kPage + cols > x.base;
+        if (TREE && in_tree && live) {
+          const int at = p0 * kPage - x.base, k = at >> 5;
+          const uint32_t *row = a.masks + (size_t)(x.row0 + tj) * kTreeWords;
+          uint32_t w[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) w[j] = k + j < 0 ? ~0u : k + j < kTreeWords ? __ldcg(row + k + j) : 0u;
+#pragma unroll
+          for (int j = 0; j < 3; ++j) tree[j] = __funnelshift_r(w[j], w[j + 1], at & 31);
+        }
         if (!mbar_sleep_warp(smem_u32(&s_full[t]), sp)) { set_status(c, kDevWaitTimeout); ok = false; break; }
         sp ^= 1;
         tc_fence_after();
@@ -479,13 +500,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(smem_u32(&s_empty[t]));
-          if (!__all_sync(0xffffffffu, hi >= SM::kCols && (lo <= 0 || na >= SM::kCols))) {   // hidden scores become -infinity
+          if (!__all_sync(0xffffffffu, hi >= SM::kCols && (lo <= 0 || na >= SM::kCols) && !in_tree)) {   // hidden scores become -infinity
             asm volatile("" ::: "memory");   // (a branch: tiles without an edge should not pay for the comparisons)
 #pragma unroll
             for (int q = 0; q < TP; ++q)
 #pragma unroll
               for (int j = 0; j < 16; ++j)
-                if (q * 16 + j >= hi || (q * 16 + j < lo && q * 16 + j >= na)) v[q][j] = 0xff800000u;
+                if (q * 16 + j >= hi || (q * 16 + j < lo && q * 16 + j >= na) || (TREE && !((tree[q / 2] >> (q % 2 * 16 + j)) & 1u)))
+                  v[q][j] = 0xff800000u;
           }
           // P = 2^(scale s - ms) against the reference m, rounded to bf16 (as V is: at most half a step, 2^-8, off); its sum
           // is not rounded.  The maximum is found on the side: m follows it only when a score has passed m by more than 2^24
@@ -649,7 +671,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       b.j1 = min(b.T, b.j0 + TB);
       b.units = 0;
       if (b.n >= b.T) {
-        b.r = chunk_range(b.n, b.T, b.j0, b.j1, W, S);
+        b.r = chunk_range(b.n, b.T, TREE ? 0 : b.j0, b.j1, W, S);   // (a node may be near the root whatever its place)
         b.units = b.r.units();
       }
       return b;
@@ -715,7 +737,33 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       int pa0 = min(off, b.r.sp), pa1 = min(off + take, b.r.sp);
       int pb0 = b.r.b0 + max(off - b.r.sp, 0), pb1 = b.r.b0 + max(off + take - b.r.sp, 0);
       int na = 0, first = 0;
-      if (W) {
+      if (TREE && W) {
+        const int base = b.n - b.T;
+        // A node's window ends with its own pair and holds its ancestors, all of them (W is at least the number of nodes); where
+        // it begins ahead of the tree follows from its position: first the lowest one's, then the others' as below.
+        na = S ? slot_sinks(c, ptrow, base, S) : 0;
+        int low = INT_MAX;
+        for (int i = lane; i < ntok; i += 32) low = min(low, slot_pos(c, ptrow, e0 - 1 + i));
+        low = __reduce_min_sync(0xffffffffu, low);
+        const int lo0 = max(0, base + 1 - W), start = window_start(low, W);
+        first = lo0 >= base ? base : slot_pos(c, ptrow, lo0) >= start ? lo0 : slot_lower_bound_warp(c, ptrow, lo0 + 1, base, start);
+        __syncwarp();
+        for (int i = lane; i < 256 && first + i < base; i += 32) Pos[i] = slot_pos(c, ptrow, first + i);
+        __syncwarp();
+        for (int i = lane; i < ntok; i += 32) {
+          const int p = slot_pos(c, ptrow, e0 - 1 + i), from = window_start(p, W);
+          int lo = first, hi = (int)min((long long)base, first + (long long)p - low);
+          if (hi - first < 256) {
+            while (lo < hi) {
+              const int mid = (lo + hi) >> 1;
+              if (Pos[mid - first] < from) lo = mid + 1; else hi = mid;
+            }
+          } else {
+            lo = slot_lower_bound(c, ptrow, lo, hi, from);
+          }
+          Wlo[ri * 256 + i] = lo;
+        }
+      } else if (W) {
         na = S ? slot_sinks(c, ptrow, b.n, S) : 0;
         // Where the first token's window begins, then the others': a window that begins d positions later begins at most d
         // slots later, so the positions of those slots decide, read together (a search of its own for a token whose
@@ -740,6 +788,8 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
           }
           Wlo[ri * 256 + i] = lo;
         }
+      }
+      if (W) {
         const int a16 = (na + kPage - 1) / kPage, w16 = first / kPage;
         if (b.r.sp == 0) {   // one run of pages: split it around the hidden ones
           pa0 = pb0;
@@ -758,7 +808,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
         x->head = head; x->seg = seg;
         x->row0 = a.lens.tok[b.s] + b.j0;
         x->ntok[0] = nt0; x->ntok[1] = ntok - nt0;
-        x->e0 = e0; x->n = b.n; x->a = na; x->w0 = first; x->e1 = e0 + ntok - 1;
+        x->e0 = e0; x->base = b.n - b.T; x->a = na; x->w0 = first; x->e1 = e0 + ntok - 1;
         x->pa0 = pa0; x->pa1 = pa1; x->pb0 = pb0; x->pb1 = pb1;
         x->part = part;
         if (part == 1) {   // for the merge, with the last CTA that the item reaches

@@ -1,0 +1,226 @@
+// Kernel 12: every sequence becomes what another one was (fkv_fork), in all layers at once.  Pages hold attention features that
+// each sequence updates for itself, so two sequences never share one: a copy is a copy of the pages.  A sequence that goes away
+// while others become what it was hands its pages to one of them: beams that only change places move page tables.
+//   k_fork_plan     one CTA: the copies' pages, taken from the free stack and, behind those, from the sequences that go away;
+//   k_fork_copy     pages: a warp takes a run of source pages, reads each once and writes up to four copies (more: it reads again);
+//                   new page tables are written aside, since the old ones are being read;
+//   k_fork_commit   tables, lengths and budgets; pages of the sequences that went away return to the stack;
+//   k_fork_record   the decode queries on record, if there is a record: the host's list of copies, element by element, so that
+//                   a cycle needs one register as the place aside.
+// Bound: bytes: every source page read once, every copy written once.
+#pragma once
+#include "fkv_dev.cuh"
+#include "fkv_attend.cuh"
+
+namespace fkv {
+
+enum : unsigned char { FORK_CHANGES = 1, FORK_MOVES = 2, FORK_FREED = 4 };
+struct ForkMap {
+  short from[kMaxBatch];    // -1: empty
+  short first[kMaxBatch];   // the first sequence that gets a copy of this one's pages (-1: none) ...
+  short next[kMaxBatch];    // ... and the next one that gets a copy of the same
+  unsigned char what[kMaxBatch];
+};
+// Copies dst <- src in order; kForkAside is a register.
+constexpr int kForkAside = kMaxBatch;
+struct ForkOps {
+  int n;
+  short dst[kMaxBatch * 3 / 2], src[kMaxBatch * 3 / 2];
+  unsigned char emptied[kMaxBatch];
+};
+// planhdr: PH_NWORK = source pages to read, PH_NEW_PAGES, PH_OLD_PAGES = pages taken and returned, PH_PUSH_START = the stack's top before, or
+// -1 where there are too few pages.  Per (layer, sequence): work = offset of its pages among those taken, tile1_start = among those returned,
+// idx[0 ..] = new length, idx[L batch ..] = offset of its pages among the source pages.
+
+__global__ void __launch_bounds__(1024) k_fork_plan(Ctx c, const __grid_constant__ ForkMap m) {
+  __shared__ int s_scan[33];
+  __shared__ unsigned long long s_need;
+  griddep_wait();
+  griddep_launch();
+  const int LB = c.L * c.batch;
+  int taken = 0, returned = 0, units = 0;
+  if (threadIdx.x == 0) s_need = 0;
+  __syncthreads();
+  for (int base = 0; base < LB; base += blockDim.x) {
+    const int i = base + threadIdx.x;
+    int need = 0, gone = 0, read = 0, len = 0;
+    if (i < LB) {
+      const int s = i % c.batch, l0 = i - s, n = __ldcg(c.len + i), what = m.what[s], r = m.from[s];
+      len = r < 0 ? 0 : __ldcg(c.len + l0 + r);
+      if ((what & FORK_CHANGES) && !(what & FORK_MOVES)) need = (len + kPage - 1) / kPage * c.Hkv;
+      if (what & FORK_FREED) gone = (n + kPage - 1) / kPage * c.Hkv;
+      if (m.first[s] >= 0) read = (n + kPage - 1) / kPage * c.Hkv;
+      if (need) atomicAdd(&s_need, (unsigned long long)need);
+    }
+    int tot;
+    const int a = taken + block_excl_scan(need, s_scan, tot); taken += tot;
+    const int b = returned + block_excl_scan(gone, s_scan, tot); returned += tot;
+    const int u = units + block_excl_scan(read, s_scan, tot); units += tot;
+    if (i < LB) {
+      c.work[i] = a;
+      c.tile1_start[i] = b;
+      c.idx[i] = len;
+      c.idx[LB + i] = u;
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const int top = __ldcg(c.ctrl + CTRL_FREE_TOP);
+    const bool ok = s_need <= (unsigned long long)top + returned;   // (the sums above may have wrapped where this fails)
+    if (!ok) set_status(c, kDevPoolExhausted);
+    c.planhdr[PH_NWORK] = units;
+    c.planhdr[PH_NEW_PAGES] = taken;
+    c.planhdr[PH_OLD_PAGES] = returned;
+    c.planhdr[PH_PUSH_START] = ok ? top : -1;
+  }
+}
+
+// The entry (layer, sequence) whose range of `offsets` holds x: the last one that begins at or before it (by a whole warp).
+__device__ __forceinline__ int fork_entry(const int *offsets, int LB, int x) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, hi = LB;   // offsets[lo] <= x, and offsets[hi] > x if hi < LB
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step;
+    const int k = __popc(__ballot_sync(0xffffffffu, at < hi && __ldcg(offsets + min(at, hi - 1)) <= x));
+    const int l = lo;
+    lo = l + k * step;
+    hi = min(hi, l + (k + 1) * step);
+  }
+  return lo;
+}
+
+__global__ void __launch_bounds__(256) k_fork_copy(Ctx c, const __grid_constant__ ForkMap m) {
+  griddep_wait();
+  griddep_launch();
+  const int top = __ldcg(c.planhdr + PH_PUSH_START);
+  if (top < 0) return;
+  const int LB = c.L * c.batch, lane = threadIdx.x & 31, warps = gridDim.x * (blockDim.x / 32), w = blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32;
+  // Page tables that move.
+  for (int i = w; i < LB; i += warps) {
+    const int s = i % c.batch;
+    if (!(m.what[s] & FORK_MOVES)) continue;
+    const int pages = (__ldcg(c.idx + i) + kPage - 1) / kPage, src = i - s + m.from[s];
+    for (int h = 0; h < c.Hkv; ++h)
+      for (int j = lane; j < pages; j += 32)
+        c.pt_new[((size_t)i * c.Hkv + h) * c.max_pages + j] = __ldcg(c.pt + ((size_t)src * c.Hkv + h) * c.max_pages + j);
+  }
+  // Copies: this warp's run of source pages.
+  const int units = __ldcg(c.planhdr + PH_NWORK), words = c.page_bytes / 16;
+  int u = (int)((long long)units * w / warps);
+  const int u_end = (int)((long long)units * (w + 1) / warps);
+  if (u >= u_end) return;
+  int e = fork_entry(c.idx + LB, LB, u);
+  // The x-th page that the call takes: from the stack's top down, then the ones that go away.
+  auto page_of = [&](int x) {
+    if (x < top) return __ldcg(c.free_stack + top - 1 - x);
+    int lo = 0, hi = LB;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (__ldcg(c.tile1_start + mid) <= x - top) lo = mid; else hi = mid;
+    }
+    const int pages = (__ldcg(c.len + lo) + kPage - 1) / kPage, i = x - top - __ldcg(c.tile1_start + lo), h = i / pages;
+    return __ldcg(c.pt + ((size_t)lo * c.Hkv + h) * c.max_pages + i - h * pages);
+  };
+  while (u < u_end) {
+    // (entries without pages to read begin where the next one does: the last of them is the one that has them)
+    while (e + 1 < LB && __ldcg(c.idx + LB + e + 1) <= u) ++e;
+    const int r = e % c.batch, l0 = e - r, pages = (__ldcg(c.len + e) + kPage - 1) / kPage;
+    const int off = u - __ldcg(c.idx + LB + e), h = off / pages, j0 = off - h * pages;
+    const int take = min(min(32, u_end - u), pages - j0);   // pages j0 .. of one head, a lane each
+    const int src = lane < take ? __ldcg(c.pt + ((size_t)e * c.Hkv + h) * c.max_pages + j0 + lane) : 0;
+    for (int s = m.first[r]; s >= 0;) {   // up to four copies at a time
+      int dst[4], nd = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        dst[k] = 0;
+        if (s < 0) continue;
+        if (lane < take) {
+          dst[k] = page_of(__ldcg(c.work + l0 + s) + off + lane);
+          c.pt_new[((size_t)(l0 + s) * c.Hkv + h) * c.max_pages + j0 + lane] = dst[k];
+        }
+        nd = k + 1;
+        s = m.next[s];
+      }
+      for (int i = 0; i < take; ++i) {
+        const uint4 *from = reinterpret_cast<const uint4 *>(c.pool + (size_t)__shfl_sync(0xffffffffu, src, i) * c.page_bytes);
+        uint4 *to[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) to[k] = reinterpret_cast<uint4 *>(c.pool + (size_t)__shfl_sync(0xffffffffu, dst[k], i) * c.page_bytes);
+        for (int b = lane; b < words; b += 32 * 8) {
+          uint4 x[8];
+#pragma unroll
+          for (int y = 0; y < 8; ++y)
+            if (b + 32 * y < words) x[y] = __ldcs(from + b + 32 * y);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (k < nd)
+#pragma unroll
+              for (int y = 0; y < 8; ++y)
+                if (b + 32 * y < words) __stcs(to[k] + b + 32 * y, x[y]);
+        }
+      }
+    }
+    u += take;
+  }
+}
+
+// grid = layers x sequences.
+__global__ void __launch_bounds__(256) k_fork_commit(Ctx c, const __grid_constant__ ForkMap m) {
+  __shared__ int s_budget[kMaxBatch];
+  griddep_wait();
+  griddep_launch();
+  const int top = __ldcg(c.planhdr + PH_PUSH_START);
+  if (top < 0) return;
+  const int i = blockIdx.x, s = i % c.batch, tid = threadIdx.x, what = m.what[s];
+  const int bottom = top - __ldcg(c.planhdr + PH_NEW_PAGES);
+  if (i == 0) {   // (the budget goes with the sequence; an emptied place keeps its own)
+    if (tid == 0) c.ctrl[CTRL_FREE_TOP] = bottom + c.planhdr[PH_OLD_PAGES];
+    static_assert(kMaxBatch <= 256, "one thread per sequence");
+    if (tid < c.batch) s_budget[tid] = c.budget[tid];
+    __syncthreads();
+    if (tid < c.batch && m.from[tid] >= 0) c.budget[tid] = s_budget[m.from[tid]];
+  }
+  if (!(what & FORK_CHANGES)) return;
+  const int n = c.len[i], n_new = c.idx[i], cnt_old = (n + kPage - 1) / kPage, cnt_new = (n_new + kPage - 1) / kPage;
+  if (what & FORK_FREED) {   // (those that would go below the stack's bottom are the ones that were taken again)
+    const int at = bottom + c.tile1_start[i];
+    for (int x = tid; x < cnt_old * c.Hkv; x += blockDim.x) {
+      const int h = x / cnt_old;
+      if (at + x >= 0) c.free_stack[at + x] = c.pt[((size_t)i * c.Hkv + h) * c.max_pages + x - h * cnt_old];
+    }
+  }
+  __syncthreads();
+  for (int x = tid; x < cnt_new * c.Hkv; x += blockDim.x) {
+    const int h = x / cnt_new;
+    const size_t at = ((size_t)i * c.Hkv + h) * c.max_pages + x - h * cnt_new;
+    c.pt[at] = c.pt_new[at];
+  }
+  if (tid == 0) c.len[i] = n_new;
+}
+
+// grid (enough threads for a sequence's record in 16-byte words, layers).  Runs behind k_fork_commit (nothing there reads the record).
+__global__ void __launch_bounds__(256) k_fork_record(Ctx c, const __grid_constant__ ForkOps ops) {
+  griddep_wait();
+  griddep_launch();
+  if (__ldcg(c.planhdr + PH_PUSH_START) < 0) return;
+  const int layer = blockIdx.y, ls0 = layer * c.batch, heads = c.Hkv * c.G;
+  const size_t t = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
+  auto run = [&](auto *all, size_t per) {   // the layer's arrays of `per` elements per sequence: element t of each
+    if (t >= per) return;
+    auto *at = all + (size_t)ls0 * per + t;
+    auto aside = at[0];
+    for (int i = 0; i < ops.n; ++i) {
+      const auto x = ops.src[i] == kForkAside ? aside : at[ops.src[i] * per];
+      if (ops.dst[i] == kForkAside) aside = x; else at[ops.dst[i] * per] = x;
+    }
+  };
+  run(reinterpret_cast<uint4 *>(c.hist_q), (size_t)c.hist_wp * heads * c.D / 8);
+  run(c.hist_mp, (size_t)c.hist_wp * heads);
+  run(c.hist_n, (size_t)c.hist_w);
+  run(c.hist_cnt, (size_t)1);
+  if (t == 0)
+    for (int s = 0; s < c.batch; ++s)
+      if (ops.emptied[s]) c.hist_cnt[ls0 + s] = 0;
+}
+
+}  // namespace fkv

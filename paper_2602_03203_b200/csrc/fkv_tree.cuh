@@ -1,0 +1,158 @@
+// Kernel 10: draft trees around the attention (k_append_chunk<true>, k_chunk_attend<D, true>): masks from parents, the accepted
+// path moved together, and the read-out of a chunk.
+#pragma once
+#include "fkv_dev.cuh"
+#include "fkv_attend.cuh"
+#include "fkv_chunk.cuh"
+
+namespace fkv {
+
+// ---------------------------------------------------------------- masks
+// mask(j) = {j} u mask(parent(j)), by doubling: after round r a node's mask holds its 2^r nearest ancestors and its pointer the next
+// one, so the rounds are log2 of the depth.  grid = sequences, a thread per node.  A parent that does not come before its node is an
+// error: the node becomes a root.  Bound: latency (a launch, one read, a few rounds in shared memory).
+__global__ void __launch_bounds__(kTreeNodes) k_tree_masks(Ctx c, const __grid_constant__ ChunkLens lens, const int32_t *parents, uint32_t *masks) {
+  __shared__ uint32_t m[2][kTreeWords][kTreeNodes];
+  __shared__ short up[2][kTreeNodes];
+  griddep_wait();
+  griddep_launch();
+  const int row0 = lens.tok[blockIdx.x], T = lens.tok[blockIdx.x + 1] - row0, j = threadIdx.x;
+  if (T == 0) return;
+  int p = -1;
+  if (j < T) {
+    p = __ldcg(parents + row0 + j);
+    if (p < -1 || p >= j) { set_status(c, kDevBadIndex); p = -1; }
+  }
+  uint32_t own[kTreeWords];
+#pragma unroll
+  for (int w = 0; w < kTreeWords; ++w) own[w] = w == j / 32 ? 1u << (j & 31) : 0u;
+  for (int r = 0; __syncthreads_or(p >= 0); r ^= 1) {   // (the barrier also ends the reads of this half two rounds ago)
+#pragma unroll
+    for (int w = 0; w < kTreeWords; ++w) m[r][w][j] = own[w];
+    up[r][j] = (short)p;
+    __syncthreads();
+    if (p >= 0) {
+#pragma unroll
+      for (int w = 0; w < kTreeWords; ++w) own[w] |= m[r][w][p];
+      p = up[r][p];
+    }
+  }
+  if (j < T) {
+    uint4 *out = reinterpret_cast<uint4 *>(masks + (size_t)(row0 + j) * kTreeWords);
+    out[0] = make_uint4(own[0], own[1], own[2], own[3]);
+    out[1] = make_uint4(own[4], own[5], own[6], own[7]);
+  }
+}
+
+// ---------------------------------------------------------------- the accepted path
+// grid (sequences, layers), 32 warps: of a sequence's last T pairs, the tree's, those of path[0 .. cnt) (ascending) move to the
+// places behind the pairs ahead of the tree; the length follows and the pages behind are returned.
+// A pair never moves up (path[i] >= i), and its place may be another's source: 128 / Hkv places of every head are read into
+// registers, then written, then the next ones (whose sources lie behind all places written so far).
+// Bound: latency (a launch, length and path, page ids, rows); bytes are those of the moved pairs, read and written.
+__global__ void __launch_bounds__(1024) k_commit_tree(Ctx c, int l0, const __grid_constant__ ChunkLens lens, const int32_t *path,
+                                                      const int32_t *path_len, int stride) {
+  __shared__ int s_path[kTreeNodes];
+  __shared__ int s_push;
+  griddep_wait();
+  griddep_launch();
+  const int seq = blockIdx.x, layer = l0 + blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int T = lens.tok[seq + 1] - lens.tok[seq], ls = layer * c.batch + seq;
+  if (T == 0) return;
+  const int n = __ldcg(c.len + ls), cnt = __ldcg(path_len + seq), base = n - T;
+  bool bad = base < 0 || cnt < 0 || cnt > T || cnt > stride;
+  bool moved = false;
+  if (!bad && tid < cnt) {
+    const int p = __ldcg(path + (size_t)seq * stride + tid), before = tid > 0 ? __ldcg(path + (size_t)seq * stride + tid - 1) : -1;
+    bad = p <= before || p >= T;
+    moved = p != tid;
+    s_path[tid] = p;
+  }
+  if (__syncthreads_or(bad)) {
+    if (tid == 0) set_status(c, kDevBadIndex);
+    return;
+  }
+  const int first = cnt - __syncthreads_count(moved);   // (once a pair moves, so do all behind it)
+  const int per = max(1, 128 / c.Hkv), W = c.F + 1;
+  for (int i0 = first; i0 < cnt; i0 += per) {
+    const int tasks = min(per, cnt - i0) * c.Hkv;
+    uint4 kv[4];
+    uint32_t meta[4][2];
+    auto place = [&](int t, int slot, int &r) {   // page and row of a slot of the task's head
+      r = slot % kPage;
+      return c.pool + (size_t)__ldcg(c.pt + (size_t)seg_of(c, layer, seq, t % c.Hkv) * c.max_pages + slot / kPage) * c.page_bytes;
+    };
+    auto chunk = [&](int r) { return lane < c.D / 8 ? kv_chunk_off(r, lane, c.D) : c.off_v + kv_chunk_off(r, lane - c.D / 8, c.D); };
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int t = warp + 32 * u;
+      if (t >= tasks) continue;
+      int r;
+      const uint8_t *page = place(t, base + s_path[i0 + t / c.Hkv], r);
+      if (lane < c.D / 4) kv[u] = __ldcg(reinterpret_cast<const uint4 *>(page + chunk(r)));
+      const uint32_t *row = reinterpret_cast<const uint32_t *>(meta_row(c, page, r));
+      if (lane < W) meta[u][0] = __ldcg(row + lane);
+      if (lane + 32 < W) meta[u][1] = __ldcg(row + lane + 32);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int t = warp + 32 * u;
+      if (t >= tasks) continue;
+      int r;
+      uint8_t *page = place(t, base + i0 + t / c.Hkv, r);
+      if (lane < c.D / 4) *reinterpret_cast<uint4 *>(page + chunk(r)) = kv[u];
+      uint32_t *row = reinterpret_cast<uint32_t *>(meta_row(c, page, r));
+      if (lane < W) row[lane] = meta[u][0];
+      if (lane + 32 < W) row[lane + 32] = meta[u][1];
+    }
+    __syncthreads();
+  }
+  // Pages behind the path go back to the stack (only pushes happen here; their order does not matter).
+  const int kept = (base + cnt + kPage - 1) / kPage, gone = (n + kPage - 1) / kPage - kept;
+  if (tid == 0) {
+    if (gone > 0) s_push = atomicAdd(&c.ctrl[CTRL_FREE_TOP], gone * c.Hkv);
+    c.len[ls] = base + cnt;
+    if (c.hist_w) {   // decode queries that saw pairs of the tree leave the record (see k_append_chunk)
+      const int cnt0 = c.hist_cnt[ls];
+      int q = cnt0;
+      while (q > 0 && q > cnt0 - c.hist_w && c.hist_n[(size_t)ls * c.hist_w + (q - 1) % c.hist_w] > base) --q;
+      c.hist_cnt[ls] = (q < cnt0 && cnt0 > c.hist_w) ? 0 : q;
+    }
+  }
+  __syncthreads();
+  for (int i = tid; i < gone * c.Hkv; i += blockDim.x) {
+    const int h = i / gone;
+    c.free_stack[s_push + i] = c.pt[(size_t)seg_of(c, layer, seq, h) * c.max_pages + kept + i - h * gone];
+  }
+}
+
+// ---------------------------------------------------------------- read-out
+// The last lens[s] pairs of every sequence, packed: the inverse of k_append_chunk.  A warp per pair and head.
+// Bound: bytes (read and written).
+__global__ void __launch_bounds__(256) k_export_chunk(Ctx c, int layer, const __grid_constant__ ChunkLens lens, uint8_t *k, uint8_t *v,
+                                                      float *feat, int32_t *pos) {
+  griddep_wait();
+  griddep_launch();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long tasks = (long long)lens.tok[c.batch] * c.Hkv;
+  for (long long t = (long long)blockIdx.x * 8 + warp; t < tasks; t += (long long)gridDim.x * 8) {
+    const int row = (int)(t / c.Hkv), h = (int)(t - (long long)row * c.Hkv);
+    int lo = 0, hi = c.batch;   // the sequence of the row: the last one that starts at or before it
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (lens.tok[mid] <= row) lo = mid; else hi = mid;
+    }
+    const int n = __ldcg(c.len + layer * c.batch + lo), T = lens.tok[lo + 1] - lens.tok[lo], slot = n - T + row - lens.tok[lo];
+    if (n < T) {
+      if (lane == 0 && h == 0 && row == lens.tok[lo]) set_status(c, kDevBadIndex);
+      continue;
+    }
+    uint8_t *page = c.pool + (size_t)__ldcg(c.pt + (size_t)seg_of(c, layer, lo, h) * c.max_pages + slot / kPage) * c.page_bytes;
+    const size_t at = (size_t)row * c.Hkv + h;
+    move_row<1>(c, page, slot % kPage, k ? k + at * c.D * 2 : nullptr, v ? v + at * c.D * 2 : nullptr, feat ? feat + at * c.F : nullptr,
+                pos ? pos + at : nullptr, lane, 0);
+  }
+}
+
+}  // namespace fkv
