@@ -29,6 +29,7 @@
 #include "fkv_score.cuh"
 #include "fkv_select.cuh"
 #include "fkv_tree.cuh"
+#include "fkv_tree_attend.cuh"
 #include "fkv_verify.cuh"
 
 using namespace fkv;
@@ -160,6 +161,7 @@ struct fkv_cache {
   uint64_t launches = 0;
   int sm_count = 148;
   int max_cluster[2] = {0, 0};   // largest attention cluster the device places (found at the first stand-alone launch): plain, windowed
+  int tree_clusters[2][4][kTaMaxCluster + 1] = {};   // clusters of 1 .. 16 tree CTAs that fit the device, by append's head dim and rows (0: not asked yet)
   float feature_scale = 0.f;  // softmax scale of the recorded queries (the last decode call's)
   bool timing = false, timed = false;
   CUtensorMap page_parts;     // ... as [page][64-channel part][row][64 channels]
@@ -718,6 +720,113 @@ bool trees_ok(const fkv_cache *c, const int32_t *tree_lens, int window) {
   return true;
 }
 
+// Small trees in one launch (k_tree_attend).  S: CTAs per segment.
+template <int D, int RW>
+int launch_tree_t(fkv_cache *c, const TreeArgs &a, int S, cudaStream_t st) {
+  constexpr size_t smem = TaSmem<D, RW>::bytes();
+  static_assert(smem + sizeof(TreeStore) <= kMaxSmem, "one CTA's shared memory");
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(S, c->cfg.max_batch * c->cfg.num_kv_heads);
+  cfg.blockDim = dim3(kTaThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = S; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  FKV_CUDA(cudaLaunchKernelEx(&cfg, k_tree_attend<D, RW>, c->ctx, a));
+  ++c->launches;
+  return FKV_OK;
+}
+// How many clusters of S CTAs the device holds at a time (at least 1 is said of S = 1); asked once per handle.
+template <int D, int RW>
+int tree_clusters_t(int S) {
+  constexpr size_t smem = TaSmem<D, RW>::bytes();
+  auto kern = k_tree_attend<D, RW>;
+  static SmemOptIn opt_in;
+  if (opt_in.ensure(kern, smem) != cudaSuccess || cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return -1;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(S, 1);
+  cfg.blockDim = dim3(kTaThreads);
+  cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = S; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  int n = 0;
+  const bool ok = cudaOccupancyMaxActiveClusters(&n, kern, &cfg) == cudaSuccess && n > 0;
+  (void)cudaGetLastError();
+  return ok ? n : -1;
+}
+template <int D>
+int tree_clusters(int rw, int S) {
+  return rw == 0 ? tree_clusters_t<D, 1>(S) : rw == 1 ? tree_clusters_t<D, 2>(S) : rw == 2 ? tree_clusters_t<D, 4>(S) : tree_clusters_t<D, 8>(S);
+}
+template <int D>
+int launch_tree(fkv_cache *c, const TreeArgs &a, int rw, int S, cudaStream_t st) {
+  return rw == 0 ? launch_tree_t<D, 1>(c, a, S, st) : rw == 1 ? launch_tree_t<D, 2>(c, a, S, st)
+         : rw == 2 ? launch_tree_t<D, 4>(c, a, S, st) : launch_tree_t<D, 8>(c, a, S, st);
+}
+
+// CTAs per segment with which k_tree_attend serves the call, and the form by its rows (rw); 0: the general kernels are to.
+// ahead: pairs ahead of every tree.
+int small_tree(fkv_cache *c, const int32_t *tree_lens, const int *ahead, int &rw) {
+  const int batch = c->cfg.max_batch, Hkv = c->cfg.num_kv_heads;
+  int longest = 0, segs = 0, most = 0;
+  long long total = 0;
+  for (int s = 0; s < batch; ++s) {
+    if (tree_lens[s] == 0) continue;
+    const int pages = (ahead[s] + tree_lens[s] + kPage - 1) / kPage;
+    longest = std::max(longest, tree_lens[s]);
+    most = std::max(most, pages);
+    total += (long long)pages * Hkv;
+    segs += Hkv;
+  }
+  const int rows = longest * c->cfg.group_size;
+  if (segs == 0 || rows > kTaRows || segs > c->sm_count) return 0;
+  rw = rows <= 16 ? 0 : rows <= 32 ? 1 : rows <= 64 ? 2 : 3;
+  int S = std::min(std::min(kTaMaxCluster, c->sm_count / segs), std::max(1, most / kAttendMinPages));
+  for (; S > 0; --S) {   // the largest cluster of which the device holds all at once
+    int &fit = c->tree_clusters[c->cfg.head_dim == 128][rw][S];
+    if (fit == 0) fit = c->cfg.head_dim == 128 ? tree_clusters<128>(rw, S) : tree_clusters<64>(rw, S);
+    if (fit >= segs) break;
+  }
+  if (S == 0) return 0;
+  // The general kernels share the pages evenly over the SMs but take some 20 us longer to start and to join; a page takes an SM
+  // about 0.2 us.
+  return (most + S - 1) / S <= total / c->sm_count + 80 ? S : 0;
+}
+
+int launch_small_tree(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos, const int32_t *keep_lens,
+                      const int32_t *tree_lens, const ChunkLens &lens, const uint32_t *masks, const void *q, float scale, void *out, float *lse,
+                      int rw, int S, cudaStream_t st) {
+  const int batch = c->cfg.max_batch, D = c->cfg.head_dim;
+  TreeArgs a;
+  a.layer = layer; a.append = k != nullptr;
+  a.scale_log2 = (scale == 0.f ? 1.f / sqrtf((float)D) : scale) * 1.4426950408889634f;
+  a.q = (const __nv_bfloat16 *)q; a.out = (__nv_bfloat16 *)out; a.lse = lse; a.masks = masks;
+  a.k = (const uint8_t *)k; a.v = (const uint8_t *)v; a.pos = pos; a.lens = lens;
+  a.keep = ChunkKeep{};
+  if (keep_lens) {
+    a.keep.use = 1;
+    for (int s = 0; s < batch; ++s) a.keep.keep[s] = keep_lens[s];
+  }
+  if (int e = D == 128 ? launch_tree<128>(c, a, rw, S, st) : launch_tree<64>(c, a, rw, S, st)) return e;
+  if (a.append)
+    for (int s = 0; s < batch; ++s) {
+      int &n = c->h_len[(size_t)layer * batch + s];
+      n = (keep_lens ? keep_lens[s] : n) + tree_lens[s];
+    }
+  return FKV_OK;
+}
+
 // A cluster of CTAs per sequence: as many as keep the card at about one CTA per SM, so that a single sequence's rows are read by
 // eight SMs and a large batch's by all of them.
 template <class T, bool Q>
@@ -1265,6 +1374,12 @@ int fkv_tree_attn(fkv_cache *c, int layer, const void *q, const int32_t *tree_le
   if (int e = check_tree(c, tree_lens, lens, masks, window)) return e;
   if (lens.tok[c->cfg.max_batch] > 0 && (!out || !aligned(out, 16) || !aligned(lse_out, 4))) return FKV_ERR_INVALID_ARG;
   if (!chunk_is_stored(c, layer, tree_lens)) return FKV_ERR_INVALID_ARG;
+  if (window == 0) {
+    int ahead[kMaxBatch], rw;
+    for (int s = 0; s < c->cfg.max_batch; ++s) ahead[s] = c->h_len[(size_t)layer * c->cfg.max_batch + s] - tree_lens[s];
+    if (const int S = small_tree(c, tree_lens, ahead, rw))
+      return launch_small_tree(c, layer, nullptr, nullptr, nullptr, nullptr, tree_lens, lens, masks, q, scale, out, lse_out, rw, S, (cudaStream_t)stream);
+  }
   return launch_chunk_attend(c, layer, q, tree_lens, lens, window, sinks, scale, out, lse_out, masks, (cudaStream_t)stream);
 }
 
@@ -1276,6 +1391,12 @@ int fkv_append_tree_attn(fkv_cache *c, int layer, const void *k, const void *v, 
   if (int e = check_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens)) return e;
   if (int e = check_tree(c, tree_lens, lens, masks, window)) return e;
   if (lens.tok[c->cfg.max_batch] > 0 && (!out || !aligned(out, 16) || !aligned(lse_out, 4))) return FKV_ERR_INVALID_ARG;
+  if (window == 0) {
+    int ahead[kMaxBatch], rw;
+    for (int s = 0; s < c->cfg.max_batch; ++s) ahead[s] = keep_lens ? keep_lens[s] : c->h_len[(size_t)layer * c->cfg.max_batch + s];
+    if (const int S = small_tree(c, tree_lens, ahead, rw))
+      return launch_small_tree(c, layer, k, v, pos, keep_lens, tree_lens, lens, masks, q, scale, out, lse_out, rw, S, (cudaStream_t)stream);
+  }
   if (int e = ensure_page_rows_map(c)) return e;   // (what can fail does so before anything is stored)
   if (int e = launch_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens, masks, (cudaStream_t)stream)) return e;
   return launch_chunk_attend(c, layer, q, tree_lens, lens, window, sinks, scale, out, lse_out, masks, (cudaStream_t)stream);
