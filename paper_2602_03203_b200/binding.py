@@ -6,6 +6,7 @@ library has not been built, or no CUDA device is present, calls raise.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import operator
 import os
@@ -138,6 +139,11 @@ def _stream():
     if _raw_stream is not None:
         return ctypes.c_void_p(_raw_stream(torch.cuda.current_device()))
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+def _stream_on(dev):
+    """The current stream of a device, as an address."""
+    return _raw_stream(dev.index) if _raw_stream is not None else torch.cuda.current_stream(dev).cuda_stream
 
 
 class Cache:
@@ -332,8 +338,7 @@ class Cache:
         total, c = sum(chunk_lens), self.cfg
         for name, t in tensors.items():
             heads = c.num_kv_heads * (1 if name in ("k", "v") else c.group_size)
-            want = ((total, heads) if name == "lse" else (total,) if name in ("pos", "parents") else
-                    (total, TREE_WORDS) if name == "masks" else (total, heads, c.head_dim))
+            want = (total, heads) if name == "lse" else (total,) if name == "pos" else (total, heads, c.head_dim)
             if t is not None and tuple(t.shape) != want:
                 raise ValueError(f"{name}: expected shape {want}, got {tuple(t.shape)}")
         self._check_place(*tensors.values())
@@ -392,134 +397,170 @@ class Cache:
         _check(lib().fkv_export_features(self._h, layer, seq, _ptr(out, torch.float32), _stream()), "fkv_export_features")
         return out
 
-    # -- draft trees: nodes are packed like the tokens of a chunk, parents ahead of their children, node 0 the root
+    # -- draft trees: nodes are packed like the tokens of a chunk, parents ahead of their children, node 0 the root.  These calls
+    # come once per layer and step and their kernels take ten microseconds: a tensor is checked and turned into an address in one go.
+    def _here(self):
+        """The cache's device, which has to be the current one."""
+        dev = self.workspace.device
+        if torch.cuda.current_device() != dev.index:
+            raise ValueError(f"the cache is on {dev}, the current device is cuda:{torch.cuda.current_device()}")
+        return dev
+
+    @staticmethod
+    def _at(name, t, dtype, shape, dev):
+        """The address of a contiguous tensor of this type and shape on the cache's device."""
+        if t.shape != shape or t.dtype is not dtype or t.device != dev or not t.is_contiguous():
+            raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}, got {t.dtype} "
+                             f"{tuple(t.shape)} on {t.device}, contiguous={t.is_contiguous()}")
+        return t.data_ptr()
+
+    def _per_sequence(self, x, what):
+        """One 32-bit integer per sequence as the host array that the library reads: (array to keep alive, address)."""
+        if len(x) != self.cfg.max_batch:
+            raise ValueError(f"{what}: expected {self.cfg.max_batch} entries, one per sequence, got {len(x)}")
+        try:
+            a = array.array("i", x)
+        except OverflowError:
+            raise ValueError(f"{what}: {[i for i in x if not -2 ** 31 <= i < 2 ** 31]} does not fit 32 bits") from None
+        return a, a.buffer_info()[0]
+
     def tree_masks(self, parents, tree_lens, out=None):
         """Which nodes of its tree every node sees, its ancestors and itself, as bits: int32 [nodes][8].  parents [nodes] int32: the
         parent's index inside the tree, -1 for a root."""
+        dev = self._here()
+        total = sum(tree_lens)
+        keep, lens = self._per_sequence(tree_lens, "tree_lens")
         if out is None:
-            out = torch.empty((parents.shape[0], TREE_WORDS), dtype=torch.int32, device=parents.device)
-        self._check_chunk(tree_lens, parents=parents, masks=out)
-        _check(lib().fkv_tree_masks(self._h, _ptr(parents, torch.int32), _lens(tree_lens, self.cfg.max_batch, "tree_lens"),
-                                    _ptr(out, torch.int32), _stream()), "fkv_tree_masks")
+            out = torch.empty((total, TREE_WORDS), dtype=torch.int32, device=dev)
+        _check(lib().fkv_tree_masks(self._h, self._at("parents", parents, torch.int32, (total,), dev), lens,
+                                    self._at("masks", out, torch.int32, (total, TREE_WORDS), dev), _stream_on(dev)), "fkv_tree_masks")
         return out
+
+    def _tree(self, layer, k, v, q, tree_lens, masks, pos, keep_lens, window, sinks, out, lse, scale):
+        """The three calls of trees: without q the store alone, without k the attention alone."""
+        _check_i32(layer=layer, window=window, sinks=sinks)
+        dev = self._here()
+        c, at, bf16 = self.cfg, self._at, torch.bfloat16
+        total, heads, dim = sum(tree_lens), c.num_kv_heads, c.head_dim
+        keep0, lens = self._per_sequence(tree_lens, "tree_lens")
+        seen = at("masks", masks, torch.int32, (total, TREE_WORDS), dev)
+        store = attend = ()
+        if k is not None:
+            kv = (total, heads, dim)
+            keep1, kept = (None, None) if keep_lens is None else self._per_sequence(keep_lens, "keep_lens")
+            store = (at("k", k, bf16, kv, dev), at("v", v, bf16, kv, dev),
+                     None if pos is None else at("pos", pos, torch.int32, (total,), dev), kept)
+        if q is not None:
+            rows = (total, heads * c.group_size, dim)
+            if out is None:
+                out = torch.empty_like(q)
+            attend = (window, sinks, scale, at("out", out, bf16, rows, dev),
+                      None if lse is None else at("lse", lse, torch.float32, rows[:2], dev))
+            query = at("q", q, bf16, rows, dev)
+            if k is None:
+                _check(lib().fkv_tree_attn(self._h, layer, query, lens, seen, *attend, _stream_on(dev)), "fkv_tree_attn")
+            else:
+                _check(lib().fkv_append_tree_attn(self._h, layer, *store, lens, seen, query, *attend, _stream_on(dev)),
+                       "fkv_append_tree_attn")
+            return out
+        _check(lib().fkv_append_tree(self._h, layer, *store, lens, seen, _stream_on(dev)), "fkv_append_tree")
 
     def append_tree(self, layer, k, v, tree_lens, masks, pos=None, keep_lens=None):
         """append_chunk for the nodes of draft trees (a node's position is one behind its parent's)."""
-        _check_i32(layer=layer)
-        self._check_chunk(tree_lens, k=k, v=v, pos=pos, masks=masks)
-        lens, keep = _lens(tree_lens, self.cfg.max_batch, "tree_lens"), _lens(keep_lens, self.cfg.max_batch, "keep_lens")
-        _check(lib().fkv_append_tree(self._h, layer, _ptr(k, torch.bfloat16), _ptr(v, torch.bfloat16), _ptr(pos, torch.int32), keep,
-                                     lens, _ptr(masks, torch.int32), _stream()), "fkv_append_tree")
+        self._tree(layer, k, v, None, tree_lens, masks, pos, keep_lens, 0, 0, None, None, 0.0)
 
     def tree_attn(self, layer, q, tree_lens, masks, window=0, sinks=0, out=None, lse=None, scale=0.0):
         """chunk_attn for the nodes of draft trees: over the pairs ahead of the tree and those of it that the masks name."""
-        _check_i32(layer=layer, window=window, sinks=sinks)
-        if out is None:
-            out = torch.empty_like(q)
-        self._check_chunk(tree_lens, q=q, out=out, lse=lse, masks=masks)
-        _check(lib().fkv_tree_attn(self._h, layer, _ptr(q, torch.bfloat16), _lens(tree_lens, self.cfg.max_batch, "tree_lens"),
-                                   _ptr(masks, torch.int32), window, sinks, scale, _ptr(out, torch.bfloat16),
-                                   _ptr(lse, torch.float32), _stream()), "fkv_tree_attn")
-        return out
+        return self._tree(layer, None, None, q, tree_lens, masks, None, None, window, sinks, out, lse, scale)
 
     def append_tree_attn(self, layer, k, v, q, tree_lens, masks, pos=None, keep_lens=None, window=0, sinks=0, out=None, lse=None,
                          scale=0.0):
         """append_tree(k, v) then tree_attn(q) in one call."""
-        _check_i32(layer=layer, window=window, sinks=sinks)
-        if out is None:
-            out = torch.empty_like(q)
-        self._check_chunk(tree_lens, k=k, v=v, q=q, out=out, lse=lse, pos=pos, masks=masks)
-        lens, keep = _lens(tree_lens, self.cfg.max_batch, "tree_lens"), _lens(keep_lens, self.cfg.max_batch, "keep_lens")
-        _check(lib().fkv_append_tree_attn(self._h, layer, _ptr(k, torch.bfloat16), _ptr(v, torch.bfloat16), _ptr(pos, torch.int32),
-                                          keep, lens, _ptr(masks, torch.int32), _ptr(q, torch.bfloat16), window, sinks, scale,
-                                          _ptr(out, torch.bfloat16), _ptr(lse, torch.float32), _stream()), "fkv_append_tree_attn")
-        return out
+        return self._tree(layer, k, v, q, tree_lens, masks, pos, keep_lens, window, sinks, out, lse, scale)
 
-    def _verified(self, tree_lens, out, device, **nodes):
-        """The checked inputs' results: path [batch][nodes], path_len [batch] and tokens [batch][nodes], int32."""
-        batch, total = self.cfg.max_batch, sum(tree_lens)
-        for name, t in nodes.items():
-            if t is not None and tuple(t.shape) != (total,):
-                raise ValueError(f"{name}: expected shape {(total,)}, got {tuple(t.shape)}")
+    def _found(self, tree_lens, out, dev):
+        """The results of a verification: path [batch][n], path_len [batch], tokens [batch][n], int32, and their addresses."""
+        batch, i32 = self.cfg.max_batch, torch.int32
         if out is None:
             width = max(1, max(tree_lens))
-            out = tuple(torch.empty(s, dtype=torch.int32, device=device) for s in ((batch, width), (batch,), (batch, width)))
+            both = torch.empty((2, batch, width), dtype=i32, device=dev)
+            out = (both[0], torch.empty((batch,), dtype=i32, device=dev), both[1])
         path, path_len, tokens = out
-        if path.dim() != 2 or path.shape[0] != batch or tokens.shape != path.shape or tuple(path_len.shape) != (batch,):
-            raise ValueError(f"out: expected shapes ({batch}, n), ({batch},), ({batch}, n), got {[tuple(t.shape) for t in out]}")
-        self._check_place(*nodes.values(), *out)
-        return out
+        if path.dim() != 2:
+            raise ValueError(f"path: expected two dimensions, got {tuple(path.shape)}")
+        shape = (batch, path.shape[1])
+        return out, (self._at("path", path, i32, shape, dev), self._at("path_len", path_len, i32, shape[:1], dev),
+                     self._at("tokens", tokens, i32, shape, dev), shape[1])
 
     def verify_tree(self, tokens, parents, tree_lens, target, u_accept, u_sample, draft=None, out=None):
         """Which drafts stand and the token after them (speculative sampling with the caller's uniform numbers).  target and draft
         [nodes][vocab] fp32 or bf16, the probabilities of the token after every node (draft None: the drafts are the draft head's
         choice, not samples); tokens, parents [nodes] int32, u_accept [nodes], u_sample [batch] fp32.
         Returns (path [batch][n], path_len [batch], tokens [batch][n]) with n = the longest tree."""
-        lens = _lens(tree_lens, self.cfg.max_batch, "tree_lens")
-        path, path_len, given = self._verified(tree_lens, out, tokens.device, tokens=tokens, parents=parents, u_accept=u_accept)
-        total, dtype = sum(tree_lens), target.dtype
-        if dtype not in (torch.float32, torch.bfloat16):
+        dev = self._here()
+        keep, lens = self._per_sequence(tree_lens, "tree_lens")
+        total, dtype, at = sum(tree_lens), target.dtype, self._at
+        if dtype is not torch.float32 and dtype is not torch.bfloat16:
             raise ValueError(f"target: expected float32 or bfloat16, got {dtype}")
-        rows = []
+        if target.dim() != 2:
+            raise ValueError(f"target: expected two dimensions, got {tuple(target.shape)}")
+        rows, shape = [], (total, target.shape[1])
         for name, t in (("target", target), ("draft", draft)):
             if t is None:
-                rows += [None, 0]
+                rows += (None, 0)
                 continue
-            if t.dim() != 2 or t.shape[0] != total or t.shape[1] != target.shape[1] or t.dtype is not dtype:
-                raise ValueError(f"{name}: expected {dtype} [{total}][vocab], got {t.dtype} {tuple(t.shape)}")
-            if t.numel() and t.stride(1) != 1 and t.shape[1] > 1:
+            if t.shape != shape or t.dtype is not dtype or t.device != dev:
+                raise ValueError(f"{name}: expected {dtype} {shape} on {dev}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+            step, one = t.stride()
+            if one != 1 and shape[1] > 1 and total:
                 raise ValueError(f"{name}: a row's elements must be next to one another")
-            rows += [ctypes.c_void_p(t.data_ptr()), max(t.stride(0), t.shape[1]) if total < 2 else t.stride(0)]
-        if tuple(u_sample.shape) != (self.cfg.max_batch,):
-            raise ValueError(f"u_sample: expected shape {(self.cfg.max_batch,)}, got {tuple(u_sample.shape)}")
-        self._check_place(target, draft, u_sample)
-        _check(lib().fkv_verify_tree(self._h, _ptr(tokens, torch.int32), _ptr(parents, torch.int32), lens, *rows,
-                                     0 if dtype is torch.float32 else 1, target.shape[1], _ptr(u_accept, torch.float32),
-                                     _ptr(u_sample, torch.float32), _ptr(path, torch.int32), _ptr(path_len, torch.int32),
-                                     _ptr(given, torch.int32), path.shape[1], _stream()), "fkv_verify_tree")
-        return path, path_len, given
+            rows += (t.data_ptr(), step if total > 1 else shape[1])
+        out, found = self._found(tree_lens, out, dev)
+        _check(lib().fkv_verify_tree(self._h, at("tokens", tokens, torch.int32, (total,), dev), at("parents", parents, torch.int32, (total,), dev),
+                                     lens, *rows, 0 if dtype is torch.float32 else 1, shape[1],
+                                     at("u_accept", u_accept, torch.float32, (total,), dev),
+                                     at("u_sample", u_sample, torch.float32, (self.cfg.max_batch,), dev), *found, _stream_on(dev)), "fkv_verify_tree")
+        return out
 
     def verify_tree_greedy(self, tokens, parents, tree_lens, choice, out=None):
         """verify_tree at temperature 0: choice [nodes] int32 is the target's own token after every node."""
-        lens = _lens(tree_lens, self.cfg.max_batch, "tree_lens")
-        path, path_len, given = self._verified(tree_lens, out, tokens.device, tokens=tokens, parents=parents, choice=choice)
-        _check(lib().fkv_verify_tree_greedy(self._h, _ptr(tokens, torch.int32), _ptr(parents, torch.int32), lens,
-                                            _ptr(choice, torch.int32), _ptr(path, torch.int32), _ptr(path_len, torch.int32),
-                                            _ptr(given, torch.int32), path.shape[1], _stream()), "fkv_verify_tree_greedy")
-        return path, path_len, given
+        dev = self._here()
+        keep, lens = self._per_sequence(tree_lens, "tree_lens")
+        shape, at, i32 = (sum(tree_lens),), self._at, torch.int32
+        out, found = self._found(tree_lens, out, dev)
+        _check(lib().fkv_verify_tree_greedy(self._h, at("tokens", tokens, i32, shape, dev), at("parents", parents, i32, shape, dev), lens,
+                                            at("choice", choice, i32, shape, dev), *found, _stream_on(dev)), "fkv_verify_tree_greedy")
+        return out
 
     def commit_tree(self, tree_lens, path, path_len, layer=ALL_LAYERS):
         """The accepted nodes' pairs move together behind the pairs ahead of the tree, the others are dropped.  The host learns the
         new lengths by sync_lengths()."""
         _check_i32(layer=layer)
-        batch = self.cfg.max_batch
-        if path.dim() != 2 or path.shape[0] != batch or tuple(path_len.shape) != (batch,):
-            raise ValueError(f"path, path_len: expected shapes ({batch}, n), ({batch},), got {tuple(path.shape)}, {tuple(path_len.shape)}")
-        self._check_place(path, path_len)
-        _check(lib().fkv_commit_tree(self._h, layer, _lens(tree_lens, batch, "tree_lens"), _ptr(path, torch.int32),
-                                     _ptr(path_len, torch.int32), path.shape[1], _stream()), "fkv_commit_tree")
+        dev = self._here()
+        keep, lens = self._per_sequence(tree_lens, "tree_lens")
+        _, found = self._found(tree_lens, (path, path_len, path), dev)
+        _check(lib().fkv_commit_tree(self._h, layer, lens, found[0], found[1], found[3], _stream_on(dev)), "fkv_commit_tree")
 
     # -- sequences that are copied, change places or end
     def fork(self, source):
         """Sequence s becomes what sequence source[s] was, in all layers (s itself: it stays; -1: it is emptied)."""
-        self._check_place()
-        _check(lib().fkv_fork(self._h, _lens(source, self.cfg.max_batch, "source"), _stream()), "fkv_fork")
+        dev = self._here()
+        keep, at = self._per_sequence(source, "source")
+        _check(lib().fkv_fork(self._h, at, _stream_on(dev)), "fkv_fork")
 
     def export_chunk(self, layer, chunk_lens, out=None):
         """Dense copy of the last chunk_lens[s] pairs of every sequence: k, v [tokens][Hkv][D], features [tokens][Hkv][6 g], positions
         [tokens][Hkv].  out: four such tensors (None: not wanted)."""
         _check_i32(layer=layer)
-        total, c = sum(chunk_lens), self.cfg
-        shapes = [(total, c.num_kv_heads, n) for n in (c.head_dim, c.head_dim, self.feat_dim)] + [(total, c.num_kv_heads)]
+        dev = self._here()
+        keep, lens = self._per_sequence(chunk_lens, "chunk_lens")
+        c, total = self.cfg, sum(chunk_lens)
+        shapes = ((total, c.num_kv_heads, c.head_dim),) * 2 + ((total, c.num_kv_heads, self.feat_dim), (total, c.num_kv_heads))
         types = (torch.bfloat16, torch.bfloat16, torch.float32, torch.int32)
         if out is None:
-            out = tuple(torch.empty(s, dtype=t, device=self.workspace.device) for s, t in zip(shapes, types))
-        for t, s in zip(out, shapes):
-            if t is not None and tuple(t.shape) != s:
-                raise ValueError(f"out: expected shape {s}, got {tuple(t.shape)}")
-        self._check_place(*out)
-        _check(lib().fkv_export_chunk(self._h, layer, _lens(chunk_lens, c.max_batch, "chunk_lens"),
-                                      *(_ptr(t, d) for t, d in zip(out, types)), _stream()), "fkv_export_chunk")
+            out = tuple(torch.empty(s, dtype=t, device=dev) for s, t in zip(shapes, types))
+        to = [None if t is None else self._at("out", t, d, s, dev) for t, d, s in zip(out, types, shapes)]
+        _check(lib().fkv_export_chunk(self._h, layer, lens, *to, _stream_on(dev)), "fkv_export_chunk")
         return out
 
     # -- staged entry points

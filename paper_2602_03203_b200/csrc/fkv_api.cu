@@ -161,7 +161,7 @@ struct fkv_cache {
   uint64_t launches = 0;
   int sm_count = 148;
   int max_cluster[2] = {0, 0};   // largest attention cluster the device places (found at the first stand-alone launch): plain, windowed
-  int tree_clusters[2][4][kTaMaxCluster + 1] = {};   // clusters of 1 .. 16 tree CTAs that fit the device, by append's head dim and rows (0: not asked yet)
+  int tree_clusters[2][3][kTaMaxCluster + 1] = {};   // clusters of 1 .. 16 tree CTAs that fit the device, by append's head dim and rows (0: not asked yet)
   float feature_scale = 0.f;  // softmax scale of the recorded queries (the last decode call's)
   bool timing = false, timed = false;
   CUtensorMap page_parts;     // ... as [page][64-channel part][row][64 channels]
@@ -767,12 +767,11 @@ int tree_clusters_t(int S) {
 }
 template <int D>
 int tree_clusters(int rw, int S) {
-  return rw == 0 ? tree_clusters_t<D, 1>(S) : rw == 1 ? tree_clusters_t<D, 2>(S) : rw == 2 ? tree_clusters_t<D, 4>(S) : tree_clusters_t<D, 8>(S);
+  return rw == 0 ? tree_clusters_t<D, 2>(S) : rw == 1 ? tree_clusters_t<D, 4>(S) : tree_clusters_t<D, 8>(S);
 }
 template <int D>
 int launch_tree(fkv_cache *c, const TreeArgs &a, int rw, int S, cudaStream_t st) {
-  return rw == 0 ? launch_tree_t<D, 1>(c, a, S, st) : rw == 1 ? launch_tree_t<D, 2>(c, a, S, st)
-         : rw == 2 ? launch_tree_t<D, 4>(c, a, S, st) : launch_tree_t<D, 8>(c, a, S, st);
+  return rw == 0 ? launch_tree_t<D, 2>(c, a, S, st) : rw == 1 ? launch_tree_t<D, 4>(c, a, S, st) : launch_tree_t<D, 8>(c, a, S, st);
 }
 
 // CTAs per segment with which k_tree_attend serves the call, and the form by its rows (rw); 0: the general kernels are to.
@@ -791,7 +790,7 @@ int small_tree(fkv_cache *c, const int32_t *tree_lens, const int *ahead, int &rw
   }
   const int rows = longest * c->cfg.group_size;
   if (segs == 0 || rows > kTaRows || segs > c->sm_count) return 0;
-  rw = rows <= 16 ? 0 : rows <= 32 ? 1 : rows <= 64 ? 2 : 3;
+  rw = rows <= 32 ? 0 : rows <= 64 ? 1 : 2;
   int S = std::min(std::min(kTaMaxCluster, c->sm_count / segs), std::max(1, most / kAttendMinPages));
   for (; S > 0; --S) {   // the largest cluster of which the device holds all at once
     int &fit = c->tree_clusters[c->cfg.head_dim == 128][rw][S];
@@ -827,12 +826,12 @@ int launch_small_tree(fkv_cache *c, int layer, const void *k, const void *v, con
   return FKV_OK;
 }
 
-// A cluster of CTAs per sequence: as many as keep the card at about one CTA per SM, so that a single sequence's rows are read by
-// eight SMs and a large batch's by all of them.
+// A cluster of CTAs per sequence: eight, or as many as the SMs hold at a time for all sequences: a pass is a chain of reads, so a
+// large batch too goes by how many pieces are in flight (64 rows of 130001 in 16 bits: 18.1 us with clusters of two).
 template <class T, bool Q>
 int launch_verify_t(fkv_cache *c, const VerifyArgs &a, cudaStream_t st) {
   int cs = 1;
-  while (cs < kVerMaxCluster && cs * 2 * c->cfg.max_batch <= c->sm_count) cs *= 2;
+  while (cs < kVerMaxCluster && cs * 2 * c->cfg.max_batch <= kVerCtasPerSm * c->sm_count) cs *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(c->cfg.max_batch * cs);
   cfg.blockDim = dim3(kVerThreads);
@@ -1452,10 +1451,16 @@ int fkv_export_chunk(fkv_cache *c, int layer, const int32_t *chunk_lens, void *k
   if (!c || !layer_ok(c, layer) || !chunk_lens || !make_lens(c, chunk_lens, lens)) return FKV_ERR_INVALID_ARG;
   if (!chunk_is_stored(c, layer, chunk_lens)) return FKV_ERR_INVALID_ARG;
   if (!aligned(k, 16) || !aligned(v, 16) || !aligned(feat, 4) || !aligned(pos, 4)) return FKV_ERR_INVALID_ARG;
-  const long long tasks = (long long)lens.tok[c->cfg.max_batch] * c->cfg.num_kv_heads;
-  if (tasks == 0 || (!k && !v && !feat && !pos)) return FKV_OK;
+  if (lens.tok[c->cfg.max_batch] == 0 || (!k && !v && !feat && !pos)) return FKV_OK;
+  ExportBlocks b;
+  b.blk[0] = 0;
+  for (int s = 0; s < kMaxBatch; ++s) {
+    const int t = lens.tok[s + 1] - lens.tok[s];
+    b.blk[s + 1] = b.blk[s] + (t > 0 ? (t + kPage - 1) / kPage + 1 : 0);
+  }
+  const long long tasks = (long long)b.blk[kMaxBatch] * c->cfg.num_kv_heads;
   const int grid = (int)std::min<long long>((tasks + 7) / 8, 8LL * c->sm_count);
-  FKV_CUDA(launch_waiting(k_export_chunk, dim3(grid), 256, 0, (cudaStream_t)stream, c->ctx, layer, lens, (uint8_t *)k, (uint8_t *)v, feat, pos));
+  FKV_CUDA(launch_waiting(k_export_chunk, dim3(grid), 256, 0, (cudaStream_t)stream, c->ctx, layer, lens, b, (uint8_t *)k, (uint8_t *)v, feat, pos));
   ++c->launches;
   return FKV_OK;
 }
@@ -1471,7 +1476,11 @@ int fkv_fork(fkv_cache *c, const int32_t *from, void *stream) {
   cudaStream_t st = (cudaStream_t)stream;
   FKV_CUDA(launch_waiting(k_fork_plan, dim3(1), 1024, 0, st, c->ctx, m));
   ++c->launches;
-  FKV_CUDA(launch_waiting(k_fork_copy, dim3(2 * c->sm_count), 256, 0, st, c->ctx, m));
+  const int warps = (int)std::min<size_t>(kForkMaxWarps, (kMaxSmem - 1024) / (2 * (size_t)c->ctx.page_bytes));
+  const size_t smem = (size_t)warps * 2 * c->ctx.page_bytes;
+  static SmemOptIn opt_in;
+  FKV_CUDA(opt_in.ensure(k_fork_copy, kMaxSmem - 1024));
+  FKV_CUDA(launch_waiting(k_fork_copy, dim3(c->sm_count), warps * 32, smem, st, c->ctx, m));
   ++c->launches;
   FKV_CUDA(launch_waiting(k_fork_commit, dim3(L * batch), 256, 0, st, c->ctx, m));
   ++c->launches;

@@ -2,7 +2,7 @@
 // each sequence updates for itself, so two sequences never share one: a copy is a copy of the pages.  A sequence that goes away
 // while others become what it was hands its pages to one of them: beams that only change places move page tables.
 //   k_fork_plan     one CTA: the copies' pages, taken from the free stack and, behind those, from the sequences that go away;
-//   k_fork_copy     pages: a warp takes a run of source pages, reads each once and writes up to four copies (more: it reads again);
+//   k_fork_copy     pages: a warp takes a run of source pages, reads each once and writes up to eight copies (more: it reads again);
 //                   new page tables are written aside, since the old ones are being read;
 //   k_fork_commit   tables, lengths and budgets; pages of the sequences that went away return to the stack;
 //   k_fork_record   the decode queries on record, if there is a record: the host's list of copies, element by element, so that
@@ -89,12 +89,32 @@ __device__ __forceinline__ int fork_entry(const int *offsets, int LB, int x) {
   return lo;
 }
 
-__global__ void __launch_bounds__(256) k_fork_copy(Ctx c, const __grid_constant__ ForkMap m) {
+constexpr int kForkMaxWarps = 16, kForkGroup = 8;
+
+__device__ __forceinline__ void cp_bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// Shared memory -> global, both 16-byte aligned, size a multiple of 16; completion by the issuing thread's groups.
+__device__ __forceinline__ void bulk_s2g(void *dst, uint32_t src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
+}
+
+// One CTA per SM; a warp has two page buffers in shared memory and moves a run of source pages through them by bulk copies: a page
+// is read while the one before it is written, to all its copies (up to eight; it is read again for more).
+__global__ void __launch_bounds__(kForkMaxWarps * 32) k_fork_copy(Ctx c, const __grid_constant__ ForkMap m) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ uint64_t bars[kForkMaxWarps][2];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x / 32, warps = gridDim.x * nw, w = warp * gridDim.x + blockIdx.x;
+  if (lane == 0) {
+    mbar_init(smem_u32(&bars[warp][0]), 1);
+    mbar_init(smem_u32(&bars[warp][1]), 1);
+    fence_barrier_init();
+    fence_proxy_async();
+  }
+  __syncwarp();
   griddep_wait();
   griddep_launch();
   const int top = __ldcg(c.planhdr + PH_PUSH_START);
   if (top < 0) return;
-  const int LB = c.L * c.batch, lane = threadIdx.x & 31, warps = gridDim.x * (blockDim.x / 32), w = blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32;
+  const int LB = c.L * c.batch;
   // Page tables that move.
   for (int i = w; i < LB; i += warps) {
     const int s = i % c.batch;
@@ -105,7 +125,7 @@ __global__ void __launch_bounds__(256) k_fork_copy(Ctx c, const __grid_constant_
         c.pt_new[((size_t)i * c.Hkv + h) * c.max_pages + j] = __ldcg(c.pt + ((size_t)src * c.Hkv + h) * c.max_pages + j);
   }
   // Copies: this warp's run of source pages.
-  const int units = __ldcg(c.planhdr + PH_NWORK), words = c.page_bytes / 16;
+  const int units = __ldcg(c.planhdr + PH_NWORK);
   int u = (int)((long long)units * w / warps);
   const int u_end = (int)((long long)units * (w + 1) / warps);
   if (u >= u_end) return;
@@ -121,17 +141,25 @@ __global__ void __launch_bounds__(256) k_fork_copy(Ctx c, const __grid_constant_
     const int pages = (__ldcg(c.len + lo) + kPage - 1) / kPage, i = x - top - __ldcg(c.tile1_start + lo), h = i / pages;
     return __ldcg(c.pt + ((size_t)lo * c.Hkv + h) * c.max_pages + i - h * pages);
   };
-  while (u < u_end) {
+  const uint32_t buf = smem_u32(smem) + (uint32_t)(warp * 2 * c.page_bytes), bytes = (uint32_t)c.page_bytes;
+  uint32_t turn = 0;   // pages read so far: buffer and parity follow
+  auto read_page = [&](uint32_t t, int page) {   // (lane 0) once the writes from this buffer have been taken out of it
+    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    mbar_arrive_expect_tx(smem_u32(&bars[warp][t & 1]), bytes);
+    bulk_g2s(buf + (t & 1) * bytes, c.pool + (size_t)page * bytes, bytes, smem_u32(&bars[warp][t & 1]));
+  };
+  bool ok = true;
+  while (u < u_end && ok) {
     // (entries without pages to read begin where the next one does: the last of them is the one that has them)
     while (e + 1 < LB && __ldcg(c.idx + LB + e + 1) <= u) ++e;
     const int r = e % c.batch, l0 = e - r, pages = (__ldcg(c.len + e) + kPage - 1) / kPage;
     const int off = u - __ldcg(c.idx + LB + e), h = off / pages, j0 = off - h * pages;
     const int take = min(min(32, u_end - u), pages - j0);   // pages j0 .. of one head, a lane each
     const int src = lane < take ? __ldcg(c.pt + ((size_t)e * c.Hkv + h) * c.max_pages + j0 + lane) : 0;
-    for (int s = m.first[r]; s >= 0;) {   // up to four copies at a time
-      int dst[4], nd = 0;
+    for (int s = m.first[r]; s >= 0 && ok;) {
+      int dst[kForkGroup], nd = 0;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < kForkGroup; ++k) {
         dst[k] = 0;
         if (s < 0) continue;
         if (lane < take) {
@@ -141,27 +169,24 @@ __global__ void __launch_bounds__(256) k_fork_copy(Ctx c, const __grid_constant_
         nd = k + 1;
         s = m.next[s];
       }
-      for (int i = 0; i < take; ++i) {
-        const uint4 *from = reinterpret_cast<const uint4 *>(c.pool + (size_t)__shfl_sync(0xffffffffu, src, i) * c.page_bytes);
-        uint4 *to[4];
+      if (lane == 0) read_page(turn, src);
+      for (int i = 0; i < take && ok; ++i) {
+        const int next = __shfl_sync(0xffffffffu, src, (i + 1) & 31);
+        if (lane == 0 && i + 1 < take) read_page(turn + 1, next);
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars[warp][turn & 1]), (turn >> 1) & 1));
+        if (!ok) { set_status(c, kDevWaitTimeout); break; }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) to[k] = reinterpret_cast<uint4 *>(c.pool + (size_t)__shfl_sync(0xffffffffu, dst[k], i) * c.page_bytes);
-        for (int b = lane; b < words; b += 32 * 8) {
-          uint4 x[8];
-#pragma unroll
-          for (int y = 0; y < 8; ++y)
-            if (b + 32 * y < words) x[y] = __ldcs(from + b + 32 * y);
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (k < nd)
-#pragma unroll
-              for (int y = 0; y < 8; ++y)
-                if (b + 32 * y < words) __stcs(to[k] + b + 32 * y, x[y]);
+        for (int k = 0; k < kForkGroup; ++k) {
+          const int to = __shfl_sync(0xffffffffu, dst[k], i);
+          if (lane == 0 && k < nd) bulk_s2g(c.pool + (size_t)to * bytes, buf + (turn & 1) * bytes, bytes);
         }
+        if (lane == 0) cp_bulk_commit();
+        ++turn;
       }
     }
     u += take;
   }
+  if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");   // all writes are out
 }
 
 // grid = layers x sequences.

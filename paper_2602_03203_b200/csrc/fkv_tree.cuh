@@ -128,30 +128,59 @@ __global__ void __launch_bounds__(1024) k_commit_tree(Ctx c, int l0, const __gri
 }
 
 // ---------------------------------------------------------------- read-out
-// The last lens[s] pairs of every sequence, packed: the inverse of k_append_chunk.  A warp per pair and head.
+// The last lens[s] pairs of every sequence, packed: the inverse of k_append_chunk.  A warp per page and head: its pairs lie one after
+// another, so eight of them are asked for together (a warp per pair has one row in flight behind two dependent reads: 3.4 TB/s where
+// this has ...).  blk: the first of a sequence's pages in the list of all (a page more than its pairs fill: they may begin inside one).
 // Bound: bytes (read and written).
-__global__ void __launch_bounds__(256) k_export_chunk(Ctx c, int layer, const __grid_constant__ ChunkLens lens, uint8_t *k, uint8_t *v,
-                                                      float *feat, int32_t *pos) {
+struct ExportBlocks {
+  int blk[kMaxBatch + 1];
+};
+__global__ void __launch_bounds__(256) k_export_chunk(Ctx c, int layer, const __grid_constant__ ChunkLens lens,
+                                                      const __grid_constant__ ExportBlocks b, uint8_t *k, uint8_t *v, float *feat, int32_t *pos) {
   griddep_wait();
   griddep_launch();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const long long tasks = (long long)lens.tok[c.batch] * c.Hkv;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, W = c.F + 1, nch = c.D / 8;
+  const long long tasks = (long long)b.blk[c.batch] * c.Hkv;
   for (long long t = (long long)blockIdx.x * 8 + warp; t < tasks; t += (long long)gridDim.x * 8) {
-    const int row = (int)(t / c.Hkv), h = (int)(t - (long long)row * c.Hkv);
-    int lo = 0, hi = c.batch;   // the sequence of the row: the last one that starts at or before it
+    const int block = (int)(t / c.Hkv), h = (int)(t - (long long)block * c.Hkv);
+    int lo = 0, hi = c.batch;   // the block's sequence: the last one that starts at or before it
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (lens.tok[mid] <= row) lo = mid; else hi = mid;
+      if (b.blk[mid] <= block) lo = mid; else hi = mid;
     }
-    const int n = __ldcg(c.len + layer * c.batch + lo), T = lens.tok[lo + 1] - lens.tok[lo], slot = n - T + row - lens.tok[lo];
-    if (n < T) {
-      if (lane == 0 && h == 0 && row == lens.tok[lo]) set_status(c, kDevBadIndex);
+    const int n = __ldcg(c.len + layer * c.batch + lo), T = lens.tok[lo + 1] - lens.tok[lo], first = n - T;
+    if (first < 0) {
+      if (lane == 0 && h == 0 && block == b.blk[lo]) set_status(c, kDevBadIndex);
       continue;
     }
-    uint8_t *page = c.pool + (size_t)__ldcg(c.pt + (size_t)seg_of(c, layer, lo, h) * c.max_pages + slot / kPage) * c.page_bytes;
-    const size_t at = (size_t)row * c.Hkv + h;
-    move_row<1>(c, page, slot % kPage, k ? k + at * c.D * 2 : nullptr, v ? v + at * c.D * 2 : nullptr, feat ? feat + at * c.F : nullptr,
-                pos ? pos + at : nullptr, lane, 0);
+    const int pg = first / kPage + block - b.blk[lo], r0 = max(first - pg * kPage, 0), r1 = min(n - pg * kPage, kPage);
+    if (r0 >= r1) continue;
+    const uint8_t *page = c.pool + (size_t)__ldcg(c.pt + (size_t)seg_of(c, layer, lo, h) * c.max_pages + pg) * c.page_bytes;
+    const size_t at0 = (size_t)(lens.tok[lo] + pg * kPage - first) * c.Hkv + h;   // row of the page's pair 0, if that is one
+    const bool on = lane < 2 * nch && (lane < nch ? k : v) != nullptr;
+    for (int r8 = r0; r8 < r1; r8 += 8) {
+      uint4 x[8];
+      uint32_t m[8][2];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int r = r8 + u;
+        if (r >= r1) continue;
+        if (on) x[u] = __ldcs(reinterpret_cast<const uint4 *>(page + (lane < nch ? 0 : c.off_v) + kv_chunk_off(r, lane % nch, c.D)));
+        const uint32_t *row = reinterpret_cast<const uint32_t *>(meta_row(c, page, r));
+        if (lane < W) m[u][0] = __ldcs(row + lane);
+        if (lane + 32 < W) m[u][1] = __ldcs(row + lane + 32);
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int r = r8 + u;
+        if (r >= r1) continue;
+        const size_t at = at0 + (size_t)r * c.Hkv;
+        if (on) __stcs(reinterpret_cast<uint4 *>((lane < nch ? k : v) + at * c.D * 2 + (lane % nch) * 16), x[u]);
+        if (feat && lane < c.F) __stcs(feat + at * c.F + lane, __uint_as_float(m[u][0]));
+        if (feat && lane + 32 < c.F) __stcs(feat + at * c.F + lane + 32, __uint_as_float(m[u][1]));
+        if (pos && lane == (c.F & 31)) pos[at] = (int32_t)(c.F < 32 ? m[u][0] : m[u][1]);
+      }
+    }
   }
 }
 

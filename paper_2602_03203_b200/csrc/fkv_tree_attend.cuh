@@ -6,7 +6,7 @@
 //
 // Shape: grid (S, sequences x KV heads); the S CTAs of a segment are one cluster, each with a run of its pages.
 //   warp 8      copies pages (one bulk copy each: K and V rows as they lie) into a ring;
-//   warps 0-7   RW of them share a page, 16 query rows each; 8 / RW pages are worked on at a time.  S^T = K Q^T with the pairs on
+//   warps 0-7   RW of them share two pages, 16 query rows each; 8 / RW such pairs are worked on at a time.  S^T = K Q^T with the pairs on
 //               the M axis (16 of a page, mma m16n8k16 with two column tiles), so that P^T needs only a transpose in registers to
 //               become the B operand of O^T = V^T P^T.  Softmax in fp32; P is rounded to bf16 (as V is: half a step, 2^-8, off);
 //   warp 9      the store's page arithmetic (as k_append_chunk: prefix sums over the sequences) and the lengths.
@@ -19,6 +19,7 @@
 #include "fkv_dev.cuh"
 #include "fkv_attend.cuh"
 #include "fkv_chunk.cuh"
+#include "fkv_features.cuh"
 
 namespace fkv {
 
@@ -42,7 +43,7 @@ struct TreeArgs {
 template <int D, int RW>
 struct TaSmem {
   static constexpr int kSlots = D == 128 ? 16 : 32, kPageKv = 4 * D * kPage, kGroups = kTaWarps / RW, kR = RW * 16;
-  static_assert(kSlots % kGroups == 0, "a slot belongs to one group of warps: its barriers carry one parity bit");
+  static_assert(kSlots % (2 * kGroups) == 0 && kSlots > 2 * kGroups, "a slot belongs to one group of warps: its barriers carry one parity bit");
   static constexpr size_t kRing = (size_t)kSlots * kPageKv;
   static constexpr int kRow = D + 4;                                       // a row of a partial result: O, m, l
   static_assert((size_t)kTaRows * kRow * 4 <= kRing, "the warps' results meet where the ring was");
@@ -333,91 +334,124 @@ __global__ void __launch_bounds__(kTaThreads, 1) k_tree_attend(Ctx c, const __gr
     const int krow = ((lane >> 3) & 1) * 8 + (lane & 7), khi = lane >> 4;
     const int vrow = (lane >> 4) * 8 + (lane & 7), vhi = (lane >> 3) & 1;
     const uint32_t rt_zero = gridDim.z - 1;   // 0 at run time, unknown at compile time
-    for (int i = kg; i < npg; i += KG) {
-      const int slot_i = i % SLOTS, slot0 = (pg0 + i) * kPage;
-      if (!mbar_wait(smem_u32(&full[slot_i]), (i / SLOTS) & 1)) { set_status(c, kDevWaitTimeout); break; }
-      const uint32_t kbase = smem_u32(smem + (size_t)slot_i * PAGE_KV), vbase = kbase + 2 * D;
-      float s[2][4] = {};
+    // Two pages at a time: a page's chain (scores, softmax, product) is latency, and two of them fill each other's gaps.
+    for (int i = kg * 2; i < npg; i += KG * 2) {
+      const bool two = i + 1 < npg;
+      const int sl[2] = {i % SLOTS, (i + 1) % SLOTS};
+      bool ok = mbar_wait(smem_u32(&full[sl[0]]), (i / SLOTS) & 1);
+      if (two) ok = ok && mbar_wait(smem_u32(&full[sl[1]]), ((i + 1) / SLOTS) & 1);
+      if (!ok) { set_status(c, kDevWaitTimeout); break; }
+      const int slot0 = (pg0 + i) * kPage;
+      // (without a second page the first one's rows stand in for it, and none of its pairs is seen)
+      const uint32_t kb[2] = {smem_u32(smem + (size_t)sl[0] * PAGE_KV), smem_u32(smem + (size_t)sl[two ? 1 : 0] * PAGE_KV)};
+      float s[2][2][4] = {};
 #pragma unroll
       for (int ks = 0; ks < KSQ; ++ks) {
-        uint32_t x[4];
-        ldsm_x4(x, kbase + kv_chunk_off(krow, ks * 2 + khi, D));
+        uint32_t x[2][4];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) mma_bf16(s[t], x[0], x[1], x[2], x[3], qb[ks][t][0], qb[ks][t][1]);
+        for (int b = 0; b < 2; ++b) ldsm_x4(x[b], kb[b] + kv_chunk_off(krow, ks * 2 + khi, D));
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int t = 0; t < 2; ++t) mma_bf16(s[b][t], x[b][0], x[b][1], x[b][2], x[b][3], qb[ks][t][0], qb[ks][t][1]);
       }
-      // This lane: pairs gid and gid + 8 of the page, rows 2 tig and 2 tig + 1 of each column tile.
-      const bool edge = slot0 + kPage > kp;   // pairs of the tree, or none
-      float v[2][4];
+      // This lane: pairs gid and gid + 8 of each page, rows 2 tig and 2 tig + 1 of each column tile.
+      const int seen_end = two ? lim : min(lim, slot0 + kPage);
+      if (slot0 + 2 * kPage > min(kp, seen_end)) {   // pairs of the tree, or none
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int r = rw * 16 + t * 8 + 2 * tig + e, node = r / G;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {
+                const int slot = slot0 + b * kPage + gid + u * 8, j = slot - kp;
+                const bool sees = slot < seen_end && r < rows && (j < 0 || (j <= node && ((s_mask[node * kTreeWords + (j >> 5)] >> (j & 31)) & 1u)));
+                if (!sees) s[b][t][u * 2 + e] = -INFINITY;
+              }
+          }
+      }
+      // The reference of a row moves when a score has passed it by more than 2^24 (or there is none yet): until then P is at most
+      // 2^24, which bf16 holds as exactly as 1, and nothing is rescaled.
+      bool grow = false;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[t][e] = s[t][e] * a.scale_log2;
-      if (edge) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = rw * 16 + t * 8 + 2 * tig + (e & 1), slot = slot0 + gid + (e >> 1) * 8, node = r / G, j = slot - kp;
-            const bool sees = slot < lim && r < rows && (j < 0 || (j <= node && ((s_mask[node * kTreeWords + (j >> 5)] >> (j & 31)) & 1u)));
-            if (!sees) v[t][e] = -INFINITY;
-          }
-      }
-      uint32_t pb[2][2];
-      float cc[2][2];
-      bool moved = false;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        float mx0 = fmaxf(v[t][0], v[t][2]), mx1 = fmaxf(v[t][1], v[t][3]);
-#pragma unroll
-        for (int sh = 4; sh < 32; sh <<= 1) {
-          mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, sh));
-          mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, sh));
+        for (int e = 0; e < 2; ++e) {
+          const float top = fmaxf(fmaxf(s[0][t][e], s[0][t][2 + e]), fmaxf(s[1][t][e], s[1][t][2 + e]));
+          grow = grow || top * a.scale_log2 > m_run[t][e] + kChunkGrow;
         }
-        mx0 = fmaxf(mx0, m_run[t][0]);
-        mx1 = fmaxf(mx1, m_run[t][1]);
-        const float z0 = mx0 == -INFINITY ? 0.f : mx0, z1 = mx1 == -INFINITY ? 0.f : mx1;   // (a row that has seen nothing)
-        moved = moved || mx0 != m_run[t][0] || mx1 != m_run[t][1];
-        cc[t][0] = exp2f(m_run[t][0] - z0);
-        cc[t][1] = exp2f(m_run[t][1] - z1);
-        const float e0 = exp2f(v[t][0] - z0), e1 = exp2f(v[t][1] - z1), e2 = exp2f(v[t][2] - z0), e3 = exp2f(v[t][3] - z1);
-        l_run[t][0] = l_run[t][0] * cc[t][0] + e0 + e2;
-        l_run[t][1] = l_run[t][1] * cc[t][1] + e1 + e3;
-        m_run[t][0] = mx0;
-        m_run[t][1] = mx1;
-        pb[t][0] = movmatrix_trans(pack_bf16(e0, e1));
-        pb[t][1] = movmatrix_trans(pack_bf16(e2, e3));
-      }
-      if (__any_sync(0xffffffffu, moved)) {
+      if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2; ++t) {
+          float f[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float top = fmaxf(fmaxf(s[0][t][e], s[0][t][2 + e]), fmaxf(s[1][t][e], s[1][t][2 + e])) * a.scale_log2;
+#pragma unroll
+            for (int sh = 4; sh < 32; sh <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, sh));
+            top = fmaxf(top, m_run[t][e]);
+            f[e] = top == -INFINITY ? 1.f : ex2(m_run[t][e] - top);
+            m_run[t][e] = top;
+            l_run[t][e] *= f[e];
+          }
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt) {
-            o[mt][t][0] *= cc[t][0]; o[mt][t][1] *= cc[t][1]; o[mt][t][2] *= cc[t][0]; o[mt][t][3] *= cc[t][1];
+            o[mt][t][0] *= f[0]; o[mt][t][1] *= f[1]; o[mt][t][2] *= f[0]; o[mt][t][3] *= f[1];
           }
+        }
+      }
+      uint32_t pb[2][2][2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const float z0 = m_run[t][0] == -INFINITY ? 0.f : m_run[t][0], z1 = m_run[t][1] == -INFINITY ? 0.f : m_run[t][1];   // (a row that has seen nothing)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const float e0 = ex2(fmaf(s[b][t][0], a.scale_log2, -z0)), e1 = ex2(fmaf(s[b][t][1], a.scale_log2, -z1));
+          const float e2 = ex2(fmaf(s[b][t][2], a.scale_log2, -z0)), e3 = ex2(fmaf(s[b][t][3], a.scale_log2, -z1));
+          l_run[t][0] += e0 + e2;
+          l_run[t][1] += e1 + e3;
+          pb[b][t][0] = movmatrix_trans(pack_bf16(e0, e1));
+          pb[b][t][1] = movmatrix_trans(pack_bf16(e2, e3));
+        }
       }
       // V rows behind the last pair are left out of the product (zero times an infinity is not zero): pairs 2 tig, 2 tig + 1 and
       // those eight further on.
-      uint32_t keep_lo = ~0u, keep_hi = ~0u;
-      if (slot0 + kPage > lim) {
-        const int left = lim - slot0;
-        auto both = [&](int p) { return (p < left ? 0xffffu : 0u) | (p + 1 < left ? 0xffff0000u : 0u); };
-        keep_lo = both(2 * tig);
-        keep_hi = both(2 * tig + 8);
-      }
+      if (slot0 + 2 * kPage <= seen_end) {
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        uint32_t x[4];
-        ldsm_x4_trans(x, vbase + kv_chunk_off(vrow, mt * 2 + vhi, D));
-        x[0] &= keep_lo; x[1] &= keep_lo; x[2] &= keep_hi; x[3] &= keep_hi;
+        for (int mt = 0; mt < MT; ++mt) {
+          uint32_t x[2][4];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) mma_bf16(o[mt][t], x[0], x[1], x[2], x[3], pb[t][0], pb[t][1]);
+          for (int b = 0; b < 2; ++b) ldsm_x4_trans(x[b], kb[b] + 2 * D + kv_chunk_off(vrow, mt * 2 + vhi, D));
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) mma_bf16(o[mt][t], x[b][0], x[b][1], x[b][2], x[b][3], pb[b][t][0], pb[b][t][1]);
+        }
+      } else {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const int left = seen_end - slot0 - b * kPage;
+          auto both = [&](int p) { return (p < left ? 0xffffu : 0u) | (p + 1 < left ? 0xffff0000u : 0u); };
+          const uint32_t keep_lo = both(2 * tig), keep_hi = both(2 * tig + 8);
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            uint32_t x[4];
+            ldsm_x4_trans(x, kb[b] + 2 * D + kv_chunk_off(vrow, mt * 2 + vhi, D));
+            x[0] &= keep_lo; x[1] &= keep_lo; x[2] &= keep_hi; x[3] &= keep_hi;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) mma_bf16(o[mt][t], x[0], x[1], x[2], x[3], pb[b][t][0], pb[b][t][1]);
+          }
+        }
       }
-      // Every read of the page has to be complete before the arrival is seen: its address depends on the products' results.
+      // Every read of the pages has to be complete before the arrivals are seen: their addresses depend on the products' results.
       uint32_t done = 0;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) done |= __float_as_uint(o[mt][0][0]) | __float_as_uint(o[mt][1][0]);
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&empty[slot_i]) + (done & rt_zero));
+      if (lane < (two ? 2 : 1)) mbar_arrive(smem_u32(&empty[sl[lane & 1]]) + (done & rt_zero));
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -464,7 +498,7 @@ __global__ void __launch_bounds__(kTaThreads, 1) k_tree_attend(Ctx c, const __gr
     acc = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int g = 0; g < parts; ++g) M = fmaxf(M, p[g * step + D]);
     for (int g = 0; g < parts; ++g) {
-      const float mgr = p[g * step + D], f = mgr == -INFINITY ? 0.f : exp2f(mgr - M);
+      const float mgr = p[g * step + D], f = mgr == -INFINITY ? 0.f : ex2(mgr - M);
       L = f == 0.f ? L : fmaf(f, p[g * step + D + 1], L);
       if (lane * 4 < D && f != 0.f) {
         const float4 x = *reinterpret_cast<const float4 *>(p + g * step + lane * 4);

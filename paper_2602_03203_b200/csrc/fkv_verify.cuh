@@ -30,6 +30,7 @@ constexpr int kVerPiece = 256;                    // tokens of a piece: eight pe
 constexpr int kVerMaxVocab = 1 << 20;
 constexpr int kVerPieces = kVerMaxVocab / kVerPiece;
 constexpr int kVerMaxCluster = 8;
+constexpr int kVerCtasPerSm = 2;                  // that fit at a time
 
 struct VerifyArgs {
   const void *target, *draft;      // rows of a token's successor probabilities, one per node
@@ -63,7 +64,7 @@ __device__ __forceinline__ double warp_sum(double x) {
 }
 
 template <class T, bool Q>
-__global__ void __launch_bounds__(kVerThreads) k_verify_tree(Ctx c, const __grid_constant__ VerifyArgs a) {
+__global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx c, const __grid_constant__ VerifyArgs a) {
   __shared__ double s_sum[kVerPieces];              // sums of this CTA's pieces
   __shared__ double s_all[2][kVerMaxCluster];       // the CTAs' sums, of this pass and of the last
   __shared__ double s_part[kVerWarps];
