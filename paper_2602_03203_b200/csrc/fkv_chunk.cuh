@@ -466,18 +466,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       for (int i = i0; i < nt; i += step) {
         const int p0 = tl.first(i), cols = tl.pages(i) * kPage;
         const int hi = min(cols, e - p0 * kPage), lo = wlo - p0 * kPage, na = x.a - p0 * kPage;
-        // The tile's bits of the row's mask: ones for pairs ahead of the tree.
-        uint32_t tree[3] = {~0u, ~0u, ~0u};
         const bool in_tree = TREE && p0 * kPage + cols > x.base;
-        if (TREE && in_tree && live) {
-          const int at = p0 * kPage - x.base, k = at >> 5;
-          const uint32_t *row = a.masks + (size_t)(x.row0 + tj) * kTreeWords;
-          uint32_t w[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) w[j] = k + j < 0 ? ~0u : k + j < kTreeWords ? __ldcg(row + k + j) : 0u;
-#pragma unroll
-          for (int j = 0; j < 3; ++j) tree[j] = __funnelshift_r(w[j], w[j + 1], at & 31);
-        }
         if (!mbar_sleep_warp(smem_u32(&s_full[t]), sp)) { set_status(c, kDevWaitTimeout); ok = false; break; }
         sp ^= 1;
         tc_fence_after();
@@ -502,12 +491,30 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
           if (lane == 0) mbar_arrive(smem_u32(&s_empty[t]));
           if (!__all_sync(0xffffffffu, hi >= SM::kCols && (lo <= 0 || na >= SM::kCols) && !in_tree)) {   // hidden scores become -infinity
             asm volatile("" ::: "memory");   // (a branch: tiles without an edge should not pay for the comparisons)
+            if constexpr (TREE) {
+              // The row's seen pairs as bits: the tree's mask (ones for pairs ahead of the tree) within the range and the window.
+              uint32_t see[3];
+              const int at = p0 * kPage - x.base, k = at >> 5;
+              const uint32_t *row = a.masks + (size_t)(x.row0 + tj) * kTreeWords;
+              uint32_t w[4];
 #pragma unroll
-            for (int q = 0; q < TP; ++q)
+              for (int j = 0; j < 4; ++j) w[j] = !live || k + j < 0 ? ~0u : k + j < kTreeWords ? __ldcg(row + k + j) : 0u;
+              auto below = [](int e) { return e <= 0 ? 0u : e >= 32 ? ~0u : (1u << e) - 1u; };   // bits under e
 #pragma unroll
-              for (int j = 0; j < 16; ++j)
-                if (q * 16 + j >= hi || (q * 16 + j < lo && q * 16 + j >= na) || (TREE && !((tree[q / 2] >> (q % 2 * 16 + j)) & 1u)))
-                  v[q][j] = 0xff800000u;
+              for (int j = 0; j < 3; ++j)
+                see[j] = __funnelshift_r(w[j], w[j + 1], at & 31) & below(hi - 32 * j) & (below(na - 32 * j) | ~below(lo - 32 * j));
+#pragma unroll
+              for (int q = 0; q < TP; ++q)
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                  if (!((see[q / 2] >> (q % 2 * 16 + j)) & 1u)) v[q][j] = 0xff800000u;
+            } else {
+#pragma unroll
+              for (int q = 0; q < TP; ++q)
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                  if (q * 16 + j >= hi || (q * 16 + j < lo && q * 16 + j >= na)) v[q][j] = 0xff800000u;
+            }
           }
           // P = 2^(scale s - ms) against the reference m, rounded to bf16 (as V is: at most half a step, 2^-8, off); its sum
           // is not rounded.  The maximum is found on the side: m follows it only when a score has passed m by more than 2^24
