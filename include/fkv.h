@@ -435,7 +435,7 @@ int fkv_commit_tree(fkv_cache *c, int layer, const int32_t *tree_lens, const int
  * whole call does nothing (FKV_DEV_POOL_EXHAUSTED).  Only enqueues kernels; a replayed call does the same to what it finds.
  *
  * fkv_export_chunk: dense copy of the last chunk_lens[s] pairs of every sequence of a layer, packed, the inverse of fkv_append_chunk:
- * k, v dev [tokens][Hkv][D] bf16 (16-byte aligned), feat dev [tokens][Hkv][F] fp32, pos dev [tokens][Hkv] int32 (after an eviction the
+ * k, v dev [tokens][Hkv][D] bf16 (16-byte aligned), feat dev [tokens][Hkv][F] fp32 (8-byte aligned), pos dev [tokens][Hkv] int32 (after an eviction the
  * heads keep pairs of different positions); any may be NULL.  FKV_ERR_INVALID_ARG if a chunk is longer than its segment.
  */
 int fkv_fork(fkv_cache *c, const int32_t *from, void *stream);

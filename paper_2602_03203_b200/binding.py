@@ -478,13 +478,14 @@ class Cache:
         """append_tree(k, v) then tree_attn(q) in one call."""
         return self._tree(layer, k, v, q, tree_lens, masks, pos, keep_lens, window, sinks, out, lse, scale)
 
-    def _found(self, tree_lens, out, dev):
-        """The results of a verification: path [batch][n], path_len [batch], tokens [batch][n], int32, and their addresses."""
+    def _found(self, tree_lens, out, dev, like=None):
+        """The results of a verification: path [batch][n], path_len [batch], tokens [batch][n], int32 (where none are given: made on
+        the device of `like`), and their addresses."""
         batch, i32 = self.cfg.max_batch, torch.int32
         if out is None:
             width = max(1, max(tree_lens))
-            both = torch.empty((2, batch, width), dtype=i32, device=dev)
-            out = (both[0], torch.empty((batch,), dtype=i32, device=dev), both[1])
+            path = like.new_empty((batch, width))
+            out = (path, like.new_empty(batch), torch.empty_like(path))
         path, path_len, tokens = out
         if path.dim() != 2:
             raise ValueError(f"path: expected two dimensions, got {tuple(path.shape)}")
@@ -515,8 +516,9 @@ class Cache:
             if one != 1 and shape[1] > 1 and total:
                 raise ValueError(f"{name}: a row's elements must be next to one another")
             rows += (t.data_ptr(), step if total > 1 else shape[1])
-        out, found = self._found(tree_lens, out, dev)
-        _check(lib().fkv_verify_tree(self._h, at("tokens", tokens, torch.int32, (total,), dev), at("parents", parents, torch.int32, (total,), dev),
+        drafts = at("tokens", tokens, torch.int32, (total,), dev)
+        out, found = self._found(tree_lens, out, dev, tokens)
+        _check(lib().fkv_verify_tree(self._h, drafts, at("parents", parents, torch.int32, (total,), dev),
                                      lens, *rows, 0 if dtype is torch.float32 else 1, shape[1],
                                      at("u_accept", u_accept, torch.float32, (total,), dev),
                                      at("u_sample", u_sample, torch.float32, (self.cfg.max_batch,), dev), *found, _stream_on(dev)), "fkv_verify_tree")
@@ -527,8 +529,9 @@ class Cache:
         dev = self._here()
         keep, lens = self._per_sequence(tree_lens, "tree_lens")
         shape, at, i32 = (sum(tree_lens),), self._at, torch.int32
-        out, found = self._found(tree_lens, out, dev)
-        _check(lib().fkv_verify_tree_greedy(self._h, at("tokens", tokens, i32, shape, dev), at("parents", parents, i32, shape, dev), lens,
+        drafts = at("tokens", tokens, i32, shape, dev)
+        out, found = self._found(tree_lens, out, dev, tokens)
+        _check(lib().fkv_verify_tree_greedy(self._h, drafts, at("parents", parents, i32, shape, dev), lens,
                                             at("choice", choice, i32, shape, dev), *found, _stream_on(dev)), "fkv_verify_tree_greedy")
         return out
 

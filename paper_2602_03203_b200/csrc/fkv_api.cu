@@ -1450,7 +1450,7 @@ int fkv_export_chunk(fkv_cache *c, int layer, const int32_t *chunk_lens, void *k
   ChunkLens lens;
   if (!c || !layer_ok(c, layer) || !chunk_lens || !make_lens(c, chunk_lens, lens)) return FKV_ERR_INVALID_ARG;
   if (!chunk_is_stored(c, layer, chunk_lens)) return FKV_ERR_INVALID_ARG;
-  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(feat, 4) || !aligned(pos, 4)) return FKV_ERR_INVALID_ARG;
+  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(feat, 8) || !aligned(pos, 4)) return FKV_ERR_INVALID_ARG;
   if (lens.tok[c->cfg.max_batch] == 0 || (!k && !v && !feat && !pos)) return FKV_OK;
   ExportBlocks b;
   b.blk[0] = 0;
@@ -1459,8 +1459,13 @@ int fkv_export_chunk(fkv_cache *c, int layer, const int32_t *chunk_lens, void *k
     b.blk[s + 1] = b.blk[s] + (t > 0 ? (t + kPage - 1) / kPage + 1 : 0);
   }
   const long long tasks = (long long)b.blk[kMaxBatch] * c->cfg.num_kv_heads;
-  const int grid = (int)std::min<long long>((tasks + 7) / 8, 8LL * c->sm_count);
-  FKV_CUDA(launch_waiting(k_export_chunk, dim3(grid), 256, 0, (cudaStream_t)stream, c->ctx, layer, lens, b, (uint8_t *)k, (uint8_t *)v, feat, pos));
+  const int most = (int)std::min<size_t>(kExportMaxWarps, (kMaxSmem - 2048) / (2 * (size_t)c->ctx.page_bytes));
+  const int warps = (int)std::min<long long>(most, (tasks + c->sm_count - 1) / c->sm_count);
+  const int grid = (int)std::min<long long>((tasks + warps - 1) / warps, c->sm_count);
+  static SmemOptIn opt_in;
+  FKV_CUDA(opt_in.ensure(k_export_chunk, kMaxSmem - 2048));
+  FKV_CUDA(launch_waiting(k_export_chunk, dim3(grid), warps * 32, (size_t)warps * 2 * c->ctx.page_bytes, (cudaStream_t)stream, c->ctx, layer,
+                          lens, b, (uint8_t *)k, (uint8_t *)v, feat, pos));
   ++c->launches;
   return FKV_OK;
 }

@@ -128,59 +128,94 @@ __global__ void __launch_bounds__(1024) k_commit_tree(Ctx c, int l0, const __gri
 }
 
 // ---------------------------------------------------------------- read-out
-// The last lens[s] pairs of every sequence, packed: the inverse of k_append_chunk.  A warp per page and head: its pairs lie one after
-// another, so eight of them are asked for together (a warp per pair has one row in flight behind two dependent reads: 3.4 TB/s where
-// this has ...).  blk: the first of a sequence's pages in the list of all (a page more than its pairs fill: they may begin inside one).
-// Bound: bytes (read and written).
+// The last lens[s] pairs of every sequence, packed: the inverse of k_append_chunk.  A warp per page and head, with two page buffers in
+// shared memory: a page is copied in (one bulk copy) while the rows of the one before it go out.  blk: the first of a sequence's pages in
+// the list of all (a page more than its pairs fill: they may begin inside one).
+// Bound: bytes (read and written).  32768 pairs of 8 heads (160 MB read, as many written): a warp per pair 95 us, a warp per page with
+// eight rows in registers 70.
 struct ExportBlocks {
   int blk[kMaxBatch + 1];
 };
-__global__ void __launch_bounds__(256) k_export_chunk(Ctx c, int layer, const __grid_constant__ ChunkLens lens,
-                                                      const __grid_constant__ ExportBlocks b, uint8_t *k, uint8_t *v, float *feat, int32_t *pos) {
+constexpr int kExportMaxWarps = 16;
+__global__ void __launch_bounds__(kExportMaxWarps * 32) k_export_chunk(Ctx c, int layer, const __grid_constant__ ChunkLens lens,
+                                                                       const __grid_constant__ ExportBlocks b, uint8_t *k, uint8_t *v,
+                                                                       float *feat, int32_t *pos) {
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ uint64_t bars[kExportMaxWarps][2];
+  __shared__ int s_first[kMaxBatch];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x / 32, nch = c.D / 8;
+  if (lane == 0) {
+    mbar_init(smem_u32(&bars[warp][0]), 1);
+    mbar_init(smem_u32(&bars[warp][1]), 1);
+    fence_barrier_init();
+  }
   griddep_wait();
   griddep_launch();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, W = c.F + 1, nch = c.D / 8;
-  const long long tasks = (long long)b.blk[c.batch] * c.Hkv;
-  for (long long t = (long long)blockIdx.x * 8 + warp; t < tasks; t += (long long)gridDim.x * 8) {
+  for (int s = threadIdx.x; s < c.batch; s += blockDim.x) {
+    const int T = lens.tok[s + 1] - lens.tok[s], first = __ldcg(c.len + layer * c.batch + s) - T;
+    s_first[s] = first;
+    if (first < 0 && blockIdx.x == 0) set_status(c, kDevBadIndex);
+  }
+  __syncthreads();
+  const long long tasks = (long long)b.blk[c.batch] * c.Hkv, step = (long long)gridDim.x * nw;
+  const uint32_t bytes = (uint32_t)(feat || pos ? c.page_bytes : 64 * c.D);
+  struct Task { int r0, r1, page; size_t at0; };
+  auto task = [&](long long t) {
+    Task x{0, 0, 0, 0};
+    if (t >= tasks) return x;
     const int block = (int)(t / c.Hkv), h = (int)(t - (long long)block * c.Hkv);
     int lo = 0, hi = c.batch;   // the block's sequence: the last one that starts at or before it
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (b.blk[mid] <= block) lo = mid; else hi = mid;
     }
-    const int n = __ldcg(c.len + layer * c.batch + lo), T = lens.tok[lo + 1] - lens.tok[lo], first = n - T;
-    if (first < 0) {
-      if (lane == 0 && h == 0 && block == b.blk[lo]) set_status(c, kDevBadIndex);
-      continue;
+    const int first = s_first[lo], n = first + lens.tok[lo + 1] - lens.tok[lo];
+    if (first < 0) return x;
+    const int pg = first / kPage + block - b.blk[lo];
+    x.r0 = max(first - pg * kPage, 0);
+    x.r1 = min(n - pg * kPage, kPage);
+    if (x.r0 >= x.r1) return x;
+    x.page = __ldcg(c.pt + (size_t)seg_of(c, layer, lo, h) * c.max_pages + pg);
+    x.at0 = (size_t)(lens.tok[lo] + pg * kPage - first) * c.Hkv + h;   // row of the page's pair 0, if that is one
+    return x;
+  };
+  uint32_t turn = 0;   // pages copied so far: buffer and parity follow
+  uint8_t *buf = smem + (size_t)warp * 2 * c.page_bytes;
+  auto copy = [&](const Task &x, uint32_t i) {
+    if (x.r0 >= x.r1 || lane != 0) return;
+    const uint32_t bar = smem_u32(&bars[warp][i & 1]);
+    mbar_arrive_expect_tx(bar, bytes);
+    bulk_g2s(smem_u32(buf + (i & 1) * c.page_bytes), c.pool + (size_t)x.page * c.page_bytes, bytes, bar);
+  };
+  const int half = c.F / 2, inv = 65536 / half + 1;   // (a row's features in pairs; i / half for i < 384)
+  long long t = (long long)warp * gridDim.x + blockIdx.x;
+  Task x = task(t);
+  copy(x, turn);
+  while (t < tasks) {
+    const Task nx = task(t + step);
+    const bool any = x.r0 < x.r1;
+    copy(nx, turn + (any ? 1 : 0));
+    if (any) {
+      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bars[warp][turn & 1]), (turn >> 1) & 1))) { set_status(c, kDevWaitTimeout); break; }
+      const uint8_t *page = buf + (turn & 1) * c.page_bytes;
+      uint8_t *to = lane < nch ? k : v;
+      if (lane < 2 * nch && to)
+#pragma unroll 8
+        for (int r = x.r0; r < x.r1; ++r)
+          __stcs(reinterpret_cast<uint4 *>(to + (x.at0 + (size_t)r * c.Hkv) * c.D * 2 + (lane % nch) * 16),
+                 *reinterpret_cast<const uint4 *>(page + (lane < nch ? 0 : c.off_v) + kv_chunk_off(r, lane % nch, c.D)));
+      if (feat)
+        for (int i = lane; i < (x.r1 - x.r0) * half; i += 32) {
+          const int rr = (i * inv) >> 16, r = x.r0 + rr, f = (i - rr * half) * 2;
+          const float *row = meta_row(c, page, r) + f;
+          __stcs(reinterpret_cast<float2 *>(feat + (x.at0 + (size_t)r * c.Hkv) * c.F + f), make_float2(row[0], row[1]));
+        }
+      if (pos && x.r0 + lane < x.r1) pos[x.at0 + (size_t)(x.r0 + lane) * c.Hkv] = reinterpret_cast<const int32_t *>(meta_row(c, page, x.r0 + lane))[c.F];
+      __syncwarp();   // (the buffer's next copy comes after these reads)
+      ++turn;
     }
-    const int pg = first / kPage + block - b.blk[lo], r0 = max(first - pg * kPage, 0), r1 = min(n - pg * kPage, kPage);
-    if (r0 >= r1) continue;
-    const uint8_t *page = c.pool + (size_t)__ldcg(c.pt + (size_t)seg_of(c, layer, lo, h) * c.max_pages + pg) * c.page_bytes;
-    const size_t at0 = (size_t)(lens.tok[lo] + pg * kPage - first) * c.Hkv + h;   // row of the page's pair 0, if that is one
-    const bool on = lane < 2 * nch && (lane < nch ? k : v) != nullptr;
-    for (int r8 = r0; r8 < r1; r8 += 8) {
-      uint4 x[8];
-      uint32_t m[8][2];
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int r = r8 + u;
-        if (r >= r1) continue;
-        if (on) x[u] = __ldcs(reinterpret_cast<const uint4 *>(page + (lane < nch ? 0 : c.off_v) + kv_chunk_off(r, lane % nch, c.D)));
-        const uint32_t *row = reinterpret_cast<const uint32_t *>(meta_row(c, page, r));
-        if (lane < W) m[u][0] = __ldcs(row + lane);
-        if (lane + 32 < W) m[u][1] = __ldcs(row + lane + 32);
-      }
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int r = r8 + u;
-        if (r >= r1) continue;
-        const size_t at = at0 + (size_t)r * c.Hkv;
-        if (on) __stcs(reinterpret_cast<uint4 *>((lane < nch ? k : v) + at * c.D * 2 + (lane % nch) * 16), x[u]);
-        if (feat && lane < c.F) __stcs(feat + at * c.F + lane, __uint_as_float(m[u][0]));
-        if (feat && lane + 32 < c.F) __stcs(feat + at * c.F + lane + 32, __uint_as_float(m[u][1]));
-        if (pos && lane == (c.F & 31)) pos[at] = (int32_t)(c.F < 32 ? m[u][0] : m[u][1]);
-      }
-    }
+    x = nx;
+    t += step;
   }
 }
 

@@ -126,16 +126,17 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
     return false;
   };
   // A lane's eight weights of a piece: tokens lane, lane + 32, ... of it.
-  auto piece = [&](int pc, double alpha, double (&w)[8]) {
+  auto load = [&](int pc, T (&pv)[8], T (&qv)[8]) {
     const T *pr = row_p(cur), *qr = Q ? row_q(cur) : nullptr;
     const int x0 = pc * kVerPiece + lane;
-    T pv[8], qv[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const bool in = x0 + 32 * i < V;
       pv[i] = in ? pr[x0 + 32 * i] : T(0.f);
       if (Q) qv[i] = in ? qr[x0 + 32 * i] : T(0.f);
     }
+  };
+  auto weights = [&](int pc, const T (&pv)[8], const T (&qv)[8], double alpha, double (&w)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] = weight((double)to_f32(pv[i]), Q ? (double)to_f32(qv[i]) : 0.0, alpha);
     if (!Q) {
@@ -144,18 +145,26 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
       if (hit)
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (tried(x0 + 32 * i)) w[i] = 0.0;
+          if (tried(pc * kVerPiece + lane + 32 * i)) w[i] = 0.0;
     }
   };
   // The sum over the vocabulary, the same in every CTA; the pieces' sums stay in s_sum, the CTAs' in s_all[turn ^ 1].
   auto pass = [&](double alpha) {
     double sum = 0.0;
-    for (int pc = c0 + warp; pc < c1; pc += kVerWarps) {
-      double w[8];
-      piece(pc, alpha, w);
-      const double x = warp_sum(((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7])));
-      if (lane == 0) s_sum[pc - c0] = x;
-      sum += x;
+#pragma unroll 1
+    for (int pc = c0 + warp; pc < c1; pc += 2 * kVerWarps) {   // two pieces are asked for together
+      T pv[2][8], qv[2][8];
+      load(pc, pv[0], qv[0]);
+      if (pc + kVerWarps < c1) load(pc + kVerWarps, pv[1], qv[1]);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        if (pc + b * kVerWarps >= c1) break;
+        double w[8];
+        weights(pc + b * kVerWarps, pv[b], qv[b], alpha, w);
+        const double x = warp_sum(((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7])));
+        if (lane == 0) s_sum[pc + b * kVerWarps - c0] = x;
+        sum += x;
+      }
     }
     if (lane == 0) s_part[warp] = sum;
     __syncthreads();
@@ -248,7 +257,11 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
   }
   if (at < 0) return;   // (cannot be: the owner holds something)
   double w[8];
-  piece(c0 + at, alpha, w);
+  {
+    T pv[8], qv[8];
+    load(c0 + at, pv, qv);
+    weights(c0 + at, pv, qv, alpha, w);
+  }
   int found = -1;
   run = before;
 #pragma unroll
