@@ -161,7 +161,7 @@ struct fkv_cache {
   uint64_t launches = 0;
   int sm_count = 148;
   int max_cluster[2] = {0, 0};   // largest attention cluster the device places (found at the first stand-alone launch): plain, windowed
-  int tree_clusters[2][3][kTaMaxCluster + 1] = {};   // clusters of 1 .. 16 tree CTAs that fit the device, by append's head dim and rows (0: not asked yet)
+  int tree_clusters[kTaMaxCluster + 1] = {};   // clusters of 1 .. 16 tree CTAs that fit the device (0: not asked yet, -1: none)
   float feature_scale = 0.f;  // softmax scale of the recorded queries (the last decode call's)
   bool timing = false, timed = false;
   CUtensorMap page_parts;     // ... as [page][64-channel part][row][64 channels]
@@ -582,9 +582,9 @@ int check_append_chunk(const fkv_cache *c, int layer, const void *k, const void 
   return FKV_OK;
 }
 
-// masks: of a draft tree, else NULL.
+// masks: of a draft tree, else NULL.  behind: its attention was launched just now (see the kernel).
 int launch_append_chunk(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos, const int32_t *keep_lens,
-                        const int32_t *chunk_lens, const ChunkLens &lens, const uint32_t *masks, cudaStream_t st) {
+                        const int32_t *chunk_lens, const ChunkLens &lens, const uint32_t *masks, bool behind, cudaStream_t st) {
   const int batch = c->cfg.max_batch;
   // (A roll-back to the lengths that the host knows is launched all the same: replayed, it meets others.)
   if (lens.tok[batch] == 0 && !keep_lens) return FKV_OK;
@@ -597,7 +597,7 @@ int launch_append_chunk(fkv_cache *c, int layer, const void *k, const void *v, c
   const long long tasks = (long long)lens.tok[batch] * c->cfg.num_kv_heads;
   const int grid = (int)std::max<long long>(1, std::min<long long>((tasks + 7) / 8, 4LL * c->sm_count));
   FKV_CUDA(launch_waiting(masks ? k_append_chunk<true> : k_append_chunk<false>, dim3(grid), 256, 0, st, c->ctx, layer, (const uint8_t *)k,
-                          (const uint8_t *)v, pos, lens, keep, masks));
+                          (const uint8_t *)v, pos, lens, keep, masks, behind ? 1 : 0));
   ++c->launches;
   for (int s = 0; s < batch; ++s) {
     int &n = c->h_len[(size_t)layer * batch + s];
@@ -720,110 +720,101 @@ bool trees_ok(const fkv_cache *c, const int32_t *tree_lens, int window) {
   return true;
 }
 
-// Small trees in one launch (k_tree_attend).  S: CTAs per segment.
-template <int D, int RW>
-int launch_tree_t(fkv_cache *c, const TreeArgs &a, int S, cudaStream_t st) {
-  constexpr size_t smem = TaSmem<D, RW>::bytes();
-  static_assert(smem + sizeof(TreeStore) <= kMaxSmem, "one CTA's shared memory");
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(S, c->cfg.max_batch * c->cfg.num_kv_heads);
-  cfg.blockDim = dim3(kTaThreads);
+// Trees whose attention is one launch of clusters (k_tree_attend).
+template <int D>
+int tree_attend_config(cudaLaunchConfig_t &cfg, cudaLaunchAttribute (&at)[2], int S, int y, cudaStream_t st) {
+  constexpr size_t smem = TaSmem<D>::bytes();
+  static_assert(smem <= kMaxSmem, "one CTA's shared memory");
+  static SmemOptIn opt_in;
+  FKV_CUDA(opt_in.ensure(k_tree_attend<D>, smem));
+  cfg = cudaLaunchConfig_t{};
+  cfg.gridDim = dim3(S, y);
+  cfg.blockDim = dim3(kChunkThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute at[2];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = S; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 2;
-  FKV_CUDA(cudaLaunchKernelEx(&cfg, k_tree_attend<D, RW>, c->ctx, a));
-  ++c->launches;
-  return FKV_OK;
-}
-// How many clusters of S CTAs the device holds at a time (at least 1 is said of S = 1); asked once per handle.
-template <int D, int RW>
-int tree_clusters_t(int S) {
-  constexpr size_t smem = TaSmem<D, RW>::bytes();
-  auto kern = k_tree_attend<D, RW>;
-  static SmemOptIn opt_in;
-  if (opt_in.ensure(kern, smem) != cudaSuccess || cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
-    (void)cudaGetLastError();
-    return -1;
-  }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(S, 1);
-  cfg.blockDim = dim3(kTaThreads);
-  cfg.dynamicSmemBytes = smem;
-  cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = S; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = at;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
+  return FKV_OK;
+}
+// How many clusters of S CTAs the device holds at a time (-1: none).
+template <int D>
+int tree_clusters(int S) {
+  cudaLaunchConfig_t cfg;
+  cudaLaunchAttribute at[2];
   int n = 0;
-  const bool ok = cudaOccupancyMaxActiveClusters(&n, kern, &cfg) == cudaSuccess && n > 0;
+  const bool ok = tree_attend_config<D>(cfg, at, S, 1, nullptr) == FKV_OK &&
+                  cudaFuncSetAttribute(k_tree_attend<D>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                  (cfg.numAttrs = 1, cudaOccupancyMaxActiveClusters(&n, k_tree_attend<D>, &cfg) == cudaSuccess) && n > 0;
   (void)cudaGetLastError();
   return ok ? n : -1;
 }
-template <int D>
-int tree_clusters(int rw, int S) {
-  return rw == 0 ? tree_clusters_t<D, 2>(S) : rw == 1 ? tree_clusters_t<D, 4>(S) : tree_clusters_t<D, 8>(S);
-}
-template <int D>
-int launch_tree(fkv_cache *c, const TreeArgs &a, int rw, int S, cudaStream_t st) {
-  return rw == 0 ? launch_tree_t<D, 2>(c, a, S, st) : rw == 1 ? launch_tree_t<D, 4>(c, a, S, st) : launch_tree_t<D, 8>(c, a, S, st);
-}
 
-// CTAs per segment with which k_tree_attend serves the call, and the form by its rows (rw); 0: the general kernels are to.
-// ahead: pairs ahead of every tree.
-int small_tree(fkv_cache *c, const int32_t *tree_lens, const int *ahead, int &rw) {
-  const int batch = c->cfg.max_batch, Hkv = c->cfg.num_kv_heads;
-  int longest = 0, segs = 0, most = 0;
-  long long total = 0;
+// CTAs per block of query rows with which k_tree_attend serves the call; 0: the general kernel is to.  ahead: pairs ahead of every tree.
+int small_tree(fkv_cache *c, const int32_t *tree_lens, const int *ahead) {
+  const int batch = c->cfg.max_batch, Hkv = c->cfg.num_kv_heads, block = kChunkRows / c->cfg.group_size;
+  long long total = 0, segs = 0;
+  int most = 0;
   for (int s = 0; s < batch; ++s) {
     if (tree_lens[s] == 0) continue;
-    const int pages = (ahead[s] + tree_lens[s] + kPage - 1) / kPage;
-    longest = std::max(longest, tree_lens[s]);
+    const int blocks = (tree_lens[s] + block - 1) / block, pages = (ahead[s] + tree_lens[s] + kPage - 1) / kPage + 1;
     most = std::max(most, pages);
-    total += (long long)pages * Hkv;
-    segs += Hkv;
+    segs += (long long)blocks * Hkv;
+    total += (long long)blocks * Hkv * pages;
   }
-  const int rows = longest * c->cfg.group_size;
-  if (segs == 0 || rows > kTaRows || segs > c->sm_count) return 0;
-  rw = rows <= 32 ? 0 : rows <= 64 ? 1 : 2;
-  int S = std::min(std::min(kTaMaxCluster, c->sm_count / segs), std::max(1, most / kAttendMinPages));
-  for (; S > 0; --S) {   // the largest cluster of which the device holds all at once
-    int &fit = c->tree_clusters[c->cfg.head_dim == 128][rw][S];
-    if (fit == 0) fit = c->cfg.head_dim == 128 ? tree_clusters<128>(rw, S) : tree_clusters<64>(rw, S);
+  if (segs == 0 || segs > c->sm_count) return 0;
+  // The largest cluster of which the device holds all at once, with a few pages at least for every CTA.
+  int S = (int)std::min<long long>(std::min<long long>(kTaMaxCluster, c->sm_count / segs), std::max(1, most / kAttendMinPages));
+  for (; S > 0; --S) {
+    int &fit = c->tree_clusters[S];
+    if (fit == 0) fit = c->cfg.head_dim == 128 ? tree_clusters<128>(S) : tree_clusters<64>(S);
     if (fit >= segs) break;
   }
   if (S == 0) return 0;
-  // The general kernels share the pages evenly over the SMs but take some 20 us longer to start and to join; a page takes an SM
-  // about 0.2 us.
-  return (most + S - 1) / S <= total / c->sm_count + 80 ? S : 0;
+  // The general kernel shares the pages evenly over the SMs but starts and joins some 20 us later; a page takes an SM 0.15 us.
+  return (most + S - 1) / S <= total / c->sm_count + 100 ? S : 0;
 }
 
-int launch_small_tree(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos, const int32_t *keep_lens,
-                      const int32_t *tree_lens, const ChunkLens &lens, const uint32_t *masks, const void *q, float scale, void *out, float *lse,
-                      int rw, int S, cudaStream_t st) {
-  const int batch = c->cfg.max_batch, D = c->cfg.head_dim;
+template <int D>
+int launch_tree_attend_t(fkv_cache *c, const CUtensorMap (&in)[3], const TreeArgs &a, int S, cudaStream_t st) {
+  cudaLaunchConfig_t cfg;
+  cudaLaunchAttribute at[2];
+  if (int e = tree_attend_config<D>(cfg, at, S, c->cfg.max_batch * c->cfg.num_kv_heads * a.blocks, st)) return e;
+  FKV_CUDA(cudaLaunchKernelEx(&cfg, k_tree_attend<D>, c->ctx, c->page_rows, c->page_parts, in[0], in[1], in[2], a));
+  ++c->launches;
+  return FKV_OK;
+}
+
+// k, v: of a tree that is not stored yet (the store is launched behind, see k_append_chunk), else NULL.
+int launch_tree_attend(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *keep_lens, const int32_t *tree_lens,
+                       const ChunkLens &lens, const uint32_t *masks, const void *q, float scale, void *out, float *lse, int S, cudaStream_t st) {
+  const int batch = c->cfg.max_batch, D = c->cfg.head_dim, Hkv = c->cfg.num_kv_heads, block = kChunkRows / c->cfg.group_size;
+  if (int e = ensure_page_rows_map(c)) return e;
   TreeArgs a;
   a.layer = layer; a.append = k != nullptr;
   a.scale_log2 = (scale == 0.f ? 1.f / sqrtf((float)D) : scale) * 1.4426950408889634f;
-  a.q = (const __nv_bfloat16 *)q; a.out = (__nv_bfloat16 *)out; a.lse = lse; a.masks = masks;
-  a.k = (const uint8_t *)k; a.v = (const uint8_t *)v; a.pos = pos; a.lens = lens;
+  a.out = (__nv_bfloat16 *)out; a.lse = lse; a.masks = masks; a.lens = lens;
+  a.blocks = 1;
+  for (int s = 0; s < batch; ++s) a.blocks = std::max(a.blocks, (tree_lens[s] + block - 1) / block);
   a.keep = ChunkKeep{};
   if (keep_lens) {
     a.keep.use = 1;
     for (int s = 0; s < batch; ++s) a.keep.keep[s] = keep_lens[s];
   }
-  if (int e = D == 128 ? launch_tree<128>(c, a, rw, S, st) : launch_tree<64>(c, a, rw, S, st)) return e;
-  if (a.append)
-    for (int s = 0; s < batch; ++s) {
-      int &n = c->h_len[(size_t)layer * batch + s];
-      n = (keep_lens ? keep_lens[s] : n) + tree_lens[s];
-    }
-  return FKV_OK;
+  CUtensorMap in[3];
+  if (int e = query_map(c, q, lens.tok[batch], c->cfg.group_size, block, &in[0])) return e;
+  in[1] = in[2] = in[0];
+  if (k) {   // [tokens][Hkv][D] as (64 channels, tokens, parts of 64 channels, heads): a box = 16 tokens of a head, one part (K) or all (V)
+    const cuuint64_t dims[4] = {64, (cuuint64_t)lens.tok[batch], (cuuint64_t)(D / 64), (cuuint64_t)Hkv};
+    const cuuint64_t strides[3] = {(cuuint64_t)(2 * D * Hkv), 128, (cuuint64_t)(2 * D)};
+    const cuuint32_t box_k[4] = {64, kPage, 1, 1}, box_v[4] = {64, kPage, (cuuint32_t)(D / 64), 1};
+    if (int e = tensor_map(&in[1], const_cast<void *>(k), 4, dims, strides, box_k, CU_TENSOR_MAP_SWIZZLE_128B)) return e;
+    if (int e = tensor_map(&in[2], const_cast<void *>(v), 4, dims, strides, box_v, CU_TENSOR_MAP_SWIZZLE_128B)) return e;
+  }
+  return D == 128 ? launch_tree_attend_t<128>(c, in, a, S, st) : launch_tree_attend_t<64>(c, in, a, S, st);
 }
 
 // A cluster of CTAs per sequence: eight, or as many as the SMs hold at a time for all sequences: a pass is a chain of reads, so a
@@ -1292,7 +1283,7 @@ int fkv_append_chunk(fkv_cache *c, int layer, const void *k, const void *v, cons
                      const int32_t *chunk_lens, void *stream) {
   ChunkLens lens;
   if (int e = check_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens)) return e;
-  return launch_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens, nullptr, (cudaStream_t)stream);
+  return launch_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens, nullptr, false, (cudaStream_t)stream);
 }
 
 int fkv_chunk_attn(fkv_cache *c, int layer, const void *q, const int32_t *chunk_lens, int32_t window, int32_t sinks, float scale,
@@ -1312,7 +1303,7 @@ int fkv_append_chunk_attn(fkv_cache *c, int layer, const void *k, const void *v,
   if (int e = check_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens)) return e;
   if (lens.tok[c->cfg.max_batch] > 0 && (!out || !aligned(out, 16) || !aligned(lse_out, 4))) return FKV_ERR_INVALID_ARG;
   if (int e = ensure_page_rows_map(c)) return e;   // (what can fail does so before anything is stored)
-  if (int e = launch_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens, nullptr, (cudaStream_t)stream)) return e;
+  if (int e = launch_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens, nullptr, false, (cudaStream_t)stream)) return e;
   return launch_chunk_attend(c, layer, q, chunk_lens, lens, window, sinks, scale, out, lse_out, nullptr, (cudaStream_t)stream);
 }
 
@@ -1363,7 +1354,7 @@ int fkv_append_tree(fkv_cache *c, int layer, const void *k, const void *v, const
   ChunkLens lens;
   if (int e = check_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens)) return e;
   if (int e = check_tree(c, tree_lens, lens, masks, 0)) return e;
-  return launch_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens, masks, (cudaStream_t)stream);
+  return launch_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens, masks, false, (cudaStream_t)stream);
 }
 
 int fkv_tree_attn(fkv_cache *c, int layer, const void *q, const int32_t *tree_lens, const uint32_t *masks, int32_t window, int32_t sinks,
@@ -1374,10 +1365,10 @@ int fkv_tree_attn(fkv_cache *c, int layer, const void *q, const int32_t *tree_le
   if (lens.tok[c->cfg.max_batch] > 0 && (!out || !aligned(out, 16) || !aligned(lse_out, 4))) return FKV_ERR_INVALID_ARG;
   if (!chunk_is_stored(c, layer, tree_lens)) return FKV_ERR_INVALID_ARG;
   if (window == 0) {
-    int ahead[kMaxBatch], rw;
+    int ahead[kMaxBatch];
     for (int s = 0; s < c->cfg.max_batch; ++s) ahead[s] = c->h_len[(size_t)layer * c->cfg.max_batch + s] - tree_lens[s];
-    if (const int S = small_tree(c, tree_lens, ahead, rw))
-      return launch_small_tree(c, layer, nullptr, nullptr, nullptr, nullptr, tree_lens, lens, masks, q, scale, out, lse_out, rw, S, (cudaStream_t)stream);
+    if (const int S = small_tree(c, tree_lens, ahead))
+      return launch_tree_attend(c, layer, nullptr, nullptr, nullptr, tree_lens, lens, masks, q, scale, out, lse_out, S, (cudaStream_t)stream);
   }
   return launch_chunk_attend(c, layer, q, tree_lens, lens, window, sinks, scale, out, lse_out, masks, (cudaStream_t)stream);
 }
@@ -1391,13 +1382,15 @@ int fkv_append_tree_attn(fkv_cache *c, int layer, const void *k, const void *v, 
   if (int e = check_tree(c, tree_lens, lens, masks, window)) return e;
   if (lens.tok[c->cfg.max_batch] > 0 && (!out || !aligned(out, 16) || !aligned(lse_out, 4))) return FKV_ERR_INVALID_ARG;
   if (window == 0) {
-    int ahead[kMaxBatch], rw;
+    int ahead[kMaxBatch];
     for (int s = 0; s < c->cfg.max_batch; ++s) ahead[s] = keep_lens ? keep_lens[s] : c->h_len[(size_t)layer * c->cfg.max_batch + s];
-    if (const int S = small_tree(c, tree_lens, ahead, rw))
-      return launch_small_tree(c, layer, k, v, pos, keep_lens, tree_lens, lens, masks, q, scale, out, lse_out, rw, S, (cudaStream_t)stream);
+    if (const int S = small_tree(c, tree_lens, ahead)) {
+      if (int e = launch_tree_attend(c, layer, k, v, keep_lens, tree_lens, lens, masks, q, scale, out, lse_out, S, (cudaStream_t)stream)) return e;
+      return launch_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens, masks, true, (cudaStream_t)stream);
+    }
   }
   if (int e = ensure_page_rows_map(c)) return e;   // (what can fail does so before anything is stored)
-  if (int e = launch_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens, masks, (cudaStream_t)stream)) return e;
+  if (int e = launch_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens, masks, false, (cudaStream_t)stream)) return e;
   return launch_chunk_attend(c, layer, q, tree_lens, lens, window, sinks, scale, out, lse_out, masks, (cudaStream_t)stream);
 }
 

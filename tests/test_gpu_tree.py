@@ -178,18 +178,25 @@ def test_scale_and_rows_behind_the_last_node():
 
 
 def test_chain_equals_a_chunk():
-    """A tree without branches is a chunk: the same products, in the same tiles."""
-    a, b = Case(2, 4, 128, [300, 17]), Case(2, 4, 128, [300, 17])
+    """A tree without branches is a chunk.  In a layer with a window both are the same products in the same tiles; without one the
+    two calls may be different kernels, and each is within the bounds of the 64-bit form."""
     lens = [37, 5]
-    k, v, q = a.chunk(lens)
-    la, lb = torch.empty(q.shape[:2], device="cuda"), torch.empty(q.shape[:2], device="cuda")
-    masks = a.cache.tree_masks(packed([[j - 1 for j in range(t)] for t in lens]), lens)
-    x = a.cache.append_tree_attn(0, k, v, q, lens, masks, lse=la)
-    y = b.cache.append_chunk_attn(0, k, v, q, lens, lse=lb)
-    assert torch.equal(x, y) and torch.equal(la, lb)
-    for s in range(2):
-        for m, n in zip(a.cache.export_head(0, s, 1), b.cache.export_head(0, s, 1)):
-            assert torch.equal(m, n)
+    chain = [[j - 1 for j in range(t)] for t in lens]
+    for window in (512, 0):
+        a, b = Case(2, 4, 128, [300, 17]), Case(2, 4, 128, [300, 17])
+        k, v, q = a.chunk(lens)
+        la, lb = torch.empty(q.shape[:2], device="cuda"), torch.empty(q.shape[:2], device="cuda")
+        masks = a.cache.tree_masks(packed(chain), lens)
+        x = a.cache.append_tree_attn(0, k, v, q, lens, masks, window=window, lse=la)
+        y = b.cache.append_chunk_attn(0, k, v, q, lens, window=window, lse=lb)
+        if window:
+            assert torch.equal(x, y) and torch.equal(la, lb)
+        extend(a, k, v, chain)
+        check(a, x, la, q, chain, window)
+        check(a, y, lb, q, chain, window)
+        for s in range(2):
+            for m, n in zip(a.cache.export_head(0, s, 1), b.cache.export_head(0, s, 1)):
+                assert torch.equal(m, n)
 
 
 def test_masks_of_other_kinds_and_rows_that_see_nothing():
