@@ -161,7 +161,7 @@ struct fkv_cache {
   uint64_t launches = 0;
   int sm_count = 148;
   int max_cluster[2] = {0, 0};   // largest attention cluster the device places (found at the first stand-alone launch): plain, windowed
-  int tree_clusters[kTaMaxCluster + 1] = {};   // clusters of 1 .. 16 tree CTAs that fit the device (0: not asked yet, -1: none)
+  int tree_clusters[2][kTaMaxCluster + 1] = {};   // clusters of 1 .. 16 tree CTAs (plain, windowed) that fit the device (0: not asked yet, -1: none)
   float feature_scale = 0.f;  // softmax scale of the recorded queries (the last decode call's)
   bool timing = false, timed = false;
   CUtensorMap page_parts;     // ... as [page][64-channel part][row][64 channels]
@@ -721,12 +721,12 @@ bool trees_ok(const fkv_cache *c, const int32_t *tree_lens, int window) {
 }
 
 // Trees whose attention is one launch of clusters (k_tree_attend).
-template <int D>
+template <int D, bool WIN>
 int tree_attend_config(cudaLaunchConfig_t &cfg, cudaLaunchAttribute (&at)[2], int S, int y, cudaStream_t st) {
   constexpr size_t smem = TaSmem<D>::bytes();
   static_assert(smem <= kMaxSmem, "one CTA's shared memory");
   static SmemOptIn opt_in;
-  FKV_CUDA(opt_in.ensure(k_tree_attend<D>, smem));
+  FKV_CUDA(opt_in.ensure(k_tree_attend<D, WIN>, smem));
   cfg = cudaLaunchConfig_t{};
   cfg.gridDim = dim3(S, y);
   cfg.blockDim = dim3(kChunkThreads);
@@ -741,26 +741,28 @@ int tree_attend_config(cudaLaunchConfig_t &cfg, cudaLaunchAttribute (&at)[2], in
   return FKV_OK;
 }
 // How many clusters of S CTAs the device holds at a time (-1: none).
-template <int D>
+template <int D, bool WIN>
 int tree_clusters(int S) {
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute at[2];
   int n = 0;
-  const bool ok = tree_attend_config<D>(cfg, at, S, 1, nullptr) == FKV_OK &&
-                  cudaFuncSetAttribute(k_tree_attend<D>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
-                  (cfg.numAttrs = 1, cudaOccupancyMaxActiveClusters(&n, k_tree_attend<D>, &cfg) == cudaSuccess) && n > 0;
+  const bool ok = tree_attend_config<D, WIN>(cfg, at, S, 1, nullptr) == FKV_OK &&
+                  cudaFuncSetAttribute(k_tree_attend<D, WIN>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                  (cfg.numAttrs = 1, cudaOccupancyMaxActiveClusters(&n, k_tree_attend<D, WIN>, &cfg) == cudaSuccess) && n > 0;
   (void)cudaGetLastError();
   return ok ? n : -1;
 }
 
 // CTAs per block of query rows with which k_tree_attend serves the call; 0: the general kernel is to.  ahead: pairs ahead of every tree.
-int small_tree(fkv_cache *c, const int32_t *tree_lens, const int *ahead) {
+int small_tree(fkv_cache *c, const int32_t *tree_lens, const int *ahead, int window, int sinks) {
   const int batch = c->cfg.max_batch, Hkv = c->cfg.num_kv_heads, block = kChunkRows / c->cfg.group_size;
   long long total = 0, segs = 0;
   int most = 0;
   for (int s = 0; s < batch; ++s) {
     if (tree_lens[s] == 0) continue;
-    const int blocks = (tree_lens[s] + block - 1) / block, pages = (ahead[s] + tree_lens[s] + kPage - 1) / kPage + 1;
+    const int blocks = (tree_lens[s] + block - 1) / block, all = (ahead[s] + tree_lens[s] + kPage - 1) / kPage + 1;
+    // (a window of W positions holds at most W pairs)
+    const int pages = window ? (int)std::min<long long>(all, ((long long)window + std::min(sinks, ahead[s]) + tree_lens[s]) / kPage + 3) : all;
     most = std::max(most, pages);
     segs += (long long)blocks * Hkv;
     total += (long long)blocks * Hkv * pages;
@@ -769,8 +771,11 @@ int small_tree(fkv_cache *c, const int32_t *tree_lens, const int *ahead) {
   // The largest cluster of which the device holds all at once, with a few pages at least for every CTA.
   int S = (int)std::min<long long>(std::min<long long>(kTaMaxCluster, c->sm_count / segs), std::max(1, most / kAttendMinPages));
   for (; S > 0; --S) {
-    int &fit = c->tree_clusters[S];
-    if (fit == 0) fit = c->cfg.head_dim == 128 ? tree_clusters<128>(S) : tree_clusters<64>(S);
+    int &fit = c->tree_clusters[window > 0][S];
+    if (fit == 0) {
+      if (window > 0) fit = c->cfg.head_dim == 128 ? tree_clusters<128, true>(S) : tree_clusters<64, true>(S);
+      else fit = c->cfg.head_dim == 128 ? tree_clusters<128, false>(S) : tree_clusters<64, false>(S);
+    }
     if (fit >= segs) break;
   }
   if (S == 0) return 0;
@@ -778,23 +783,24 @@ int small_tree(fkv_cache *c, const int32_t *tree_lens, const int *ahead) {
   return (most + S - 1) / S <= total / c->sm_count + 100 ? S : 0;
 }
 
-template <int D>
+template <int D, bool WIN>
 int launch_tree_attend_t(fkv_cache *c, const CUtensorMap (&in)[3], const TreeArgs &a, int S, cudaStream_t st) {
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute at[2];
-  if (int e = tree_attend_config<D>(cfg, at, S, c->cfg.max_batch * c->cfg.num_kv_heads * a.blocks, st)) return e;
-  FKV_CUDA(cudaLaunchKernelEx(&cfg, k_tree_attend<D>, c->ctx, c->page_rows, c->page_parts, in[0], in[1], in[2], a));
+  if (int e = tree_attend_config<D, WIN>(cfg, at, S, c->cfg.max_batch * c->cfg.num_kv_heads * a.blocks, st)) return e;
+  FKV_CUDA(cudaLaunchKernelEx(&cfg, k_tree_attend<D, WIN>, c->ctx, c->page_rows, c->page_parts, in[0], in[1], in[2], a));
   ++c->launches;
   return FKV_OK;
 }
 
 // k, v: of a tree that is not stored yet (the store is launched behind, see k_append_chunk), else NULL.
 int launch_tree_attend(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *keep_lens, const int32_t *tree_lens,
-                       const ChunkLens &lens, const uint32_t *masks, const void *q, float scale, void *out, float *lse, int S, cudaStream_t st) {
+                       const ChunkLens &lens, const uint32_t *masks, const int32_t *pos, const void *q, int window, int sinks, float scale, void *out,
+                       float *lse, int S, cudaStream_t st) {
   const int batch = c->cfg.max_batch, D = c->cfg.head_dim, Hkv = c->cfg.num_kv_heads, block = kChunkRows / c->cfg.group_size;
   if (int e = ensure_page_rows_map(c)) return e;
   TreeArgs a;
-  a.layer = layer; a.append = k != nullptr;
+  a.layer = layer; a.append = k != nullptr; a.window = window; a.sinks = window ? sinks : 0; a.pos = pos;
   a.scale_log2 = (scale == 0.f ? 1.f / sqrtf((float)D) : scale) * 1.4426950408889634f;
   a.out = (__nv_bfloat16 *)out; a.lse = lse; a.masks = masks; a.lens = lens;
   a.blocks = 1;
@@ -814,7 +820,8 @@ int launch_tree_attend(fkv_cache *c, int layer, const void *k, const void *v, co
     if (int e = tensor_map(&in[1], const_cast<void *>(k), 4, dims, strides, box_k, CU_TENSOR_MAP_SWIZZLE_128B)) return e;
     if (int e = tensor_map(&in[2], const_cast<void *>(v), 4, dims, strides, box_v, CU_TENSOR_MAP_SWIZZLE_128B)) return e;
   }
-  return D == 128 ? launch_tree_attend_t<128>(c, in, a, S, st) : launch_tree_attend_t<64>(c, in, a, S, st);
+  if (window) return D == 128 ? launch_tree_attend_t<128, true>(c, in, a, S, st) : launch_tree_attend_t<64, true>(c, in, a, S, st);
+  return D == 128 ? launch_tree_attend_t<128, false>(c, in, a, S, st) : launch_tree_attend_t<64, false>(c, in, a, S, st);
 }
 
 // A cluster of CTAs per sequence: eight, or as many as the SMs hold at a time for all sequences: a pass is a chain of reads, so a
@@ -1364,12 +1371,11 @@ int fkv_tree_attn(fkv_cache *c, int layer, const void *q, const int32_t *tree_le
   if (int e = check_tree(c, tree_lens, lens, masks, window)) return e;
   if (lens.tok[c->cfg.max_batch] > 0 && (!out || !aligned(out, 16) || !aligned(lse_out, 4))) return FKV_ERR_INVALID_ARG;
   if (!chunk_is_stored(c, layer, tree_lens)) return FKV_ERR_INVALID_ARG;
-  if (window == 0) {
-    int ahead[kMaxBatch];
-    for (int s = 0; s < c->cfg.max_batch; ++s) ahead[s] = c->h_len[(size_t)layer * c->cfg.max_batch + s] - tree_lens[s];
-    if (const int S = small_tree(c, tree_lens, ahead))
-      return launch_tree_attend(c, layer, nullptr, nullptr, nullptr, tree_lens, lens, masks, q, scale, out, lse_out, S, (cudaStream_t)stream);
-  }
+  int ahead[kMaxBatch];
+  for (int s = 0; s < c->cfg.max_batch; ++s) ahead[s] = c->h_len[(size_t)layer * c->cfg.max_batch + s] - tree_lens[s];
+  if (const int S = small_tree(c, tree_lens, ahead, window, sinks))
+    return launch_tree_attend(c, layer, nullptr, nullptr, nullptr, tree_lens, lens, masks, nullptr, q, window, sinks, scale, out, lse_out, S,
+                              (cudaStream_t)stream);
   return launch_chunk_attend(c, layer, q, tree_lens, lens, window, sinks, scale, out, lse_out, masks, (cudaStream_t)stream);
 }
 
@@ -1381,13 +1387,13 @@ int fkv_append_tree_attn(fkv_cache *c, int layer, const void *k, const void *v, 
   if (int e = check_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens)) return e;
   if (int e = check_tree(c, tree_lens, lens, masks, window)) return e;
   if (lens.tok[c->cfg.max_batch] > 0 && (!out || !aligned(out, 16) || !aligned(lse_out, 4))) return FKV_ERR_INVALID_ARG;
-  if (window == 0) {
-    int ahead[kMaxBatch];
-    for (int s = 0; s < c->cfg.max_batch; ++s) ahead[s] = keep_lens ? keep_lens[s] : c->h_len[(size_t)layer * c->cfg.max_batch + s];
-    if (const int S = small_tree(c, tree_lens, ahead)) {
-      if (int e = launch_tree_attend(c, layer, k, v, keep_lens, tree_lens, lens, masks, q, scale, out, lse_out, S, (cudaStream_t)stream)) return e;
-      return launch_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens, masks, true, (cudaStream_t)stream);
-    }
+  int ahead[kMaxBatch];
+  for (int s = 0; s < c->cfg.max_batch; ++s) ahead[s] = keep_lens ? keep_lens[s] : c->h_len[(size_t)layer * c->cfg.max_batch + s];
+  if (const int S = small_tree(c, tree_lens, ahead, window, sinks)) {
+    if (int e = launch_tree_attend(c, layer, k, v, keep_lens, tree_lens, lens, masks, pos, q, window, sinks, scale, out, lse_out, S,
+                                   (cudaStream_t)stream))
+      return e;
+    return launch_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens, masks, true, (cudaStream_t)stream);
   }
   if (int e = ensure_page_rows_map(c)) return e;   // (what can fail does so before anything is stored)
   if (int e = launch_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens, masks, false, (cudaStream_t)stream)) return e;

@@ -1,5 +1,5 @@
-// Kernel 10b: attention of draft trees where a launch's fixed cost counts - short caches, few sequences, no window:
-//     out_j = sum_i softmax_i(scale <q_j, k_i>) v_i  over the pairs ahead of the tree, j's ancestors and j itself.
+// Kernel 10b: attention of draft trees where a launch's fixed cost counts - short caches, few sequences:
+//     out_j = sum_i softmax_i(scale <q_j, k_i>) v_i  over the pairs ahead of the tree (window, sinks), j's ancestors and j itself.
 // Bound: bytes, 4 D per pair and KV head; for short caches and small trees the latency of one launch and its chain of reads.
 // k_chunk_attend computes the same for items of any number that it finds and cuts by itself, and joins them by a second kernel:
 // 20 us of a step that has 5 us of bytes (16 nodes over 8192 pairs).  Here the host says which CTA does what.
@@ -22,10 +22,13 @@ namespace fkv {
 
 constexpr int kTaMaxCluster = 16;
 constexpr int kTaRecvRows = 140;      // most of ceil(128 / S) S over S <= 16
+constexpr int kTaPos = 128;           // positions that are looked at together behind the first window's begin
 
 struct TreeArgs {
   int layer, append, blocks;          // append: the tree is not stored yet
+  int window, sinks;
   float scale_log2;
+  const int32_t *pos;                 // append: the nodes' positions or null (one behind the parent's)
   __nv_bfloat16 *out;
   float *lse;
   const uint32_t *masks;
@@ -40,7 +43,8 @@ struct TaSmem {
   static constexpr size_t kOffK = CS::kTile, kOffV = kOffK + CS::kSlots * CS::kKv, kOffRecv = kOffV + CS::kSlots * CS::kKv;
   static_assert((size_t)2 * kChunkRows * kRow * 4 <= kOffRecv, "the streams' results meet where the operands were");
   static constexpr size_t kOffBars = kOffRecv + (size_t)kTaRecvRows * kRow * 4;
-  static constexpr size_t bytes() { return 1024 + kOffBars + 256; }
+  static constexpr size_t kOffWin = kOffBars + 256;              // the search: positions, first slots of the nodes' windows, results
+  static constexpr size_t bytes() { return 1024 + kOffWin + (kTaPos + kChunkRows + 4) * 4; }
 };
 
 // 16 rows of a head in the caller's keys (64 channels) or values (all): per 64 channels 16 rows of 128 swizzled bytes.
@@ -51,7 +55,7 @@ __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap *tm, in
       : "memory");
 }
 
-template <int D>
+template <int D, bool WIN>
 __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(Ctx c, const __grid_constant__ CUtensorMap tmk,
                                                                   const __grid_constant__ CUtensorMap tmv,
                                                                   const __grid_constant__ CUtensorMap tmq,
@@ -108,15 +112,73 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(Ctx c, const _
   const bool bad = kp < 0 || kp > n_old || kp + T > c.cap;   // (the store says so where there is one)
   if (bad && T > 0 && !a.append && rank == 0 && head == 0 && threadIdx.x == 0) set_status(c, kDevBadIndex);
   const bool active = there && !bad;
-  // Units of 16 rows: stored pages, then (append) groups of nodes; this CTA's run of them in key tiles of up to TP, pages and nodes apart.
-  const int np = a.append ? (kp + kPage - 1) / kPage : (kp + j1 + kPage - 1) / kPage, nu = np + (a.append ? (j1 + kPage - 1) / kPage : 0);
-  const int per = (nu + S - 1) / S, u0 = min(nu, rank * per), u1 = min(nu, u0 + per);
-  const int pa = min(u0, np), pb = min(u1, np), ga = max(u0, np) - np, gb = max(u1, np) - np;
-  const int na = (pb - pa + TP - 1) / TP, nt = active ? na + (gb - ga + TP - 1) / TP : 0;
-  auto first = [&](int i) { return i < na ? pa + TP * i : ga + TP * (i - na); };   // of tile i: its first page, or group
-  auto units = [&](int i) { return min(TP, (i < na ? pb : gb) - first(i)); };
   const int stored = a.append ? kp : kp + T;       // pairs that the pages hold
   const int *ptrow = c.pt + (size_t)(ls * c.Hkv + head) * c.max_pages;
+  int *s_pos = reinterpret_cast<int *>(smem + SM::kOffWin), *s_wlo = s_pos + kTaPos, *s_win = s_wlo + kChunkRows;
+  // With a window: of the pairs ahead of the tree the block's nodes see slots [0, wa) (sinks) and from s_wlo[node] on, wb the first of these.
+  int wa = 0, wb = 0;
+  if (WIN) {   // (a window holds all of the tree: it is not shorter than the tree has nodes)
+    if (warp == 1 && active) {
+      const int W = a.window;
+      // The lowest position of the block's nodes: stored ones, given ones, or by the number of nodes on their paths.
+      const int lo0 = max(0, kp + 1 - W);
+      const int x0 = kp > 0 ? slot_pos(c, ptrow, min(lo0, kp - 1)) : 0;
+      const int last = a.append && !a.pos && kp > 0 ? slot_pos(c, ptrow, kp - 1) : -1;
+      const int sk = a.sinks ? slot_sinks(c, ptrow, kp, a.sinks) : 0;
+      int p[4], low = INT_MAX;   // (a block has at most 128 nodes)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int j = j0 + lane + 32 * u;
+        p[u] = INT_MAX;
+        if (j >= j1) continue;
+        if (!a.append) {
+          p[u] = slot_pos(c, ptrow, kp + j);
+        } else if (a.pos) {
+          p[u] = __ldcg(a.pos + row0 + j);
+        } else {
+          const uint32_t *row = a.masks + (size_t)(row0 + j) * kTreeWords;
+          p[u] = last;
+#pragma unroll
+          for (int w = 0; w < kTreeWords; ++w) p[u] += __popc(__ldcg(row + w));
+        }
+        low = min(low, p[u]);
+      }
+      low = __reduce_min_sync(0xffffffffu, low);
+      const int start = window_start(low, W);
+      const int f = lo0 >= kp ? kp : x0 >= start ? lo0 : slot_lower_bound_warp(c, ptrow, lo0 + 1, kp, start);
+      for (int i = lane; i < kTaPos && f + i < kp; i += 32) s_pos[i] = slot_pos(c, ptrow, f + i);
+      __syncwarp();
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {   // a window that begins d positions later begins at most d slots later
+        const int j = j0 + lane + 32 * u;
+        if (j >= j1) continue;
+        const int from = window_start(p[u], W);
+        int lo = f, hi = (int)min((long long)kp, f + (long long)p[u] - low);
+        if (hi - f < kTaPos) {
+          while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (s_pos[mid - f] < from) lo = mid + 1; else hi = mid;
+          }
+        } else {
+          lo = slot_lower_bound(c, ptrow, lo, hi, from);
+        }
+        s_wlo[j - j0] = lo;
+      }
+      if (lane == 0) { s_win[0] = sk; s_win[1] = max(sk, f); }
+    }
+    __syncthreads();
+    if (active) { wa = s_win[0]; wb = s_win[1]; }
+  }
+  // Units of 16 rows: pages of the sinks, the other pages, then (append) groups of nodes; this CTA's run of them in key tiles of up to TP,
+  // the three kinds apart.
+  const int np = a.append ? (kp + kPage - 1) / kPage : (kp + j1 + kPage - 1) / kPage;
+  const int sp_all = (wa + kPage - 1) / kPage, wp = max(sp_all, wb / kPage), nb = sp_all + max(0, np - wp), nu = nb + (a.append ? (j1 + kPage - 1) / kPage : 0);
+  const int per = (nu + S - 1) / S, u0 = min(nu, rank * per), u1 = min(nu, u0 + per);
+  const int s0 = min(u0, sp_all), s1 = min(u1, sp_all), shift = wp - sp_all;
+  const int pa = min(max(u0, sp_all), nb) + shift, pb = min(max(u1, sp_all), nb) + shift, ga = max(u0, nb) - nb, gb = max(u1, nb) - nb;
+  const int ns = (s1 - s0 + TP - 1) / TP, na = ns + (pb - pa + TP - 1) / TP, nt = active ? na + (gb - ga + TP - 1) / TP : 0;
+  auto first = [&](int i) { return i < ns ? s0 + TP * i : i < na ? pa + TP * (i - ns) : ga + TP * (i - na); };   // of tile i: its first page, or group
+  auto units = [&](int i) { return min(TP, (i < ns ? s1 : i < na ? pb : gb) - first(i)); };
 
   float m = -INFINITY, l = 0.f;
   if (warp >= 4) {
@@ -125,6 +187,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(Ctx c, const _
     const bool live = tok < TPT && node < j1;
     const bool any = __any_sync(0xffffffffu, live);
     const uint32_t ts = tmem_base + ((uint32_t)(quarter * 32) << 16) + t * CS::kStream, tp = ts + CS::kColP, to = ts + CS::kColO;
+    const int wlo = WIN && live ? s_wlo[tok] : 0;
     uint32_t sp = 0, pe = 1;
     bool ok = true;
     for (int i = t; i < nt; i += 2) {
@@ -133,6 +196,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(Ctx c, const _
       const int at = i < na ? f * kPage - kp : f * kPage;
       const int hi = live ? min(cols, min(node + 1 - at, i < na ? stored - f * kPage : INT_MAX)) : INT_MAX;
       const bool in_tree = at + cols > 0;
+      const int lo = WIN && i < na ? wlo - f * kPage : 0, sk = WIN ? wa - f * kPage : 0;   // with a window: columns [0, sk) and from lo on
       if (!mbar_sleep_warp(smem_u32(&s_full[t]), sp)) { set_status(c, kDevWaitTimeout); break; }
       sp ^= 1;
       tc_fence_after();
@@ -153,7 +217,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(Ctx c, const _
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&s_empty[t]));
-        if (!__all_sync(0xffffffffu, hi >= CS::kCols && !in_tree)) {   // hidden scores become -infinity
+        if (!__all_sync(0xffffffffu, hi >= CS::kCols && (!WIN || lo <= 0 || sk >= CS::kCols) && !in_tree)) {   // hidden scores become -infinity
           asm volatile("" ::: "memory");
           uint32_t see[3];
           const int k = at >> 5;
@@ -163,7 +227,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(Ctx c, const _
           for (int j = 0; j < 4; ++j) w[j] = !live || k + j < 0 ? ~0u : k + j < kTreeWords ? __ldcg(row + k + j) : 0u;
           auto below = [](int e) { return e <= 0 ? 0u : e >= 32 ? ~0u : (1u << e) - 1u; };   // bits under e
 #pragma unroll
-          for (int j = 0; j < 3; ++j) see[j] = __funnelshift_r(w[j], w[j + 1], at & 31) & below(hi - 32 * j);
+          for (int j = 0; j < 3; ++j) see[j] = __funnelshift_r(w[j], w[j + 1], at & 31) & below(hi - 32 * j) & (WIN ? below(sk - 32 * j) | ~below(lo - 32 * j) : ~0u);
 #pragma unroll
           for (int q = 0; q < TP; ++q)
 #pragma unroll
@@ -261,11 +325,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(Ctx c, const _
                        kd + (uint64_t)(((ks >> 2) * TP * (int)PAGE_HALF + (ks & 3) * 32) >> 4), idesc, ks > 0);
         umma_commit_if(on, smem_u32(&s_full[t]));
       } else {
-        // Rows behind the last pair are cleared (P is zero there, but zero times an infinity is not).
-        const int rows16 = i < na ? stored - first(i) * kPage : T - first(i) * kPage;
-        if (rows16 < n16 * kPage) {
-          for (int e = lane; e < (n16 * kPage - rows16) * NQ * 8; e += 32) {
-            const int row = rows16 + e / (NQ * 8), ch = e % (NQ * 8);
+        // Rows that no node of the block sees, behind the last pair or between sinks and windows, are cleared (P is zero there, but
+        // zero times an infinity is not).
+        const int f16 = first(i) * kPage, end = i < na ? stored : T, gap0 = WIN && i < na ? wa : 0, gap1 = WIN && i < na ? wb : 0;
+        if (f16 + n16 * kPage > end || (f16 < gap1 && f16 + n16 * kPage > gap0)) {
+          for (int e = lane; e < n16 * kPage * NQ * 8; e += 32) {
+            const int row = e / (NQ * 8), ch = e % (NQ * 8), at = f16 + row;
+            if (at < end && (at < gap0 || at >= gap1)) continue;
             *reinterpret_cast<uint4 *>(Vt + slot * CS::kKv + (size_t)((row / kPage * NQ + (ch >> 3)) * kPage + row % kPage) * 128 +
                                        (ch & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
           }
