@@ -389,38 +389,27 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(Ctx c, const _
     if (a.lse && lane == 0) a.lse[orow] = L == 0.f ? -INFINITY : (M * a.scale_log2 + log2f(L)) * 0.6931471805599453f;
   };
   auto weight = [&](float mi, float M) { return mi == -INFINITY ? 0.f : ex2((mi - M) * a.scale_log2); };
-  // ---- a warp joins the streams of four rows at a time and sends them to their owners ----
+  // ---- a warp per row joins the streams and sends the row to its owner.  (A short loop: this code runs a few times per launch, and
+  // to fetch it costs more than its arithmetic; four rows at a time take 1.5 us longer.) ----
   constexpr int NW = kChunkThreads / 32;
-  for (int rb = warp; rb < rows; rb += 4 * NW) {
-    float4 acc[4];
-    float M[4], L[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int r = rb + u * NW;
-      if (r >= rows) continue;
-      const float *p = mg + (size_t)r * ROW, *q = p + kChunkRows * ROW;
-      const float2 x = *reinterpret_cast<const float2 *>(p + D), y = *reinterpret_cast<const float2 *>(q + D);
-      M[u] = fmaxf(x.x, y.x);
-      const float fx = weight(x.x, M[u]), fy = weight(y.x, M[u]);
-      L[u] = fx * x.y + fy * y.y;   // (l is 0 where nothing was seen)
-      acc[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (lane * 4 < D) {   // (what was never written is not read)
-        const float4 v = fx != 0.f ? *reinterpret_cast<const float4 *>(p + lane * 4) : acc[u];
-        const float4 w = fy != 0.f ? *reinterpret_cast<const float4 *>(q + lane * 4) : acc[u];
-        acc[u] = make_float4(fx * v.x + fy * w.x, fx * v.y + fy * w.y, fx * v.z + fy * w.z, fx * v.w + fy * w.w);
-      }
+#pragma unroll 1
+  for (int r = warp; r < rows; r += NW) {
+    const float *p = mg + (size_t)r * ROW, *q = p + kChunkRows * ROW;
+    const float2 x = *reinterpret_cast<const float2 *>(p + D), y = *reinterpret_cast<const float2 *>(q + D);
+    const float M = fmaxf(x.x, y.x), fx = weight(x.x, M), fy = weight(y.x, M), L = fx * x.y + fy * y.y;   // (l is 0 where nothing was seen)
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (lane * 4 < D) {   // (what was never written is not read)
+      const float4 v = fx != 0.f ? *reinterpret_cast<const float4 *>(p + lane * 4) : acc;
+      const float4 w = fy != 0.f ? *reinterpret_cast<const float4 *>(q + lane * 4) : acc;
+      acc = make_float4(fx * v.x + fy * w.x, fx * v.y + fy * w.y, fx * v.z + fy * w.z, fx * v.w + fy * w.w);
     }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int r = rb + u * NW;
-      if (r >= rows) continue;
-      if (S == 1) {
-        finish(r, acc[u], M[u], L[u]);
-      } else {
-        const uint32_t to = dsmem_addr(smem_u32(recv + (size_t)(r / S * S + rank) * ROW), r % S);
-        if (lane * 4 < D) dsmem_st4(to + lane * 16, acc[u]);
-        if (lane == 0) dsmem_st2(to + D * 4, M[u], L[u]);
-      }
+    if (S == 1) {
+      finish(r, acc, M, L);
+    } else {
+      const int block = r / S;
+      const uint32_t to = dsmem_addr(smem_u32(recv + (size_t)(block * S + rank) * ROW), r - block * S);
+      if (lane * 4 < D) dsmem_st4(to + lane * 16, acc);
+      if (lane == 0) dsmem_st2(to + D * 4, M, L);
     }
   }
   if (S == 1) return;
@@ -439,10 +428,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(Ctx c, const _
     for (int sh = 8; sh >= 1; sh >>= 1) L += __shfl_xor_sync(0xffffffffu, L, sh);
     L = __shfl_sync(0xffffffffu, L, 0);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int s = 0; s < kTaMaxCluster; ++s) {
+#pragma unroll 4
+    for (int s = 0; s < S; ++s) {
       const float fs = __shfl_sync(0xffffffffu, f, s);
-      if (s < S && lane * 4 < D) {
+      if (lane * 4 < D) {
         const float4 v = *reinterpret_cast<const float4 *>(p + s * ROW + lane * 4);
         acc.x = fmaf(fs, v.x, acc.x); acc.y = fmaf(fs, v.y, acc.y); acc.z = fmaf(fs, v.z, acc.z); acc.w = fmaf(fs, v.w, acc.w);
       }
