@@ -1478,7 +1478,7 @@ int fkv_fork(fkv_cache *c, const int32_t *from, void *stream) {
   ForkOps ops;
   if (!make_fork(c, from, m, ops)) return FKV_OK;
   cudaStream_t st = (cudaStream_t)stream;
-  FKV_CUDA(launch_waiting(k_fork_plan, dim3(1), 1024, 0, st, c->ctx, m));
+  FKV_CUDA(launch_waiting(k_fork_plan, dim3(1), std::min(1024, (L * batch + 31) / 32 * 32), 0, st, c->ctx, m));
   ++c->launches;
   const int warps = (int)std::min<size_t>(kForkMaxWarps, (kMaxSmem - 1024) / (2 * (size_t)c->ctx.page_bytes));
   const size_t smem = (size_t)warps * 2 * c->ctx.page_bytes;
@@ -1486,7 +1486,7 @@ int fkv_fork(fkv_cache *c, const int32_t *from, void *stream) {
   FKV_CUDA(opt_in.ensure(k_fork_copy, kMaxSmem - 1024));
   FKV_CUDA(launch_waiting(k_fork_copy, dim3(c->sm_count), warps * 32, smem, st, c->ctx, m));
   ++c->launches;
-  FKV_CUDA(launch_waiting(k_fork_commit, dim3(L * batch), 256, 0, st, c->ctx, m));
+  FKV_CUDA(launch_waiting(k_fork_commit, dim3(L * batch, c->cfg.num_kv_heads), 256, 0, st, c->ctx, m));
   ++c->launches;
   if (c->cfg.feature_window > 0) {
     const size_t words = (size_t)c->ctx.hist_wp * c->cfg.num_kv_heads * c->cfg.group_size * c->cfg.head_dim / 8;

@@ -30,8 +30,9 @@ struct ForkOps {
 };
 // planhdr: PH_NWORK = source pages to read, PH_NEW_PAGES, PH_OLD_PAGES = pages taken and returned, PH_PUSH_START = the stack's top before, or
 // -1 where there are too few pages.  Per (layer, sequence): work = offset of its pages among those taken, tile1_start = among those returned,
-// idx[0 ..] = new length, idx[L batch ..] = offset of its pages among the source pages.
+// idx[0 ..] = new length, idx[L batch ..] = offset of its pages among the source pages, idx[2 L batch ..] = old length.
 
+// blockDim: a multiple of 32, up to 1024.
 __global__ void __launch_bounds__(1024) k_fork_plan(Ctx c, const __grid_constant__ ForkMap m) {
   __shared__ int s_scan[33];
   __shared__ unsigned long long s_need;
@@ -43,9 +44,10 @@ __global__ void __launch_bounds__(1024) k_fork_plan(Ctx c, const __grid_constant
   __syncthreads();
   for (int base = 0; base < LB; base += blockDim.x) {
     const int i = base + threadIdx.x;
-    int need = 0, gone = 0, read = 0, len = 0;
+    int need = 0, gone = 0, read = 0, len = 0, n = 0;
     if (i < LB) {
-      const int s = i % c.batch, l0 = i - s, n = __ldcg(c.len + i), what = m.what[s], r = m.from[s];
+      const int s = i % c.batch, l0 = i - s, what = m.what[s], r = m.from[s];
+      n = __ldcg(c.len + i);
       len = r < 0 ? 0 : __ldcg(c.len + l0 + r);
       if ((what & FORK_CHANGES) && !(what & FORK_MOVES)) need = (len + kPage - 1) / kPage * c.Hkv;
       if (what & FORK_FREED) gone = (n + kPage - 1) / kPage * c.Hkv;
@@ -61,6 +63,7 @@ __global__ void __launch_bounds__(1024) k_fork_plan(Ctx c, const __grid_constant
       c.tile1_start[i] = b;
       c.idx[i] = len;
       c.idx[LB + i] = u;
+      c.idx[2 * LB + i] = n;
     }
   }
   __syncthreads();
@@ -93,8 +96,8 @@ constexpr int kForkMaxWarps = 16, kForkGroup = 8;
 
 __device__ __forceinline__ void cp_bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 // Shared memory -> global, both 16-byte aligned, size a multiple of 16; completion by the issuing thread's groups.
-__device__ __forceinline__ void bulk_s2g(void *dst, uint32_t src, uint32_t bytes) {
-  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
+__device__ __forceinline__ void bulk_s2g_hint(void *dst, uint32_t src, uint32_t bytes, uint64_t pol) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group.L2::cache_hint [%0], [%1], %2, %3;" ::"l"(dst), "r"(src), "r"(bytes), "l"(pol) : "memory");
 }
 
 // One CTA per SM; a warp has two page buffers in shared memory and moves a run of source pages through them by bulk copies: a page
@@ -142,11 +145,12 @@ __global__ void __launch_bounds__(kForkMaxWarps * 32) k_fork_copy(Ctx c, const _
     return __ldcg(c.pt + ((size_t)lo * c.Hkv + h) * c.max_pages + i - h * pages);
   };
   const uint32_t buf = smem_u32(smem) + (uint32_t)(warp * 2 * c.page_bytes), bytes = (uint32_t)c.page_bytes;
+  const uint64_t policy = l2_policy_evict_first();   // (more than L2 holds passes through: 77 -> 73 us for 80 MB to three copies)
   uint32_t turn = 0;   // pages read so far: buffer and parity follow
   auto read_page = [&](uint32_t t, int page) {   // (lane 0) once the writes from this buffer have been taken out of it
     asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
     mbar_arrive_expect_tx(smem_u32(&bars[warp][t & 1]), bytes);
-    bulk_g2s(buf + (t & 1) * bytes, c.pool + (size_t)page * bytes, bytes, smem_u32(&bars[warp][t & 1]));
+    bulk_g2s_hint(buf + (t & 1) * bytes, c.pool + (size_t)page * bytes, bytes, smem_u32(&bars[warp][t & 1]), policy);
   };
   bool ok = true;
   while (u < u_end && ok) {
@@ -178,7 +182,7 @@ __global__ void __launch_bounds__(kForkMaxWarps * 32) k_fork_copy(Ctx c, const _
 #pragma unroll
         for (int k = 0; k < kForkGroup; ++k) {
           const int to = __shfl_sync(0xffffffffu, dst[k], i);
-          if (lane == 0 && k < nd) bulk_s2g(c.pool + (size_t)to * bytes, buf + (turn & 1) * bytes, bytes);
+          if (lane == 0 && k < nd) bulk_s2g_hint(c.pool + (size_t)to * bytes, buf + (turn & 1) * bytes, bytes, policy);
         }
         if (lane == 0) cp_bulk_commit();
         ++turn;
@@ -189,16 +193,16 @@ __global__ void __launch_bounds__(kForkMaxWarps * 32) k_fork_copy(Ctx c, const _
   if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");   // all writes are out
 }
 
-// grid = layers x sequences.
+// grid (layers x sequences, heads).
 __global__ void __launch_bounds__(256) k_fork_commit(Ctx c, const __grid_constant__ ForkMap m) {
   __shared__ int s_budget[kMaxBatch];
   griddep_wait();
   griddep_launch();
   const int top = __ldcg(c.planhdr + PH_PUSH_START);
   if (top < 0) return;
-  const int i = blockIdx.x, s = i % c.batch, tid = threadIdx.x, what = m.what[s];
+  const int i = blockIdx.x, h = blockIdx.y, s = i % c.batch, tid = threadIdx.x, what = m.what[s], LB = c.L * c.batch;
   const int bottom = top - __ldcg(c.planhdr + PH_NEW_PAGES);
-  if (i == 0) {   // (the budget goes with the sequence; an emptied place keeps its own)
+  if (i == 0 && h == 0) {   // (the budget goes with the sequence; an emptied place keeps its own)
     if (tid == 0) c.ctrl[CTRL_FREE_TOP] = bottom + c.planhdr[PH_OLD_PAGES];
     static_assert(kMaxBatch <= 256, "one thread per sequence");
     if (tid < c.batch) s_budget[tid] = c.budget[tid];
@@ -206,21 +210,18 @@ __global__ void __launch_bounds__(256) k_fork_commit(Ctx c, const __grid_constan
     if (tid < c.batch && m.from[tid] >= 0) c.budget[tid] = s_budget[m.from[tid]];
   }
   if (!(what & FORK_CHANGES)) return;
-  const int n = c.len[i], n_new = c.idx[i], cnt_old = (n + kPage - 1) / kPage, cnt_new = (n_new + kPage - 1) / kPage;
+  const int n = __ldcg(c.idx + 2 * LB + i), n_new = __ldcg(c.idx + i), cnt_old = (n + kPage - 1) / kPage, cnt_new = (n_new + kPage - 1) / kPage;
+  int *ptrow = c.pt + ((size_t)i * c.Hkv + h) * c.max_pages;
+  const int *ptnew = c.pt_new + ((size_t)i * c.Hkv + h) * c.max_pages;
   if (what & FORK_FREED) {   // (those that would go below the stack's bottom are the ones that were taken again)
-    const int at = bottom + c.tile1_start[i];
-    for (int x = tid; x < cnt_old * c.Hkv; x += blockDim.x) {
-      const int h = x / cnt_old;
-      if (at + x >= 0) c.free_stack[at + x] = c.pt[((size_t)i * c.Hkv + h) * c.max_pages + x - h * cnt_old];
-    }
+    const int at = bottom + __ldcg(c.tile1_start + i) + h * cnt_old;
+    for (int x = tid; x < cnt_old; x += blockDim.x)
+      if (at + x >= 0) c.free_stack[at + x] = ptrow[x];
+    __syncthreads();
   }
-  __syncthreads();
-  for (int x = tid; x < cnt_new * c.Hkv; x += blockDim.x) {
-    const int h = x / cnt_new;
-    const size_t at = ((size_t)i * c.Hkv + h) * c.max_pages + x - h * cnt_new;
-    c.pt[at] = c.pt_new[at];
-  }
-  if (tid == 0) c.len[i] = n_new;
+#pragma unroll 4
+  for (int x = tid; x < cnt_new; x += blockDim.x) ptrow[x] = __ldcg(ptnew + x);
+  if (tid == 0 && h == 0) c.len[i] = n_new;
 }
 
 // grid (enough threads for a sequence's record in 16-byte words, layers).  Runs behind k_fork_commit (nothing there reads the record).
