@@ -409,10 +409,10 @@ class Cache:
     @staticmethod
     def _at(name, t, dtype, shape, dev):
         """The address of a contiguous tensor of this type and shape on the cache's device."""
-        if t.shape != shape or t.dtype is not dtype or t.device != dev or not t.is_contiguous():
-            raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}, got {t.dtype} "
-                             f"{tuple(t.shape)} on {t.device}, contiguous={t.is_contiguous()}")
-        return t.data_ptr()
+        if t.dtype is dtype and t.shape == shape and t.device == dev and t.is_contiguous():
+            return t.data_ptr()
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}, contiguous={t.is_contiguous()}")
 
     def _per_sequence(self, x, what):
         """One 32-bit integer per sequence as the host array that the library reads: (array to keep alive, address)."""
@@ -430,9 +430,10 @@ class Cache:
         dev = self._here()
         total = sum(tree_lens)
         keep, lens = self._per_sequence(tree_lens, "tree_lens")
+        up = self._at("parents", parents, torch.int32, (total,), dev)
         if out is None:
-            out = torch.empty((total, TREE_WORDS), dtype=torch.int32, device=dev)
-        _check(lib().fkv_tree_masks(self._h, self._at("parents", parents, torch.int32, (total,), dev), lens,
+            out = parents.new_empty((total, TREE_WORDS))
+        _check(lib().fkv_tree_masks(self._h, up, lens,
                                     self._at("masks", out, torch.int32, (total, TREE_WORDS), dev), _stream_on(dev)), "fkv_tree_masks")
         return out
 
@@ -561,7 +562,7 @@ class Cache:
         shapes = ((total, c.num_kv_heads, c.head_dim),) * 2 + ((total, c.num_kv_heads, self.feat_dim), (total, c.num_kv_heads))
         types = (torch.bfloat16, torch.bfloat16, torch.float32, torch.int32)
         if out is None:
-            out = tuple(torch.empty(s, dtype=t, device=dev) for s, t in zip(shapes, types))
+            out = tuple(self.workspace.new_empty(s, dtype=t) for s, t in zip(shapes, types))
         to = [None if t is None else self._at("out", t, d, s, dev) for t, d, s in zip(out, types, shapes)]
         _check(lib().fkv_export_chunk(self._h, layer, lens, *to, _stream_on(dev)), "fkv_export_chunk")
         return out

@@ -829,7 +829,7 @@ int launch_tree_attend(fkv_cache *c, int layer, const void *k, const void *v, co
 template <class T, bool Q>
 int launch_verify_t(fkv_cache *c, const VerifyArgs &a, cudaStream_t st) {
   int cs = 1;
-  while (cs < kVerMaxCluster && cs * 2 * c->cfg.max_batch <= kVerCtasPerSm * c->sm_count) cs *= 2;
+  while (cs < kVerParts && cs * 2 * c->cfg.max_batch <= kVerCtasPerSm * c->sm_count) cs *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(c->cfg.max_batch * cs);
   cfg.blockDim = dim3(kVerThreads);

@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(256) k_fork_commit(Ctx c, const __grid_constan
   if (what & FORK_FREED) {   // (those that would go below the stack's bottom are the ones that were taken again)
     const int at = bottom + __ldcg(c.tile1_start + i) + h * cnt_old;
     for (int x = tid; x < cnt_old; x += blockDim.x)
-      if (at + x >= 0) c.free_stack[at + x] = ptrow[x];
+      if (at + x >= 0) c.free_stack[at + x] = __ldcg(ptrow + x);
     __syncthreads();
   }
 #pragma unroll 4

@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(1024) k_commit_tree(Ctx c, int l0, const __gri
   __syncthreads();
   for (int i = tid; i < gone * c.Hkv; i += blockDim.x) {
     const int h = i / gone;
-    c.free_stack[s_push + i] = c.pt[(size_t)seg_of(c, layer, seq, h) * c.max_pages + kept + i - h * gone];
+    c.free_stack[s_push + i] = __ldcg(c.pt + (size_t)seg_of(c, layer, seq, h) * c.max_pages + kept + i - h * gone);
   }
 }
 

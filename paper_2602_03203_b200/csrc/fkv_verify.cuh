@@ -15,8 +15,9 @@
 // The walk itself runs in every thread alike, on numbers gathered ahead of it (p and q of every node's own token: one read).
 // A pass is cut into pieces of 256 tokens; their sums stay in shared memory, so the piece that holds the drawn token is found
 // there and read once more.  Everything is fp64: products of two fp32 numbers are exact, and sums over 10^5 terms that are
-// compared with u lose nothing that fp32 inputs hold.  A sequence is a cluster of CTAs, each with a share of the
-// pieces; sums meet through distributed shared memory, in the order of the ranks: the same in all CTAs and in every run.
+// compared with u lose nothing that fp32 inputs hold.  A sequence is a cluster of up to eight CTAs; its pieces are eight parts, summed
+// each in the same order whichever CTA has it, and the parts' sums meet through distributed shared memory: results are the same bits
+// in all CTAs, in every run and in every batch.
 // Bound: bytes of the rows that are read; for few sequences latency (gather, pass, exchange, piece: four dependent reads).
 #pragma once
 #include "fkv_dev.cuh"
@@ -29,7 +30,7 @@ constexpr int kVerThreads = 512, kVerWarps = kVerThreads / 32;
 constexpr int kVerPiece = 256;                    // tokens of a piece: eight per lane
 constexpr int kVerMaxVocab = 1 << 20;
 constexpr int kVerPieces = kVerMaxVocab / kVerPiece;
-constexpr int kVerMaxCluster = 8;
+constexpr int kVerParts = 8;                      // of a row's pieces; CTAs of a cluster: 1, 2, 4 or 8
 constexpr int kVerCtasPerSm = 2;                  // that fit at a time
 
 struct VerifyArgs {
@@ -66,8 +67,8 @@ __device__ __forceinline__ double warp_sum(double x) {
 template <class T, bool Q>
 __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx c, const __grid_constant__ VerifyArgs a) {
   __shared__ double s_sum[kVerPieces];              // sums of this CTA's pieces
-  __shared__ double s_all[2][kVerMaxCluster];       // the CTAs' sums, of this pass and of the last
-  __shared__ double s_part[kVerWarps];
+  __shared__ double s_all[2][kVerParts];            // the parts' sums, of this pass and of the last
+  __shared__ double s_warp[kVerParts][kVerWarps];
   __shared__ double s_p[kTreeNodes], s_q[kTreeNodes];
   __shared__ float s_u[kTreeNodes];
   __shared__ int s_tok[kTreeNodes];
@@ -97,8 +98,8 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
     s_tok[tid] = ok ? x : -1;
     s_par[tid] = (short)p;
     s_u[tid] = __ldcg(a.u_accept + row0 + tid);
-    s_p[tid] = ok ? fmax((double)to_f32(row_p(p)[x]), 0.0) : 0.0;   // (NaN and negative numbers count as 0)
-    if (Q) s_q[tid] = ok ? (double)to_f32(row_q(p)[x]) : 0.0;
+    s_p[tid] = ok ? fmax((double)to_f32(__ldcg(row_p(p) + x)), 0.0) : 0.0;   // (NaN and negative numbers count as 0)
+    if (Q) s_q[tid] = ok ? (double)to_f32(__ldcg(row_q(p) + x)) : 0.0;
   }
   __syncthreads();
   if (tid < nodes) {
@@ -115,7 +116,9 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
   __syncthreads();
 
   const int pieces = (V + kVerPiece - 1) / kVerPiece;
-  const int c0 = (int)((long long)pieces * rank / cs), c1 = (int)((long long)pieces * (rank + 1) / cs);
+  const int per = kVerParts / cs;   // this CTA's parts are [rank per, (rank + 1) per)
+  auto begin = [&](int part) { return (int)((long long)pieces * part / kVerParts); };
+  const int c0 = begin(rank * per);
   int turn = 0;
   int cur = 0, len = 0;
   // What R is without its divisor: p - alpha q, or p without the tokens of cur's children.
@@ -132,8 +135,8 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const bool in = x0 + 32 * i < V;
-      pv[i] = in ? pr[x0 + 32 * i] : T(0.f);
-      if (Q) qv[i] = in ? qr[x0 + 32 * i] : T(0.f);
+      pv[i] = in ? __ldcg(pr + x0 + 32 * i) : T(0.f);
+      if (Q) qv[i] = in ? __ldcg(qr + x0 + 32 * i) : T(0.f);
     }
   };
   auto weights = [&](int pc, const T (&pv)[8], const T (&qv)[8], double alpha, double (&w)[8]) {
@@ -148,34 +151,33 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
           if (tried(pc * kVerPiece + lane + 32 * i)) w[i] = 0.0;
     }
   };
-  // The sum over the vocabulary, the same in every CTA; the pieces' sums stay in s_sum, the CTAs' in s_all[turn ^ 1].
+  // The sum over the vocabulary, the same in every CTA; the pieces' sums stay in s_sum, the parts' in s_all[turn ^ 1].
   auto pass = [&](double alpha) {
-    double sum = 0.0;
+    for (int part = 0; part < per; ++part) {
+      const int b0 = begin(rank * per + part), b1 = begin(rank * per + part + 1);
+      double sum = 0.0;
 #pragma unroll 1
-    for (int pc = c0 + warp; pc < c1; pc += 2 * kVerWarps) {   // two pieces are asked for together
-      T pv[2][8], qv[2][8];
-      load(pc, pv[0], qv[0]);
-      if (pc + kVerWarps < c1) load(pc + kVerWarps, pv[1], qv[1]);
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        if (pc + b * kVerWarps >= c1) break;
+      for (int pc = b0 + warp; pc < b1; pc += kVerWarps) {
+        T pv[8], qv[8];
+        load(pc, pv, qv);
         double w[8];
-        weights(pc + b * kVerWarps, pv[b], qv[b], alpha, w);
+        weights(pc, pv, qv, alpha, w);
         const double x = warp_sum(((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7])));
-        if (lane == 0) s_sum[pc + b * kVerWarps - c0] = x;
+        if (lane == 0) s_sum[pc - c0] = x;
         sum += x;
       }
+      if (lane == 0) s_warp[part][warp] = sum;
     }
-    if (lane == 0) s_part[warp] = sum;
     __syncthreads();
-    if (tid < cs) {
+    for (int e = tid; e < per * cs; e += kVerThreads) {   // (part, CTA that it goes to)
+      const int part = e / cs;
       double all = 0.0;
-      for (int i = 0; i < kVerWarps; ++i) all += s_part[i];
-      dsmem_st_f64(dsmem_addr(smem_u32(&s_all[turn][rank]), tid), all);
+      for (int i = 0; i < kVerWarps; ++i) all += s_warp[part][i];
+      dsmem_st_f64(dsmem_addr(smem_u32(&s_all[turn][rank * per + part]), e - part * cs), all);
     }
     cluster_sync_all();   // (a CTA's next pass writes the other half; this one is written again behind the next barrier)
     double all = 0.0;
-    for (int i = 0; i < cs; ++i) all += s_all[turn][i];
+    for (int i = 0; i < kVerParts; ++i) all += s_all[turn][i];
     turn ^= 1;
     return all;
   };
@@ -223,23 +225,24 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
   }
   if (!summed) S = pass(Q ? alpha : 0.0);
   if (rank == 0 && tid == 0) a.path_len[seq] = len;
-  // The next token: the CTA, the piece, then the place at which the running sum exceeds u S.
+  // The next token: the part, the piece, then the place at which the running sum exceeds u S.
   const double *all = s_all[turn ^ 1];
   const double t = (double)__ldcg(a.u_sample + seq) * S;
   int owner = -1;
   double before = 0.0, run = 0.0;
-  for (int i = 0; i < cs; ++i) {
+  for (int i = 0; i < kVerParts; ++i) {
     if (all[i] > 0.0 && (owner < 0 || run <= t)) {   // (the last one that holds anything, where rounding leaves t behind all)
       owner = i;
       before = run;
     }
     run += all[i];
   }
-  if (owner != rank || warp != 0) return;   // (owner < 0: no mass at all, and out keeps its -1)
+  if (owner < 0 || owner / per != rank || warp != 0) return;   // (owner < 0: no mass at all, and out keeps its -1)
+  const int b0 = begin(owner), b1 = begin(owner + 1);
   int at = -1;
   run = before;
-  for (int b = 0; b < c1 - c0; b += 32) {
-    const double x = b + lane < c1 - c0 ? s_sum[b + lane] : 0.0;
+  for (int b = b0; b < b1; b += 32) {
+    const double x = b + lane < b1 ? s_sum[b + lane - c0] : 0.0;
     double inc = x;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -259,8 +262,8 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
   double w[8];
   {
     T pv[8], qv[8];
-    load(c0 + at, pv, qv);
-    weights(c0 + at, pv, qv, alpha, w);
+    load(at, pv, qv);
+    weights(at, pv, qv, alpha, w);
   }
   int found = -1;
   run = before;
@@ -280,7 +283,7 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
     if (some) found = 32 * i + 31 - __clz(some);
     run += __shfl_sync(0xffffffffu, inc, 31);
   }
-  if (lane == 0) out[len - 1] = (c0 + at) * kVerPiece + found;
+  if (lane == 0) out[len - 1] = at * kVerPiece + found;
 }
 
 // Temperature zero: the target's own choice after every node is known, and the walk takes the child that has it (the one with
