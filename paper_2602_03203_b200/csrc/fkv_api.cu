@@ -161,7 +161,7 @@ struct fkv_cache {
   uint64_t launches = 0;
   int sm_count = 148;
   int max_cluster[2] = {0, 0};   // largest attention cluster the device places (found at the first stand-alone launch): plain, windowed
-  int tree_clusters[2][kTaMaxCluster + 1] = {};   // clusters of 1 .. 16 tree CTAs (plain, windowed) that fit the device (0: not asked yet, -1: none)
+  int tree_clusters[2][2][kTaMaxCluster + 1] = {};   // clusters of 1 .. 16 tree CTAs (windowed, half) that fit the device (0: not asked yet, -1: none)
   float feature_scale = 0.f;  // softmax scale of the recorded queries (the last decode call's)
   bool timing = false, timed = false;
   CUtensorMap page_parts;     // ... as [page][64-channel part][row][64 channels]
@@ -582,9 +582,9 @@ int check_append_chunk(const fkv_cache *c, int layer, const void *k, const void 
   return FKV_OK;
 }
 
-// masks: of a draft tree, else NULL.  behind: its attention was launched just now (see the kernel).
+// masks: of a draft tree, else NULL.
 int launch_append_chunk(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *pos, const int32_t *keep_lens,
-                        const int32_t *chunk_lens, const ChunkLens &lens, const uint32_t *masks, bool behind, cudaStream_t st) {
+                        const int32_t *chunk_lens, const ChunkLens &lens, const uint32_t *masks, cudaStream_t st) {
   const int batch = c->cfg.max_batch;
   // (A roll-back to the lengths that the host knows is launched all the same: replayed, it meets others.)
   if (lens.tok[batch] == 0 && !keep_lens) return FKV_OK;
@@ -597,7 +597,7 @@ int launch_append_chunk(fkv_cache *c, int layer, const void *k, const void *v, c
   const long long tasks = (long long)lens.tok[batch] * c->cfg.num_kv_heads;
   const int grid = (int)std::max<long long>(1, std::min<long long>((tasks + 7) / 8, 4LL * c->sm_count));
   FKV_CUDA(launch_waiting(masks ? k_append_chunk<true> : k_append_chunk<false>, dim3(grid), 256, 0, st, c->ctx, layer, (const uint8_t *)k,
-                          (const uint8_t *)v, pos, lens, keep, masks, behind ? 1 : 0));
+                          (const uint8_t *)v, pos, lens, keep, masks));
   ++c->launches;
   for (int s = 0; s < batch; ++s) {
     int &n = c->h_len[(size_t)layer * batch + s];
@@ -720,13 +720,13 @@ bool trees_ok(const fkv_cache *c, const int32_t *tree_lens, int window) {
   return true;
 }
 
-// Trees whose attention is one launch of clusters (k_tree_attend).
-template <int D, bool WIN>
+// Trees whose attention (and store) is one launch of clusters (k_tree_attend).
+template <int D, bool WIN, bool HALF>
 int tree_attend_config(cudaLaunchConfig_t &cfg, cudaLaunchAttribute (&at)[2], int S, int y, cudaStream_t st) {
   constexpr size_t smem = TaSmem<D>::bytes();
   static_assert(smem <= kMaxSmem, "one CTA's shared memory");
   static SmemOptIn opt_in;
-  FKV_CUDA(opt_in.ensure(k_tree_attend<D, WIN>, smem));
+  FKV_CUDA(opt_in.ensure(k_tree_attend<D, WIN, HALF>, smem));
   cfg = cudaLaunchConfig_t{};
   cfg.gridDim = dim3(S, y);
   cfg.blockDim = dim3(kChunkThreads);
@@ -741,77 +741,100 @@ int tree_attend_config(cudaLaunchConfig_t &cfg, cudaLaunchAttribute (&at)[2], in
   return FKV_OK;
 }
 // How many clusters of S CTAs the device holds at a time (-1: none).
-template <int D, bool WIN>
+template <int D, bool WIN, bool HALF>
 int tree_clusters(int S) {
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute at[2];
   int n = 0;
-  const bool ok = tree_attend_config<D, WIN>(cfg, at, S, 1, nullptr) == FKV_OK &&
-                  cudaFuncSetAttribute(k_tree_attend<D, WIN>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
-                  (cfg.numAttrs = 1, cudaOccupancyMaxActiveClusters(&n, k_tree_attend<D, WIN>, &cfg) == cudaSuccess) && n > 0;
+  const bool ok = tree_attend_config<D, WIN, HALF>(cfg, at, S, 1, nullptr) == FKV_OK &&
+                  cudaFuncSetAttribute(k_tree_attend<D, WIN, HALF>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                  (cfg.numAttrs = 1, cudaOccupancyMaxActiveClusters(&n, k_tree_attend<D, WIN, HALF>, &cfg) == cudaSuccess) && n > 0;
   (void)cudaGetLastError();
   return ok ? n : -1;
 }
+template <int D, bool WIN, bool HALF>
+int launch_tree_attend_t(fkv_cache *c, const CUtensorMap (&in)[3], const TreeArgs &a, int S, int store, cudaStream_t st) {
+  cudaLaunchConfig_t cfg;
+  cudaLaunchAttribute at[2];
+  if (int e = tree_attend_config<D, WIN, HALF>(cfg, at, S, a.rows_y + store, st)) return e;
+  FKV_CUDA(cudaLaunchKernelEx(&cfg, k_tree_attend<D, WIN, HALF>, c->ctx, c->page_rows, c->page_parts, in[0], in[1], in[2], a));
+  ++c->launches;
+  return FKV_OK;
+}
+// The forms of the kernel by head dimension, window and rows.
+#define FKV_TREE_FORM(f, ...)                                                                                                  \
+  (c->cfg.head_dim == 128 ? win ? half ? f<128, true, true>(__VA_ARGS__) : f<128, true, false>(__VA_ARGS__)                    \
+                                : half ? f<128, false, true>(__VA_ARGS__) : f<128, false, false>(__VA_ARGS__)                  \
+                          : win ? half ? f<64, true, true>(__VA_ARGS__) : f<64, true, false>(__VA_ARGS__)                      \
+                                : half ? f<64, false, true>(__VA_ARGS__) : f<64, false, false>(__VA_ARGS__))
 
-// CTAs per block of query rows with which k_tree_attend serves the call; 0: the general kernel is to.  ahead: pairs ahead of every tree.
-int small_tree(fkv_cache *c, const int32_t *tree_lens, const int *ahead, int window, int sinks) {
-  const int batch = c->cfg.max_batch, Hkv = c->cfg.num_kv_heads, block = kChunkRows / c->cfg.group_size;
-  long long total = 0, segs = 0;
+// How k_tree_attend serves a call: CTAs per block of query rows (0: the general kernel is to serve it), clusters that store, rows twice.
+struct TreeShape {
+  int S = 0, store = 0;
+  bool half = false;
+  int block = 0;   // nodes of a block of query rows
+};
+// ahead: pairs ahead of every tree.
+TreeShape tree_shape(fkv_cache *c, const int32_t *tree_lens, const int *ahead, int window, int sinks, bool append) {
+  const int batch = c->cfg.max_batch, Hkv = c->cfg.num_kv_heads, G = c->cfg.group_size;
+  TreeShape r;
+  int longest = 0;
+  for (int s = 0; s < batch; ++s) longest = std::max(longest, tree_lens[s]);
+  r.half = longest * G <= kChunkRows / 2;
+  r.block = (r.half ? kChunkRows / 2 : kChunkRows) / G;
+  long long total = 0, segs = 0, tokens = 0;
   int most = 0;
   for (int s = 0; s < batch; ++s) {
     if (tree_lens[s] == 0) continue;
-    const int blocks = (tree_lens[s] + block - 1) / block, all = (ahead[s] + tree_lens[s] + kPage - 1) / kPage + 1;
+    const int blocks = (tree_lens[s] + r.block - 1) / r.block, all = (ahead[s] + tree_lens[s] + kPage - 1) / kPage + 1;
     // (a window of W positions holds at most W pairs)
     const int pages = window ? (int)std::min<long long>(all, ((long long)window + std::min(sinks, ahead[s]) + tree_lens[s]) / kPage + 3) : all;
     most = std::max(most, pages);
     segs += (long long)blocks * Hkv;
     total += (long long)blocks * Hkv * pages;
+    tokens += tree_lens[s];
   }
-  if (segs == 0 || segs > c->sm_count) return 0;
-  // The largest cluster of which the device holds all at once, with a few pages at least for every CTA.
+  if (segs == 0 || segs > c->sm_count) return r;
+  // The largest cluster of which the device holds all at once, one that stores among them, with a few pages at least for every CTA.
+  const bool win = window > 0, half = r.half;
   int S = (int)std::min<long long>(std::min<long long>(kTaMaxCluster, c->sm_count / segs), std::max(1, most / kAttendMinPages));
+  int fit = 0;
   for (; S > 0; --S) {
-    int &fit = c->tree_clusters[window > 0][S];
-    if (fit == 0) {
-      if (window > 0) fit = c->cfg.head_dim == 128 ? tree_clusters<128, true>(S) : tree_clusters<64, true>(S);
-      else fit = c->cfg.head_dim == 128 ? tree_clusters<128, false>(S) : tree_clusters<64, false>(S);
-    }
-    if (fit >= segs) break;
+    int &known = c->tree_clusters[win][half][S];
+    if (known == 0) known = FKV_TREE_FORM(tree_clusters, S);
+    fit = known;
+    if (fit >= segs + (append ? 1 : 0)) break;
   }
-  if (S == 0) return 0;
-  // The general kernel shares the pages evenly over the SMs but starts and joins some 20 us later; a page takes an SM 0.15 us.
-  return (most + S - 1) / S <= total / c->sm_count + 100 ? S : 0;
+  if (S == 0) return r;
+  // The general kernels share the pages evenly over the SMs but start and join some 20 us later; a page takes an SM 0.15 us.
+  if ((most + S - 1) / S > total / c->sm_count + 100) return r;
+  r.S = S;
+  const long long warps = (long long)S * (kChunkThreads / 32);   // a pair and head each
+  if (append) r.store = (int)std::max<long long>(1, std::min<long long>((tokens * Hkv + warps - 1) / warps, fit - segs));
+  return r;
 }
 
-template <int D, bool WIN>
-int launch_tree_attend_t(fkv_cache *c, const CUtensorMap (&in)[3], const TreeArgs &a, int S, cudaStream_t st) {
-  cudaLaunchConfig_t cfg;
-  cudaLaunchAttribute at[2];
-  if (int e = tree_attend_config<D, WIN>(cfg, at, S, c->cfg.max_batch * c->cfg.num_kv_heads * a.blocks, st)) return e;
-  FKV_CUDA(cudaLaunchKernelEx(&cfg, k_tree_attend<D, WIN>, c->ctx, c->page_rows, c->page_parts, in[0], in[1], in[2], a));
-  ++c->launches;
-  return FKV_OK;
-}
-
-// k, v: of a tree that is not stored yet (the store is launched behind, see k_append_chunk), else NULL.
+// k, v: of a tree that is not stored yet, else NULL.
 int launch_tree_attend(fkv_cache *c, int layer, const void *k, const void *v, const int32_t *keep_lens, const int32_t *tree_lens,
                        const ChunkLens &lens, const uint32_t *masks, const int32_t *pos, const void *q, int window, int sinks, float scale, void *out,
-                       float *lse, int S, cudaStream_t st) {
-  const int batch = c->cfg.max_batch, D = c->cfg.head_dim, Hkv = c->cfg.num_kv_heads, block = kChunkRows / c->cfg.group_size;
+                       float *lse, const TreeShape &shape, cudaStream_t st) {
+  const int batch = c->cfg.max_batch, D = c->cfg.head_dim, Hkv = c->cfg.num_kv_heads;
   if (int e = ensure_page_rows_map(c)) return e;
   TreeArgs a;
-  a.layer = layer; a.append = k != nullptr; a.window = window; a.sinks = window ? sinks : 0; a.pos = pos;
+  a.layer = layer; a.append = k != nullptr; a.window = window; a.sinks = window ? sinks : 0;
+  a.k = (const uint8_t *)k; a.v = (const uint8_t *)v; a.pos = pos;
   a.scale_log2 = (scale == 0.f ? 1.f / sqrtf((float)D) : scale) * 1.4426950408889634f;
   a.out = (__nv_bfloat16 *)out; a.lse = lse; a.masks = masks; a.lens = lens;
   a.blocks = 1;
-  for (int s = 0; s < batch; ++s) a.blocks = std::max(a.blocks, (tree_lens[s] + block - 1) / block);
+  for (int s = 0; s < batch; ++s) a.blocks = std::max(a.blocks, (tree_lens[s] + shape.block - 1) / shape.block);
+  a.rows_y = batch * Hkv * a.blocks;
   a.keep = ChunkKeep{};
   if (keep_lens) {
     a.keep.use = 1;
     for (int s = 0; s < batch; ++s) a.keep.keep[s] = keep_lens[s];
   }
   CUtensorMap in[3];
-  if (int e = query_map(c, q, lens.tok[batch], c->cfg.group_size, block, &in[0])) return e;
+  if (int e = query_map(c, q, lens.tok[batch], c->cfg.group_size, shape.block, &in[0])) return e;
   in[1] = in[2] = in[0];
   if (k) {   // [tokens][Hkv][D] as (64 channels, tokens, parts of 64 channels, heads): a box = 16 tokens of a head, one part (K) or all (V)
     const cuuint64_t dims[4] = {64, (cuuint64_t)lens.tok[batch], (cuuint64_t)(D / 64), (cuuint64_t)Hkv};
@@ -820,8 +843,14 @@ int launch_tree_attend(fkv_cache *c, int layer, const void *k, const void *v, co
     if (int e = tensor_map(&in[1], const_cast<void *>(k), 4, dims, strides, box_k, CU_TENSOR_MAP_SWIZZLE_128B)) return e;
     if (int e = tensor_map(&in[2], const_cast<void *>(v), 4, dims, strides, box_v, CU_TENSOR_MAP_SWIZZLE_128B)) return e;
   }
-  if (window) return D == 128 ? launch_tree_attend_t<128, true>(c, in, a, S, st) : launch_tree_attend_t<64, true>(c, in, a, S, st);
-  return D == 128 ? launch_tree_attend_t<128, false>(c, in, a, S, st) : launch_tree_attend_t<64, false>(c, in, a, S, st);
+  const bool win = window > 0, half = shape.half;
+  if (int e = FKV_TREE_FORM(launch_tree_attend_t, c, in, a, shape.S, shape.store, st)) return e;
+  if (k)
+    for (int s = 0; s < batch; ++s) {
+      int &n = c->h_len[(size_t)layer * batch + s];
+      n = (keep_lens ? keep_lens[s] : n) + tree_lens[s];
+    }
+  return FKV_OK;
 }
 
 // A cluster of CTAs per sequence: eight, or as many as the SMs hold at a time for all sequences: a pass is a chain of reads, so a
@@ -1290,7 +1319,7 @@ int fkv_append_chunk(fkv_cache *c, int layer, const void *k, const void *v, cons
                      const int32_t *chunk_lens, void *stream) {
   ChunkLens lens;
   if (int e = check_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens)) return e;
-  return launch_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens, nullptr, false, (cudaStream_t)stream);
+  return launch_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens, nullptr, (cudaStream_t)stream);
 }
 
 int fkv_chunk_attn(fkv_cache *c, int layer, const void *q, const int32_t *chunk_lens, int32_t window, int32_t sinks, float scale,
@@ -1310,7 +1339,7 @@ int fkv_append_chunk_attn(fkv_cache *c, int layer, const void *k, const void *v,
   if (int e = check_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens)) return e;
   if (lens.tok[c->cfg.max_batch] > 0 && (!out || !aligned(out, 16) || !aligned(lse_out, 4))) return FKV_ERR_INVALID_ARG;
   if (int e = ensure_page_rows_map(c)) return e;   // (what can fail does so before anything is stored)
-  if (int e = launch_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens, nullptr, false, (cudaStream_t)stream)) return e;
+  if (int e = launch_append_chunk(c, layer, k, v, pos, keep_lens, chunk_lens, lens, nullptr, (cudaStream_t)stream)) return e;
   return launch_chunk_attend(c, layer, q, chunk_lens, lens, window, sinks, scale, out, lse_out, nullptr, (cudaStream_t)stream);
 }
 
@@ -1361,7 +1390,7 @@ int fkv_append_tree(fkv_cache *c, int layer, const void *k, const void *v, const
   ChunkLens lens;
   if (int e = check_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens)) return e;
   if (int e = check_tree(c, tree_lens, lens, masks, 0)) return e;
-  return launch_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens, masks, false, (cudaStream_t)stream);
+  return launch_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens, masks, (cudaStream_t)stream);
 }
 
 int fkv_tree_attn(fkv_cache *c, int layer, const void *q, const int32_t *tree_lens, const uint32_t *masks, int32_t window, int32_t sinks,
@@ -1373,8 +1402,9 @@ int fkv_tree_attn(fkv_cache *c, int layer, const void *q, const int32_t *tree_le
   if (!chunk_is_stored(c, layer, tree_lens)) return FKV_ERR_INVALID_ARG;
   int ahead[kMaxBatch];
   for (int s = 0; s < c->cfg.max_batch; ++s) ahead[s] = c->h_len[(size_t)layer * c->cfg.max_batch + s] - tree_lens[s];
-  if (const int S = small_tree(c, tree_lens, ahead, window, sinks))
-    return launch_tree_attend(c, layer, nullptr, nullptr, nullptr, tree_lens, lens, masks, nullptr, q, window, sinks, scale, out, lse_out, S,
+  const TreeShape shape = tree_shape(c, tree_lens, ahead, window, sinks, false);
+  if (shape.S)
+    return launch_tree_attend(c, layer, nullptr, nullptr, nullptr, tree_lens, lens, masks, nullptr, q, window, sinks, scale, out, lse_out, shape,
                               (cudaStream_t)stream);
   return launch_chunk_attend(c, layer, q, tree_lens, lens, window, sinks, scale, out, lse_out, masks, (cudaStream_t)stream);
 }
@@ -1389,14 +1419,12 @@ int fkv_append_tree_attn(fkv_cache *c, int layer, const void *k, const void *v, 
   if (lens.tok[c->cfg.max_batch] > 0 && (!out || !aligned(out, 16) || !aligned(lse_out, 4))) return FKV_ERR_INVALID_ARG;
   int ahead[kMaxBatch];
   for (int s = 0; s < c->cfg.max_batch; ++s) ahead[s] = keep_lens ? keep_lens[s] : c->h_len[(size_t)layer * c->cfg.max_batch + s];
-  if (const int S = small_tree(c, tree_lens, ahead, window, sinks)) {
-    if (int e = launch_tree_attend(c, layer, k, v, keep_lens, tree_lens, lens, masks, pos, q, window, sinks, scale, out, lse_out, S,
-                                   (cudaStream_t)stream))
-      return e;
-    return launch_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens, masks, true, (cudaStream_t)stream);
-  }
+  const TreeShape shape = tree_shape(c, tree_lens, ahead, window, sinks, true);
+  if (shape.S)
+    return launch_tree_attend(c, layer, k, v, keep_lens, tree_lens, lens, masks, pos, q, window, sinks, scale, out, lse_out, shape,
+                              (cudaStream_t)stream);
   if (int e = ensure_page_rows_map(c)) return e;   // (what can fail does so before anything is stored)
-  if (int e = launch_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens, masks, false, (cudaStream_t)stream)) return e;
+  if (int e = launch_append_chunk(c, layer, k, v, pos, keep_lens, tree_lens, lens, masks, (cudaStream_t)stream)) return e;
   return launch_chunk_attend(c, layer, q, tree_lens, lens, window, sinks, scale, out, lse_out, masks, (cudaStream_t)stream);
 }
 

@@ -70,18 +70,17 @@ struct ChunkKeep {
 // Bound: bytes (8 D a pair and KV head, read and written); back to back 4.7 us for 5 tokens, 5.3 for 256, 12.7 for 2048 on 8 heads
 // (a launch and four dependent reads: length, page, last position, free stack).
 // TREE: the chunk is a draft tree (kernel 10); a node's position is one behind its parent's, so it follows from the number
-// of its ancestors in `masks`.  behind: the launch before this one is the tree's attention, which has been waiting for the launches
-// before it and has read the lengths when this one starts; they run side by side, and this one ends last.
+// of its ancestors in `masks`.
 template <bool TREE>
 __global__ void __launch_bounds__(256) k_append_chunk(Ctx c, int layer, const uint8_t *k, const uint8_t *v, const int32_t *pos,
                                                       const __grid_constant__ ChunkLens lens,
-                                                      const __grid_constant__ ChunkKeep keep, const uint32_t *masks, int behind) {
+                                                      const __grid_constant__ ChunkKeep keep, const uint32_t *masks) {
   static_assert(kMaxBatch <= 256, "one thread per sequence");
   __shared__ int s_scan[33];
   __shared__ int s_keep[kMaxBatch], s_old[kMaxBatch], s_pop[kMaxBatch], s_push[kMaxBatch];
   __shared__ int s_last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (!TREE || !behind) griddep_wait();
+  griddep_wait();
   griddep_launch();
   const int s = tid;
   int n_old = 0, kp = 0, T = 0, pop = 0, push = 0, bad = 0;
@@ -165,7 +164,6 @@ __global__ void __launch_bounds__(256) k_append_chunk(Ctx c, int layer, const ui
   if (tid == 0) s_last = atomicAdd(&c.ctrl[CTRL_CHUNK_TICKET], 1) == (int)gridDim.x - 1;
   __syncthreads();
   if (!s_last) return;
-  if (TREE && behind) griddep_wait();   // (whatever comes after this launch comes after the attention too; it still reads page tables)
   __threadfence();
   if (tid == 0) c.ctrl[CTRL_CHUNK_TICKET] = 0;
   if (exhausted) return;

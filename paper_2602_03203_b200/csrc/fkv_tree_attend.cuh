@@ -8,11 +8,15 @@
 // each with a run of its pages.  Inside a CTA everything is as in k_chunk_attend with one tile of query rows (the same tensor
 // memory, the same softmax): key tiles go to two streams in turn.
 //   warp 0 / 2  tensor copies of Q and K / of V          warp 1 / 3  tcgen05.mma  S = Q K^T / O += P V          warps 4-11  softmax
+// HALF: a launch whose trees all have at most 64 query rows has them twice in the tile, and the second half of the threads takes the
+// second half of every key tile's columns: the same products, half the exponentials per thread, four results to join instead of two
+// (16 nodes over 8192 pairs: ... us with it, 18.3 without).
 // The streams' results meet in shared memory, the CTAs' through distributed shared memory: CTA r of a cluster owns rows r, r + S, ...,
 // receives them from all and writes them.
 //
-// A call that also stores the tree reads its keys and values from the caller's tensors, not from the pages: nothing here waits for the
-// store, which is a launch of its own (k_append_chunk) that starts as soon as every CTA here has read the lengths, and runs beside it.
+// A call that also stores the tree reads its keys and values from the caller's tensors, not from the pages, so no CTA waits for the store:
+// some more clusters of the same launch do it (as k_append_chunk does), and of all CTAs the last one to have read the lengths or stored its
+// pairs moves the lengths and the free stack.
 #pragma once
 #include "fkv_dev.cuh"
 #include "fkv_attend.cuh"
@@ -27,7 +31,9 @@ constexpr int kTaPos = 128;           // positions that are looked at together b
 struct TreeArgs {
   int layer, append, blocks;          // append: the tree is not stored yet
   int window, sinks;
+  int rows_y;                         // rows of the grid that attend; those behind store
   float scale_log2;
+  const uint8_t *k, *v;               // append: [tokens][Hkv][D] bf16
   const int32_t *pos;                 // append: the nodes' positions or null (one behind the parent's)
   __nv_bfloat16 *out;
   float *lse;
@@ -36,12 +42,159 @@ struct TreeArgs {
   ChunkKeep keep;
 };
 
+// What every sequence keeps, takes and returns in a store; worked out by one warp.
+struct TreeStore {
+  int keep[kMaxBatch], old[kMaxBatch], pop[kMaxBatch], push[kMaxBatch];
+  int pops, pushes, top, exhausted;
+};
+__device__ __forceinline__ void tree_store_plan(const Ctx &c, const TreeArgs &a, TreeStore &ts) {
+  const int lane = threadIdx.x & 31;
+  int pop[8], push[8], pops = 0, pushes = 0;   // a lane: eight sequences in a row
+  const int top = __ldcg(c.ctrl + CTRL_FREE_TOP);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int s = lane * 8 + i;
+    pop[i] = push[i] = 0;
+    if (s < c.batch) {
+      const int nq = __ldcg(c.len + a.layer * c.batch + s), t = a.lens.tok[s + 1] - a.lens.tok[s];
+      int kp = a.keep.use ? a.keep.keep[s] : nq;
+      if (kp > nq || kp + t > c.cap) kp = -1;
+      ts.keep[s] = kp;
+      ts.old[s] = nq;
+      if (kp >= 0) {
+        const int delta = (kp + t + kPage - 1) / kPage - (nq + kPage - 1) / kPage;
+        pop[i] = delta > 0 ? delta * c.Hkv : 0;
+        push[i] = delta < 0 ? -delta * c.Hkv : 0;
+      }
+    }
+    pops += pop[i];
+    pushes += push[i];
+  }
+  int ip = pops, iq = pushes;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, ip, o), y = __shfl_up_sync(0xffffffffu, iq, o);
+    if (lane >= o) { ip += x; iq += y; }
+  }
+  int at = ip - pops, bt = iq - pushes;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int s = lane * 8 + i;
+    if (s < c.batch) { ts.pop[s] = at; ts.push[s] = bt; }
+    at += pop[i];
+    bt += push[i];
+  }
+  const int all = __shfl_sync(0xffffffffu, ip, 31), back = __shfl_sync(0xffffffffu, iq, 31);
+  if (lane == 0) { ts.pops = all; ts.pushes = back; ts.top = top; ts.exhausted = all > top + back; }
+  __syncwarp();
+}
+// The i-th page that sequence q returns: of every head the same number, behind the pages that hold what stays.
+__device__ __forceinline__ int tree_store_returned(const Ctx &c, const TreeArgs &a, const TreeStore &ts, int q, int i) {
+  const int kept = (ts.keep[q] + a.lens.tok[q + 1] - a.lens.tok[q] + kPage - 1) / kPage, cnt = (ts.old[q] + kPage - 1) / kPage - kept, h = i / cnt;
+  return __ldcg(c.pt + (size_t)seg_of(c, a.layer, q, h) * c.max_pages + kept + i - h * cnt);
+}
+// By the last CTA (one warp of it): returned pages go where the taken ones came from and above, the stack's top and the lengths move,
+// decode queries of dropped tokens leave the record (see the end of k_append_chunk).
+__device__ __noinline__ void tree_store_finish(const Ctx &c, const TreeArgs &a, TreeStore &ts) {
+  const int lane = threadIdx.x & 31;
+  __threadfence();
+  tree_store_plan(c, a, ts);
+  if (lane == 0) {
+    c.ctrl[CTRL_CHUNK_TICKET] = 0;
+    if (ts.exhausted) set_status(c, kDevPoolExhausted);
+  }
+  for (int q = 0; q < c.batch; ++q) {
+    if (ts.keep[q] < 0) {
+      if (lane == 0) set_status(c, a.keep.use && a.keep.keep[q] > ts.old[q] ? kDevBadIndex : kDevCapacity);
+      continue;
+    }
+    if (ts.exhausted) continue;
+    const int cnt = ((ts.old[q] + kPage - 1) / kPage - (ts.keep[q] + a.lens.tok[q + 1] - a.lens.tok[q] + kPage - 1) / kPage) * c.Hkv;
+    for (int i = lane; i < cnt; i += 32) {
+      const int at = ts.top - ts.pops + ts.push[q] + i;
+      if (at >= 0) c.free_stack[at] = tree_store_returned(c, a, ts, q, i);
+    }
+  }
+  __syncwarp();
+  if (ts.exhausted) return;
+  if (lane == 0) c.ctrl[CTRL_FREE_TOP] = ts.top - ts.pops + ts.pushes;
+  for (int s = lane; s < c.batch; s += 32) {
+    const int kp = ts.keep[s], ls = a.layer * c.batch + s;
+    if (kp < 0) continue;
+    c.len[ls] = kp + a.lens.tok[s + 1] - a.lens.tok[s];
+    if (c.hist_w && kp < ts.old[s]) {
+      const int cnt0 = __ldcg(c.hist_cnt + ls);
+      int cnt = cnt0;
+      while (cnt > 0 && cnt > cnt0 - c.hist_w && __ldcg(c.hist_n + (size_t)ls * c.hist_w + (cnt - 1) % c.hist_w) > kp) --cnt;
+      c.hist_cnt[ls] = (cnt < cnt0 && cnt0 > c.hist_w) ? 0 : cnt;
+    }
+  }
+}
+// A CTA's turn in the store's order of arrival, by a whole warp: whether it is the last one.
+__device__ __forceinline__ bool tree_store_last(const Ctx &c) {
+  int last = 0;
+  if ((threadIdx.x & 31) == 0) {
+    __threadfence();
+    last = atomicAdd(&c.ctrl[CTRL_CHUNK_TICKET], 1) == (int)(gridDim.x * gridDim.y) - 1;
+  }
+  return __shfl_sync(0xffffffffu, last, 0) != 0;
+}
+// CTA x of the ones that store: a warp per pair and head.
+__device__ __noinline__ void tree_store_cta(const Ctx &c, const TreeArgs &a, TreeStore &ts, int x, int ctas) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x / 32;
+  if (warp == 0) tree_store_plan(c, a, ts);
+  __syncthreads();
+  const int tasks = ts.exhausted ? 0 : a.lens.tok[c.batch] * c.Hkv;
+  for (int t = x * nw + warp; t < tasks; t += ctas * nw) {
+    const int row = t / c.Hkv, h = t - row * c.Hkv;
+    int q = 0, hi = c.batch;   // the sequence of the row: the last one that starts at or before it
+    while (hi - q > 1) {
+      const int mid = (q + hi) >> 1;
+      if (a.lens.tok[mid] <= row) q = mid; else hi = mid;
+    }
+    const int kp = ts.keep[q];
+    if (kp < 0) continue;
+    const int j = row - a.lens.tok[q], slot = kp + j, pg = slot / kPage, np_old = (ts.old[q] + kPage - 1) / kPage;
+    const int grow = (kp + a.lens.tok[q + 1] - a.lens.tok[q] + kPage - 1) / kPage - np_old;
+    int *ptrow = c.pt + (size_t)seg_of(c, a.layer, q, h) * c.max_pages;
+    int pid;
+    if (pg < np_old) {
+      pid = __ldcg(ptrow + pg);
+    } else {
+      const int y = ts.pop[q] + h * grow + pg - np_old;   // the y-th page that the call takes
+      if (y < ts.top) {
+        pid = __ldcg(c.free_stack + ts.top - 1 - y);
+      } else {
+        int r = 0, end = c.batch;   // the sequence that returns page y - top: the last one whose pages begin at or before it
+        while (end - r > 1) {
+          const int mid = (r + end) >> 1;
+          if (ts.push[mid] <= y - ts.top) r = mid; else end = mid;
+        }
+        pid = tree_store_returned(c, a, ts, r, y - ts.top - ts.push[r]);
+      }
+      if (lane == 0 && (slot % kPage == 0 || j == 0)) ptrow[pg] = pid;
+    }
+    int32_t pdef = 0;
+    if (!a.pos) {   // one behind the parent's: the last pair's and the number of nodes that this one sees
+      pdef = (int)__reduce_add_sync(0xffffffffu, lane < kTreeWords ? __popc(__ldcg(a.masks + (size_t)row * kTreeWords + lane)) : 0) - 1;
+      if (kp > 0) pdef += slot_pos(c, ptrow, kp - 1) + 1;
+    }
+    const size_t at = ((size_t)row * c.Hkv + h) * c.D * 2;
+    move_row<0>(c, c.pool + (size_t)pid * c.page_bytes, slot % kPage, const_cast<uint8_t *>(a.k) + at, const_cast<uint8_t *>(a.v) + at, nullptr,
+                a.pos ? const_cast<int32_t *>(a.pos) + row : nullptr, lane, pdef);
+  }
+  __threadfence();
+  __syncthreads();
+  if (warp == 0 && tree_store_last(c)) tree_store_finish(c, a, ts);
+}
+
 template <int D>
 struct TaSmem {
   using CS = ChunkSmem<D>;
   static constexpr int kRow = D + 4;                             // a row of a partial result: O, m, l
   static constexpr size_t kOffK = CS::kTile, kOffV = kOffK + CS::kSlots * CS::kKv, kOffRecv = kOffV + CS::kSlots * CS::kKv;
   static_assert((size_t)2 * kChunkRows * kRow * 4 <= kOffRecv, "the streams' results meet where the operands were");
+  static_assert(sizeof(TreeStore) <= (size_t)kTaRecvRows * kRow * 4, "the last CTA's plan, ahead of any row that it receives");
   static constexpr size_t kOffBars = kOffRecv + (size_t)kTaRecvRows * kRow * 4;
   static constexpr size_t kOffWin = kOffBars + 256;              // the search: positions, first slots of the nodes' windows, results
   static constexpr size_t bytes() { return 1024 + kOffWin + (kTaPos + kChunkRows + 4) * 4; }
@@ -55,8 +208,49 @@ __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap *tm, in
       : "memory");
 }
 
-template <int D, bool WIN>
-__global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(Ctx c, const __grid_constant__ CUtensorMap tmk,
+__device__ __forceinline__ void tmem_ld8_issue(uint32_t taddr, uint32_t (&r)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ld8_wait(uint32_t (&r)[8]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7])
+               :
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%4], {%0, %1, %2, %3};" ::"r"(a), "r"(b), "r"(c), "r"(d), "r"(taddr) : "memory");
+}
+// chunk_weights for columns in groups of eight.
+template <int NG, class Ready>
+__device__ __forceinline__ void half_weights(const uint32_t (&v)[NG][8], float scale_log2, float ms, uint32_t tp, Ready ready, float &lt, float &mx) {
+  float m2[2] = {-INFINITY, -INFINITY};
+  float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+  const float2 sc = make_float2(scale_log2, scale_log2), off = make_float2(-ms, -ms);
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    uint32_t p[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 z = make_float2(__uint_as_float(v[g][2 * j]), __uint_as_float(v[g][2 * j + 1]));
+      float2 x = __ffma2_rn(z, sc, off);
+      x.x = ex2(x.x);
+      x.y = ex2(x.y);
+      m2[j & 1] = max3(m2[j & 1], z.x, z.y);
+      l2[j & 1] = __fadd2_rn(l2[j & 1], x);
+      p[j] = pack_bf16(x.x, x.y);
+    }
+    if (g == 0) ready();
+    tmem_st4(tp + g * 4, p[0], p[1], p[2], p[3]);
+  }
+  mx = fmaxf(m2[0], m2[1]);
+  lt = (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
+}
+
+template <int D, bool WIN, bool HALF>
+__global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(const __grid_constant__ Ctx c, const __grid_constant__ CUtensorMap tmk,
                                                                   const __grid_constant__ CUtensorMap tmv,
                                                                   const __grid_constant__ CUtensorMap tmq,
                                                                   const __grid_constant__ CUtensorMap tki,
@@ -66,6 +260,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(Ctx c, const _
   using SM = TaSmem<D>;
   constexpr int NS = CS::kSlots, NQ = D / 64, TP = CS::kPages, ROW = SM::kRow;
   constexpr uint32_t PAGE_HALF = kPage * 128;
+  constexpr int BR = HALF ? kChunkRows / 2 : kChunkRows, HC = CS::kCols / 2;   // query rows of a block; columns of half a key tile
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   uint8_t *Qt = smem, *Kt = smem + SM::kOffK, *Vt = smem + SM::kOffV;
@@ -74,8 +269,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(Ctx c, const _
   uint64_t *k_full = bars, *k_empty = k_full + NS, *v_full = k_empty + NS, *v_empty = v_full + NS, *q_full = v_empty + NS;
   uint64_t *s_full = q_full + 1, *s_empty = s_full + 2, *p_full = s_empty + 2, *p_empty = p_full + 2, *mma_done = p_empty + 2;
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(mma_done + 1);
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, G = c.G, TPT = kChunkRows / G;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, G = c.G, TPT = BR / G;
   const int S = gridDim.x, rank = blockIdx.x, head = blockIdx.y % c.Hkv, sb = blockIdx.y / c.Hkv, seq = sb / a.blocks;
+  if ((int)blockIdx.y >= a.rows_y) {
+    griddep_wait();
+    griddep_launch();
+    tree_store_cta(c, a, *reinterpret_cast<TreeStore *>(smem), (blockIdx.y - a.rows_y) * S + rank, (gridDim.y - a.rows_y) * S);
+    return;
+  }
   const int row0 = a.lens.tok[seq], T = a.lens.tok[seq + 1] - row0, j0 = (sb - seq * a.blocks) * TPT, j1 = min(T, j0 + TPT);   // nodes [j0, j1)
 
   if (warp == 3) tmem_alloc(smem_u32(tmem_slot), 512);
@@ -98,16 +299,21 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(Ctx c, const _
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   griddep_wait();
-  if (S > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // "I am running" (waited for ahead of the exchange)
+  griddep_launch();
   const bool there = j0 < j1;
   if (there && warp == 0 && lane == 0) {   // (the queries do not depend on the lengths)
-    mbar_arrive_expect_tx(smem_u32(q_full), (uint32_t)(NQ * TPT * G * 128));
-    for (int q = 0; q < NQ; ++q) tma_chunk_q(smem_u32(Qt + (size_t)q * 128 * 128), &tmq, q * 64, head * G, row0 + j0, smem_u32(q_full));
+    mbar_arrive_expect_tx(smem_u32(q_full), (uint32_t)(NQ * TPT * G * 128 * (HALF ? 2 : 1)));
+    for (int q = 0; q < NQ; ++q)
+      for (int h = 0; h < (HALF ? 2 : 1); ++h)
+        tma_chunk_q(smem_u32(Qt + (size_t)q * 128 * 128 + (size_t)h * BR * 128), &tmq, q * 64, head * G, row0 + j0, smem_u32(q_full));
   }
   const int ls = a.layer * c.batch + seq;
   const int n_old = __ldcg(c.len + ls);
-  __syncthreads();
-  griddep_launch();   // every thread has read the length: the store may begin
+  __syncthreads();   // every thread has read the length
+  if (a.append && warp == 1 && tree_store_last(c)) tree_store_finish(c, a, *reinterpret_cast<TreeStore *>(recv));
+  __syncwarp();
+  // "I am running, and my place for the rows that I receive is free": waited for ahead of the exchange.
+  if (S > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   const int kp = a.append ? (a.keep.use ? a.keep.keep[seq] : n_old) : n_old - T;   // pairs ahead of the tree
   const bool bad = kp < 0 || kp > n_old || kp + T > c.cap;   // (the store says so where there is one)
   if (bad && T > 0 && !a.append && rank == 0 && head == 0 && threadIdx.x == 0) set_status(c, kDevBadIndex);
@@ -183,20 +389,27 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(Ctx c, const _
   float m = -INFINITY, l = 0.f;
   if (warp >= 4) {
     // ---------------- softmax: thread = query row, warpgroup = stream (see k_chunk_attend) ----------------
-    const int t = (warp - 4) >> 2, quarter = warp & 3, R = quarter * 32 + lane, tok = R / G, node = j0 + tok;
+    const int t = (warp - 4) >> 2, quarter = warp & 3, R = quarter * 32 + lane, tok = R % BR / G, node = j0 + tok;
+    const int c0 = HALF ? R / BR * HC : 0;   // this thread's first column of every key tile (the same in a warp)
     const bool live = tok < TPT && node < j1;
     const bool any = __any_sync(0xffffffffu, live);
     const uint32_t ts = tmem_base + ((uint32_t)(quarter * 32) << 16) + t * CS::kStream, tp = ts + CS::kColP, to = ts + CS::kColO;
     const int wlo = WIN && live ? s_wlo[tok] : 0;
     uint32_t sp = 0, pe = 1;
     bool ok = true;
+    if (HALF) {   // the other half's weights are zero all along
+#pragma unroll
+      for (int g = 0; g < HC / 8; ++g) tmem_st4(tp + (HC - c0) / 2 + g * 4, 0u, 0u, 0u, 0u);
+      tmem_st_wait();
+    }
     for (int i = t; i < nt; i += 2) {
       const int f = first(i), cols = units(i) * kPage;
-      // Node of the tile's first column, and the columns that hold pairs up to the row's own.
-      const int at = i < na ? f * kPage - kp : f * kPage;
-      const int hi = live ? min(cols, min(node + 1 - at, i < na ? stored - f * kPage : INT_MAX)) : INT_MAX;
-      const bool in_tree = at + cols > 0;
-      const int lo = WIN && i < na ? wlo - f * kPage : 0, sk = WIN ? wa - f * kPage : 0;   // with a window: columns [0, sk) and from lo on
+      // Node of the thread's first column in the tile, and the columns that hold pairs up to the row's own.
+      const int at = (i < na ? f * kPage - kp : f * kPage) + c0;
+      const int hi = live ? min(cols - c0, min(node + 1 - at, i < na ? stored - f * kPage - c0 : INT_MAX)) : INT_MAX;
+      const bool in_tree = at - c0 + cols > 0;
+      const int lo = WIN && i < na ? wlo - f * kPage - c0 : 0, sk = WIN ? wa - f * kPage - c0 : 0;   // with a window: columns [0, sk) and from lo on
+      constexpr int NCOL = HALF ? HC : CS::kCols;
       if (!mbar_sleep_warp(smem_u32(&s_full[t]), sp)) { set_status(c, kDevWaitTimeout); break; }
       sp ^= 1;
       tc_fence_after();
@@ -209,15 +422,22 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(Ctx c, const _
         tc_fence_after();
       };
       if (any) {
-        uint32_t v[TP][16];
+        uint32_t v[HALF ? HC / 8 : TP][HALF ? 8 : 16];
+        if constexpr (HALF) {
 #pragma unroll
-        for (int q = 0; q < TP; ++q) tmem_ld16_issue(ts + q * 16, v[q]);
+          for (int g = 0; g < HC / 8; ++g) tmem_ld8_issue(ts + c0 + g * 8, v[g]);
 #pragma unroll
-        for (int q = 0; q < TP; ++q) tmem_ld16_wait(v[q]);
+          for (int g = 0; g < HC / 8; ++g) tmem_ld8_wait(v[g]);
+        } else {
+#pragma unroll
+          for (int q = 0; q < TP; ++q) tmem_ld16_issue(ts + q * 16, v[q]);
+#pragma unroll
+          for (int q = 0; q < TP; ++q) tmem_ld16_wait(v[q]);
+        }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&s_empty[t]));
-        if (!__all_sync(0xffffffffu, hi >= CS::kCols && (!WIN || lo <= 0 || sk >= CS::kCols) && !in_tree)) {   // hidden scores become -infinity
+        if (!__all_sync(0xffffffffu, hi >= NCOL && (!WIN || lo <= 0 || sk >= NCOL) && !in_tree)) {   // hidden scores become -infinity
           asm volatile("" ::: "memory");
           uint32_t see[3];
           const int k = at >> 5;
@@ -227,15 +447,21 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(Ctx c, const _
           for (int j = 0; j < 4; ++j) w[j] = !live || k + j < 0 ? ~0u : k + j < kTreeWords ? __ldcg(row + k + j) : 0u;
           auto below = [](int e) { return e <= 0 ? 0u : e >= 32 ? ~0u : (1u << e) - 1u; };   // bits under e
 #pragma unroll
-          for (int j = 0; j < 3; ++j) see[j] = __funnelshift_r(w[j], w[j + 1], at & 31) & below(hi - 32 * j) & (WIN ? below(sk - 32 * j) | ~below(lo - 32 * j) : ~0u);
+          for (int j = 0; j < 3; ++j)
+            see[j] = __funnelshift_r(w[j], w[j + 1], at & 31) & below(hi - 32 * j) & (WIN ? below(sk - 32 * j) | ~below(lo - 32 * j) : ~0u);
+          constexpr int W = HALF ? 8 : 16;
 #pragma unroll
-          for (int q = 0; q < TP; ++q)
+          for (int q = 0; q < NCOL / W; ++q)
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-              if (!((see[q / 2] >> (q % 2 * 16 + j)) & 1u)) v[q][j] = 0xff800000u;
+            for (int j = 0; j < W; ++j)
+              if (!((see[(q * W + j) / 32] >> ((q * W + j) % 32)) & 1u)) v[q][j] = 0xff800000u;
         }
         float mx, lt;
-        chunk_weights<TP>(v, a.scale_log2, m == -INFINITY ? 0.f : m * a.scale_log2, tp, wait_products, lt, mx);
+        auto weights = [&](float ms) {
+          if constexpr (HALF) half_weights<HC / 8>(v, a.scale_log2, ms, tp + c0 / 2, wait_products, lt, mx);
+          else chunk_weights<TP>(v, a.scale_log2, ms, tp, wait_products, lt, mx);
+        };
+        weights(m == -INFINITY ? 0.f : m * a.scale_log2);
         const bool grow = mx > m && (mx - m) * a.scale_log2 > kChunkGrow;
         if (__any_sync(0xffffffffu, grow)) {
           tmem_st_wait();
@@ -253,7 +479,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(Ctx c, const _
               tmem_st16(to + q, o);
             }
           }
-          chunk_weights<TP>(v, a.scale_log2, m == -INFINITY ? 0.f : m * a.scale_log2, tp, wait_products, lt, mx);
+          weights(m == -INFINITY ? 0.f : m * a.scale_log2);
         }
         l += lt;
         tmem_st_wait();
@@ -389,19 +615,28 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(Ctx c, const _
     if (a.lse && lane == 0) a.lse[orow] = L == 0.f ? -INFINITY : (M * a.scale_log2 + log2f(L)) * 0.6931471805599453f;
   };
   auto weight = [&](float mi, float M) { return mi == -INFINITY ? 0.f : ex2((mi - M) * a.scale_log2); };
-  // ---- a warp per row joins the streams and sends the row to its owner.  (A short loop: this code runs a few times per launch, and
-  // to fetch it costs more than its arithmetic; four rows at a time take 1.5 us longer.) ----
-  constexpr int NW = kChunkThreads / 32;
+  // ---- a warp per row joins its results (of two streams, and of two halves) and sends it to its owner.  (A short loop: this code runs a
+  // few times per launch, and to fetch it costs more than its arithmetic; four rows at a time take 1.5 us longer.) ----
+  constexpr int NW = kChunkThreads / 32, NP = HALF ? 4 : 2;
 #pragma unroll 1
   for (int r = warp; r < rows; r += NW) {
-    const float *p = mg + (size_t)r * ROW, *q = p + kChunkRows * ROW;
-    const float2 x = *reinterpret_cast<const float2 *>(p + D), y = *reinterpret_cast<const float2 *>(q + D);
-    const float M = fmaxf(x.x, y.x), fx = weight(x.x, M), fy = weight(y.x, M), L = fx * x.y + fy * y.y;   // (l is 0 where nothing was seen)
+    const float *p = mg + (size_t)r * ROW;
+    float2 x[NP];
+    float M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      x[i] = *reinterpret_cast<const float2 *>(p + i * BR * ROW + D);
+      M = fmaxf(M, x[i].x);
+    }
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (lane * 4 < D) {   // (what was never written is not read)
-      const float4 v = fx != 0.f ? *reinterpret_cast<const float4 *>(p + lane * 4) : acc;
-      const float4 w = fy != 0.f ? *reinterpret_cast<const float4 *>(q + lane * 4) : acc;
-      acc = make_float4(fx * v.x + fy * w.x, fx * v.y + fy * w.y, fx * v.z + fy * w.z, fx * v.w + fy * w.w);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const float f = weight(x[i].x, M);
+      L = fmaf(f, x[i].y, L);   // (l is 0 where nothing was seen)
+      if (lane * 4 < D && f != 0.f) {   // (what was never written is not read)
+        const float4 v = *reinterpret_cast<const float4 *>(p + i * BR * ROW + lane * 4);
+        acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
+      }
     }
     if (S == 1) {
       finish(r, acc, M, L);
