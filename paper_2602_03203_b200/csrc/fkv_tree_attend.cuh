@@ -223,15 +223,16 @@ __device__ __forceinline__ void tmem_ld8_wait(uint32_t (&r)[8]) {
 __device__ __forceinline__ void tmem_st4(uint32_t taddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%4], {%0, %1, %2, %3};" ::"r"(a), "r"(b), "r"(c), "r"(d), "r"(taddr) : "memory");
 }
-// chunk_weights for columns in groups of eight.
+// chunk_weights for columns in groups of eight.  P is stored when all of it has been worked out: its columns are free only when the products
+// with the tile before are done, and the exponentials run meanwhile.
 template <int NG, class Ready>
 __device__ __forceinline__ void half_weights(const uint32_t (&v)[NG][8], float scale_log2, float ms, uint32_t tp, Ready ready, float &lt, float &mx) {
   float m2[2] = {-INFINITY, -INFINITY};
   float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
   const float2 sc = make_float2(scale_log2, scale_log2), off = make_float2(-ms, -ms);
+  uint32_t p[NG][4];
 #pragma unroll
   for (int g = 0; g < NG; ++g) {
-    uint32_t p[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const float2 z = make_float2(__uint_as_float(v[g][2 * j]), __uint_as_float(v[g][2 * j + 1]));
@@ -240,11 +241,12 @@ __device__ __forceinline__ void half_weights(const uint32_t (&v)[NG][8], float s
       x.y = ex2(x.y);
       m2[j & 1] = max3(m2[j & 1], z.x, z.y);
       l2[j & 1] = __fadd2_rn(l2[j & 1], x);
-      p[j] = pack_bf16(x.x, x.y);
+      p[g][j] = pack_bf16(x.x, x.y);
     }
-    if (g == 0) ready();
-    tmem_st4(tp + g * 4, p[0], p[1], p[2], p[3]);
   }
+  ready();
+#pragma unroll
+  for (int g = 0; g < NG; ++g) tmem_st4(tp + g * 4, p[g][0], p[g][1], p[g][2], p[g][3]);
   mx = fmaxf(m2[0], m2[1]);
   lt = (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
 }
