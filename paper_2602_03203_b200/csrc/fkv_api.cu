@@ -729,7 +729,7 @@ int tree_attend_config(cudaLaunchConfig_t &cfg, cudaLaunchAttribute (&at)[2], in
   FKV_CUDA(opt_in.ensure(k_tree_attend<D, WIN, HALF>, smem));
   cfg = cudaLaunchConfig_t{};
   cfg.gridDim = dim3(S, y);
-  cfg.blockDim = dim3(kChunkThreads);
+  cfg.blockDim = dim3(kTaThreads<HALF>);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   at[0].id = cudaLaunchAttributeClusterDimension;
@@ -809,7 +809,7 @@ TreeShape tree_shape(fkv_cache *c, const int32_t *tree_lens, const int *ahead, i
   // The general kernels share the pages evenly over the SMs but start and join some 20 us later; a page takes an SM 0.15 us.
   if ((most + S - 1) / S > total / c->sm_count + 100) return r;
   r.S = S;
-  const long long warps = (long long)S * (kChunkThreads / 32);   // a pair and head each
+  const long long warps = (long long)S * ((half ? kTaThreads<true> : kTaThreads<false>) / 32);   // a pair and head each
   if (append) r.store = (int)std::max<long long>(1, std::min<long long>((tokens * Hkv + warps - 1) / warps, fit - segs));
   return r;
 }

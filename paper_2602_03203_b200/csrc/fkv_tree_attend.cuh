@@ -7,7 +7,7 @@
 // Shape: grid (S, sequences x KV heads x blocks of 128 query rows = (128 / g nodes) x (g heads)); the S CTAs of a block are one cluster,
 // each with a run of its pages.  Inside a CTA everything is as in k_chunk_attend with one tile of query rows (the same tensor
 // memory, the same softmax): key tiles go to two streams in turn.
-//   warp 0 / 2  tensor copies of Q and K / of V          warp 1 / 3  tcgen05.mma  S = Q K^T / O += P V          warps 4-11  softmax
+//   warps 0, 2 (and 12, 13)  tensor copies of Q, K and V  warp 1 / 3  tcgen05.mma  S = Q K^T / O += P V          warps 4-11  softmax
 // HALF: a launch whose trees all have at most 64 query rows has them twice in the tile, and the second half of the threads takes the
 // second half of every key tile's columns: the same products, half the exponentials per thread, four results to join instead of two
 // (16 nodes over 8192 pairs: ... us with it, 18.3 without).
@@ -26,6 +26,8 @@ namespace fkv {
 
 constexpr int kTaMaxCluster = 16;
 constexpr int kTaRecvRows = 140;      // most of ceil(128 / S) S over S <= 16
+template <bool HALF>
+constexpr int kTaThreads = kChunkThreads + (HALF ? 64 : 0);   // (a thread with half a tile's columns leaves registers for two more warps)
 constexpr int kTaPos = 128;           // positions that are looked at together behind the first window's begin
 
 struct TreeArgs {
@@ -252,7 +254,7 @@ __device__ __forceinline__ void half_weights(const uint32_t (&v)[NG][8], float s
 }
 
 template <int D, bool WIN, bool HALF>
-__global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(const __grid_constant__ Ctx c, const __grid_constant__ CUtensorMap tmk,
+__global__ void __launch_bounds__(kTaThreads<HALF>, 1) k_tree_attend(const __grid_constant__ Ctx c, const __grid_constant__ CUtensorMap tmk,
                                                                   const __grid_constant__ CUtensorMap tmv,
                                                                   const __grid_constant__ CUtensorMap tmq,
                                                                   const __grid_constant__ CUtensorMap tki,
@@ -262,6 +264,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(const __grid_c
   using SM = TaSmem<D>;
   constexpr int NS = CS::kSlots, NQ = D / 64, TP = CS::kPages, ROW = SM::kRow;
   constexpr uint32_t PAGE_HALF = kPage * 128;
+  constexpr int THREADS = kTaThreads<HALF>;
   constexpr int BR = HALF ? kChunkRows / 2 : kChunkRows, HC = CS::kCols / 2;   // query rows of a block; columns of half a key tile
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -389,7 +392,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(const __grid_c
   auto units = [&](int i) { return min(TP, (i < ns ? s1 : i < na ? pb : gb) - first(i)); };
 
   float m = -INFINITY, l = 0.f;
-  if (warp >= 4) {
+  if (warp >= 4 && warp < 12) {
     // ---------------- softmax: thread = query row, warpgroup = stream (see k_chunk_attend) ----------------
     const int t = (warp - 4) >> 2, quarter = warp & 3, R = quarter * 32 + lane, tok = R % BR / G, node = j0 + tok;
     const int c0 = HALF ? R / BR * HC : 0;   // this thread's first column of every key tile (the same in a warp)
@@ -494,23 +497,26 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(const __grid_c
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&p_full[t]));
     }
-  } else if (warp == 0 || warp == 2) {
+  } else if (warp == 0 || warp == 2 || warp >= 12) {
     // ---------------- copies of K / V, a lane per copy ----------------
-    const bool keys = warp == 0;
+    // A warp takes 100 - 150 cycles to issue a copy.  For a tile of five pages that is 1450 cycles of K (ten copies) on one warp, more than all
+    // the rest of 64 rows takes, so two warps share K and two V there.
+    const bool keys = warp == 0 || warp == 12, lead = warp < 12;
     uint64_t *full = keys ? k_full : v_full, *empty = keys ? k_empty : v_empty;
-    uint8_t *base = keys ? Kt : Vt;
     FeatRing rr{0, 0};
     uint32_t armed = 0, armed_par = 0;    // bit s: slot s has been armed / its last parity
-    const int pg = lane & 7, half = lane >> 3;
-    const bool on = keys ? half < NQ : half == 0;
-    uint8_t *mine = base + (keys ? (size_t)half * TP * PAGE_HALF + (size_t)pg * PAGE_HALF : (size_t)pg * NQ * PAGE_HALF);
-    auto page_id = [&](int i) { return i < nt && i < na && pg < units(i) ? __ldcg(ptrow + first(i) + pg) : 0; };
+    constexpr int CW = (THREADS - kChunkThreads) / 64 + 1;   // warps for K, and for V
+    const int all = keys ? NQ * TP : TP, share = (all + CW - 1) / CW, e = lane + (lead ? 0 : share);   // this lane's copy of a tile: (channels, page) of K
+    const bool on = lane < share && e < all;
+    const int pg = e % TP, half = e / TP;
+    uint8_t *mine = keys ? Kt + (size_t)half * TP * PAGE_HALF + (size_t)pg * PAGE_HALF : Vt + (size_t)pg * NQ * PAGE_HALF;
+    auto page_id = [&](int i) { return on && i < nt && i < na && pg < units(i) ? __ldcg(ptrow + first(i) + pg) : 0; };
     int id = page_id(0);
     for (int i = 0; i < nt; ++i) {
       const int idn = page_id(i + 1), n16 = units(i);
       if (!mbar_sleep_warp(smem_u32(&empty[rr.i]), rr.ph ^ 1)) { set_status(c, kDevWaitTimeout); break; }
       const uint32_t bar = smem_u32(&full[rr.i]), dst = smem_u32(mine + rr.i * CS::kKv);
-      if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(n16 * NQ) * PAGE_HALF);
+      if (lead && lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)(n16 * NQ) * PAGE_HALF);   // (of both warps)
       armed |= 1u << rr.i;
       armed_par = (armed_par & ~(1u << rr.i)) | ((uint32_t)rr.ph << rr.i);
       __syncwarp();
@@ -525,7 +531,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(const __grid_c
 #pragma unroll
     for (int s = 0; s < NS; ++s)   // no copy may be in flight at the exit
       if (((armed >> s) & 1u) && !mbar_sleep_warp(smem_u32(&full[s]), (armed_par >> s) & 1u)) set_status(c, kDevWaitTimeout);
-    if (keys && there && !mbar_sleep_warp(smem_u32(q_full), 0)) set_status(c, kDevWaitTimeout);
+    if (warp == 0 && there && !mbar_sleep_warp(smem_u32(q_full), 0)) set_status(c, kDevWaitTimeout);
   } else {
     // ---------------- multiplies: a warp stays together, lane 0 issues ----------------
     const bool scores = warp == 1;
@@ -585,7 +591,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(const __grid_c
   tc_fence_after();
   if (active) {
     // ---- the streams' results: [stream][row][O, m, l] ----
-    if (warp >= 4) {
+    if (warp >= 4 && warp < 12) {
       const int t = (warp - 4) >> 2, quarter = warp & 3, R = quarter * 32 + lane;
       const uint32_t to = tmem_base + ((uint32_t)(quarter * 32) << 16) + t * CS::kStream + CS::kColO;
       float *r = mg + (size_t)(t * kChunkRows + R) * ROW;
@@ -619,7 +625,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_tree_attend(const __grid_c
   auto weight = [&](float mi, float M) { return mi == -INFINITY ? 0.f : ex2((mi - M) * a.scale_log2); };
   // ---- a warp per row joins its results (of two streams, and of two halves) and sends it to its owner.  (A short loop: this code runs a
   // few times per launch, and to fetch it costs more than its arithmetic; four rows at a time take 1.5 us longer.) ----
-  constexpr int NW = kChunkThreads / 32, NP = HALF ? 4 : 2;
+  constexpr int NW = THREADS / 32, NP = HALF ? 4 : 2;
 #pragma unroll 1
   for (int r = warp; r < rows; r += NW) {
     const float *p = mg + (size_t)r * ROW;
