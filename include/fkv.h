@@ -372,7 +372,8 @@ int fkv_chunk_features(fkv_cache *c, int layer, const void *q, const float *lse,
  * ahead of the tree as a chunk's token does (with window > 0 those inside the window of its own position, and the sinks), and the pairs
  * of the tree that its mask names up to its own (other masks than fkv_tree_masks writes are welcome; a node that sees nothing gets
  * zeros, and -infinity as its log-sum-exp).  A window must not be shorter than the longest tree, so that it holds every ancestor.
- * k and v of a tree must be finite.  fkv_append_tree_attn: the two calls in one.  Errors and stream capture as for the chunk calls.
+ * k and v of a tree must be finite.  A tree's own positions do not grow from pair to pair: commit it or roll it back (keep_lens) before
+ * a call that goes by positions (windows, fkv_append without pos).  fkv_append_tree_attn: the two calls in one.  Errors and stream capture as for the chunk calls.
  *
  * fkv_verify_tree: which drafts stand, and the token after them, so that every token is distributed as the target says (speculative
  * sampling; siblings are tried in the order of their indices).  Per sequence, from a = node 0 with R = p = target[a]:
@@ -399,7 +400,7 @@ int fkv_chunk_features(fkv_cache *c, int layer, const void *q, const float *lse,
  * pairs ahead of the tree, the others are dropped and their pages returned, in one layer or (FKV_ALL_LAYERS) in all.  path and path_len:
  * dev, as fkv_verify_tree writes them: ascending indices inside the tree; path_len[s] = 0 drops the whole tree.  A path that is not, or
  * a tree longer than its segment, sets FKV_DEV_BAD_INDEX and leaves the sequence as it is.  What a pair holds moves with it, so
- * fkv_chunk_features may follow with the path's queries and log-sum-exps.  Decode queries on record that saw pairs of the tree leave the
+ * fkv_chunk_features may follow with the path's queries and log-sum-exps (gathered, chunk_lens = path_len).  Decode queries on record that saw pairs of the tree leave the
  * record.  The new lengths are known to the device alone: call fkv_sync_lengths before any call that goes by the host's (until then the
  * host's are those with the whole trees; fkv_append_tree and fkv_append_chunk with keep_lens may follow at once).
  */
@@ -432,7 +433,8 @@ int fkv_commit_tree(fkv_cache *c, int layer, const int32_t *tree_lens, const int
  * holds goes with it: pairs, features, positions, decode queries on record, its budget (an emptied place keeps its own).  Sequences never
  * share pages (each keeps features of its own in them): of a sequence that goes away while others become what it was, one takes the pages
  * over and the others get copies.  The pages of sequences that go away serve the copies; if these and the free ones are too few the
- * whole call does nothing (FKV_DEV_POOL_EXHAUSTED).  Only enqueues kernels; a replayed call does the same to what it finds.
+ * whole call does nothing (FKV_DEV_POOL_EXHAUSTED).  Only enqueues kernels; a replayed call does the same to what it finds (call
+ * fkv_sync_lengths after the last replay).
  *
  * fkv_export_chunk: dense copy of the last chunk_lens[s] pairs of every sequence of a layer, packed, the inverse of fkv_append_chunk:
  * k, v dev [tokens][Hkv][D] bf16 (16-byte aligned), feat dev [tokens][Hkv][F] fp32 (8-byte aligned), pos dev [tokens][Hkv] int32 (after an eviction the

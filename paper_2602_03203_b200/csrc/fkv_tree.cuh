@@ -10,7 +10,7 @@ namespace fkv {
 // ---------------------------------------------------------------- masks
 // mask(j) = {j} u mask(parent(j)), by doubling: after round r a node's mask holds its 2^r nearest ancestors and its pointer the next
 // one, so the rounds are log2 of the depth.  grid = sequences, a thread per node.  A parent that does not come before its node is an
-// error: the node becomes a root.  Bound: latency (a launch, one read, a few rounds in shared memory).
+// error: the node becomes a root.  Bound: latency (a launch, one read, a few rounds in shared memory): 1.7 us for 16 nodes, 3.2 for 256.
 __global__ void __launch_bounds__(kTreeNodes) k_tree_masks(Ctx c, const __grid_constant__ ChunkLens lens, const int32_t *parents, uint32_t *masks) {
   __shared__ uint32_t m[2][kTreeWords][kTreeNodes];
   __shared__ short up[2][kTreeNodes];
@@ -49,7 +49,8 @@ __global__ void __launch_bounds__(kTreeNodes) k_tree_masks(Ctx c, const __grid_c
 // places behind the pairs ahead of the tree; the length follows and the pages behind are returned.
 // A pair never moves up (path[i] >= i), and its place may be another's source: 128 / Hkv places of every head are read into
 // registers, then written, then the next ones (whose sources lie behind all places written so far).
-// Bound: latency (a launch, length and path, page ids, rows); bytes are those of the moved pairs, read and written.
+// Bound: latency (a launch, length and path, page ids, rows); bytes are those of the moved pairs, read and written.  Back to back with
+// the store of the tree 6.8 us, of which the store takes 5.0.
 __global__ void __launch_bounds__(1024) k_commit_tree(Ctx c, int l0, const __grid_constant__ ChunkLens lens, const int32_t *path,
                                                       const int32_t *path_len, int stride) {
   __shared__ int s_path[kTreeNodes];
@@ -131,8 +132,8 @@ __global__ void __launch_bounds__(1024) k_commit_tree(Ctx c, int l0, const __gri
 // The last lens[s] pairs of every sequence, packed: the inverse of k_append_chunk.  A warp per page and head, with two page buffers in
 // shared memory: a page is copied in (one bulk copy) while the rows of the one before it go out.  blk: the first of a sequence's pages in
 // the list of all (a page more than its pairs fill: they may begin inside one).
-// Bound: bytes (read and written).  32768 pairs of 8 heads (160 MB read, as many written): a warp per pair 95 us, a warp per page with
-// eight rows in registers 70.
+// Bound: bytes (read and written).  32768 pairs of 8 heads (160 MB read, as many written) 59.5 us = 5.4 TB/s, 0.94 of a library copy of the same
+// size (55.8); a warp per pair took 95, a warp per page with eight rows in registers 70.
 struct ExportBlocks {
   int blk[kMaxBatch + 1];
 };

@@ -1,8 +1,10 @@
 // Kernel 10b: attention of draft trees where a launch's fixed cost counts - short caches, few sequences:
 //     out_j = sum_i softmax_i(scale <q_j, k_i>) v_i  over the pairs ahead of the tree (window, sinks), j's ancestors and j itself.
 // Bound: bytes, 4 D per pair and KV head; for short caches and small trees the latency of one launch and its chain of reads.
-// k_chunk_attend computes the same for items of any number that it finds and cuts by itself, and joins them by a second kernel:
-// 20 us of a step that has 5 us of bytes (16 nodes over 8192 pairs).  Here the host says which CTA does what.
+// k_chunk_attend computes the same for items of any number that it finds and cuts by itself, behind a store and ahead of a join that are
+// launches of their own: 38 us for 16 nodes over 8192 pairs (8 KV heads, g = 4, D = 128), whose bytes take 5.  Here the host says which CTA
+// does what, and the call is one launch: 17.0 us.  (256 nodes with a window of 4096: 32.9 us for 75; 33 nodes over 512 pairs, D = 64: 11.9
+// for 28.6; all back to back at 1.96 GHz.)
 //
 // Shape: grid (S, sequences x KV heads x blocks of 128 query rows = (128 / g nodes) x (g heads)); the S CTAs of a block are one cluster,
 // each with a run of its pages.  Inside a CTA everything is as in k_chunk_attend with one tile of query rows (the same tensor
@@ -10,13 +12,20 @@
 //   warps 0, 2 (and 12, 13)  tensor copies of Q, K and V  warp 1 / 3  tcgen05.mma  S = Q K^T / O += P V          warps 4-11  softmax
 // HALF: a launch whose trees all have at most 64 query rows has them twice in the tile, and the second half of the threads takes the
 // second half of every key tile's columns: the same products, half the exponentials per thread, four results to join instead of two
-// (16 nodes over 8192 pairs: ... us with it, 18.3 without).
+// (16 nodes over 8192 pairs: 16.9 us with it, 18.2 without).
 // The streams' results meet in shared memory, the CTAs' through distributed shared memory: CTA r of a cluster owns rows r, r + S, ...,
 // receives them from all and writes them.
 //
 // A call that also stores the tree reads its keys and values from the caller's tensors, not from the pages, so no CTA waits for the store:
 // some more clusters of the same launch do it (as k_append_chunk does), and of all CTAs the last one to have read the lengths or stored its
 // pairs moves the lengths and the free stack.
+//
+// Where the 17 us go (clocks of one CTA of 10 to a block, cold caches): 0.5 the length, 4 the first scores (page numbers, then pages: two reads of
+// memory one after another, descriptors), 1 the first softmax, 0.7 for each of 10 more key tiles (on 80 SMs, 57 GB/s each: a ring of 120 KB at
+// the latency of a loaded memory), 0.8 results to shared memory, 1.5 their exchange, 1 the cluster's barrier, 0.9 the join.  Looked at and left out:
+// pages asked for into L2 ahead of their copies (the first tile then waits behind them: 18.6 us), one copy for a whole page, K and V in one
+// ring (a slot is held from its copy to the product with P: 18.4), V by 16-byte copies of a warp (26.5), products by mma.sync with the pairs on
+// the M axis (8 cycles for 16 x 8 x 16: 25 us at 64 rows).
 #pragma once
 #include "fkv_dev.cuh"
 #include "fkv_attend.cuh"
