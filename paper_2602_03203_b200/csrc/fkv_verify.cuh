@@ -107,14 +107,17 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
   __syncthreads();
   if (tid < nodes) {
     int first = -1, next = -1;
-    const int par = s_par[tid];
+    bool again = false;   // the token of a sibling before: nothing is left of it when this node is tried
+    const int par = s_par[tid], x = s_tok[tid];
     for (int i = nodes - 1; i > 0; --i) {
       const int p = s_par[i];
       if (p == tid) first = i;
       if (p == par && i > tid) next = i;
+      if (!Q) again = again || (p == par && i < tid && s_tok[i] == x);
     }
     s_first[tid] = (short)first;
     s_next[tid] = (short)next;
+    if (again) s_p[tid] = 0.0;
   }
   __syncthreads();
 
@@ -126,11 +129,6 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
   int cur = 0, len = 0;
   // What R is without its divisor: p - alpha q, or p without the tokens of cur's children.
   auto weight = [&](double p, double q, double alpha) { return Q ? fmax(fma(-alpha, q, p), 0.0) : fmax(p, 0.0); };
-  auto tried = [&](int x) {   // (Q = false) one of the rejected tokens?
-    for (int i = s_first[cur]; i >= 0; i = s_next[i])
-      if (s_tok[i] == x) return true;
-    return false;
-  };
   // A lane's eight weights of a piece: tokens lane, lane + 32, ... of it.
   auto load = [&](int pc, T (&pv)[8], T (&qv)[8]) {
     const T *pr = row_p(cur), *qr = Q ? row_q(cur) : nullptr;
@@ -145,14 +143,17 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
   auto weights = [&](int pc, const T (&pv)[8], const T (&qv)[8], double alpha, double (&w)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] = weight((double)to_f32(pv[i]), Q ? (double)to_f32(qv[i]) : 0.0, alpha);
-    if (!Q) {
-      bool hit = false;
-      for (int i = s_first[cur]; i >= 0; i = s_next[i]) hit = hit || s_tok[i] / kVerPiece == pc;
-      if (hit)
+    if (!Q)   // without the rejected tokens: those of cur's children, looked for by the whole warp
+      for (int j0 = 0; j0 < nodes; j0 += 32) {
+        const int j = j0 + lane, x = j < nodes && s_par[j] == cur ? s_tok[j] : -1;
+        unsigned in = __ballot_sync(0xffffffffu, x >= 0 && x / kVerPiece == pc);
+        for (; in; in &= in - 1) {
+          const int at = __shfl_sync(0xffffffffu, x, __ffs(in) - 1) % kVerPiece;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (tried(pc * kVerPiece + lane + 32 * i)) w[i] = 0.0;
-    }
+          for (int i = 0; i < 8; ++i)
+            if (at == lane + 32 * i) w[i] = 0.0;
+        }
+      }
   };
   // The sum over the vocabulary, the same in every CTA; the pieces' sums stay in s_sum, the parts' in s_all[turn ^ 1].
   auto pass = [&](double alpha) {
@@ -194,10 +195,7 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
       ch = s_next[ch];
       continue;
     }
-    double x = s_p[ch];
-    const double u = (double)s_u[ch];
-    if (!Q)   // (the token of a sibling that was rejected: nothing is left of it)
-      for (int i = s_first[cur]; i != ch; i = s_next[i]) x = s_tok[i] == s_tok[ch] ? 0.0 : x;
+    const double x = s_p[ch], u = (double)s_u[ch];
     const bool ok = Q ? u * s_q[ch] * S < weight(x, s_q[ch], alpha) : u * S < x;
     if (ok) {
       if (rank == 0 && tid == 0) {

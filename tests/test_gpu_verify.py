@@ -98,6 +98,22 @@ def test_batches_of_every_cluster_size():
                 assert alone[1] == [n] and alone[0][0][:n] == got[0][s][:n] and alone[2][0][:n] == got[2][s][:n]
 
 
+@pytest.mark.parametrize("sampled", [True, False])
+@pytest.mark.parametrize("vocab", [300, 40000])
+def test_as_many_siblings_as_a_tree_holds(sampled, vocab):
+    """255 children of one node, most of them rejected; many tokens come twice or more in the small vocabulary."""
+    for seed in range(4):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        x = problem([256, 256], vocab, 255, sampled, torch.float32, seed, noise=6.0)
+        x["trees"] = [[-1] + [0] * 255, [-1] + [0] * 200 + [200] * 55]
+        x["parents"] = torch.tensor([p for t in x["trees"] for p in t], dtype=torch.int32, device="cuda")
+        x["tokens"] = torch.randint(0, vocab, (512,), generator=g, device="cuda", dtype=torch.int32)
+        if seed == 0:
+            x["u"] = torch.full_like(x["u"], 0.9999)
+        got, status = run(x)
+        assert got == want(x) and status == 0
+
+
 def small(parents, tokens, p, q=None, u=None, us=0.5, **kw):
     """One sequence from lists."""
     t = len(parents)
