@@ -159,9 +159,8 @@ struct fkv_cache {
   std::vector<uint8_t> loaded;  // [L][Hkv] scorer present
   std::vector<uint8_t> staging;
   uint64_t launches = 0;
-  int sm_count = 148;
+  int sm_count = 148, device = 0;
   int max_cluster[2] = {0, 0};   // largest attention cluster the device places (found at the first stand-alone launch): plain, windowed
-  int tree_clusters[2][2][kTaMaxCluster + 1] = {};   // clusters of 1 .. 16 tree CTAs (windowed, half) that fit the device (0: not asked yet, -1: none)
   float feature_scale = 0.f;  // softmax scale of the recorded queries (the last decode call's)
   bool timing = false, timed = false;
   CUtensorMap page_parts;     // ... as [page][64-channel part][row][64 channels]
@@ -796,13 +795,15 @@ TreeShape tree_shape(fkv_cache *c, const int32_t *tree_lens, const int *ahead, i
   }
   if (segs == 0 || segs > c->sm_count) return r;
   // The largest cluster of which the device holds all at once, one that stores among them, with a few pages at least for every CTA.
+  // (asked of the runtime once per device and form: 0 is not asked yet, -1 none)
+  static std::atomic<int> clusters[64][2][2][2][kTaMaxCluster + 1] = {};
   const bool win = window > 0, half = r.half;
   int S = (int)std::min<long long>(std::min<long long>(kTaMaxCluster, c->sm_count / segs), std::max(1, most / kAttendMinPages));
   int fit = 0;
   for (; S > 0; --S) {
-    int &known = c->tree_clusters[win][half][S];
-    if (known == 0) known = FKV_TREE_FORM(tree_clusters, S);
-    fit = known;
+    std::atomic<int> &known = clusters[c->device & 63][c->cfg.head_dim == 128][win][half][S];
+    fit = known.load();
+    if (fit == 0) known.store(fit = FKV_TREE_FORM(tree_clusters, S));
     if (fit >= segs + (append ? 1 : 0)) break;
   }
   if (S == 0) return r;
@@ -1001,6 +1002,7 @@ int fkv_init_cache(const fkv_config *cfg, void *dev_workspace, size_t bytes, voi
   c->loaded.assign((size_t)cfg->num_layers * cfg->num_kv_heads, 0);
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
+  c->device = dev;
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&c->sm_count, cudaDevAttrMultiProcessorCount, dev);
   cudaStream_t st = (cudaStream_t)stream;
   // Zero everything: freshly taken pages then hold finite values in the slots not yet written.
