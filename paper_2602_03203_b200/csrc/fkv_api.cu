@@ -793,7 +793,7 @@ TreeShape tree_shape(fkv_cache *c, const int32_t *tree_lens, const int *ahead, i
     total += (long long)blocks * Hkv * pages;
     tokens += tree_lens[s];
   }
-  if (segs == 0 || segs > c->sm_count) return r;
+  if (segs == 0 || segs > std::min(c->sm_count, kTaMaxBlocks)) return r;
   // The largest cluster of which the device holds all at once, one that stores among them, with a few pages at least for every CTA.
   // (asked of the runtime once per device and form: 0 is not asked yet, -1 none)
   static std::atomic<int> clusters[64][2][2][2][kTaMaxCluster + 1] = {};
@@ -826,9 +826,13 @@ int launch_tree_attend(fkv_cache *c, int layer, const void *k, const void *v, co
   a.k = (const uint8_t *)k; a.v = (const uint8_t *)v; a.pos = pos;
   a.scale_log2 = (scale == 0.f ? 1.f / sqrtf((float)D) : scale) * 1.4426950408889634f;
   a.out = (__nv_bfloat16 *)out; a.lse = lse; a.masks = masks; a.lens = lens;
-  a.blocks = 1;
-  for (int s = 0; s < batch; ++s) a.blocks = std::max(a.blocks, (tree_lens[s] + shape.block - 1) / shape.block);
-  a.rows_y = batch * Hkv * a.blocks;
+  int blocks = 0;
+  for (int s = 0; s < batch; ++s)
+    for (int b = 0; b * shape.block < tree_lens[s]; ++b, ++blocks) {
+      a.seq[blocks] = (uint8_t)s;
+      a.block[blocks] = (uint8_t)b;
+    }
+  a.rows_y = blocks * Hkv;
   a.keep = ChunkKeep{};
   if (keep_lens) {
     a.keep.use = 1;
@@ -854,12 +858,13 @@ int launch_tree_attend(fkv_cache *c, int layer, const void *k, const void *v, co
   return FKV_OK;
 }
 
-// A cluster of CTAs per sequence: eight, or as many as the SMs hold at a time for all sequences: a pass is a chain of reads, so a
+// A cluster of CTAs per sequence: eight, or as many as the SMs hold at a time for all that have a tree: a pass is a chain of reads, so a
 // large batch too goes by how many pieces are in flight (64 rows of 130001 in 16 bits: 18.1 us with clusters of two).
 template <class T, bool Q>
 int launch_verify_t(fkv_cache *c, const VerifyArgs &a, cudaStream_t st) {
-  int cs = 1;
-  while (cs < kVerParts && cs * 2 * c->cfg.max_batch <= kVerCtasPerSm * c->sm_count) cs *= 2;
+  int cs = 1, trees = 0;
+  for (int s = 0; s < c->cfg.max_batch; ++s) trees += a.lens.tok[s + 1] > a.lens.tok[s];
+  while (cs < kVerParts && cs * 2 * trees <= kVerCtasPerSm * c->sm_count) cs *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(c->cfg.max_batch * cs);
   cfg.blockDim = dim3(kVerThreads);

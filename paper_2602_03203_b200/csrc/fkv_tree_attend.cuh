@@ -6,8 +6,8 @@
 // does what, and the call is one launch: 17.0 us.  (256 nodes with a window of 4096: 32.9 us for 75; 33 nodes over 512 pairs, D = 64: 11.9
 // for 28.6; all back to back at 1.96 GHz.)
 //
-// Shape: grid (S, sequences x KV heads x blocks of 128 query rows = (128 / g nodes) x (g heads)); the S CTAs of a block are one cluster,
-// each with a run of its pages.  Inside a CTA everything is as in k_chunk_attend with one tile of query rows (the same tensor
+// Shape: grid (S, blocks of 128 query rows = (128 / g nodes) x (g heads) of the sequences that have a tree, x KV heads); the S CTAs of a
+// block are one cluster, each with a run of its pages.  Inside a CTA everything is as in k_chunk_attend with one tile of query rows (the same tensor
 // memory, the same softmax): key tiles go to two streams in turn.
 //   warps 0, 2 (and 12, 13)  tensor copies of Q, K and V  warp 1 / 3  tcgen05.mma  S = Q K^T / O += P V          warps 4-11  softmax
 // HALF: a launch whose trees all have at most 64 query rows has them twice in the tile, and the second half of the threads takes the
@@ -34,13 +34,14 @@
 namespace fkv {
 
 constexpr int kTaMaxCluster = 16;
+constexpr int kTaMaxBlocks = 160;     // blocks of a launch, of one KV head (all clusters fit the device at once)
 constexpr int kTaRecvRows = 140;      // most of ceil(128 / S) S over S <= 16
 template <bool HALF>
 constexpr int kTaThreads = kChunkThreads + (HALF ? 64 : 0);   // (a thread with half a tile's columns leaves registers for two more warps)
 constexpr int kTaPos = 128;           // positions that are looked at together behind the first window's begin
 
 struct TreeArgs {
-  int layer, append, blocks;          // append: the tree is not stored yet
+  int layer, append;                  // append: the tree is not stored yet
   int window, sinks;
   int rows_y;                         // rows of the grid that attend; those behind store
   float scale_log2;
@@ -51,7 +52,9 @@ struct TreeArgs {
   const uint32_t *masks;
   ChunkLens lens;
   ChunkKeep keep;
+  uint8_t seq[kTaMaxBlocks], block[kTaMaxBlocks];   // of every block: its sequence, and which of its blocks
 };
+static_assert(kMaxBatch <= 256, "a sequence in eight bits");
 
 // What every sequence keeps, takes and returns in a store; worked out by one warp.
 struct TreeStore {
@@ -114,16 +117,20 @@ __device__ __noinline__ void tree_store_finish(const Ctx &c, const TreeArgs &a, 
     c.ctrl[CTRL_CHUNK_TICKET] = 0;
     if (ts.exhausted) set_status(c, kDevPoolExhausted);
   }
-  for (int q = 0; q < c.batch; ++q) {
-    if (ts.keep[q] < 0) {
-      if (lane == 0) set_status(c, a.keep.use && a.keep.keep[q] > ts.old[q] ? kDevBadIndex : kDevCapacity);
-      continue;
+  for (int q0 = 0; q0 < c.batch; q0 += 32) {   // a lane per sequence says what there is to do, all lanes do it
+    int cnt = 0;
+    if (q0 + lane < c.batch) {
+      const int s = q0 + lane, kp = ts.keep[s], old = ts.old[s];
+      if (kp < 0) set_status(c, a.keep.use && a.keep.keep[s] > old ? kDevBadIndex : kDevCapacity);
+      else cnt = ((old + kPage - 1) / kPage - (kp + a.lens.tok[s + 1] - a.lens.tok[s] + kPage - 1) / kPage) * c.Hkv;
     }
     if (ts.exhausted) continue;
-    const int cnt = ((ts.old[q] + kPage - 1) / kPage - (ts.keep[q] + a.lens.tok[q + 1] - a.lens.tok[q] + kPage - 1) / kPage) * c.Hkv;
-    for (int i = lane; i < cnt; i += 32) {
-      const int at = ts.top - ts.pops + ts.push[q] + i;
-      if (at >= 0) c.free_stack[at] = tree_store_returned(c, a, ts, q, i);
+    for (unsigned left = __ballot_sync(0xffffffffu, cnt > 0); left; left &= left - 1) {
+      const int l = __ffs(left) - 1, q = q0 + l, all = __shfl_sync(0xffffffffu, cnt, l);
+      for (int i = lane; i < all; i += 32) {
+        const int at = ts.top - ts.pops + ts.push[q] + i;
+        if (at >= 0) c.free_stack[at] = tree_store_returned(c, a, ts, q, i);
+      }
     }
   }
   __syncwarp();
@@ -284,14 +291,14 @@ __global__ void __launch_bounds__(kTaThreads<HALF>, 1) k_tree_attend(const __gri
   uint64_t *s_full = q_full + 1, *s_empty = s_full + 2, *p_full = s_empty + 2, *p_empty = p_full + 2, *mma_done = p_empty + 2;
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(mma_done + 1);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, G = c.G, TPT = BR / G;
-  const int S = gridDim.x, rank = blockIdx.x, head = blockIdx.y % c.Hkv, sb = blockIdx.y / c.Hkv, seq = sb / a.blocks;
+  const int S = gridDim.x, rank = blockIdx.x, head = blockIdx.y % c.Hkv, sb = blockIdx.y / c.Hkv;
   if ((int)blockIdx.y >= a.rows_y) {
     griddep_wait();
     griddep_launch();
     tree_store_cta(c, a, *reinterpret_cast<TreeStore *>(smem), (blockIdx.y - a.rows_y) * S + rank, (gridDim.y - a.rows_y) * S);
     return;
   }
-  const int row0 = a.lens.tok[seq], T = a.lens.tok[seq + 1] - row0, j0 = (sb - seq * a.blocks) * TPT, j1 = min(T, j0 + TPT);   // nodes [j0, j1)
+  const int seq = a.seq[sb], row0 = a.lens.tok[seq], T = a.lens.tok[seq + 1] - row0, j0 = a.block[sb] * TPT, j1 = min(T, j0 + TPT);   // nodes [j0, j1)
 
   if (warp == 3) tmem_alloc(smem_u32(tmem_slot), 512);
   if (threadIdx.x == 0) {
@@ -314,8 +321,7 @@ __global__ void __launch_bounds__(kTaThreads<HALF>, 1) k_tree_attend(const __gri
   const uint32_t tmem_base = *tmem_slot;
   griddep_wait();
   griddep_launch();
-  const bool there = j0 < j1;
-  if (there && warp == 0 && lane == 0) {   // (the queries do not depend on the lengths)
+  if (warp == 0 && lane == 0) {   // (the queries do not depend on the lengths)
     mbar_arrive_expect_tx(smem_u32(q_full), (uint32_t)(NQ * TPT * G * 128 * (HALF ? 2 : 1)));
     for (int q = 0; q < NQ; ++q)
       for (int h = 0; h < (HALF ? 2 : 1); ++h)
@@ -330,8 +336,8 @@ __global__ void __launch_bounds__(kTaThreads<HALF>, 1) k_tree_attend(const __gri
   if (S > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   const int kp = a.append ? (a.keep.use ? a.keep.keep[seq] : n_old) : n_old - T;   // pairs ahead of the tree
   const bool bad = kp < 0 || kp > n_old || kp + T > c.cap;   // (the store says so where there is one)
-  if (bad && T > 0 && !a.append && rank == 0 && head == 0 && threadIdx.x == 0) set_status(c, kDevBadIndex);
-  const bool active = there && !bad;
+  if (bad && !a.append && rank == 0 && head == 0 && threadIdx.x == 0) set_status(c, kDevBadIndex);
+  const bool active = !bad;
   const int stored = a.append ? kp : kp + T;       // pairs that the pages hold
   const int *ptrow = c.pt + (size_t)(ls * c.Hkv + head) * c.max_pages;
   int *s_pos = reinterpret_cast<int *>(smem + SM::kOffWin), *s_wlo = s_pos + kTaPos, *s_win = s_wlo + kChunkRows;
@@ -540,7 +546,7 @@ __global__ void __launch_bounds__(kTaThreads<HALF>, 1) k_tree_attend(const __gri
 #pragma unroll
     for (int s = 0; s < NS; ++s)   // no copy may be in flight at the exit
       if (((armed >> s) & 1u) && !mbar_sleep_warp(smem_u32(&full[s]), (armed_par >> s) & 1u)) set_status(c, kDevWaitTimeout);
-    if (warp == 0 && there && !mbar_sleep_warp(smem_u32(q_full), 0)) set_status(c, kDevWaitTimeout);
+    if (warp == 0 && !mbar_sleep_warp(smem_u32(q_full), 0)) set_status(c, kDevWaitTimeout);
   } else {
     // ---------------- multiplies: a warp stays together, lane 0 issues ----------------
     const bool scores = warp == 1;

@@ -169,6 +169,19 @@ def test_as_many_sequences_as_the_card_has_room_for_and_more(D, g, Hkv, batch, w
     run_tree(c, make_trees(lens), window)
 
 
+@pytest.mark.parametrize("window", [0, 256])
+@pytest.mark.parametrize("D,g,Hkv,batch", [(128, 4, 8, 64), (64, 8, 2, 256), (128, 1, 1, 256)])
+def test_few_trees_in_many_places(D, g, Hkv, batch, window):
+    """One launch whose blocks are those of the sequences that have a tree: two blocks and more of one, the last place, gaps."""
+    lens = [0] * batch
+    for s, n in ((0, 3), (batch // 3, 40), (batch - 1, 17)):
+        lens[s] = n
+    c = Case(Hkv, g, D, [700 if s % 5 == 0 or n else 1 for s, n in enumerate(lens)])
+    before = c.cache.launch_count()
+    run_tree(c, make_trees(lens), window=window, sinks=4 if window else 0)
+    assert c.cache.launch_count() - before == 2   # masks, and everything else
+
+
 @pytest.mark.parametrize("window,sinks", [(0, 0), (256, 4)])
 @pytest.mark.parametrize("D,g", [(128, 4), (64, 7)])
 def test_large_trees_of_large_batches(D, g, window, sinks):
