@@ -182,6 +182,21 @@ def test_few_trees_in_many_places(D, g, Hkv, batch, window):
     assert c.cache.launch_count() - before == 2   # masks, and everything else
 
 
+@pytest.mark.parametrize("calls", ["append_tree", "append_tree_attn"])
+def test_a_call_without_trees_rolls_back(calls):
+    c = Case(2, 4, 64, [40, 0, 17])
+    lens, keep = [0, 0, 0], [9, 0, 16]
+    k, v, q = c.chunk(lens)
+    masks = torch.empty((0, binding.TREE_WORDS), dtype=torch.int32, device="cuda")
+    getattr(c.cache, calls)(0, k, v, *([q] if calls.endswith("attn") else []), lens, masks, keep_lens=keep)
+    assert c.cache.lengths(0) == keep and c.status() == 0
+    extend(c, k, v, [[], [], []], keep)
+    run_tree(c, make_trees([5, 3, 0]))   # (and goes on from there)
+    c.cache.commit_tree([0, 0, 0], torch.empty((3, 1), dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda"))
+    c.cache.sync_lengths()
+    assert c.cache.lengths(0) == [14, 3, 16] and c.status() == 0
+
+
 @pytest.mark.parametrize("window,sinks", [(0, 0), (256, 4)])
 @pytest.mark.parametrize("D,g", [(128, 4), (64, 7)])
 def test_large_trees_of_large_batches(D, g, window, sinks):
