@@ -1513,13 +1513,17 @@ int fkv_fork(fkv_cache *c, const int32_t *from, void *stream) {
   ForkOps ops;
   if (!make_fork(c, from, m, ops)) return FKV_OK;
   cudaStream_t st = (cudaStream_t)stream;
-  FKV_CUDA(launch_waiting(k_fork_plan, dim3(1), std::min(1024, (L * batch + 31) / 32 * 32), 0, st, c->ctx, m));
-  ++c->launches;
-  const int warps = (int)std::min<size_t>(kForkMaxWarps, (kMaxSmem - 1024) / (2 * (size_t)c->ctx.page_bytes));
+  const bool own = L * batch <= kForkOwn;
+  if (!own) {
+    FKV_CUDA(launch_waiting(k_fork_plan, dim3(1), 1024, 0, st, c->ctx, m));
+    ++c->launches;
+  }
+  constexpr size_t room = kMaxSmem - 1024 - 3 * kForkOwn * 4;
+  const int warps = (int)std::min<size_t>(kForkMaxWarps, room / (2 * (size_t)c->ctx.page_bytes));
   const size_t smem = (size_t)warps * 2 * c->ctx.page_bytes;
-  static SmemOptIn opt_in;
-  FKV_CUDA(opt_in.ensure(k_fork_copy, kMaxSmem - 1024));
-  FKV_CUDA(launch_waiting(k_fork_copy, dim3(c->sm_count), warps * 32, smem, st, c->ctx, m));
+  static SmemOptIn opt_in[2];
+  FKV_CUDA(own ? opt_in[1].ensure(k_fork_copy<true>, room) : opt_in[0].ensure(k_fork_copy<false>, room));
+  FKV_CUDA(launch_waiting(own ? k_fork_copy<true> : k_fork_copy<false>, dim3(c->sm_count), warps * 32, smem, st, c->ctx, m));
   ++c->launches;
   FKV_CUDA(launch_waiting(k_fork_commit, dim3(L * batch, c->cfg.num_kv_heads), 256, 0, st, c->ctx, m));
   ++c->launches;

@@ -170,6 +170,30 @@ def test_a_large_batch():
         c.check_stored()
 
 
+@pytest.mark.parametrize("layers", [2, 3])
+def test_many_layers_of_a_large_batch(layers):
+    """512 and 768 entries (layer, sequence)."""
+    batch, rng = 256, random.Random(layers)
+    cache = binding.Cache(layers, 2, 1, 64, batch, 16, 48)
+    total, lens, parts = cache.device_status()[1], [], []
+    for layer in range(layers):
+        n = [rng.choice((0, 1, 7, 16, 17, 33)) for _ in range(batch)]
+        k = torch.randn((sum(n), 2, 64), device="cuda").to(torch.bfloat16)
+        cache.append_chunk(layer, k, -k, n)
+        lens.append(n)
+        parts.append(k.split(n))
+    for source in ([rng.randrange(-1, batch) for _ in range(batch)], [(s + 1) % batch for s in range(batch)], [s // 8 * 8 for s in range(batch)]):
+        cache.fork(source)
+        for layer in range(layers):
+            old, part = lens[layer], parts[layer]
+            lens[layer] = [old[r] if r >= 0 else 0 for r in source]
+            parts[layer] = [part[r] if r >= 0 else part[0][:0] for r in source]
+            k, v, _, _ = cache.export_chunk(layer, lens[layer])
+            assert cache.lengths(layer) == lens[layer] and torch.equal(k, torch.cat(parts[layer])) and torch.equal(v, -k)
+        used = sum(-(-n // 16) * 2 for row in lens for n in row)
+        assert cache.device_status() == (0, total - used)
+
+
 def test_refusals():
     c = Case(1, 1, 64, [5, 6, 7])
     for bad in ([0, 1, 3], [0, 1, -2], [2 ** 20, 1, 2]):
