@@ -117,6 +117,11 @@ def _mask(seq_mask, max_batch):
     return arr, ctypes.cast(arr, ctypes.c_void_p)
 
 
+def _i32(x):
+    """Whether an integer fits int32_t."""
+    return -2 ** 31 <= x < 2 ** 31
+
+
 def _check_i32(**ints):
     """Integers that the library takes as int32_t: ctypes would cut larger ones off without a word."""
     for name, x in ints.items():
@@ -409,7 +414,7 @@ class Cache:
     @staticmethod
     def _at(name, t, dtype, shape, dev):
         """The address of a contiguous tensor of this type and shape on the cache's device."""
-        if t.dtype is dtype and t.shape == shape and t.device == dev and t.is_contiguous():
+        if t.dtype is dtype and t.shape == shape and t.get_device() == dev.index and t.is_contiguous():
             return t.data_ptr()
         raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}, got {t.dtype} "
                          f"{tuple(t.shape)} on {t.device}, contiguous={t.is_contiguous()}")
@@ -433,13 +438,16 @@ class Cache:
         up = self._at("parents", parents, torch.int32, (total,), dev)
         if out is None:
             out = parents.new_empty((total, TREE_WORDS))
-        _check(lib().fkv_tree_masks(self._h, up, lens,
-                                    self._at("masks", out, torch.int32, (total, TREE_WORDS), dev), _stream_on(dev)), "fkv_tree_masks")
+            to = out.data_ptr()
+        else:
+            to = self._at("masks", out, torch.int32, (total, TREE_WORDS), dev)
+        _check(lib().fkv_tree_masks(self._h, up, lens, to, _stream_on(dev)), "fkv_tree_masks")
         return out
 
     def _tree(self, layer, k, v, q, tree_lens, masks, pos, keep_lens, window, sinks, out, lse, scale):
         """The three calls of trees: without q the store alone, without k the attention alone."""
-        _check_i32(layer=layer, window=window, sinks=sinks)
+        if not (_i32(layer) and _i32(window) and _i32(sinks)):
+            _check_i32(layer=layer, window=window, sinks=sinks)
         dev = self._here()
         c, at, bf16 = self.cfg, self._at, torch.bfloat16
         total, heads, dim = sum(tree_lens), c.num_kv_heads, c.head_dim
@@ -453,11 +461,13 @@ class Cache:
                      None if pos is None else at("pos", pos, torch.int32, (total,), dev), kept)
         if q is not None:
             rows = (total, heads * c.group_size, dim)
+            query = at("q", q, bf16, rows, dev)
             if out is None:
                 out = torch.empty_like(q)
-            attend = (window, sinks, scale, at("out", out, bf16, rows, dev),
-                      None if lse is None else at("lse", lse, torch.float32, rows[:2], dev))
-            query = at("q", q, bf16, rows, dev)
+                to = out.data_ptr()
+            else:
+                to = at("out", out, bf16, rows, dev)
+            attend = (window, sinks, scale, to, None if lse is None else at("lse", lse, torch.float32, rows[:2], dev))
             if k is None:
                 _check(lib().fkv_tree_attn(self._h, layer, query, lens, seen, *attend, _stream_on(dev)), "fkv_tree_attn")
             else:
@@ -485,8 +495,9 @@ class Cache:
         batch, i32 = self.cfg.max_batch, torch.int32
         if out is None:
             width = max(1, max(tree_lens))
-            path = like.new_empty((batch, width))
-            out = (path, like.new_empty(batch), torch.empty_like(path))
+            path, tokens = like.new_empty((2, batch, width)).unbind()
+            path_len = like.new_empty(batch)
+            return (path, path_len, tokens), (path.data_ptr(), path_len.data_ptr(), tokens.data_ptr(), width)
         path, path_len, tokens = out
         if path.dim() != 2:
             raise ValueError(f"path: expected two dimensions, got {tuple(path.shape)}")
@@ -563,7 +574,9 @@ class Cache:
         types = (torch.bfloat16, torch.bfloat16, torch.float32, torch.int32)
         if out is None:
             out = tuple(self.workspace.new_empty(s, dtype=t) for s, t in zip(shapes, types))
-        to = [None if t is None else self._at("out", t, d, s, dev) for t, d, s in zip(out, types, shapes)]
+            to = [t.data_ptr() for t in out]
+        else:
+            to = [None if t is None else self._at("out", t, d, s, dev) for t, d, s in zip(out, types, shapes)]
         _check(lib().fkv_export_chunk(self._h, layer, lens, *to, _stream_on(dev)), "fkv_export_chunk")
         return out
 
