@@ -3,7 +3,7 @@
 // Bound: bytes, 4 D per pair and KV head; for short caches and small trees the latency of one launch and its chain of reads.
 // k_chunk_attend computes the same for items of any number that it finds and cuts by itself, behind a store and ahead of a join that are
 // launches of their own: 38 us for 16 nodes over 8192 pairs (8 KV heads, g = 4, D = 128), whose bytes take 5.  Here the host says which CTA
-// does what, and the call is one launch: 17.0 us.  (256 nodes with a window of 4096: 32.9 us for 75; 33 nodes over 512 pairs, D = 64: 11.9
+// does what, and the call is one launch: 16.9 us.  (256 nodes with a window of 4096: 32.7 us for 75; 33 nodes over 512 pairs, D = 64: 11.6
 // for 28.6; all back to back at 1.96 GHz.)
 //
 // Shape: grid (S, blocks of 128 query rows = (128 / g nodes) x (g heads) of the sequences that have a tree, x KV heads); the S CTAs of a

@@ -20,7 +20,7 @@
 // in all CTAs, in every run and in every batch.
 // Bound: bytes of the rows that are read; for few sequences latency (gather, pass, exchange, piece: four dependent reads).  Back to back,
 // vocabulary 130001: five drafts of one sequence 8.2 us, 16 trees of up to 32 nodes with siblings 14.9 (two to four passes on the
-// longest way), 64 sequences without draft probabilities in bf16 14.6 (floor 2.5 us of bytes).  Two pieces at a time per warp gain
+// longest way), 64 sequences without draft probabilities in bf16 14.1 (floor 2.5 us of bytes).  Two pieces at a time per warp gain
 // nothing (9.1 and 16.0: the registers for them spill).
 #pragma once
 #include "fkv_dev.cuh"
