@@ -49,6 +49,7 @@ constexpr int kChunkInfo = 8;         // words that describe a CTA's unfinished 
 constexpr float kChunkGrow = 24.f;    // log2 of the growth of a row's maximum that O is rescaled for
 constexpr int kTreeNodes = 256;       // most nodes of a draft tree
 constexpr int kTreeWords = kTreeNodes / 32;   // words of a node's mask: bit i says that it sees node i
+constexpr int kTreeOne = 2, kTreeTwo = 3;  // what a page counts in an item of a tree with one query tile, and with two
 constexpr int kChunkItems = 3;        // items in use: being finished, being worked on, being read ahead
 
 // Prefix sums of the chunk lengths over the sequences, and the pairs that stay (use == 0: all of them).
@@ -663,7 +664,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
     }
     if (lane == 0) Blk[batch] = NB;
     __syncwarp();
-    struct Block { int s, j0, j1, n, T; ChunkRange r; int units; };
+    // What a page counts in the line: in batches of trees items with one query tile and with two come together, and a page takes the
+    // latter half as long again (3200 cycles per key tile for 2000: two tiles are bound by products and exponentials, one by the pages'
+    // way here).  16 trees of up to 64 nodes, 18 to a tile, over up to 32768 pairs: 199 us where all pages count alike, 179 at 2 : 3 (180 at
+    // 5 : 7 and 5 : 8, 182 at 5 : 6, 200 at 1 : 2).  Batches of other chunks have items with two tiles above all.
+    struct Block { int s, j0, j1, n, T; ChunkRange r; int units, weight; };
     auto block = [&](int f) {
       Block b;
       int lo = 0, hi = batch;
@@ -677,9 +682,10 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       b.j0 = (f - Blk[lo]) * TB;
       b.j1 = min(b.T, b.j0 + TB);
       b.units = 0;
+      b.weight = !TREE ? 1 : b.j1 - b.j0 > TPT ? kTreeTwo : kTreeOne;
       if (b.n >= b.T) {
         b.r = chunk_range(b.n, b.T, TREE ? 0 : b.j0, b.j1, W, S);   // (a node may be near the root whatever its place)
-        b.units = b.r.units();
+        b.units = b.r.units() * b.weight;
       }
       return b;
     };
@@ -691,7 +697,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
     const long long total = P * c.Hkv;
     // (long divisions take hundreds of cycles, and the first tile waits for these)
     auto quotient = [](long long x, long long y) { return (x | y) >> 32 ? x / y : (long long)((unsigned)x / (unsigned)y); };
-    const long long per = max((long long)kChunkMinPages, quotient(total + gridDim.x - 1, gridDim.x));
+    const long long per = max((long long)kChunkMinPages * (TREE ? kTreeOne : 1), quotient(total + gridDim.x - 1, gridDim.x));
     long long u = per * blockIdx.x;
     const long long u_end = min(total, u + per);
     int *info = c.chunk_info + blockIdx.x * kChunkInfo;
@@ -741,8 +747,11 @@ __global__ void __launch_bounds__(kChunkThreads, 1) k_chunk_attend(Ctx c, const 
       const int *ptrow = c.pt + (size_t)seg * c.max_pages;
       // This CTA's pages of the item: [pa0, pa1) at the front, [pb0, pb1) behind; with a window, less the pages that the
       // stored positions show to be hidden from every token.
-      int pa0 = min(off, b.r.sp), pa1 = min(off + take, b.r.sp);
-      int pb0 = b.r.b0 + max(off - b.r.sp, 0), pb1 = b.r.b0 + max(off + take - b.r.sp, 0);
+      // (a cut inside a page: the page is the CTA's that has its beginning)
+      auto page_at = [&](int o) { return !TREE ? o : (int)((unsigned)(o + b.weight - 1) / (unsigned)b.weight); };
+      const int o0 = page_at(off), o1 = page_at(off + take);
+      int pa0 = min(o0, b.r.sp), pa1 = min(o1, b.r.sp);
+      int pb0 = b.r.b0 + max(o0 - b.r.sp, 0), pb1 = b.r.b0 + max(o1 - b.r.sp, 0);
       int na = 0, first = 0;
       if (TREE && W) {
         const int base = b.n - b.T;
