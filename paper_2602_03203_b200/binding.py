@@ -437,7 +437,7 @@ class Cache:
         keep, lens = self._per_sequence(tree_lens, "tree_lens")
         up = self._at("parents", parents, torch.int32, (total,), dev)
         if out is None:
-            out = parents.new_empty((total, TREE_WORDS))
+            out = torch.empty(total, TREE_WORDS, dtype=torch.int32, device=dev)
             to = out.data_ptr()
         else:
             to = self._at("masks", out, torch.int32, (total, TREE_WORDS), dev)
@@ -489,14 +489,13 @@ class Cache:
         """append_tree(k, v) then tree_attn(q) in one call."""
         return self._tree(layer, k, v, q, tree_lens, masks, pos, keep_lens, window, sinks, out, lse, scale)
 
-    def _found(self, tree_lens, out, dev, like=None):
-        """The results of a verification: path [batch][n], path_len [batch], tokens [batch][n], int32 (where none are given: made on
-        the device of `like`), and their addresses."""
+    def _found(self, tree_lens, out, dev):
+        """The results of a verification: path [batch][n], path_len [batch], tokens [batch][n], int32, and their addresses."""
         batch, i32 = self.cfg.max_batch, torch.int32
         if out is None:
             width = max(1, max(tree_lens))
-            path, tokens = like.new_empty((2, batch, width)).unbind()
-            path_len = like.new_empty(batch)
+            path, path_len = torch.empty(batch, width, dtype=i32, device=dev), torch.empty(batch, dtype=i32, device=dev)
+            tokens = torch.empty_like(path)
             return (path, path_len, tokens), (path.data_ptr(), path_len.data_ptr(), tokens.data_ptr(), width)
         path, path_len, tokens = out
         if path.dim() != 2:
@@ -529,7 +528,7 @@ class Cache:
                 raise ValueError(f"{name}: a row's elements must be next to one another")
             rows += (t.data_ptr(), step if total > 1 else shape[1])
         drafts = at("tokens", tokens, torch.int32, (total,), dev)
-        out, found = self._found(tree_lens, out, dev, tokens)
+        out, found = self._found(tree_lens, out, dev)
         _check(lib().fkv_verify_tree(self._h, drafts, at("parents", parents, torch.int32, (total,), dev),
                                      lens, *rows, 0 if dtype is torch.float32 else 1, shape[1],
                                      at("u_accept", u_accept, torch.float32, (total,), dev),
@@ -542,7 +541,7 @@ class Cache:
         keep, lens = self._per_sequence(tree_lens, "tree_lens")
         shape, at, i32 = (sum(tree_lens),), self._at, torch.int32
         drafts = at("tokens", tokens, i32, shape, dev)
-        out, found = self._found(tree_lens, out, dev, tokens)
+        out, found = self._found(tree_lens, out, dev)
         _check(lib().fkv_verify_tree_greedy(self._h, drafts, at("parents", parents, i32, shape, dev), lens,
                                             at("choice", choice, i32, shape, dev), *found, _stream_on(dev)), "fkv_verify_tree_greedy")
         return out
@@ -550,7 +549,8 @@ class Cache:
     def commit_tree(self, tree_lens, path, path_len, layer=ALL_LAYERS):
         """The accepted nodes' pairs move together behind the pairs ahead of the tree, the others are dropped.  The host learns the
         new lengths by sync_lengths()."""
-        _check_i32(layer=layer)
+        if not _i32(layer):
+            _check_i32(layer=layer)
         dev = self._here()
         keep, lens = self._per_sequence(tree_lens, "tree_lens")
         _, found = self._found(tree_lens, (path, path_len, path), dev)
@@ -566,16 +566,20 @@ class Cache:
     def export_chunk(self, layer, chunk_lens, out=None):
         """Dense copy of the last chunk_lens[s] pairs of every sequence: k, v [tokens][Hkv][D], features [tokens][Hkv][6 g], positions
         [tokens][Hkv].  out: four such tensors (None: not wanted)."""
-        _check_i32(layer=layer)
+        if not _i32(layer):
+            _check_i32(layer=layer)
         dev = self._here()
         keep, lens = self._per_sequence(chunk_lens, "chunk_lens")
         c, total = self.cfg, sum(chunk_lens)
-        shapes = ((total, c.num_kv_heads, c.head_dim),) * 2 + ((total, c.num_kv_heads, self.feat_dim), (total, c.num_kv_heads))
-        types = (torch.bfloat16, torch.bfloat16, torch.float32, torch.int32)
+        heads, F = c.num_kv_heads, self.feat_dim
         if out is None:
-            out = tuple(self.workspace.new_empty(s, dtype=t) for s, t in zip(shapes, types))
+            k = torch.empty(total, heads, c.head_dim, dtype=torch.bfloat16, device=dev)
+            out = (k, torch.empty_like(k), torch.empty(total, heads, F, dtype=torch.float32, device=dev),
+                   torch.empty(total, heads, dtype=torch.int32, device=dev))
             to = [t.data_ptr() for t in out]
         else:
+            shapes = ((total, heads, c.head_dim),) * 2 + ((total, heads, F), (total, heads))
+            types = (torch.bfloat16, torch.bfloat16, torch.float32, torch.int32)
             to = [None if t is None else self._at("out", t, d, s, dev) for t, d, s in zip(out, types, shapes)]
         _check(lib().fkv_export_chunk(self._h, layer, lens, *to, _stream_on(dev)), "fkv_export_chunk")
         return out
