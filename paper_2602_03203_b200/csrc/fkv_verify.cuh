@@ -88,6 +88,8 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
     if (rank == 0 && tid == 0) a.path_len[seq] = 0;
     return;
   }
+  // "I am running": waited for ahead of the walk, whose passes write into the other CTAs' shared memory (the gather hides the wait).
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   auto row_p = [&](int node) { return reinterpret_cast<const T *>(a.target) + (row0 + node) * a.target_stride; };
   auto row_q = [&](int node) { return reinterpret_cast<const T *>(a.draft) + (row0 + node) * a.draft_stride; };
   if (tid < nodes) {
@@ -120,6 +122,7 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
     if (again) s_p[tid] = 0.0;
   }
   __syncthreads();
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");   // every CTA of the cluster runs
 
   const int pieces = (V + kVerPiece - 1) / kVerPiece;
   const int per = kVerParts / cs;   // this CTA's parts are [rank per, (rank + 1) per)
