@@ -433,8 +433,9 @@ int fkv_commit_tree(fkv_cache *c, int layer, const int32_t *tree_lens, const int
  * holds goes with it: pairs, features, positions, decode queries on record, its budget (an emptied place keeps its own).  Sequences never
  * share pages (each keeps features of its own in them): of a sequence that goes away while others become what it was, one takes the pages
  * over and the others get copies.  The pages of sequences that go away serve the copies; if these and the free ones are too few the
- * whole call does nothing (FKV_DEV_POOL_EXHAUSTED).  Only enqueues kernels; a replayed call does the same to what it finds (call
- * fkv_sync_lengths after the last replay).
+ * whole call does nothing (FKV_DEV_POOL_EXHAUSTED).  Only enqueues kernels; a replayed call does the same to what it finds.  The host's
+ * lengths and budgets are those of a call that ran once and found its pages: call fkv_sync_lengths, which reads both, after the last
+ * replay and after a call that did nothing.
  *
  * fkv_export_chunk: dense copy of the last chunk_lens[s] pairs of every sequence of a layer, packed, the inverse of fkv_append_chunk:
  * k, v dev [tokens][Hkv][D] bf16 (16-byte aligned), feat dev [tokens][Hkv][F] fp32 (8-byte aligned), pos dev [tokens][Hkv] int32 (after an eviction the
@@ -515,8 +516,10 @@ int fkv_get_lengths(const fkv_cache *c, int layer, int32_t *host_out);
 int fkv_device_status(fkv_cache *c, uint32_t *status_bits, int32_t *free_pages, void *stream);
 
 /*
- * Re-read the lengths of every layer from the device into the host mirror
- * (syncs).  For callers that restored a saved copy of the workspace.
+ * Re-read the lengths of every layer and the sequences' budgets from the device
+ * into the host mirror (syncs).  After replays of captured calls, calls that
+ * ended with an error bit, fkv_commit_tree, and for callers that restored a
+ * saved copy of the workspace.
  */
 int fkv_sync_lengths(fkv_cache *c, void *stream);
 

@@ -646,7 +646,7 @@ class Cache:
         return self.workspace.clone()
 
     def restore(self, snap: torch.Tensor):
-        """Put a snapshot back (device-to-device copy) and refresh the host mirror of the lengths."""
+        """Put a snapshot back (device-to-device copy) and refresh the host mirror of the lengths and budgets."""
         self.workspace.copy_(snap)
         self.sync_lengths()
 

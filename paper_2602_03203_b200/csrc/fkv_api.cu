@@ -106,7 +106,7 @@ Layout make_layout(const fkv_config &c) {
   L.pt = take(nseg * L.max_pages * 4);
   L.pt_new = take(nseg * L.max_pages * 4);
   L.len = take((size_t)c.num_layers * c.max_batch * 4);
-  L.budget = take((size_t)c.max_batch * 4);
+  L.budget = take((size_t)c.max_batch * 4);   // (behind the lengths: fkv_sync_lengths reads both at once)
   L.sp = take((size_t)c.num_layers * c.num_kv_heads * L.sp_stride);
   L.scores = take(nseg * L.cap * 4);
   L.idx = take(nseg * L.cap * 4);
@@ -156,6 +156,7 @@ struct fkv_cache {
   Ctx ctx;
   std::vector<int> h_len;     // [L][batch] mirror of the device lengths
   std::vector<int> h_budget;  // [batch]
+  std::vector<int> mirror;    // lengths and budgets as they lie in the workspace
   std::vector<uint8_t> loaded;  // [L][Hkv] scorer present
   std::vector<uint8_t> staging;
   uint64_t launches = 0;
@@ -1004,6 +1005,7 @@ int fkv_init_cache(const fkv_config *cfg, void *dev_workspace, size_t bytes, voi
   x.chunk_part = (float *)(ws + L.chunk_part); x.chunk_ml = (float *)(ws + L.chunk_ml); x.chunk_info = (int *)(ws + L.chunk_info);
   c->h_len.assign((size_t)cfg->num_layers * cfg->max_batch, 0);
   c->h_budget.assign(cfg->max_batch, cfg->budget);
+  c->mirror.resize((L.budget - L.len) / 4 + cfg->max_batch);
   c->loaded.assign((size_t)cfg->num_layers * cfg->num_kv_heads, 0);
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -1708,8 +1710,12 @@ int fkv_device_status(fkv_cache *c, uint32_t *status_bits, int32_t *free_pages, 
 int fkv_sync_lengths(fkv_cache *c, void *stream) {
   if (!c) return FKV_ERR_INVALID_ARG;
   cudaStream_t st = (cudaStream_t)stream;
-  FKV_CUDA(cudaMemcpyAsync(c->h_len.data(), c->ctx.len, c->h_len.size() * 4, cudaMemcpyDeviceToHost, st));
+  // Lengths and budgets in one copy (the budgets follow in the workspace): a fork moves both, and when it ran, or whether it found
+  // the pages to do anything, the device alone knows.
+  FKV_CUDA(cudaMemcpyAsync(c->mirror.data(), c->ctx.len, c->mirror.size() * 4, cudaMemcpyDeviceToHost, st));
   FKV_CUDA(cudaStreamSynchronize(st));
+  std::copy_n(c->mirror.begin(), c->h_len.size(), c->h_len.begin());
+  std::copy_n(c->mirror.end() - c->cfg.max_batch, c->cfg.max_batch, c->h_budget.begin());
   return FKV_OK;
 }
 
