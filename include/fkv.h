@@ -386,7 +386,9 @@ int fkv_chunk_features(fkv_cache *c, int layer, const void *q, const float *lse,
  * comes again has probability 0).
  * tokens, parents: dev [tokens] int32 (tokens[node 0] is not read; nodes that node 0 does not lead to are never reached; one whose token
  * is outside the vocabulary is passed over).  target, draft: dev [tokens][vocab] of dtype FKV_F32 or FKV_BF16, rows target_stride and
- * draft_stride elements apart (row a: the token after node a); taken as they are, not normalised, NaN and negative ones as 0.
+ * draft_stride elements apart (row a: the token after node a); taken as they are, not normalised, NaN and negative ones as 0.  A child
+ * whose own draft[a][x] is NaN is rejected whatever its number: of a token that no known probability drew nothing can be said, and R, in
+ * which the NaN counts as 0, gives the next one.  The draft's row of a node is read only where it has children.
  * u_accept: dev [tokens] fp32 (entry 0 of a tree is not read), u_sample: dev [max_batch] fp32, uniform in [0, 1): the library draws no
  * random numbers itself.  vocab at most 2^20.
  * path: dev [max_batch][path_stride] int32, the accepted nodes from node 0 down, -1 behind them; path_len: dev [max_batch] int32, their

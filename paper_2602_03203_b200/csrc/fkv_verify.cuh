@@ -104,7 +104,10 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
     s_par[tid] = (short)p;
     s_u[tid] = __ldcg(a.u_accept + row0 + tid);
     s_p[tid] = ok ? fmax((double)to_f32(__ldcg(row_p(p) + x)), 0.0) : 0.0;   // (NaN and negative numbers count as 0)
-    if (Q) s_q[tid] = ok ? (double)to_f32(__ldcg(row_q(p) + x)) : 0.0;
+    if (Q) {
+      const double q = ok ? (double)to_f32(__ldcg(row_q(p) + x)) : 0.0;
+      s_q[tid] = q < 0.0 ? 0.0 : q;   // (NaN stays: no comparison with it holds, so the draft is refused)
+    }
   }
   __syncthreads();
   if (tid < nodes) {
@@ -130,17 +133,20 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
   const int c0 = begin(rank * per);
   int turn = 0;
   int cur = 0, len = 0;
-  // What R is without its divisor: p - alpha q, or p without the tokens of cur's children.
-  auto weight = [&](double p, double q, double alpha) { return Q ? fmax(fma(-alpha, q, p), 0.0) : fmax(p, 0.0); };
+  // What R is without its divisor: p - alpha q, or p without the tokens of cur's children.  NaN and negative numbers of either row count as
+  // 0; where nothing was rejected (alpha = 0) R is p, whatever the draft's row holds (minus zero times an infinity is no zero).
+  auto weight = [&](double p, double q, double alpha) { return fmax(Q && alpha != 0.0 ? fma(-alpha, fmax(q, 0.0), p) : p, 0.0); };
   // A lane's eight weights of a piece: tokens lane, lane + 32, ... of it.
-  auto load = [&](int pc, T (&pv)[8], T (&qv)[8]) {
-    const T *pr = row_p(cur), *qr = Q ? row_q(cur) : nullptr;
+  // (The draft's row is read where something was rejected: a leaf's is in general never filled.)
+  auto load = [&](int pc, T (&pv)[8], T (&qv)[8], double alpha) {
+    const bool both = Q && alpha != 0.0;
+    const T *pr = row_p(cur), *qr = both ? row_q(cur) : nullptr;
     const int x0 = pc * kVerPiece + lane;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const bool in = x0 + 32 * i < V;
       pv[i] = in ? __ldcg(pr + x0 + 32 * i) : T(0.f);
-      if (Q) qv[i] = in ? __ldcg(qr + x0 + 32 * i) : T(0.f);
+      if (Q) qv[i] = both && in ? __ldcg(qr + x0 + 32 * i) : T(0.f);
     }
   };
   auto weights = [&](int pc, const T (&pv)[8], const T (&qv)[8], double alpha, double (&w)[8]) {
@@ -166,7 +172,7 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
 #pragma unroll 1
       for (int pc = b0 + warp; pc < b1; pc += kVerWarps) {
         T pv[8], qv[8];
-        load(pc, pv, qv);
+        load(pc, pv, qv, alpha);
         double w[8];
         weights(pc, pv, qv, alpha, w);
         const double x = warp_sum(((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7])));
@@ -214,7 +220,7 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
       continue;
     }
     if (Q) {
-      alpha = summed ? alpha + S : 1.0;
+      alpha = summed ? alpha + S : 1.0;   // (never 0)
       S = pass(alpha);
       summed = true;
       if (!(S > 0.0)) {   // nothing is left of p: a rejection that had no probability; p itself serves
@@ -266,7 +272,7 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
   double w[8];
   {
     T pv[8], qv[8];
-    load(at, pv, qv);
+    load(at, pv, qv, alpha);
     weights(at, pv, qv, alpha, w);
   }
   int found = -1;
