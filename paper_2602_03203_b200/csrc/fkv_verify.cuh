@@ -306,9 +306,12 @@ __global__ void __launch_bounds__(32) k_verify_greedy(Ctx c, const __grid_consta
   const int seq = blockIdx.x, lane = threadIdx.x, row0 = a.lens.tok[seq], nodes = a.lens.tok[seq + 1] - row0;
   int32_t *path = a.path + (size_t)seq * a.stride, *out = a.out + (size_t)seq * a.stride;
   for (int j = lane; j < nodes; j += 32) {
-    const int p = j > 0 ? __ldcg(a.parents + row0 + j) : -1;
-    if (p >= j || p < -1) set_status(c, kDevBadIndex);
-    s_par[j] = (short)(p >= j ? -1 : p);
+    int p = j > 0 ? __ldcg(a.parents + row0 + j) : -1;
+    if (p >= j || p < -1) {   // (a node that nothing leads to; 16 bits hold what is left)
+      set_status(c, kDevBadIndex);
+      p = -1;
+    }
+    s_par[j] = (short)p;
     s_tok[j] = __ldcg(a.tokens + row0 + j);
     s_want[j] = __ldcg(choice + row0 + j);
   }
