@@ -1476,8 +1476,7 @@ int fkv_commit_tree(fkv_cache *c, int layer, const int32_t *tree_lens, const int
   const int l0 = layer == FKV_ALL_LAYERS ? 0 : layer, nl = layer == FKV_ALL_LAYERS ? c->cfg.num_layers : 1;
   for (int l = l0; l < l0 + nl; ++l)
     if (!chunk_is_stored(c, l, tree_lens)) return FKV_ERR_INVALID_ARG;
-  if (nl > 65535) return FKV_ERR_INVALID_ARG;   // (the grid's second dimension)
-  FKV_CUDA(launch_waiting(k_commit_tree, dim3(c->cfg.max_batch, nl), 1024, 0, (cudaStream_t)stream, c->ctx, l0, lens, path, path_len, path_stride));
+  FKV_CUDA(launch_waiting(k_commit_tree, dim3(nl, c->cfg.max_batch), 1024, 0, (cudaStream_t)stream, c->ctx, l0, lens, path, path_len, path_stride));
   ++c->launches;
   return FKV_OK;
 }
@@ -1531,7 +1530,7 @@ int fkv_fork(fkv_cache *c, const int32_t *from, void *stream) {
   ++c->launches;
   if (c->cfg.feature_window > 0) {
     const size_t words = (size_t)c->ctx.hist_wp * c->cfg.num_kv_heads * c->cfg.group_size * c->cfg.head_dim / 8;
-    FKV_CUDA(launch_waiting(k_fork_record, dim3((unsigned)((words + 255) / 256), L), 256, 0, st, c->ctx, ops));
+    FKV_CUDA(launch_waiting(k_fork_record, dim3(L, (unsigned)((words + 255) / 256)), 256, 0, st, c->ctx, ops));
     ++c->launches;
   }
   int old[kMaxBatch];

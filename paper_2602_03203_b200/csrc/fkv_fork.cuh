@@ -265,13 +265,13 @@ __global__ void __launch_bounds__(256) k_fork_commit(Ctx c, const __grid_constan
   if (tid == 0 && h == 0) c.len[i] = n_new;
 }
 
-// grid (enough threads for a sequence's record in 16-byte words, layers).  Runs behind k_fork_commit (nothing there reads the record).
+// grid (layers, enough threads for a sequence's record in 16-byte words).  Runs behind k_fork_commit (nothing there reads the record).
 __global__ void __launch_bounds__(256) k_fork_record(Ctx c, const __grid_constant__ ForkOps ops) {
   griddep_wait();
   griddep_launch();
   if (__ldcg(c.planhdr + PH_PUSH_START) < 0) return;
-  const int layer = blockIdx.y, ls0 = layer * c.batch, heads = c.Hkv * c.G;
-  const size_t t = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
+  const int layer = blockIdx.x, ls0 = layer * c.batch, heads = c.Hkv * c.G;
+  const size_t t = (size_t)blockIdx.y * blockDim.x + threadIdx.x;
   auto run = [&](auto *all, size_t per) {   // the layer's arrays of `per` elements per sequence: element t of each
     if (t >= per) return;
     auto *at = all + (size_t)ls0 * per + t;

@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(kTreeNodes) k_tree_masks(Ctx c, const __grid_c
 }
 
 // ---------------------------------------------------------------- the accepted path
-// grid (sequences, layers), 32 warps: of a sequence's last T pairs, the tree's, those of path[0 .. cnt) (ascending) move to the
+// grid (layers, sequences), 32 warps: of a sequence's last T pairs, the tree's, those of path[0 .. cnt) (ascending) move to the
 // places behind the pairs ahead of the tree; the length follows and the pages behind are returned.
 // A pair never moves up (path[i] >= i), and its place may be another's source: 128 / Hkv places of every head are read into
 // registers, then written, then the next ones (whose sources lie behind all places written so far).
@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(1024) k_commit_tree(Ctx c, int l0, const __gri
   __shared__ int s_push;
   griddep_wait();
   griddep_launch();
-  const int seq = blockIdx.x, layer = l0 + blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int seq = blockIdx.y, layer = l0 + blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int T = lens.tok[seq + 1] - lens.tok[seq], ls = layer * c.batch + seq;
   if (T == 0) return;
   const int n = __ldcg(c.len + ls), cnt = __ldcg(path_len + seq), base = n - T;
