@@ -219,7 +219,13 @@ __global__ void __launch_bounds__(kForkMaxWarps * 32) k_fork_copy(Ctx c, const _
         const int next = __shfl_sync(0xffffffffu, src, (i + 1) & 31);
         if (lane == 0 && i + 1 < take) read_page(turn + 1, next);
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars[warp][turn & 1]), (turn >> 1) & 1));
-        if (!ok) { set_status(c, kDevWaitTimeout); break; }
+        if (!ok) {
+          set_status(c, kDevWaitTimeout);
+          // (no copy may be in flight at the exit: once more for this one, and for the next)
+          mbar_wait(smem_u32(&bars[warp][turn & 1]), (turn >> 1) & 1);
+          if (i + 1 < take) mbar_wait(smem_u32(&bars[warp][(turn + 1) & 1]), ((turn + 1) >> 1) & 1);
+          break;
+        }
 #pragma unroll
         for (int k = 0; k < kForkGroup; ++k) {
           const int to = __shfl_sync(0xffffffffu, dst[k], i);

@@ -197,7 +197,13 @@ __global__ void __launch_bounds__(kExportMaxWarps * 32) k_export_chunk(Ctx c, in
     const bool any = x.r0 < x.r1;
     copy(nx, turn + (any ? 1 : 0));
     if (any) {
-      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bars[warp][turn & 1]), (turn >> 1) & 1))) { set_status(c, kDevWaitTimeout); break; }
+      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bars[warp][turn & 1]), (turn >> 1) & 1))) {
+        set_status(c, kDevWaitTimeout);
+        // (no copy may be in flight at the exit: once more for this one, and for the next)
+        mbar_wait(smem_u32(&bars[warp][turn & 1]), (turn >> 1) & 1);
+        if (nx.r0 < nx.r1) mbar_wait(smem_u32(&bars[warp][(turn + 1) & 1]), ((turn + 1) >> 1) & 1);
+        break;
+      }
       const uint8_t *page = buf + (turn & 1) * c.page_bytes;
       uint8_t *to = lane < nch ? k : v;
       if (lane < 2 * nch && to)
