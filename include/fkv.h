@@ -367,7 +367,8 @@ int fkv_chunk_features(fkv_cache *c, int layer, const void *q, const float *lse,
  * node sets FKV_DEV_BAD_INDEX and counts as -1.
  *
  * fkv_append_tree: fkv_append_chunk for the nodes of trees.  pos NULL: a node's position is one more than its parent's, a root's the
- * one after the last pair that stays; given positions must be behind that of the last pair that stays.
+ * one after the last pair that stays (with masks of another kind: as many further as the mask names nodes ahead of its own); given
+ * positions must be behind that of the last pair that stays.
  * fkv_tree_attn: fkv_chunk_attn for the nodes of trees, which are the last tree_lens[s] pairs of their segments: a node sees the pairs
  * ahead of the tree as a chunk's token does (with window > 0 those inside the window of its own position, and the sinks), and the pairs
  * of the tree that its mask names up to its own (other masks than fkv_tree_masks writes are welcome; a node that sees nothing gets

@@ -71,7 +71,11 @@ struct ChunkKeep {
 // Bound: bytes (8 D a pair and KV head, read and written); back to back 4.7 us for 5 tokens, 5.3 for 256, 12.7 for 2048 on 8 heads
 // (a launch and four dependent reads: length, page, last position, free stack).
 // TREE: the chunk is a draft tree (kernel 10); a node's position is one behind its parent's, so it follows from the number
-// of its ancestors in `masks`.
+// of its ancestors: the nodes ahead of it that its mask names (whatever else a caller's own mask says, it is behind the last pair's).
+__device__ __forceinline__ int tree_before(uint32_t word, int w, int j) {   // those in word w of node j's mask
+  const int e = j - 32 * w;
+  return __popc(word & (e <= 0 ? 0u : e >= 32 ? ~0u : (1u << e) - 1u));
+}
 template <bool TREE>
 __global__ void __launch_bounds__(256) k_append_chunk(Ctx c, int layer, const uint8_t *k, const uint8_t *v, const int32_t *pos,
                                                       const __grid_constant__ ChunkLens lens,
@@ -150,7 +154,7 @@ __global__ void __launch_bounds__(256) k_append_chunk(Ctx c, int layer, const ui
         if (lane == 0 && (slot % kPage == 0 || j == 0)) ptrow[pg] = pid;
       }
       int32_t pdef = j;
-      if (TREE && !pos) pdef = (int)__reduce_add_sync(0xffffffffu, lane < kTreeWords ? __popc(__ldcg(masks + (size_t)row * kTreeWords + lane)) : 0) - 1;
+      if (TREE && !pos) pdef = __reduce_add_sync(0xffffffffu, lane < kTreeWords ? tree_before(__ldcg(masks + (size_t)row * kTreeWords + lane), lane, j) : 0);
       if (!pos && kp_s > 0) {   // the position after the last pair that stays
         const uint8_t *prev = c.pool + (size_t)__ldcg(ptrow + (kp_s - 1) / kPage) * c.page_bytes;
         pdef = __ldcg(reinterpret_cast<const int32_t *>(meta_row(c, prev, (kp_s - 1) % kPage)) + c.F) + 1 + pdef;

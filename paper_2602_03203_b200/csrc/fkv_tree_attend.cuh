@@ -193,8 +193,8 @@ __device__ __noinline__ void tree_store_cta(const Ctx &c, const TreeArgs &a, Tre
       if (lane == 0 && (slot % kPage == 0 || j == 0)) ptrow[pg] = pid;
     }
     int32_t pdef = 0;
-    if (!a.pos) {   // one behind the parent's: the last pair's and the number of nodes that this one sees
-      pdef = (int)__reduce_add_sync(0xffffffffu, lane < kTreeWords ? __popc(__ldcg(a.masks + (size_t)row * kTreeWords + lane)) : 0) - 1;
+    if (!a.pos) {   // one behind the parent's
+      pdef = __reduce_add_sync(0xffffffffu, lane < kTreeWords ? tree_before(__ldcg(a.masks + (size_t)row * kTreeWords + lane), lane, j) : 0);
       if (kp > 0) pdef += slot_pos(c, ptrow, kp - 1) + 1;
     }
     const size_t at = ((size_t)row * c.Hkv + h) * c.D * 2;
@@ -363,9 +363,9 @@ __global__ void __launch_bounds__(kTaThreads<HALF>, 1) k_tree_attend(const __gri
           p[u] = __ldcg(a.pos + row0 + j);
         } else {
           const uint32_t *row = a.masks + (size_t)(row0 + j) * kTreeWords;
-          p[u] = last;
+          p[u] = last + 1;
 #pragma unroll
-          for (int w = 0; w < kTreeWords; ++w) p[u] += __popc(__ldcg(row + w));
+          for (int w = 0; w < kTreeWords; ++w) p[u] += tree_before(__ldcg(row + w), w, j);
         }
         low = min(low, p[u]);
       }
