@@ -133,11 +133,10 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
   const int c0 = begin(rank * per);
   int turn = 0;
   int cur = 0, len = 0;
-  // What R is without its divisor: p - alpha q, or p without the tokens of cur's children.  NaN and negative numbers of either row count as
-  // 0; where nothing was rejected (alpha = 0) R is p, whatever the draft's row holds (minus zero times an infinity is no zero).
-  auto weight = [&](double p, double q, double alpha) { return fmax(Q && alpha != 0.0 ? fma(-alpha, fmax(q, 0.0), p) : p, 0.0); };
+  // What R is without its divisor: p - alpha q, or p without the tokens of cur's children.
+  auto weight = [&](double p, double q, double alpha) { return Q ? fmax(fma(-alpha, q, p), 0.0) : fmax(p, 0.0); };
   // A lane's eight weights of a piece: tokens lane, lane + 32, ... of it.
-  // (The draft's row is read where something was rejected: a leaf's is in general never filled.)
+  // (The draft's row is read where something was rejected: a leaf's is in general never filled.  R is p elsewhere.)
   auto load = [&](int pc, T (&pv)[8], T (&qv)[8], double alpha) {
     const bool both = Q && alpha != 0.0;
     const T *pr = row_p(cur), *qr = both ? row_q(cur) : nullptr;
@@ -151,7 +150,8 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
   };
   auto weights = [&](int pc, const T (&pv)[8], const T (&qv)[8], double alpha, double (&w)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = weight((double)to_f32(pv[i]), Q ? (double)to_f32(qv[i]) : 0.0, alpha);
+    for (int i = 0; i < 8; ++i)   // (NaN and negative numbers count as 0; in 64 bits the comparison costs a fifth of a pass)
+      w[i] = weight((double)to_f32(pv[i]), Q ? (double)fmaxf(to_f32(qv[i]), 0.f) : 0.0, alpha);
     if (!Q)   // without the rejected tokens: those of cur's children, looked for by the whole warp
       for (int j0 = 0; j0 < nodes; j0 += 32) {
         const int j = j0 + lane, x = j < nodes && s_par[j] == cur ? s_tok[j] : -1;
