@@ -373,6 +373,7 @@ int fkv_chunk_features(fkv_cache *c, int layer, const void *q, const float *lse,
  * ahead of the tree as a chunk's token does (with window > 0 those inside the window of its own position, and the sinks), and the pairs
  * of the tree that its mask names up to its own (other masks than fkv_tree_masks writes are welcome; a node that sees nothing gets
  * zeros, and -infinity as its log-sum-exp).  A window must not be shorter than the longest tree, so that it holds every ancestor.
+ * As in fkv_chunk_attn, P is rounded to bf16 for the product with V (as V is); everything else is fp32.
  * k and v of a tree must be finite.  A tree's own positions do not grow from pair to pair: commit it or roll it back (keep_lens) before
  * a call that goes by positions (windows, fkv_append without pos).  fkv_append_tree_attn: the two calls in one.  Errors and stream capture as for the chunk calls.
  *

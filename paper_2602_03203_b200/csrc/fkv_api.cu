@@ -808,7 +808,11 @@ TreeShape tree_shape(fkv_cache *c, const int32_t *tree_lens, const int *ahead, i
     if (fit >= segs + (append ? 1 : 0)) break;
   }
   if (S == 0) return r;
-  // The general kernels share the pages evenly over the SMs but start and join some 20 us later; a page takes an SM 0.15 us.
+  // The general kernels share the pages evenly over the SMs, but start and join 10 - 30 us later; a page takes a cluster's CTA 0.15 - 0.18 us,
+  // and an SM 0.21 where all of them read.  Both timed, D = 128, pages of the longest CTA here : most that the rule lets through: 16 nodes,
+  // 8 heads 205 : 210 41.0 us by clusters, 54.4 by the general kernels; 410 : 321 72.4 and 73.5; 820 : 542 138 and 120.  64 nodes 342 : 321
+  // 72.8 and 69.2.  Four uneven sequences 342 : 176 60.3 and 48.1; eight 258 : 201 59.1 and 55.6.  The border is off by most where one head
+  // is all there is (129 : 113, 27.6 and 53.3; 513 : 155, 84.5 and 60.4) and for 256 nodes over 16384 pairs (521 : 550, 105.7 and 98.9).
   if ((most + S - 1) / S > total / c->sm_count + 100) return r;
   r.S = S;
   const long long warps = (long long)S * ((half ? kTaThreads<true> : kTaThreads<false>) / 32);   // a pair and head each

@@ -11,6 +11,8 @@
 // Bound: bytes: every source page read once, every copy written once.  8192 pairs of 8 heads in two layers to three copies (80 MB read, 240
 // written) 62.9 us back to back = 5.1 TB/s, 8 of them the latency of two dependent launches (what a small fork takes; 11 with a launch for the
 // plan); writing 240 MB alone takes 37.  The copy through registers, a warp per page, took 81.
+// Pages handed over (every sequence takes another's place): 16 sequences of 4096 pairs, 4 heads 16 us, with 8 heads in 32 layers 43, 4 of 8192 with
+// 8 heads in two layers 38: bound by latency, a warp moving the tables of all heads of a (layer, sequence) one after another.
 #pragma once
 #include "fkv_dev.cuh"
 #include "fkv_attend.cuh"

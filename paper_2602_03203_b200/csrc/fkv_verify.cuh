@@ -11,6 +11,9 @@
 // a rejection costs one pass over the two rows, whatever came before it.
 // Without draft probabilities a child is a point mass: R loses its token, u_c m < p(x) decides with m = 1 - the mass of the
 // rejected ones, and only the last node's row is read.
+// Of rows that hold what no probability is, NaN and negative numbers count as 0.  A child whose own q(x) is NaN is rejected whatever its
+// number (nothing is known of how it was drawn; R then gives the next token), and q's row at a node is read as a whole only behind a
+// rejection there: a draft model has no row for a leaf, and nothing that lies in its place may count.
 //
 // The walk itself runs in every thread alike, on numbers gathered ahead of it (p and q of every node's own token: one read).
 // A pass is cut into pieces of 256 tokens; their sums stay in shared memory, so the piece that holds the drawn token is found
@@ -18,10 +21,11 @@
 // compared with u lose nothing that fp32 inputs hold.  A sequence is a cluster of up to eight CTAs; its pieces are eight parts, summed
 // each in the same order whichever CTA has it, and the parts' sums meet through distributed shared memory: results are the same bits
 // in all CTAs, in every run and in every batch.
-// Bound: bytes of the rows that are read; for few sequences latency (gather, pass, exchange, piece: four dependent reads).  Back to back,
-// vocabulary 130001: five drafts of one sequence 8.2 us, 16 trees of up to 32 nodes with siblings 14.9 (two to four passes on the
-// longest way), 64 sequences without draft probabilities in bf16 14.1 (floor 2.5 us of bytes).  Two pieces at a time per warp gain
-// nothing (9.1 and 16.0: the registers for them spill).
+// Bound: bytes of the rows that are read; for few sequences latency (gather, pass, exchange, piece: four dependent reads).  Back to back in
+// a graph, vocabulary 130001, 1965 MHz: five drafts of one sequence 8.4 - 9.5 us (six draws), 16 trees of up to 32 nodes with siblings 15.1 -
+// 22.5 (by the passes on the longest way; bf16 15.4 - 23.2), 64 sequences without draft probabilities in bf16 14.8 (floor 2.5 us of bytes).
+// One tree in a batch of 256 places 8.5, alone 8.2: a cluster without a tree writes its row of -1 and leaves.  Two pieces at a time per
+// warp gain nothing (the registers for them spill).
 #pragma once
 #include "fkv_dev.cuh"
 #include "fkv_attend.cuh"
@@ -297,7 +301,8 @@ __global__ void __launch_bounds__(kVerThreads, kVerCtasPerSm) k_verify_tree(Ctx 
 }
 
 // Temperature zero: the target's own choice after every node is known, and the walk takes the child that has it (the one with
-// the lowest index).  A warp per sequence.
+// the lowest index).  A warp per sequence.  Bound: latency of a launch and two dependent reads: 1.9 us for a tree of 6, 2.5 for 16 of 32,
+// 4.9 for 256 trees of 256.
 __global__ void __launch_bounds__(32) k_verify_greedy(Ctx c, const __grid_constant__ VerifyArgs a, const int32_t *choice) {
   __shared__ int s_tok[kTreeNodes], s_want[kTreeNodes];
   __shared__ short s_par[kTreeNodes];
